@@ -76,7 +76,7 @@ def _size(rng, lo, hi):
 
 def draw(rng):
     c = _draw(rng)
-    return {k: v for k, v in c.items() if k != "name"}
+    return {k: v - 1 if k in "TVD" and v in (768, 3072) else v for k, v in c.items() if k != "name"}
 
 
 def _draw(rng):
