@@ -100,11 +100,11 @@ def _draw(rng):
     state, grad, copy = rng.choice(("f32", "8bit")), rng.choice(("f32", "bf16")), rng.random() < 0.5
     if rng.random() < 0.3:
         return _adamw("", _size(rng, 1, 64), 0, 0, 0, state, grad, copy)
-    D, L = _size(rng, 17, 2048), _size(rng, 1, 12)
-    V = min(_size(rng, 16, 50000), 100_000_000 // D)
-    while L > 1 and L * 12 * D * D > 300_000_000:
+    P, D, L = rng.choice((1, 1, 2)), _size(rng, 17, 2048), _size(rng, 1, 12)
+    V = min(_size(rng, 16, 50000), 90_000_000 // (P * D))
+    while L > 1 and P * L * 12 * D * D > 220_000_000:
         L -= 1
-    return _adamw("", rng.choice((1, 1, 2)), D, L, V, state, grad, copy)
+    return _adamw("", P, D, L, V, state, grad, copy)
 
 
 def _tensors(c):
