@@ -406,6 +406,166 @@ LSGD_API lsgd_status lsgd_bgemm_bf16(const lsgd_bgemm_desc* desc, void* stream);
  * product's bounded waits record LSGD_DEVFLAG_WAIT_TIMEOUT there): LSGD_ERR_DEVICE_FLAG if it was set.  */
 LSGD_API lsgd_status lsgd_bgemm_check_device(uint32_t* flag_out /* HOST, may be NULL */);
 
+/* ------------------------------------------------------------------------------------------------------
+ * Operators of a language model's training step, for populations whose workers are language models: the
+ * embedding lookup and its gradient, the norms at a block boundary and their gradient, and the AdamW step.
+ * The matrix products between them are lsgd_bgemm_bf16's; the leaders' election and pulls are lsgd_elect's and
+ * lsgd_step's (objective EXTERNAL).  Each operator works on all P workers in one call: worker p's token t is
+ * row (p, t).  Conventions as above; the descriptors are HOST structs read during the call, all buffers in them
+ * are DEVICE and the caller's, and work is enqueued on `stream` without synchronising.
+ * ------------------------------------------------------------------------------------------------------ */
+typedef enum {
+  LSGD_F32 = 0,
+  LSGD_BF16 = 1
+} lsgd_dtype;
+
+/* A matrix of rows for every worker: element k of row t of worker p is data[p * stride + t * ld + k], strides in
+ * elements, not negative.  Inputs may repeat rows (ld or stride 0: one table, gain or row for all workers); outputs
+ * may not overlap themselves, except where an entry point says what a stride of 0 means for a gradient.  data is
+ * aligned to its element (LSGD_ERR_ALIGNMENT); rows that start on 16-byte boundaries and hold a multiple of 8 values
+ * are moved 16 bytes at a time.  data == NULL: the matrix is absent.                                            */
+typedef struct {
+  void* data;
+  int64_t ld;                /* elements from one row to the next                                              */
+  int64_t stride;            /* elements from one worker to the next                                           */
+} lsgd_rows;
+
+/* Embedding.  Forward: out[p][t] = scale * table[p][token[p][t]], rounded once.  Backward:
+ *   d_table[p][v] = scale * sum of d_out[p][t] over the t with token[p][t] == v   (+ d_table[p][v] if accumulate),
+ * summed in fp32 in an order fixed by the tokens alone: the same inputs give the same bits.  Without accumulate every
+ * row of d_table is written, rows of absent tokens with zeros.  d_table.stride == 0 with P > 1 (one table shared by all
+ * workers) sums over the workers.  A token outside [0, V) gives a row of zeros, adds to no gradient, and raises
+ * LSGD_DEVFLAG_BAD_INDEX (lsgd_embed_check_device).  T == 0 is legal.                                            */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_embed_desc)                                                       */
+  int32_t P;                 /* workers, >= 1                                                                  */
+  int64_t T;                 /* tokens per worker, >= 0; P T < 2^31 and P V < 2^31 (LSGD_ERR_TOO_LARGE)          */
+  int64_t V;                 /* rows of a table, >= 1                                                          */
+  int32_t D;                 /* values of a row, 1 .. 65536 (LSGD_ERR_UNSUPPORTED beyond)                       */
+  int32_t token_bytes;       /* 4: int32 tokens, 8: int64 tokens                                               */
+  int32_t table_dtype;       /* lsgd_dtype of table and d_table                                                */
+  int32_t act_dtype;         /* lsgd_dtype of out and d_out                                                    */
+  float scale;
+  int32_t accumulate;        /* backward: 0 d_table is overwritten, 1 the gradient is added to it               */
+  int64_t padding;           /* backward: a token whose row gets no gradient; -1: none                         */
+  const void* tokens;        /* [P][T], worker p's first token at element p * token_stride                     */
+  int64_t token_stride;
+  lsgd_rows table, out;      /* forward                                                                        */
+  lsgd_rows d_out, d_table;  /* backward                                                                       */
+  void* scratch;             /* backward: lsgd_embed_scratch_bytes(desc) bytes, 256-byte aligned, contents free */
+  uint64_t scratch_bytes;
+} lsgd_embed_desc;
+LSGD_API uint64_t lsgd_embed_scratch_bytes(const lsgd_embed_desc* desc);   /* 0 for a bad descriptor           */
+LSGD_API lsgd_status lsgd_embed_forward(const lsgd_embed_desc* desc, void* stream);
+LSGD_API lsgd_status lsgd_embed_backward(const lsgd_embed_desc* desc, void* stream);
+/* Synchronises the current device, then reads and clears the status word of the embedding calls on it:
+ * LSGD_ERR_DEVICE_FLAG if it was set.                                                                           */
+LSGD_API lsgd_status lsgd_embed_check_device(uint32_t* flag_out /* HOST, may be NULL */);
+
+/* The norms at the boundary of two blocks, fused with the gate and the scaled residual add between them:
+ *   u  = norm(y) w_post      (post_norm; otherwise u = y)        norm(z) = z / sqrt(mean(z^2) + eps) over a row
+ *   x' = alpha x + beta a(gate) u                                (no gate: x' = alpha x + beta u)
+ *   h  = norm(x') w_pre      (if w_pre is given)
+ * x is the residual stream, y the finished block's output, h the next block's input.  y absent: x' = x, nothing but h
+ * is computed (the first block of a network).  w_pre and h absent: x' only (the last one's end).  All arithmetic is
+ * fp32; out and h are each rounded once (h from the unrounded x').  The forward pass stores 1 / sqrt(...) of both norms
+ * for the backward pass, which reads x' as stored in `out` (with y absent: give x itself as `out`):
+ *   dx' = d_out + d norm / dx' (d_h w_pre),  dx = alpha dx',  dy, d_gate, d_w_post, d_w_pre by the chain rule.
+ * d_out absent counts as zeros.  A weight gradient that is absent is not computed; given with stride 0 and P > 1 it is the
+ * sum over the workers (one gain shared by all).  Sums over rows are fp32 in a fixed order.
+ * out may be x and dx may be d_out (same strides): every value is read before it is overwritten.                */
+typedef enum {
+  LSGD_GATE_NONE = 0,
+  LSGD_GATE_CHANNEL = 1,     /* fp32 [P][D], one value per channel; its gradient is fp32 [P][D]                */
+  LSGD_GATE_TOKEN = 2        /* act_dtype [P][T][D], one value per entry, as is its gradient                   */
+} lsgd_gate;
+typedef enum {
+  LSGD_GATE_IDENTITY = 0,
+  LSGD_GATE_SIGMOID = 1,
+  LSGD_GATE_TANH = 2
+} lsgd_gate_act;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_blocknorm_desc)                                                   */
+  int32_t P;                 /* workers, >= 1                                                                  */
+  int64_t T;                 /* rows per worker, >= 0; P T < 2^31 (LSGD_ERR_TOO_LARGE)                          */
+  int32_t D;                 /* 1 .. 8192 (LSGD_ERR_UNSUPPORTED beyond)                                         */
+  int32_t resid_dtype;       /* lsgd_dtype of x, out, d_out, dx                                                */
+  int32_t act_dtype;         /* lsgd_dtype of y, h, d_h, dy and a token gate; fp32 only with an fp32 residual    */
+  int32_t post_norm;         /* 1: y is normalised (w_post required), 0: it is not                             */
+  int32_t gate_kind;         /* lsgd_gate                                                                      */
+  int32_t gate_act;          /* lsgd_gate_act                                                                  */
+  float alpha, beta;
+  float eps;                 /* > 0                                                                            */
+  int32_t accumulate;        /* backward: 1 adds the gradients of w_post, w_pre and a channel gate to what is there */
+  lsgd_rows x, y, gate;      /* gate: rows (ld unused) per worker for CHANNEL                                  */
+  lsgd_rows w_post, w_pre;   /* fp32 [P][D], ld unused                                                         */
+  lsgd_rows out, h;
+  float* rstd_post;          /* fp32 [P*T], written forward, read backward; needed with post_norm               */
+  float* rstd_pre;           /* fp32 [P*T]; needed with w_pre                                                   */
+  lsgd_rows d_out, d_h;      /* backward inputs                                                                */
+  lsgd_rows dx, dy, d_gate;  /* backward outputs                                                               */
+  lsgd_rows d_w_post, d_w_pre; /* fp32 [P][D], ld unused                                                       */
+  void* scratch;             /* backward: lsgd_blocknorm_scratch_bytes(desc) bytes, 256-byte aligned, contents free */
+  uint64_t scratch_bytes;
+} lsgd_blocknorm_desc;
+LSGD_API uint64_t lsgd_blocknorm_scratch_bytes(const lsgd_blocknorm_desc* desc);   /* 0 for a bad descriptor    */
+LSGD_API lsgd_status lsgd_blocknorm_forward(const lsgd_blocknorm_desc* desc, void* stream);
+LSGD_API lsgd_status lsgd_blocknorm_backward(const lsgd_blocknorm_desc* desc, void* stream);
+
+/* AdamW over many tensors in one launch.  With t counted from 1,
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * Parameters are fp32, as everywhere in this library, with an optional bf16 copy for the matrix products.
+ * Moments live in one buffer each, tensor after tensor, every tensor begun at a multiple of 256 values (its "blocks");
+ * lsgd_adamw_state_values() is their length.  A fresh run starts from zeroed buffers.
+ *   LSGD_STATE_F32   m, v: float[values]
+ *   LSGD_STATE_8BIT  m, v: uint8[values], m_scale, v_scale: float[values / 256], one scale per block.  A code's value is
+ *                    a small float times its block's scale: m has a sign, 4 exponent and 3 fraction bits, v has 5 exponent
+ *                    and 3 fraction bits and no sign (1.875 is the largest, subnormals included), so m / sqrt(v) keeps the
+ *                    same range.  Moments are rounded up or down at random with the right mean: a moving average
+ *                    whose change per step is smaller than a code's spacing would otherwise never move.  The random bits
+ *                    are a hash of (seed, t, position), so a run can be repeated bit for bit.  A second moment that is not
+ *                    zero is never rounded to zero.  A block that holds a moment that is not finite reads as NaN.
+ * lsgd_adamw_create copies the HOST arrays and builds a table of the tensors on the current device (16 bytes per 4096
+ * parameters; the only allocation).  The gradients' addresses are fixed too: keep the buffers from step to step.
+ * The step counter lives on the device, so captured steps replay correctly from a CUDA graph (lr is frozen in it). */
+typedef struct lsgd_adamw_ctx* lsgd_adamw_handle;
+typedef enum {
+  LSGD_STATE_F32 = 0,
+  LSGD_STATE_8BIT = 1
+} lsgd_state_dtype;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_adamw_desc)                                                       */
+  int32_t n_tensors;         /* >= 1                                                                           */
+  const int64_t* sizes;      /* HOST [n_tensors], each >= 0                                                    */
+  float* const* params;      /* HOST [n_tensors] of DEVICE fp32 pointers, updated in place                     */
+  const void* const* grads;  /* HOST [n_tensors] of DEVICE pointers, grad_dtype                                */
+  uint16_t* const* copies;   /* HOST [n_tensors] of DEVICE bf16 pointers (entries may be NULL), or NULL          */
+  const float* weight_decay; /* HOST [n_tensors]                                                               */
+  int32_t grad_dtype;        /* lsgd_dtype                                                                     */
+  int32_t state_dtype;       /* lsgd_state_dtype                                                               */
+  void* m;                   /* DEVICE, 16-byte aligned                                                        */
+  void* v;                   /* DEVICE, 16-byte aligned                                                        */
+  float* m_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
+  float* v_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
+  double beta1, beta2;       /* in [0, 1)                                                                      */
+  double eps;                /* > 0                                                                            */
+  uint32_t seed;             /* LSGD_STATE_8BIT: of the random rounding                                        */
+  void* stream;              /* cudaStream_t; NULL = the legacy default stream                                 */
+} lsgd_adamw_desc;
+LSGD_API int64_t lsgd_adamw_state_values(int32_t n_tensors, const int64_t* sizes /* HOST */);   /* -1: bad sizes */
+LSGD_API lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* out);
+/* One step of every tensor.  lr finite and >= 0.  grad_scale: DEVICE float[1] that every gradient is multiplied by
+ * first (a clipping factor computed on the device), or NULL.                                                    */
+LSGD_API lsgd_status lsgd_adamw_step(lsgd_adamw_handle h, double lr, const float* grad_scale);
+/* The moments as the fp32 values that they stand for: m_out, v_out DEVICE float[values], 16-byte aligned, either may be
+ * NULL.  Values between a tensor's end and its last block's end are undefined for LSGD_STATE_F32's buffers, zero here. */
+LSGD_API lsgd_status lsgd_adamw_moments(lsgd_adamw_handle h, float* m_out, float* v_out);
+/* Steps taken so far.  get synchronises the stream; set (restoring a checkpoint) is enqueued on it.  n in [0, 2^31). */
+LSGD_API lsgd_status lsgd_adamw_get_step(lsgd_adamw_handle h, int64_t* n);
+LSGD_API lsgd_status lsgd_adamw_set_step(lsgd_adamw_handle h, int64_t n);
+LSGD_API lsgd_status lsgd_adamw_destroy(lsgd_adamw_handle h);   /* NULL is accepted                              */
+
 #ifdef __cplusplus
 }
 #endif

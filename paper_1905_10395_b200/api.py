@@ -59,6 +59,43 @@ class BgemmDesc(C.Structure):
                 ("stride_bias", C.c_int64), ("mask", C.c_void_p), ("ld_mask", C.c_int64), ("stride_mask", C.c_int64)]
 
 
+# lsgd_dtype, lsgd_gate, lsgd_gate_act, lsgd_state_dtype
+F32, BF16 = range(2)
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = range(3)
+GATE_IDENTITY, GATE_SIGMOID, GATE_TANH = range(3)
+STATE_F32, STATE_8BIT = range(2)
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("stride", C.c_int64)]
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("T", C.c_int64), ("V", C.c_int64), ("D", C.c_int32),
+                ("token_bytes", C.c_int32), ("table_dtype", C.c_int32), ("act_dtype", C.c_int32), ("scale", C.c_float),
+                ("accumulate", C.c_int32), ("padding", C.c_int64), ("tokens", C.c_void_p), ("token_stride", C.c_int64),
+                ("table", Rows), ("out", Rows), ("d_out", Rows), ("d_table", Rows), ("scratch", C.c_void_p),
+                ("scratch_bytes", C.c_uint64)]
+
+
+class BlocknormDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("T", C.c_int64), ("D", C.c_int32), ("resid_dtype", C.c_int32),
+                ("act_dtype", C.c_int32), ("post_norm", C.c_int32), ("gate_kind", C.c_int32), ("gate_act", C.c_int32),
+                ("alpha", C.c_float), ("beta", C.c_float), ("eps", C.c_float), ("accumulate", C.c_int32), ("x", Rows),
+                ("y", Rows), ("gate", Rows), ("w_post", Rows), ("w_pre", Rows), ("out", Rows), ("h", Rows),
+                ("rstd_post", C.c_void_p), ("rstd_pre", C.c_void_p), ("d_out", Rows), ("d_h", Rows), ("dx", Rows),
+                ("dy", Rows), ("d_gate", Rows), ("d_w_post", Rows), ("d_w_pre", Rows), ("scratch", C.c_void_p),
+                ("scratch_bytes", C.c_uint64)]
+
+
+class AdamwDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_tensors", C.c_int32), ("sizes", C.c_void_p), ("params", C.c_void_p),
+                ("grads", C.c_void_p), ("copies", C.c_void_p), ("weight_decay", C.c_void_p), ("grad_dtype", C.c_int32),
+                ("state_dtype", C.c_int32), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("seed", C.c_uint32), ("stream", C.c_void_p)]
+
+
 class Config(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("G", C.c_int32), ("group_of", C.c_void_p),
                 ("d", C.c_int64), ("ld", C.c_int64), ("eta", C.c_float), ("lambda_l", C.c_float),
@@ -126,6 +163,24 @@ def lib() -> C.CDLL:
         L.lsgd_matcomp_scratch_bytes.restype = C.c_uint64
         L.lsgd_psd_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int64]
         L.lsgd_psd_scratch_bytes.restype = C.c_uint64
+        for name, desc in (("embed", EmbedDesc), ("blocknorm", BlocknormDesc)):
+            f = getattr(L, f"lsgd_{name}_scratch_bytes")
+            f.argtypes, f.restype = [C.POINTER(desc)], C.c_uint64
+            for direction in ("forward", "backward"):
+                f = getattr(L, f"lsgd_{name}_{direction}")
+                f.argtypes, f.restype = [C.POINTER(desc), C.c_void_p], C.c_int
+        L.lsgd_embed_check_device.argtypes = [C.POINTER(C.c_uint32)]
+        L.lsgd_embed_check_device.restype = C.c_int
+        L.lsgd_adamw_state_values.argtypes = [C.c_int32, C.c_void_p]
+        L.lsgd_adamw_state_values.restype = C.c_int64
+        L.lsgd_adamw_create.argtypes = [C.POINTER(AdamwDesc), C.POINTER(H)]
+        L.lsgd_adamw_step.argtypes = [H, C.c_double, C.c_void_p]
+        L.lsgd_adamw_moments.argtypes = [H, C.c_void_p, C.c_void_p]
+        L.lsgd_adamw_get_step.argtypes = [H, C.POINTER(C.c_int64)]
+        L.lsgd_adamw_set_step.argtypes = [H, C.c_int64]
+        L.lsgd_adamw_destroy.argtypes = [H]
+        for name in ("create", "step", "moments", "get_step", "set_step", "destroy"):
+            getattr(L, f"lsgd_adamw_{name}").restype = C.c_int
         for name in ("lsgd_create", "lsgd_grad", "lsgd_elect", "lsgd_step", "lsgd_destroy", "lsgd_get_leaders",
                      "lsgd_get_loss", "lsgd_get_step", "lsgd_get_leader_counts", "lsgd_check_device",
                      "lsgd_set_eta", "lsgd_mlp_param_offsets"):
@@ -193,6 +248,24 @@ def lsgd_bgemm_check_device() -> int:
     if s not in (OK, ERR_DEVICE_FLAG):
         raise LsgdError(s, "lsgd_bgemm_check_device")
     return f.value
+
+
+def lsgd_embed_check_device() -> int:
+    """Status word of the embedding calls on the current device (read and cleared); 0 = no kernel reported anything."""
+    f = C.c_uint32()
+    s = lib().lsgd_embed_check_device(C.byref(f))
+    if s not in (OK, ERR_DEVICE_FLAG):
+        raise LsgdError(s, "lsgd_embed_check_device")
+    return f.value
+
+
+def adamw_state_values(sizes: Sequence[int]) -> int:
+    """Values of the moment buffers of lsgd_adamw: every tensor begins at a multiple of 256."""
+    a = np.ascontiguousarray(sizes, dtype=np.int64)
+    n = int(lib().lsgd_adamw_state_values(len(a), a.ctypes.data))
+    if n < 0:
+        raise LsgdError(ERR_INVALID_ARG, "lsgd_adamw_state_values")
+    return n
 
 
 def mlp_param_offsets(dims: Sequence[int]):

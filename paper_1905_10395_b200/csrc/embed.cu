@@ -1,0 +1,739 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens.
+//
+//     out[p][t] = scale * table[p][token]          d_table[p][v] = scale * sum_{t: token = v} d_out[p][t]
+//
+// Both only move rows: the lookup reads and writes each value once, the gradient reads every row of d_out once and
+// writes every row of d_table once (the rows of absent tokens with zeros).
+//
+// The gradient must not depend on timing, so no row is added with atomics.  Two ways to the same sums:
+//   few tokens   one launch.  The block of position i leaves if an earlier position holds the same token; otherwise it
+//                finds the later ones by comparing all tokens, and adds their rows in order.
+//   many tokens  positions are sorted by (worker, token) with a stable radix sort of at most kDigitBits bits a pass
+//                (a histogram and a scatter launch per pass); a warp then walks a piece of the sorted list, adding rows
+//                while the token stays the same.  A token that lies within one piece is written at once; pieces of a
+//                token that crosses piece ends leave fp32 partial rows, which a last launch adds in order.  Work is
+//                split by positions, never by token, so it stays even however often one token occurs.
+#include "lm_ops.h"
+
+namespace lsgd {
+namespace {
+
+__device__ uint32_t g_embed_status;      // LSGD_DEVFLAG_BAD_INDEX, read and cleared by lsgd_embed_check_device
+
+constexpr int kMaxD = 65536;
+constexpr uint32_t kNone = 0xFFFFFFFFu;  // key of a position that adds to no row
+
+struct Tokens {
+  const void* p;
+  int64_t stride;
+  int64_t V, padding;
+  uint32_t T, N;
+  uint32_t key_stride;                   // V, or 0 where all workers share one table's gradient
+  int bytes;
+  __device__ __forceinline__ int64_t token(uint32_t worker, uint32_t t) const {
+    const int64_t i = worker * stride + t;
+    return bytes == 8 ? static_cast<const int64_t*>(p)[i] : (int64_t) static_cast<const int32_t*>(p)[i];
+  }
+  // (worker, token) as one number, or kNone
+  __device__ __forceinline__ uint32_t key(uint32_t pos) const {
+    const uint32_t w = pos / T, t = pos - w * T;
+    const int64_t v = token(w, t);
+    if (v < 0 || v >= V) {
+      atomicOr(&g_embed_status, FLAG_BAD_INDEX);
+      return kNone;
+    }
+    return v == padding ? kNone : w * key_stride + (uint32_t)v;
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ lookup
+constexpr int kLookupThreads = 256;
+constexpr int kLookupRows = 4;           // rows whose loads a thread issues before the first store
+
+template <typename TT, typename TA, int VEC>
+__global__ void __launch_bounds__(kLookupThreads)
+embed_lookup_kernel(Tokens tok, Rows<const TT> table, Rows<TA> out, uint32_t nvec, uint32_t tx, float scale) {
+  pdl_wait();
+  const uint32_t ty = kLookupThreads / tx;
+  const uint32_t cx = threadIdx.x % tx, ry = threadIdx.x / tx;
+  const uint32_t base = (blockIdx.x * ty + ry) * kLookupRows;
+  const TT* src[kLookupRows];
+  TA* dst[kLookupRows];
+#pragma unroll
+  for (int u = 0; u < kLookupRows; ++u) {
+    src[u] = nullptr;
+    dst[u] = nullptr;
+    const uint32_t pos = base + u;
+    if (pos < tok.N) {
+      const uint32_t w = pos / tok.T, t = pos - w * tok.T;
+      const int64_t v = tok.token(w, t);
+      dst[u] = out.row(w, t);
+      if (v >= 0 && v < tok.V) src[u] = table.p + w * table.stride + v * table.ld;
+      else if (cx == 0 && blockIdx.y == 0) atomicOr(&g_embed_status, FLAG_BAD_INDEX);
+    }
+  }
+  for (uint32_t c = blockIdx.y * tx + cx; c < nvec; c += gridDim.y * tx) {
+    Pack<TT, VEC> in[kLookupRows];
+#pragma unroll
+    for (int u = 0; u < kLookupRows; ++u)
+      if (src[u]) in[u].load(src[u] + (int64_t)c * VEC);
+#pragma unroll
+    for (int u = 0; u < kLookupRows; ++u) {
+      if (!dst[u]) continue;
+      float f[VEC];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f[k] = 0.f;
+      if (src[u]) {
+        in[u].get(f);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] *= scale;
+      }
+      Pack<TA, VEC> o;
+      o.set(f);
+      o.store(dst[u] + (int64_t)c * VEC);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows of the gradient
+constexpr int kSlab = 256;               // columns that one warp carries: 8 values a lane
+
+template <typename TG>
+struct GradRows {
+  TG* p;
+  int64_t ld, stride;
+  uint32_t key_stride;
+  __device__ __forceinline__ TG* row(uint32_t key) const {
+    const uint32_t w = key_stride ? key / key_stride : 0;
+    return p + w * stride + (int64_t)(key - w * key_stride) * ld;
+  }
+};
+
+// A lane's 8 columns of a slab: one piece of 8, or pieces of VEC that are 32 VEC columns apart.
+template <int VEC>
+__device__ __forceinline__ int slab_col(int slab, int lane, int i) { return slab * kSlab + i * 32 * VEC + lane * VEC; }
+
+template <typename TG, int VEC>
+__device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, const float* acc, float scale, bool add) {
+#pragma unroll
+  for (int i = 0; i < 8 / VEC; ++i) {
+    const int col = slab_col<VEC>(slab, lane, i);
+    if (col >= D) break;
+    float f[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) f[k] = acc[i * VEC + k] * scale;
+    if (add) {
+      Pack<TG, VEC> o;
+      o.load(row + col);
+      float e[VEC];
+      o.get(e);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f[k] += e[k];
+    }
+    Pack<TG, VEC> o;
+    o.set(f);
+    o.store(row + col);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ few tokens
+constexpr int kFewTokens = 1024;
+constexpr int kFewThreads = 256;
+constexpr int kFewWarps = kFewThreads / 32;
+
+template <typename TG, typename TA, int VEC>
+__global__ void __launch_bounds__(kFewThreads)
+embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint32_t rows, uint32_t rows_per_block, int D,
+                      float scale, bool add) {
+  pdl_wait();
+  __shared__ uint32_t s_bits[kFewTokens / 32];
+  __shared__ float s_part[kFewWarps][kSlab];
+  __shared__ uint32_t s_none;
+  const int slab = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x >= tok.N) {             // rows of absent tokens: zeros
+    const uint32_t r0 = (blockIdx.x - tok.N) * rows_per_block;
+    const uint32_t n = min(rows_per_block, rows - r0);
+    for (uint32_t i = threadIdx.x; i < kFewTokens / 32; i += kFewThreads) s_bits[i] = 0;
+    __syncthreads();
+    for (uint32_t j = threadIdx.x; j < tok.N; j += kFewThreads) {
+      const uint32_t k = tok.key(j);
+      if (k >= r0 && k - r0 < n) atomicOr(&s_bits[(k - r0) >> 5], 1u << ((k - r0) & 31));
+    }
+    __syncthreads();
+    const float zero[8] = {};
+    for (uint32_t r = warp; r < n; r += kFewWarps)
+      if (!(s_bits[r >> 5] >> (r & 31) & 1)) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
+    return;
+  }
+  const uint32_t mine = tok.key(blockIdx.x);
+  if (mine == kNone) return;
+  if (threadIdx.x == 0) s_none = 0;
+  __syncthreads();
+  const uint32_t words = (tok.N + 31) / 32;
+  bool earlier = false;
+  for (uint32_t w = warp; w < words; w += kFewWarps) {
+    const uint32_t j = w * 32 + lane;
+    const bool same = j < tok.N && tok.key(j) == mine;
+    earlier |= same && j < blockIdx.x;
+    const uint32_t bits = __ballot_sync(0xFFFFFFFFu, same);
+    if (lane == 0) s_bits[w] = bits;
+  }
+  if (__syncthreads_or(earlier)) return;
+  // each warp adds the rows of a run of words; the runs are added in order
+  const uint32_t per = (words + kFewWarps - 1) / kFewWarps;
+  float acc[8] = {};
+  bool any = false;
+  for (uint32_t w = warp * per; w < min(words, (warp + 1) * per); ++w) {
+    uint32_t bits = s_bits[w];
+    any |= bits != 0;
+    while (bits) {
+      constexpr int U = 4;
+      Pack<TA, VEC> in[U][8 / VEC];
+      int n = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!bits) break;
+        const uint32_t pos = w * 32 + __ffs(bits) - 1;
+        bits &= bits - 1;
+        ++n;
+        const uint32_t p = pos / tok.T;
+        const TA* row = d_out.row(p, pos - p * tok.T);
+#pragma unroll
+        for (int i = 0; i < 8 / VEC; ++i)
+          if (slab_col<VEC>(slab, lane, i) < D) in[u][i].load(row + slab_col<VEC>(slab, lane, i));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u >= n) break;
+#pragma unroll
+        for (int i = 0; i < 8 / VEC; ++i) {
+          if (slab_col<VEC>(slab, lane, i) >= D) break;
+          float f[VEC];
+          in[u][i].get(f);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) acc[i * VEC + k] += f[k];
+        }
+      }
+    }
+  }
+  if (any) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s_part[warp][k * 32 + lane] = acc[k];
+    if (lane == 0) atomicOr(&s_none, 1u << warp);
+  }
+  __syncthreads();
+  if (warp != 0) return;
+  const uint32_t have = s_none;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float a = 0.f;
+    for (int w = 0; w < kFewWarps; ++w)
+      if (have >> w & 1) a += s_part[w][k * 32 + lane];
+    acc[k] = a;
+  }
+  write_row<TG, VEC>(grad.row(mine), slab, lane, D, acc, scale, add);
+}
+
+// ------------------------------------------------------------------------------------------------ sort
+constexpr int kDigitBits = 10;
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 4;                                  // keys a thread holds
+constexpr int kSortTile = kSortThreads * kSortItems;           // 2048
+constexpr int kMaxTiles = 128;
+
+struct SortPass {
+  const uint32_t* key_in;     // nullptr: keys are made from the tokens, positions count from 0
+  const uint32_t* pos_in;
+  uint32_t *key_out, *pos_out;
+  uint32_t* counts;           // [tiles][bins]
+  uint8_t* touched;           // first histogram only: rows that have a token
+  uint32_t N, per_tile, none_key;
+  int shift, bits, tiles;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const Tokens& tok, const SortPass& a, uint32_t i) {
+  if (a.key_in) return a.key_in[i];
+  const uint32_t k = tok.key(i);
+  return k == kNone ? a.none_key : k;      // past every row: sorted last
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+embed_histogram_kernel(Tokens tok, SortPass a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ uint32_t s_hist[];
+  const uint32_t bins = 1u << a.bits;
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) s_hist[b] = 0;
+  __syncthreads();
+  const uint32_t i0 = blockIdx.x * a.per_tile, i1 = min(a.N, i0 + a.per_tile);
+  for (uint32_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) {
+    const uint32_t k = sort_key(tok, a, i);
+    if (a.touched && k != a.none_key) a.touched[k] = 1;
+    atomicAdd(&s_hist[(k >> a.shift) & (bins - 1)], 1u);
+  }
+  __syncthreads();
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) a.counts[(size_t)blockIdx.x * bins + b] = s_hist[b];
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+embed_scatter_kernel(Tokens tok, SortPass a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ uint32_t smem[];
+  const uint32_t bins = 1u << a.bits;
+  uint32_t* s_base = smem;                                                   // [bins] next place of each digit
+  uint16_t* s_cnt = reinterpret_cast<uint16_t*>(smem + bins);                // [warps][bins]
+  __shared__ uint32_t s_warp[kSortWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+
+  // first place of each digit in this tile: all smaller digits, and this digit in earlier tiles
+  const uint32_t per = (bins + kSortThreads - 1) / kSortThreads;             // bins a thread owns, 1 or 2
+  uint32_t total[2] = {0, 0}, before[2] = {0, 0};
+  for (uint32_t q = 0; q < per; ++q) {
+    const uint32_t b = threadIdx.x * per + q;
+    if (b < bins) {
+      for (int t = 0; t < a.tiles; ++t) {
+        const uint32_t n = a.counts[(size_t)t * bins + b];
+        total[q] += n;
+        if (t < (int)blockIdx.x) before[q] += n;
+      }
+    }
+  }
+  uint32_t sum = total[0] + total[1], incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += n;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  uint32_t start = incl - sum;
+  for (int w = 0; w < warp; ++w) start += s_warp[w];
+  for (uint32_t q = 0; q < per; ++q) {
+    const uint32_t b = threadIdx.x * per + q;
+    if (b < bins) s_base[b] = start + before[q];
+    start += total[q];
+  }
+  __syncthreads();
+
+  const uint32_t i0 = blockIdx.x * a.per_tile, i1 = min(a.N, i0 + a.per_tile);
+  for (uint32_t s = i0; s < i1; s += kSortTile) {
+    for (uint32_t j = threadIdx.x; j < bins * kSortWarps / 2; j += kSortThreads) reinterpret_cast<uint32_t*>(s_cnt)[j] = 0;
+    __syncthreads();
+    uint16_t* cnt = s_cnt + warp * bins;
+    uint32_t key[kSortItems], rank[kSortItems];
+#pragma unroll
+    for (int q = 0; q < kSortItems; ++q) {                                   // a warp's keys are consecutive: the sort is stable
+      const uint32_t i = s + warp * (32 * kSortItems) + q * 32 + lane;
+      key[q] = i < i1 ? sort_key(tok, a, i) : 0;
+    }
+#pragma unroll
+    for (int q = 0; q < kSortItems; ++q) {
+      const uint32_t i = s + warp * (32 * kSortItems) + q * 32 + lane;
+      const uint32_t d = i < i1 ? (key[q] >> a.shift) & (bins - 1) : kNone;
+      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+      uint32_t prev = 0;
+      if (d != kNone) prev = cnt[d];
+      rank[q] = prev + __popc(same & ((1u << lane) - 1));
+      __syncwarp();
+      if (d != kNone && (same >> lane) == 1u) cnt[d] = (uint16_t)(prev + __popc(same));   // the last lane of the group
+      __syncwarp();
+    }
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) {            // running count over the warps
+      uint32_t run = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t n = s_cnt[w * bins + b];
+        s_cnt[w * bins + b] = (uint16_t)run;
+        run += n;
+      }
+      if (b < kSortThreads) total[0] = run;                                  // added to s_base once this sub-tile is written
+      else total[1] = run;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kSortItems; ++q) {
+      const uint32_t i = s + warp * (32 * kSortItems) + q * 32 + lane;
+      if (i < i1) {
+        const uint32_t d = (key[q] >> a.shift) & (bins - 1);
+        const uint32_t at = s_base[d] + cnt[d] + rank[q];
+        a.key_out[at] = key[q];
+        a.pos_out[at] = a.pos_in ? a.pos_in[i] : i;
+      }
+    }
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) s_base[b] += b < kSortThreads ? total[0] : total[1];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sums over the sorted list
+constexpr int kSumThreads = 256;
+constexpr int kSumWarps = kSumThreads / 32;
+
+struct SumArgs {
+  const uint32_t *key, *pos;  // sorted
+  const uint8_t* touched;     // nullptr: rows of absent tokens are left alone
+  float* part;                // [pieces][2][slabs * 256]
+  uint32_t N, T, none_key, rows;
+  uint32_t piece, pieces, slabs;
+  uint32_t sum_blocks, rows_per_block;
+  int D;
+  float scale;
+  bool add;
+};
+
+template <typename TG, typename TA, int VEC>
+__global__ void __launch_bounds__(kSumThreads)
+embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x >= a.sum_blocks) {      // rows of absent tokens: zeros
+    const uint32_t r0 = (blockIdx.x - a.sum_blocks) * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+    const float zero[8] = {};
+    for (uint32_t i = warp; i < (r1 - r0) * a.slabs; i += kSumWarps) {
+      const uint32_t r = r0 + i / a.slabs;
+      if (!a.touched[r]) write_row<TG, VEC>(grad.row(r), (int)(i % a.slabs), lane, a.D, zero, 0.f, false);
+    }
+    return;
+  }
+  const uint32_t item = blockIdx.x * kSumWarps + warp;
+  const uint32_t c = item / a.slabs;
+  const int slab = item - c * a.slabs;
+  if (c >= a.pieces) return;
+  const uint32_t i0 = c * a.piece, i1 = min(a.N, i0 + a.piece);
+  uint32_t cur = a.key[i0];
+  bool inside = i0 == 0 || a.key[i0 - 1] != cur;     // the current token began in this piece
+  float* part = a.part + ((size_t)c * 2 * a.slabs + slab) * kSlab;
+  float acc[8] = {};
+  const auto to_part = [&](int which) {
+    float* o = part + (size_t)which * a.slabs * kSlab;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k * 32 + lane] = acc[k];
+  };
+  constexpr int U = 4;
+  for (uint32_t i = i0; i < i1; i += 32) {
+    const bool live = i + lane < i1;
+    const uint32_t key = live ? a.key[i + lane] : a.none_key;
+    int64_t off = 0;
+    if (live && key != a.none_key) {
+      const uint32_t pos = a.pos[i + lane], p = pos / a.T;
+      off = p * d_out.stride + (int64_t)(pos - p * a.T) * d_out.ld;
+    }
+    const int n = min(32u, i1 - i);
+    for (int j = 0; j < n; j += U) {
+      Pack<TA, VEC> in[U][8 / VEC];
+      uint32_t kk[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int jj = min(j + u, 31);
+        kk[u] = __shfl_sync(0xFFFFFFFFu, key, jj);
+        const int64_t o = __shfl_sync(0xFFFFFFFFu, off, jj);
+        if (j + u < n && kk[u] != a.none_key) {
+          const TA* row = d_out.p + o;
+#pragma unroll
+          for (int i2 = 0; i2 < 8 / VEC; ++i2)
+            if (slab_col<VEC>(slab, lane, i2) < a.D) in[u][i2].load(row + slab_col<VEC>(slab, lane, i2));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (j + u >= n) break;
+        if (kk[u] != cur) {
+          if (inside) write_row<TG, VEC>(grad.row(cur), slab, lane, a.D, acc, a.scale, a.add);
+          else to_part(0);
+          cur = kk[u];
+          inside = true;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+        }
+        if (cur == a.none_key) return;   // the rest of the list adds to no row
+#pragma unroll
+        for (int i2 = 0; i2 < 8 / VEC; ++i2) {
+          if (slab_col<VEC>(slab, lane, i2) >= a.D) break;
+          float f[VEC];
+          in[u][i2].get(f);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) acc[i2 * VEC + k] += f[k];
+        }
+      }
+    }
+  }
+  const bool goes_on = i1 < a.N && a.key[i1] == cur;
+  if (!inside) to_part(0);
+  else if (goes_on) to_part(1);
+  else write_row<TG, VEC>(grad.row(cur), slab, lane, a.D, acc, a.scale, a.add);
+}
+
+// One block per (piece, slab): if a token begins in the piece and goes on in the next ones, its partial rows are added in
+// order -- each warp a run of pieces, then the runs.
+template <typename TG, int VEC>
+__global__ void __launch_bounds__(kSumThreads)
+embed_join_kernel(SumArgs a, GradRows<TG> grad) {
+  pdl_wait();
+  const uint32_t c = blockIdx.x / a.slabs;
+  const int slab = blockIdx.x - c * a.slabs;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t next = (c + 1) * a.piece;           // < N: the last piece has no block
+  const uint32_t k = a.key[next];
+  if (k == a.none_key || a.key[next - 1] != k) return;
+  if (c > 0 && a.key[c * a.piece - 1] == k) return;  // it began earlier
+  uint32_t last = c + 1;                             // last piece that begins with the token
+  for (;;) {
+    const uint32_t q = last + 1 + lane;
+    const bool same = q < a.pieces && a.key[q * a.piece] == k;
+    const uint32_t bits = __ballot_sync(0xFFFFFFFFu, same);
+    last += bits == 0xFFFFFFFFu ? 32 : __ffs(~bits) - 1;
+    if (bits != 0xFFFFFFFFu) break;
+  }
+  __shared__ float s_part[kSumWarps][kSlab];
+  const uint32_t n = last - c + 1;                   // partial rows
+  const uint32_t per = (n + kSumWarps - 1) / kSumWarps;
+  const float* src = a.part + (size_t)slab * kSlab + lane;
+  const size_t row = (size_t)a.slabs * kSlab;
+  float acc[8] = {};
+  const uint32_t j1 = min(n, (warp + 1) * per);
+#pragma unroll 4
+  for (uint32_t j = warp * per; j < j1; ++j) {
+    const float* p = src + ((size_t)(c + j) * 2 + (j == 0)) * row;   // the first piece's end, then whole beginnings
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q] += p[q * 32];
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) s_part[warp][q * 32 + lane] = acc[q];
+  __syncthreads();
+  if (warp != 0) return;
+  const uint32_t used = (n + per - 1) / per;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    float s = 0.f;
+    for (uint32_t w = 0; w < used; ++w) s += s_part[w][q * 32 + lane];
+    acc[q] = s;
+  }
+  write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct SortPlan {
+  uint32_t N, rows, piece, pieces, slabs, per_tile;
+  int passes, bits, tiles;
+  size_t o_touched, o_key[2], o_pos[2], o_counts, o_part, bytes;
+};
+
+SortPlan sort_plan(uint32_t N, uint32_t rows, int D) {
+  SortPlan s{};
+  s.N = N;
+  s.rows = rows;
+  int need = 1;
+  while ((rows >> need) != 0) ++need;      // keys 0 .. rows (rows: no row)
+  s.passes = (need + kDigitBits - 1) / kDigitBits;
+  s.bits = (need + s.passes - 1) / s.passes;
+  const uint32_t sub = (N + kSortTile - 1) / kSortTile;
+  s.per_tile = ((sub + kMaxTiles - 1) / kMaxTiles) * kSortTile;
+  s.tiles = (int)((N + s.per_tile - 1) / s.per_tile);
+  s.slabs = (uint32_t)((D + kSlab - 1) / kSlab);
+  s.piece = 32;
+  while (s.piece < 128 && (uint64_t)(N / (2 * s.piece)) * s.slabs >= 8192) s.piece *= 2;
+  s.pieces = (N + s.piece - 1) / s.piece;
+  size_t off = 0;
+  auto take = [&](size_t b) { size_t o = off; off += (b + 255) & ~size_t(255); return o; };
+  s.o_touched = take(rows);
+  for (int i = 0; i < 2; ++i) {
+    s.o_key[i] = take(sizeof(uint32_t) * (size_t)N);
+    s.o_pos[i] = take(sizeof(uint32_t) * (size_t)N);
+  }
+  s.o_counts = take(sizeof(uint32_t) * ((size_t)s.tiles << s.bits));
+  s.o_part = take(sizeof(float) * 2 * (size_t)s.pieces * s.slabs * kSlab);
+  s.bytes = off;
+  return s;
+}
+
+lsgd_status check_embed(const lsgd_embed_desc* e, bool backward) {
+  if (!e || e->struct_size != sizeof(lsgd_embed_desc)) return LSGD_ERR_INVALID_ARG;
+  if (e->P < 1 || e->T < 0 || e->V < 1 || e->D < 1) return LSGD_ERR_INVALID_ARG;
+  if (e->token_bytes != 4 && e->token_bytes != 8) return LSGD_ERR_INVALID_ARG;
+  if (e->table_dtype < LSGD_F32 || e->table_dtype > LSGD_BF16 || e->act_dtype < LSGD_F32 || e->act_dtype > LSGD_BF16)
+    return LSGD_ERR_INVALID_ARG;
+  if (e->D > kMaxD) return LSGD_ERR_UNSUPPORTED;
+  if (e->T >= (int64_t(1) << 31) / e->P || e->V >= (int64_t(1) << 31) / e->P) return LSGD_ERR_TOO_LARGE;
+  if (e->padding < -1 || e->padding >= e->V || e->token_stride < 0) return LSGD_ERR_INVALID_ARG;
+  if (e->P > 1 && e->token_stride > (int64_t(1) << 56) / e->P) return LSGD_ERR_TOO_LARGE;
+  if (e->T > 0 && !e->tokens) return LSGD_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(e->tokens) % e->token_bytes) return LSGD_ERR_ALIGNMENT;
+  const int tb = elem_bytes(e->table_dtype), ab = elem_bytes(e->act_dtype);
+  lsgd_status st;
+  if (!backward) {
+    if (e->T > 0 && (!e->table.data || !e->out.data)) return LSGD_ERR_INVALID_ARG;
+    if ((st = check_rows(e->table, e->P, e->V, e->D, tb, false)) != LSGD_OK) return st;
+    return check_rows(e->out, e->P, e->T, e->D, ab, true);
+  }
+  if (!e->d_table.data || (e->T > 0 && !e->d_out.data)) return LSGD_ERR_INVALID_ARG;
+  if ((st = check_rows(e->d_out, e->P, e->T, e->D, ab, false)) != LSGD_OK) return st;
+  return check_rows(e->d_table, e->P, e->V, e->D, tb, true, true);
+}
+
+bool shared_grad(const lsgd_embed_desc* e) { return e->P > 1 && e->d_table.stride == 0; }
+
+Tokens tokens_of(const lsgd_embed_desc* e, bool shared) {
+  Tokens t{};
+  t.p = e->tokens;
+  t.stride = e->token_stride;
+  t.V = e->V;
+  t.padding = e->padding;
+  t.T = (uint32_t)(e->T > 0 ? e->T : 1);
+  t.N = (uint32_t)(e->T * e->P);
+  t.key_stride = shared ? 0 : (uint32_t)e->V;
+  t.bytes = e->token_bytes;
+  return t;
+}
+
+template <typename TT, typename TA, int VEC>
+cudaError_t launch_lookup(const lsgd_embed_desc* e, cudaStream_t s) {
+  const Tokens tok = tokens_of(e, false);
+  const uint32_t nvec = (uint32_t)(e->D / VEC);
+  uint32_t tx = 1;
+  while (tx < nvec && tx < kLookupThreads) tx *= 2;
+  const uint32_t rows_per_block = kLookupThreads / tx * kLookupRows;
+  const uint32_t gx = (tok.N + rows_per_block - 1) / rows_per_block;
+  uint32_t gy = (nvec + tx - 1) / tx;      // wide rows: column groups side by side while rows alone do not fill the machine
+  if (gx >= (uint32_t)sm_count() * 8) gy = 1;
+  if (gy > 65535) gy = 65535;
+  return launch_pdl(embed_lookup_kernel<TT, TA, VEC>, dim3(gx, gy), dim3(kLookupThreads), 0, s, tok,
+                    rows_of<const TT>(e->table), rows_of<TA>(e->out), nvec, tx, e->scale);
+}
+
+template <typename TG, typename TA, int VEC>
+cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
+  const bool shared = shared_grad(e);
+  const Tokens tok = tokens_of(e, shared);
+  const uint32_t rows = shared ? (uint32_t)e->V : (uint32_t)(e->V * e->P);
+  const GradRows<TG> grad{static_cast<TG*>(e->d_table.data), e->d_table.ld, e->d_table.stride, tok.key_stride};
+  const Rows<const TA> d_out = rows_of<const TA>(e->d_out);
+  const bool add = e->accumulate != 0;
+  const uint32_t slabs = (uint32_t)((e->D + kSlab - 1) / kSlab);
+  const size_t row_bytes = (size_t)e->D * sizeof(TG);
+  uint32_t rows_per_block = (uint32_t)(65536 / (row_bytes < 64 ? 64 : row_bytes));   // about 64 KiB of zeros a block
+  if (rows_per_block < 1) rows_per_block = 1;
+  if (tok.N <= kFewTokens) {
+    const uint32_t few_rows = kFewTokens;  // bits that a block can mark
+    if (rows_per_block > few_rows) rows_per_block = few_rows;
+    if (rows_per_block < 32) rows_per_block = 32;
+    const uint32_t zero_blocks = add ? 0 : (rows + rows_per_block - 1) / rows_per_block;
+    if (tok.N + zero_blocks == 0) return cudaSuccess;
+    return launch_pdl(embed_grad_few_kernel<TG, TA, VEC>, dim3(tok.N + zero_blocks, slabs), dim3(kFewThreads), 0, s, tok, d_out,
+                      grad, rows, rows_per_block, (int)e->D, e->scale, add);
+  }
+  const SortPlan p = sort_plan(tok.N, rows, e->D);
+  char* w = static_cast<char*>(e->scratch);
+  uint8_t* touched = add ? nullptr : reinterpret_cast<uint8_t*>(w + p.o_touched);
+  cudaError_t err;
+  if (touched && (err = cudaMemsetAsync(touched, 0, rows, s)) != cudaSuccess) return err;
+  const size_t bins = size_t(1) << p.bits;
+  for (int i = 0; i < p.passes; ++i) {
+    SortPass a{};
+    a.key_in = i ? reinterpret_cast<uint32_t*>(w + p.o_key[(i - 1) & 1]) : nullptr;
+    a.pos_in = i ? reinterpret_cast<uint32_t*>(w + p.o_pos[(i - 1) & 1]) : nullptr;
+    a.key_out = reinterpret_cast<uint32_t*>(w + p.o_key[i & 1]);
+    a.pos_out = reinterpret_cast<uint32_t*>(w + p.o_pos[i & 1]);
+    a.counts = reinterpret_cast<uint32_t*>(w + p.o_counts);
+    a.touched = i ? nullptr : touched;
+    a.N = p.N;
+    a.per_tile = p.per_tile;
+    a.none_key = rows;
+    a.shift = i * p.bits;
+    a.bits = p.bits;
+    a.tiles = p.tiles;
+    if ((err = launch_pdl(embed_histogram_kernel, dim3(p.tiles), dim3(kSortThreads), bins * sizeof(uint32_t), s, tok, a)) != cudaSuccess)
+      return err;
+    if ((err = launch_pdl(embed_scatter_kernel, dim3(p.tiles), dim3(kSortThreads),
+                          bins * (sizeof(uint32_t) + kSortWarps * sizeof(uint16_t)), s, tok, a)) != cudaSuccess)
+      return err;
+  }
+  SumArgs a{};
+  a.key = reinterpret_cast<uint32_t*>(w + p.o_key[(p.passes - 1) & 1]);
+  a.pos = reinterpret_cast<uint32_t*>(w + p.o_pos[(p.passes - 1) & 1]);
+  a.touched = touched;
+  a.part = reinterpret_cast<float*>(w + p.o_part);
+  a.N = p.N;
+  a.T = tok.T;
+  a.none_key = rows;
+  a.rows = rows;
+  a.piece = p.piece;
+  a.pieces = p.pieces;
+  a.slabs = slabs;
+  a.sum_blocks = (uint32_t)(((uint64_t)p.pieces * slabs + kSumWarps - 1) / kSumWarps);
+  a.rows_per_block = rows_per_block;
+  a.D = e->D;
+  a.scale = e->scale;
+  a.add = add;
+  const uint32_t zero_blocks = add ? 0 : (rows + rows_per_block - 1) / rows_per_block;
+  if ((err = launch_pdl(embed_sum_kernel<TG, TA, VEC>, dim3(a.sum_blocks + zero_blocks), dim3(kSumThreads), 0, s, a, d_out, grad)) != cudaSuccess)
+    return err;
+  if (p.pieces > 1)
+    return launch_pdl(embed_join_kernel<TG, VEC>, dim3((p.pieces - 1) * slabs), dim3(kSumThreads), 0, s, a, grad);
+  return cudaSuccess;
+}
+
+template <int VEC>
+cudaError_t dispatch(const lsgd_embed_desc* e, bool backward, cudaStream_t s) {
+  using B = __nv_bfloat16;
+  const bool tb = e->table_dtype == LSGD_BF16, ab = e->act_dtype == LSGD_BF16;
+  if (!backward)
+    return tb ? (ab ? launch_lookup<B, B, VEC>(e, s) : launch_lookup<B, float, VEC>(e, s))
+              : (ab ? launch_lookup<float, B, VEC>(e, s) : launch_lookup<float, float, VEC>(e, s));
+  return tb ? (ab ? launch_grad<B, B, VEC>(e, s) : launch_grad<B, float, VEC>(e, s))
+            : (ab ? launch_grad<float, B, VEC>(e, s) : launch_grad<float, float, VEC>(e, s));
+}
+
+cudaError_t embed(const lsgd_embed_desc* e, bool backward, cudaStream_t s) {
+  const int tb = elem_bytes(e->table_dtype), ab = elem_bytes(e->act_dtype);
+  const lsgd_rows &table = backward ? e->d_table : e->table, &act = backward ? e->d_out : e->out;
+  const int vec = min_vec(row_vec(table, e->P, e->V, e->D, tb), row_vec(act, e->P, e->T, e->D, ab));
+  return vec == 8 ? dispatch<8>(e, backward, s) : vec == 2 ? dispatch<2>(e, backward, s) : dispatch<1>(e, backward, s);
+}
+
+}  // namespace
+}  // namespace lsgd
+
+extern "C" {
+
+uint64_t lsgd_embed_scratch_bytes(const lsgd_embed_desc* e) {
+  using namespace lsgd;
+  if (!e || e->struct_size != sizeof(lsgd_embed_desc) || e->P < 1 || e->T < 0 || e->V < 1 || e->D < 1 || e->D > kMaxD) return 0;
+  if (e->T >= (int64_t(1) << 31) / e->P || e->V >= (int64_t(1) << 31) / e->P) return 0;
+  const uint32_t N = (uint32_t)(e->T * e->P);
+  if (N <= kFewTokens) return 0;
+  return sort_plan(N, shared_grad(e) ? (uint32_t)e->V : (uint32_t)(e->V * e->P), e->D).bytes;
+}
+
+lsgd_status lsgd_embed_forward(const lsgd_embed_desc* e, void* stream) {
+  using namespace lsgd;
+  const lsgd_status st = check_embed(e, false);
+  if (st != LSGD_OK) return st;
+  if (e->T == 0) return LSGD_OK;
+  return embed(e, false, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
+}
+
+lsgd_status lsgd_embed_backward(const lsgd_embed_desc* e, void* stream) {
+  using namespace lsgd;
+  const lsgd_status st = check_embed(e, true);
+  if (st != LSGD_OK) return st;
+  const uint64_t need = lsgd_embed_scratch_bytes(e);
+  if (need && (!e->scratch || e->scratch_bytes < need)) return LSGD_ERR_INVALID_ARG;
+  if (need && reinterpret_cast<uintptr_t>(e->scratch) % 256) return LSGD_ERR_ALIGNMENT;
+  return embed(e, true, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
+}
+
+lsgd_status lsgd_embed_check_device(uint32_t* flag_out) {
+  using namespace lsgd;
+  uint32_t f = 0, zero = 0;
+  if (cudaDeviceSynchronize() != cudaSuccess) return LSGD_ERR_CUDA;
+  if (cudaMemcpyFromSymbol(&f, g_embed_status, sizeof(f)) != cudaSuccess) return LSGD_ERR_CUDA;
+  if (f && cudaMemcpyToSymbol(g_embed_status, &zero, sizeof(zero)) != cudaSuccess) return LSGD_ERR_CUDA;
+  if (flag_out) *flag_out = f;
+  return f ? LSGD_ERR_DEVICE_FLAG : LSGD_OK;
+}
+
+}  // extern "C"
