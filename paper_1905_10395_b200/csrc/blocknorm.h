@@ -1,0 +1,639 @@
+// The norms at the boundary of two blocks, with the gate and the scaled residual add between them, in one pass:
+//
+//     u = post_norm ? y r_y w_post : y,   r_y = 1 / sqrt(mean y^2 + eps)
+//     x' = alpha x + beta a(gate) u
+//     h = x' r_x w_pre,                   r_x = 1 / sqrt(mean x'^2 + eps)
+//
+// Backward, with n_x = x' r_x, n_y = y r_y (y without a post norm) and up = d_h w_pre:
+//
+//     g = d_out + r_x (up - n_x mean(up n_x)),    dx = alpha g
+//     d_gate = beta g u a',   s = beta g a w_post,   dy = r_y (s - n_y mean(s n_y))    (no post norm: dy = beta g a)
+//     d_w_pre = sum over rows of d_h n_x,         d_w_post = sum over rows of beta g a n_y
+//
+// A channel gate is a constant of its column, as the gains are: beta, a and w_post are one factor c, and the gradients of
+// w_post and of a channel gate are both that column's sum of g n_y times constants, so one running sum serves both.
+//
+// Memory-bound: every tensor is read or written once, a row stays on the SM from its load to its store.  A thread holds 16
+// values of a row -- two pieces of 8, 'threads per row' pieces apart -- and keeps the same columns for every row, so factors
+// and sums over the rows are its own: factors in its own words of shared memory, sums in registers.  Blocks are persistent
+// (one worker each); short rows share a block, the shortest a warp.  Rows are fetched one ahead by 16-byte asynchronous
+// copies into the copying thread's own words, so nothing but the sums over a row (a butterfly in the warp, one exchange
+// between the row's warps) makes a thread wait for another.  Arithmetic is on pairs (fma.rn.f32x2), the modes are template
+// parameters and addresses are running pointers: issue slots, not memory, bound the first versions of the backward pass.
+//
+// Rows of any length: where rows do not start on 16-byte boundaries but all tensors share their layout, a block takes every
+// 8th row (or a multiple), whose starts all have the same offset phi from a boundary; pieces begin phi columns before the
+// row, so all of them are aligned and only the first and the last hold foreign columns, which are masked.
+#pragma once
+#include <cstring>
+
+#include "lm_ops.h"
+
+namespace lsgd {
+namespace blocknorm {
+
+using bf16 = __nv_bfloat16;
+constexpr int E = 16;        // values of a row that a thread holds, in two halves of 8
+
+struct Args {
+  lsgd_blocknorm_desc d;
+  uint32_t T;
+  int tpr;                   // threads of a row
+  int rpb;                   // rows of a block at a time
+  int stages;                // rows in shared memory: 2, or 1 where two do not fit
+  int phased;                // rows start off 16-byte boundaries
+  float inv_d;
+  uint32_t blocks_w;         // blocks of one worker
+  float* part;               // backward: [P][blocks_w][2][D]
+};
+
+// What a launch computes.  kDirect: any strides, values moved one at a time, the mode read from the arguments.
+enum : int { kPre = 1, kY = 2, kPost = 4, kToken = 8, kDirect = -1 };
+inline __host__ __device__ int mode_of(const lsgd_blocknorm_desc& d) {
+  return (d.w_pre.data ? kPre : 0) | (d.y.data ? kY : 0) | (d.post_norm ? kPost : 0) | (d.gate_kind == LSGD_GATE_TOKEN ? kToken : 0);
+}
+
+// one file per pair of types (residual, activations); mode kDirect or mode_of()
+struct Launch {
+  int threads, mode;
+  size_t smem;
+  bool backward;
+};
+cudaError_t launch_f32_f32(const Args& a, const Launch& l, cudaStream_t s);
+cudaError_t launch_f32_bf16(const Args& a, const Launch& l, cudaStream_t s);
+cudaError_t launch_bf16_bf16(const Args& a, const Launch& l, cudaStream_t s);
+constexpr int kSmemMax = 224 * 1024;      // dynamic shared memory of a block at most
+
+#if defined(LSGD_BLOCKNORM_KERNELS)
+namespace {
+
+// ---- pairs of fp32
+__device__ __forceinline__ unsigned long long bits2(float2 a) { return *reinterpret_cast<unsigned long long*>(&a); }
+__device__ __forceinline__ float2 pair(unsigned long long u) { return *reinterpret_cast<float2*>(&u); }
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return pair(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return pair(r);
+}
+#define LSGD_EACH(k) _Pragma("unroll") for (int k = 0; k < 4; ++k)
+
+// ---- a thread's columns: half h covers col[h] .. col[h] + 7; columns outside [0, D) are foreign
+struct Cols {
+  int col[2], D, gap;
+  bool full[2], any[2];
+  __device__ __forceinline__ Cols(int t, int tpr, int D_, int phi) : D(D_), gap(tpr * 8) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      col[h] = (h * tpr + t) * 8 - phi;
+      full[h] = col[h] >= 0 && col[h] + 8 <= D;
+      any[h] = col[h] + 8 > 0 && col[h] < D;
+    }
+  }
+  __device__ __forceinline__ bool in(int h, int k) const { return (unsigned)(col[h] + k) < (unsigned)D; }
+};
+
+// ---- a thread's own words of shared memory: 16-byte unit u at [warp][u][lane], so units are immediate offsets and a quarter
+// warp is on all banks
+__device__ __forceinline__ uint4* unit_at(unsigned char* own, int u) { return reinterpret_cast<uint4*>(own + u * 512); }
+__device__ __forceinline__ void copy16(void* smem, const void* g) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <typename T>
+constexpr int units() { return (int)sizeof(T) / 2; }   // 16-byte units of a half
+
+template <typename T>
+__device__ __forceinline__ T* row_of(const lsgd_rows& r, uint32_t w, uint32_t t) {
+  return static_cast<T*>(r.data) + w * r.stride + t * r.ld;
+}
+template <typename T>
+__device__ __forceinline__ const T* end_of(const lsgd_rows& r, const Args& a) {
+  return static_cast<const T*>(r.data) + (a.d.P - 1) * r.stride + (int64_t)(a.T - 1) * r.ld + a.d.D;
+}
+
+// Half h of a row, `p` at its first column.  A piece with foreign columns is copied whole where it lies inside the
+// matrix; else its own values one by one.
+template <typename T>
+__device__ __forceinline__ void fetch_half(unsigned char* own, int u, const T* p, const lsgd_rows& r, const Args& a, const Cols& c, int h) {
+  if (!c.any[h]) return;
+  if (c.full[h] || p + 8 <= end_of<T>(r, a)) {
+#pragma unroll
+    for (int i = 0; i < units<T>(); ++i) copy16(unit_at(own, u + i), reinterpret_cast<const char*>(p) + i * 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c.in(h, k)) reinterpret_cast<T*>(unit_at(own, u + k * (int)sizeof(T) / 16))[k % (16 / sizeof(T))] = p[k];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void zero_half(unsigned char* own, int u) {
+#pragma unroll
+  for (int i = 0; i < units<T>(); ++i) *unit_at(own, u + i) = make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void mask(const Cols& c, int h, float2 (&f)[4]) {
+  if (c.full[h]) return;
+  LSGD_EACH(k) {
+    if (!c.in(h, 2 * k)) f[k].x = 0.f;
+    if (!c.in(h, 2 * k + 1)) f[k].y = 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void take_half(unsigned char* own, int u, const Cols& c, int h, float2 (&f)[4]) {
+  uint4 v[units<T>()];
+#pragma unroll
+  for (int i = 0; i < units<T>(); ++i) v[i] = *unit_at(own, u + i);
+  Pack<T, 8> p;
+  static_assert(sizeof(p) == sizeof(v), "");
+  memcpy(&p, v, sizeof(p));
+  p.get(reinterpret_cast<float*>(f));
+  mask(c, h, f);
+}
+template <typename T, bool DIRECT>
+__device__ __forceinline__ void store_half(T* p, const Cols& c, int h, const float2 (&f)[4]) {
+  Pack<T, 8> o;
+  o.set(reinterpret_cast<const float*>(f));
+  if (!DIRECT && c.full[h]) {
+    o.store(p);
+  } else if (c.any[h]) {
+    LSGD_EACH(k) {
+      Pack<T, 1> e;
+      e.set(&f[k].x);
+      if (c.in(h, 2 * k)) e.store(p + 2 * k);
+      e.set(&f[k].y);
+      if (c.in(h, 2 * k + 1)) e.store(p + 2 * k + 1);
+    }
+  }
+}
+
+// fp32 vectors, aligned to their element only; 0 at foreign columns
+__device__ __forceinline__ void vector_half(const float* v, const Cols& c, int h, float2 (&f)[4]) {
+  LSGD_EACH(k) {
+    f[k].x = c.in(h, 2 * k) ? __ldg(v + c.col[h] + 2 * k) : 0.f;
+    f[k].y = c.in(h, 2 * k + 1) ? __ldg(v + c.col[h] + 2 * k + 1) : 0.f;
+  }
+}
+__device__ __forceinline__ void keep_half(unsigned char* own, int u, const float2 (&f)[4]) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    *reinterpret_cast<float4*>(unit_at(own, u + q)) = make_float4(f[2 * q].x, f[2 * q].y, f[2 * q + 1].x, f[2 * q + 1].y);
+}
+__device__ __forceinline__ void kept_half(unsigned char* own, int u, float2 (&f)[4]) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const float4 v = *reinterpret_cast<const float4*>(unit_at(own, u + q));
+    f[2 * q] = make_float2(v.x, v.y);
+    f[2 * q + 1] = make_float2(v.z, v.w);
+  }
+}
+
+// Sum over the threads of a row; every one of them gets it.  s_red: 16 words per row of the block, zero beyond its warps.
+// A row of several warps meets at a named barrier of its own.
+__device__ __forceinline__ float row_sum(float2 a, int tpr, int sub, float* s_red) {
+  float v = a.x + a.y;
+  if (tpr < 32) {
+    for (int o = tpr >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  if (tpr == 32) return v;
+  float* row = s_red + sub * 16;
+  if ((threadIdx.x & 31) == 0) row[((int)threadIdx.x - sub * tpr) >> 5] = v;
+  asm volatile("bar.sync %0, %1;" ::"r"(sub + 1), "r"(tpr) : "memory");
+  const float4* q = reinterpret_cast<const float4*>(row);
+  float s = 0.f;
+  for (int i = 0; i < tpr; i += 128) {
+    const float4 w = *q++;
+    s += (w.x + w.y) + (w.z + w.w);
+  }
+  return s;
+}
+
+__device__ __forceinline__ float gate_value(float z, int act) {
+  if (act == LSGD_GATE_SIGMOID) return __fdividef(1.f, 1.f + __expf(-z));
+  if (act == LSGD_GATE_TANH) return tanhf(z);
+  return z;
+}
+__device__ __forceinline__ float gate_slope(float a, int act) {
+  if (act == LSGD_GATE_SIGMOID) return a * (1.f - a);
+  if (act == LSGD_GATE_TANH) return 1.f - a * a;
+  return 1.f;
+}
+__device__ __forceinline__ void gate_values(float2 (&f)[4], int act) {
+  if (act == LSGD_GATE_IDENTITY) return;
+  LSGD_EACH(k) f[k] = make_float2(gate_value(f[k].x, act), gate_value(f[k].y, act));
+}
+
+__device__ __forceinline__ float* vector_of(const lsgd_rows& r, uint32_t w) { return static_cast<float*>(r.data) + w * r.stride; }
+constexpr int kMaxRowsOfBlock = 4;        // rows of more than one warp that share a block
+constexpr int kRowWords = kMaxRowsOfBlock * 16;
+constexpr int kSums = 4;                  // exchanges in flight: two sums a row, two rows
+constexpr int kFactorUnits = 4;           // 16 fp32 values
+
+// c = beta a(channel gate) w_post at a thread's half
+__device__ __forceinline__ void factor_half(const Args& a, uint32_t w, const Cols& c, int h, bool post, bool channel, float2 (&f)[4]) {
+  LSGD_EACH(k) f[k] = both(a.d.beta);
+  float2 v[4];
+  if (post) {
+    vector_half(vector_of(a.d.w_post, w), c, h, v);
+    LSGD_EACH(k) f[k] = mul2(f[k], v[k]);
+  }
+  if (channel) {
+    vector_half(vector_of(a.d.gate, w), c, h, v);
+    gate_values(v, a.d.gate_act);
+    LSGD_EACH(k) f[k] = mul2(f[k], v[k]);
+  }
+}
+
+// A tensor that rows are read from: fetched ahead into the ring, or read in place.  p: at the first half's first column.
+template <typename T, bool DIRECT>
+struct Input {
+  const T* p;
+  int unit;                               // of the first half within a stage
+  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, const Cols& c, int unit_) {
+    p = row_of<T>(r, w, t) + c.col[0];
+    unit = unit_;
+  }
+  __device__ __forceinline__ void advance(const lsgd_rows& r, uint32_t rows) { p += (int64_t)rows * r.ld; }
+  __device__ __forceinline__ void fetch(const lsgd_rows& r, const Args& a, uint32_t rows, unsigned char* stage, bool live, const Cols& c) {
+    if constexpr (!DIRECT) {
+      if (live) {
+        fetch_half<T>(stage, unit, p, r, a, c, 0);
+        fetch_half<T>(stage, unit + units<T>(), p + c.gap, r, a, c, 1);
+        advance(r, rows);
+      } else {
+        zero_half<T>(stage, unit);
+        zero_half<T>(stage, unit + units<T>());
+      }
+    }
+  }
+  __device__ __forceinline__ void get(unsigned char* stage, bool live, const Cols& c, int h, float2 (&f)[4]) const {
+    if constexpr (!DIRECT) {
+      take_half<T>(stage, unit + h * units<T>(), c, h, f);
+    } else {
+      const T* q = p + h * c.gap;
+      LSGD_EACH(k) {
+        Pack<T, 1> e;
+        f[k] = both(0.f);
+        if (live && c.in(h, 2 * k)) { e.load(q + 2 * k); e.get(&f[k].x); }
+        if (live && c.in(h, 2 * k + 1)) { e.load(q + 2 * k + 1); e.get(&f[k].y); }
+      }
+    }
+  }
+};
+template <typename T, bool DIRECT>
+struct Output {
+  T* p;
+  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, const Cols& c) { p = row_of<T>(r, w, t) + c.col[0]; }
+  __device__ __forceinline__ void put(const Cols& c, int h, const float2 (&f)[4]) { store_half<T, DIRECT>(p + h * c.gap, c, h, f); }
+  __device__ __forceinline__ void advance(const lsgd_rows& r, uint32_t rows) { p += (int64_t)rows * r.ld; }
+};
+
+// Blocks: blockIdx.y = worker; block b of a worker takes its rows b rpb .., then those blocks_w rpb further on.
+template <typename TR, typename TA, int MODE>
+__global__ void __launch_bounds__(512, 1)
+forward_kernel(const __grid_constant__ Args a) {
+  constexpr bool DIRECT = MODE == kDirect;
+  pdl_wait();
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ __align__(16) float s_red[kSums * kRowWords];
+  const lsgd_blocknorm_desc& d = a.d;
+  const int mode = DIRECT ? mode_of(d) : MODE;
+  const bool pre = mode & kPre, has_y = mode & kY, post = mode & kPost, token = mode & kToken;
+  const bool channel = has_y && d.gate_kind == LSGD_GATE_CHANNEL;
+  const int sub = threadIdx.x / a.tpr;
+  const uint32_t w = blockIdx.y, step = a.blocks_w * a.rpb;
+  uint32_t t = blockIdx.x * a.rpb + sub;
+  const int phi = a.phased ? (int)((w * (uint64_t)d.x.stride + t * (uint64_t)d.x.ld) & 7) : 0;
+  const Cols c((int)threadIdx.x - sub * a.tpr, a.tpr, d.D, phi);
+  const int n_x = 2 * units<TR>(), n_y = has_y ? 2 * units<TA>() : 0, n_g = token ? 2 * units<TA>() : 0;
+  const int factors = (pre ? kFactorUnits : 0) + (has_y ? kFactorUnits : 0), u_c = pre ? kFactorUnits : 0;
+  const int stage = n_x + n_y + n_g;
+  unsigned char* own = smem + (threadIdx.x >> 5) * (factors + (DIRECT ? 0 : a.stages * stage)) * 512 + (threadIdx.x & 31) * 16;
+  unsigned char* ring = own + factors * 512;
+  for (int i = threadIdx.x; i < kSums * kRowWords; i += blockDim.x) s_red[i] = 0.f;
+  Input<TR, DIRECT> ix;
+  Input<TA, DIRECT> iy, ig;
+  Output<TR, DIRECT> ox;
+  Output<TA, DIRECT> oh;
+  ix.open(d.x, w, t, c, 0);
+  if (has_y) iy.open(d.y, w, t, c, n_x), ox.open(d.out, w, t, c);
+  if (token) ig.open(d.gate, w, t, c, n_x + n_y);
+  if (pre) oh.open(d.h, w, t, c);
+  const auto fetch = [&](uint32_t row, unsigned char* to) {
+    const bool live = row < a.T;
+    ix.fetch(d.x, a, step, to, live, c);
+    if (has_y) iy.fetch(d.y, a, step, to, live, c);
+    if (token) ig.fetch(d.gate, a, step, to, live, c);
+    copy_commit();
+  };
+  fetch(t, ring);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float2 f[4];
+    if (pre) {
+      vector_half(vector_of(d.w_pre, w), c, h, f);
+      keep_half(own, 2 * h, f);
+    }
+    if (has_y) {
+      factor_half(a, w, c, h, post, channel, f);
+      keep_half(own, u_c + 2 * h, f);
+    }
+  }
+  __syncthreads();
+  int slot = 0, phase = 0;
+  for (uint32_t t0 = blockIdx.x * a.rpb; t0 < a.T; t0 += step, t += step, phase ^= 2) {
+    const bool live = t < a.T;
+    unsigned char* in = ring + slot * stage * 512;
+    if (a.stages == 2) {
+      slot ^= 1;
+      fetch(t + step, ring + slot * stage * 512);
+      copy_wait<1>();
+    } else {
+      copy_wait<0>();
+    }
+    float2 x[2][4];
+    ix.get(in, live, c, 0, x[0]);
+    ix.get(in, live, c, 1, x[1]);
+    if (has_y) {
+      float2 y[2][4];
+      iy.get(in, live, c, 0, y[0]);
+      iy.get(in, live, c, 1, y[1]);
+      float rs = 1.f;
+      if (post) {
+        float2 q = both(0.f);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) LSGD_EACH(k) q = fma2(y[h][k], y[h][k], q);
+        rs = rsqrtf(row_sum(q, a.tpr, sub, s_red + phase * kRowWords) * a.inv_d + d.eps);
+        if (live && (int)threadIdx.x == sub * a.tpr) d.rstd_post[(size_t)w * a.T + t] = rs;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float2 f[4];
+        if (token) {
+          ig.get(in, live, c, h, f);
+          gate_values(f, d.gate_act);
+          LSGD_EACH(k) y[h][k] = mul2(y[h][k], f[k]);
+        }
+        kept_half(own, u_c + 2 * h, f);
+        if (post) {
+          LSGD_EACH(k) y[h][k] = mul2(y[h][k], both(rs));
+        }
+        LSGD_EACH(k) x[h][k] = fma2(f[k], y[h][k], mul2(both(d.alpha), x[h][k]));
+        if (live) ox.put(c, h, x[h]);
+      }
+      ox.advance(d.out, step);
+    }
+    if (pre) {
+      float2 q = both(0.f);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) LSGD_EACH(k) q = fma2(x[h][k], x[h][k], q);
+      const float rs = rsqrtf(row_sum(q, a.tpr, sub, s_red + (phase + 1) * kRowWords) * a.inv_d + d.eps);
+      if (live && (int)threadIdx.x == sub * a.tpr) d.rstd_pre[(size_t)w * a.T + t] = rs;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float2 f[4];
+        kept_half(own, 2 * h, f);
+        LSGD_EACH(k) x[h][k] = mul2(mul2(x[h][k], both(rs)), f[k]);
+        if (live) oh.put(c, h, x[h]);
+      }
+      oh.advance(d.h, step);
+    }
+    if (DIRECT) {
+      ix.advance(d.x, step);
+      iy.advance(d.y, step);
+      ig.advance(d.gate, step);
+    } else if (a.stages == 1) {
+      fetch(t + step, ring);
+    }
+  }
+  copy_wait<0>();
+}
+
+template <typename TR, typename TA, int MODE>
+__global__ void __launch_bounds__(512, 1)
+backward_kernel(const __grid_constant__ Args a) {
+  constexpr bool DIRECT = MODE == kDirect;
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ __align__(16) float s_red[kSums * kRowWords];
+  const lsgd_blocknorm_desc& d = a.d;
+  const int mode = DIRECT ? mode_of(d) : MODE;
+  const bool pre = mode & kPre, has_y = mode & kY, post = mode & kPost, token = mode & kToken;
+  const bool channel = has_y && d.gate_kind == LSGD_GATE_CHANNEL, has_d = d.d_out.data != nullptr;
+  const int sub = threadIdx.x / a.tpr;
+  const uint32_t w = blockIdx.y, step = a.blocks_w * a.rpb;
+  uint32_t t = blockIdx.x * a.rpb + sub;
+  const int phi = a.phased ? (int)((w * (uint64_t)d.dx.stride + t * (uint64_t)d.dx.ld) & 7) : 0;
+  const Cols c((int)threadIdx.x - sub * a.tpr, a.tpr, d.D, phi);
+  // a stage: d_out, out, d_h, y, gate
+  const int u_out = 2 * units<TR>(), u_dh = u_out + (pre ? 2 * units<TR>() : 0), u_y = u_dh + (pre ? 2 * units<TA>() : 0);
+  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), stage = u_g + (token ? 2 * units<TA>() : 0);
+  const int factors = (pre ? kFactorUnits : 0) + (has_y ? kFactorUnits : 0), u_c = pre ? kFactorUnits : 0;
+  unsigned char* own = smem + (threadIdx.x >> 5) * (factors + (DIRECT ? 0 : a.stages * stage)) * 512 + (threadIdx.x & 31) * 16;
+  unsigned char* ring = own + factors * 512;
+  for (int i = threadIdx.x; i < kSums * kRowWords; i += blockDim.x) s_red[i] = 0.f;
+  Input<TR, DIRECT> id, io;
+  Input<TA, DIRECT> ih, iy, ig;
+  Output<TR, DIRECT> ox;
+  Output<TA, DIRECT> oy, og;
+  ox.open(d.dx, w, t, c);
+  if (has_d) id.open(d.d_out, w, t, c, 0);
+  if (pre) io.open(d.out, w, t, c, u_out), ih.open(d.d_h, w, t, c, u_dh);
+  if (has_y) iy.open(d.y, w, t, c, u_y), oy.open(d.dy, w, t, c);
+  if (token) ig.open(d.gate, w, t, c, u_g), og.open(d.d_gate, w, t, c);
+  const auto fetch = [&](uint32_t row, unsigned char* to) {
+    const bool live = row < a.T;
+    if (has_d) id.fetch(d.d_out, a, step, to, live, c);
+    if (pre) {
+      io.fetch(d.out, a, step, to, live, c);
+      ih.fetch(d.d_h, a, step, to, live, c);
+    }
+    if (has_y) iy.fetch(d.y, a, step, to, live, c);
+    if (token) ig.fetch(d.gate, a, step, to, live, c);
+    copy_commit();
+  };
+  fetch(t, ring);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float2 f[4];
+    if (pre) {
+      vector_half(vector_of(d.w_pre, w), c, h, f);
+      keep_half(own, 2 * h, f);
+    }
+    if (has_y) {
+      factor_half(a, w, c, h, post, channel, f);
+      keep_half(own, u_c + 2 * h, f);
+    }
+  }
+  __syncthreads();
+  float2 sum_pre[2][4], sum_y[2][4];      // of d_h n_x and of g (a) n_y
+#pragma unroll
+  for (int h = 0; h < 2; ++h) LSGD_EACH(k) sum_pre[h][k] = sum_y[h][k] = both(0.f);
+  int slot = 0, phase = 0;
+  for (uint32_t t0 = blockIdx.x * a.rpb; t0 < a.T; t0 += step, t += step, phase ^= 2) {
+    const bool live = t < a.T;
+    const size_t r = (size_t)w * a.T + t;
+    // n: normalised rows; up: what arrives at them times the gain -- of the second norm first, then of the first
+    float2 n[2][4], up[2][4];
+    float rs = 0.f, mean = 0.f, rs_y = 0.f;
+    if (pre) rs = live ? d.rstd_pre[r] : 0.f;
+    if (post) rs_y = live ? d.rstd_post[r] : 0.f;
+    unsigned char* in = ring + slot * stage * 512;
+    if (a.stages == 2) {
+      slot ^= 1;
+      fetch(t + step, ring + slot * stage * 512);
+      copy_wait<1>();
+    } else {
+      copy_wait<0>();
+    }
+    if (pre) {
+      float2 q = both(0.f);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float2 f[4];
+        io.get(in, live, c, h, n[h]);
+        ih.get(in, live, c, h, up[h]);
+        kept_half(own, 2 * h, f);
+        LSGD_EACH(k) {
+          n[h][k] = mul2(n[h][k], both(rs));
+          sum_pre[h][k] = fma2(up[h][k], n[h][k], sum_pre[h][k]);
+          up[h][k] = mul2(up[h][k], f[k]);
+          q = fma2(up[h][k], n[h][k], q);
+        }
+      }
+      mean = -rs * (row_sum(q, a.tpr, sub, s_red + phase * kRowWords) * a.inv_d);
+    }
+    float2 q = both(0.f);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float2 g[4];                        // d_out, then the gradient of x'
+      LSGD_EACH(k) g[k] = both(0.f);
+      if (has_d) id.get(in, live, c, h, g);
+      if (pre) {
+        LSGD_EACH(k) g[k] = fma2(n[h][k], both(mean), fma2(up[h][k], both(rs), g[k]));
+      }
+      float2 b[4];
+      LSGD_EACH(k) b[k] = has_y ? mul2(both(d.alpha), g[k]) : g[k];
+      if (live) ox.put(c, h, b);
+      if (!has_y) continue;
+      iy.get(in, live, c, h, n[h]);
+      if (post) {
+        LSGD_EACH(k) n[h][k] = mul2(n[h][k], both(rs_y));
+      }
+      float2 f[4];
+      kept_half(own, u_c + 2 * h, f);
+      if (token) {
+        ig.get(in, live, c, h, b);
+        gate_values(b, d.gate_act);
+        LSGD_EACH(k) {
+          const float2 av = b[k];
+          b[k] = mul2(mul2(mul2(g[k], n[h][k]), f[k]), make_float2(gate_slope(av.x, d.gate_act), gate_slope(av.y, d.gate_act)));
+          g[k] = mul2(g[k], av);
+        }
+        if (live) og.put(c, h, b);
+      }
+      LSGD_EACH(k) {
+        sum_y[h][k] = fma2(g[k], n[h][k], sum_y[h][k]);
+        up[h][k] = mul2(g[k], f[k]);
+        q = fma2(up[h][k], n[h][k], q);
+      }
+      if (!post && live) oy.put(c, h, up[h]);
+    }
+    if (post) {
+      mean = -rs_y * (row_sum(q, a.tpr, sub, s_red + (phase + 1) * kRowWords) * a.inv_d);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        LSGD_EACH(k) up[h][k] = fma2(n[h][k], both(mean), mul2(up[h][k], both(rs_y)));
+        if (live) oy.put(c, h, up[h]);
+      }
+    }
+    ox.advance(d.dx, step);
+    oy.advance(d.dy, step);
+    og.advance(d.d_gate, step);
+    if (DIRECT) {
+      id.advance(d.d_out, step);
+      io.advance(d.out, step);
+      ih.advance(d.d_h, step);
+      iy.advance(d.y, step);
+      ig.advance(d.gate, step);
+    } else if (a.stages == 1) {
+      fetch(t + step, ring);
+    }
+  }
+  copy_wait<0>();
+  // one partial row per block for the two sums
+  float* s_sum = reinterpret_cast<float*>(smem);       // [rpb][D]
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const bool want = j == 0 ? pre && d.d_w_pre.data : (post && d.d_w_post.data) || (channel && d.d_gate.data);
+    if (!want) continue;
+    float* part = a.part + (((size_t)w * a.blocks_w + blockIdx.x) * 2 + j) * d.D;
+    float* dst = part;
+    if (a.rpb > 1) {
+      __syncthreads();                    // the factors and the previous sum have been read
+      dst = s_sum + sub * d.D;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) LSGD_EACH(k) {
+      const float2 v = j == 0 ? sum_pre[h][k] : sum_y[h][k];
+      if (c.in(h, 2 * k)) dst[c.col[h] + 2 * k] = v.x;
+      if (c.in(h, 2 * k + 1)) dst[c.col[h] + 2 * k + 1] = v.y;
+    }
+    if (a.rpb > 1) {                      // add the block's rows in order
+      __syncthreads();
+      for (int col = threadIdx.x; col < d.D; col += blockDim.x) {
+        float v = 0.f;
+        for (int q = 0; q < a.rpb; ++q) v += s_sum[q * d.D + col];
+        part[col] = v;
+      }
+    }
+  }
+}
+
+template <typename TR, typename TA, int MODE>
+cudaError_t launch_mode(const Args& a, const Launch& l, cudaStream_t s) {
+  static OncePerDevice once;
+  if (!once.here()) {
+    cudaError_t e = cudaFuncSetAttribute(forward_kernel<TR, TA, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(backward_kernel<TR, TA, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+    if (e != cudaSuccess) return e;
+    once.here() = true;
+  }
+  const dim3 grid(a.blocks_w, a.d.P), block(l.threads);
+  return l.backward ? launch_pdl(backward_kernel<TR, TA, MODE>, grid, block, l.smem, s, a)
+                    : launch_pdl(forward_kernel<TR, TA, MODE>, grid, block, l.smem, s, a);
+}
+
+template <typename TR, typename TA>
+cudaError_t launch_types(const Args& a, const Launch& l, cudaStream_t s) {
+  switch (l.mode) {
+    case kPre: return launch_mode<TR, TA, kPre>(a, l, s);
+    case kY: return launch_mode<TR, TA, kY>(a, l, s);
+    case kY | kPre: return launch_mode<TR, TA, kY | kPre>(a, l, s);
+    case kY | kPost: return launch_mode<TR, TA, kY | kPost>(a, l, s);
+    case kY | kPost | kPre: return launch_mode<TR, TA, kY | kPost | kPre>(a, l, s);
+    case kY | kToken: return launch_mode<TR, TA, kY | kToken>(a, l, s);
+    case kY | kToken | kPre: return launch_mode<TR, TA, kY | kToken | kPre>(a, l, s);
+    case kY | kToken | kPost: return launch_mode<TR, TA, kY | kToken | kPost>(a, l, s);
+    case kY | kToken | kPost | kPre: return launch_mode<TR, TA, kY | kToken | kPost | kPre>(a, l, s);
+    default: return launch_mode<TR, TA, kDirect>(a, l, s);
+  }
+}
+
+}  // namespace
+#endif  // LSGD_BLOCKNORM_KERNELS
+
+}  // namespace blocknorm
+}  // namespace lsgd
