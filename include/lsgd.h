@@ -422,8 +422,8 @@ typedef enum {
 /* A matrix of rows for every worker: element k of row t of worker p is data[p * stride + t * ld + k], strides in
  * elements, not negative.  Inputs may repeat rows (ld or stride 0: one table, gain or row for all workers); outputs
  * may not overlap themselves, except where an entry point says what a stride of 0 means for a gradient.  data is
- * aligned to its element (LSGD_ERR_ALIGNMENT); rows that start on 16-byte boundaries and hold a multiple of 8 values
- * are moved 16 bytes at a time.  data == NULL: the matrix is absent.                                            */
+ * aligned to its element (LSGD_ERR_ALIGNMENT); rows that start on multiples of 8 values are moved 8 values at a
+ * time.  data == NULL: the matrix is absent.                                            */
 typedef struct {
   void* data;
   int64_t ld;                /* elements from one row to the next                                              */
@@ -544,8 +544,8 @@ typedef struct {
   const float* weight_decay; /* HOST [n_tensors]                                                               */
   int32_t grad_dtype;        /* lsgd_dtype                                                                     */
   int32_t state_dtype;       /* lsgd_state_dtype                                                               */
-  void* m;                   /* DEVICE, 16-byte aligned                                                        */
-  void* v;                   /* DEVICE, 16-byte aligned                                                        */
+  void* m;                   /* DEVICE, 32-byte aligned                                                        */
+  void* v;                   /* DEVICE, 32-byte aligned                                                        */
   float* m_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   float* v_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   double beta1, beta2;       /* in [0, 1)                                                                      */
@@ -558,7 +558,7 @@ LSGD_API lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_h
 /* One step of every tensor.  lr finite and >= 0.  grad_scale: DEVICE float[1] that every gradient is multiplied by
  * first (a clipping factor computed on the device), or NULL.                                                    */
 LSGD_API lsgd_status lsgd_adamw_step(lsgd_adamw_handle h, double lr, const float* grad_scale);
-/* The moments as the fp32 values that they stand for: m_out, v_out DEVICE float[values], 16-byte aligned, either may be
+/* The moments as the fp32 values that they stand for: m_out, v_out DEVICE float[values], 32-byte aligned, either may be
  * NULL.  Values between a tensor's end and its last block's end are undefined for LSGD_STATE_F32's buffers, zero here. */
 LSGD_API lsgd_status lsgd_adamw_moments(lsgd_adamw_handle h, float* m_out, float* v_out);
 /* Steps taken so far.  get synchronises the stream; set (restoring a checkpoint) is enqueued on it.  n in [0, 2^31). */

@@ -39,7 +39,7 @@ struct Tensor {                           // one entry per tensor, device memory
   int64_t n;                              // values
   int64_t at;                             // first value of its moments
   float wd;
-  int32_t wide;                           // every pointer is 16-byte aligned
+  int32_t wide;                           // every pointer is aligned to 8 of its values
 };
 struct Counter {                          // steps taken; the running powers of beta1 and beta2
   double b1t, b2t;
@@ -313,7 +313,7 @@ lsgd_status check_adamw(const lsgd_adamw_desc* d) {
   }
   if (values == 0) return LSGD_OK;
   if (!d->m || !d->v) return LSGD_ERR_INVALID_ARG;
-  if (!aligned(d->m, 16) || !aligned(d->v, 16)) return LSGD_ERR_ALIGNMENT;
+  if (!aligned(d->m, 32) || !aligned(d->v, 32)) return LSGD_ERR_ALIGNMENT;
   if (d->state_dtype == LSGD_STATE_8BIT) {
     if (!d->m_scale || !d->v_scale) return LSGD_ERR_INVALID_ARG;
     if (!aligned(d->m_scale, 4) || !aligned(d->v_scale, 4)) return LSGD_ERR_ALIGNMENT;
@@ -376,6 +376,7 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* ou
   counter->b1t = counter->b2t = 1.0;
   Tensor* t = reinterpret_cast<Tensor*>(host + 256);
   Chunk* c = reinterpret_cast<Chunk*>(t + n);
+  const size_t gb = elem_bytes(desc->grad_dtype);
   int64_t at = 0;
   for (int i = 0; i < n; ++i) {
     t[i].p = desc->params[i];
@@ -384,7 +385,7 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* ou
     t[i].n = desc->sizes[i];
     t[i].at = at;
     t[i].wd = desc->weight_decay[i];
-    t[i].wide = aligned(t[i].p, 16) && aligned(t[i].g, 16) && aligned(t[i].copy, 16);
+    t[i].wide = aligned(t[i].p, 32) && aligned(t[i].g, 8 * gb) && aligned(t[i].copy, 16);
     at += padded(t[i].n);
     const uint64_t k = (uint64_t)((t[i].n + kChunk - 1) / kChunk);
     for (uint64_t q = 0; q < k; ++q) *c++ = Chunk{i, (uint32_t)q};
@@ -443,7 +444,7 @@ lsgd_status lsgd_adamw_step(lsgd_adamw_handle h, double lr, const float* grad_sc
 lsgd_status lsgd_adamw_moments(lsgd_adamw_handle h, float* m_out, float* v_out) {
   using namespace lsgd;
   if (!h) return LSGD_ERR_INVALID_ARG;
-  if (!aligned(m_out, 16) || !aligned(v_out, 16)) return LSGD_ERR_ALIGNMENT;
+  if (!aligned(m_out, 32) || !aligned(v_out, 32)) return LSGD_ERR_ALIGNMENT;
   if (!on_own_device(h)) return LSGD_ERR_STATE;
   if (h->values == 0 || (!m_out && !v_out)) return LSGD_OK;
   if (h->d.state_dtype == LSGD_STATE_F32) {

@@ -7,18 +7,9 @@ namespace {
 
 // a(z) and its derivative
 __device__ __forceinline__ float gate_at(float z, int act, float& slope) {
-  if (act == LSGD_GATE_SIGMOID) {
-    const float v = __fdividef(1.f, 1.f + __expf(-z));
-    slope = v * (1.f - v);
-    return v;
-  }
-  if (act == LSGD_GATE_TANH) {
-    const float v = tanhf(z);
-    slope = 1.f - v * v;
-    return v;
-  }
-  slope = 1.f;
-  return z;
+  const float v = act == LSGD_GATE_SIGMOID ? 1.f / (1.f + __expf(-z)) : act == LSGD_GATE_TANH ? tanhf(z) : z;
+  slope = act == LSGD_GATE_SIGMOID ? v * (1.f - v) : act == LSGD_GATE_TANH ? 1.f - v * v : 1.f;
+  return v;
 }
 
 // Adds the blocks' partial rows in order.  Block: 32 columns of one of the three sums of one worker (of all workers where
@@ -125,7 +116,7 @@ lsgd_status check_norm(const lsgd_blocknorm_desc* d, bool backward) {
 
 struct Shape {
   Launch l;
-  int tpr, rpb, stages, phased;
+  int tpr, rpb, slots, phased;
   uint32_t blocks_w;
 };
 
@@ -135,28 +126,28 @@ Shape shape_of(const lsgd_blocknorm_desc* d, bool backward) {
   s.l.mode = mode_of(*d);
   s.l.backward = backward;
   const bool pre = s.l.mode & kPre, has_y = s.l.mode & kY, token = s.l.mode & kToken;
-  // 16-byte pieces: every matrix starts on a boundary, and all rows have the same offset from one in every matrix
+  // pieces of 8 values: every matrix starts on the boundary of one, and all rows have the same offset from one in every matrix
   bool pieces = true, first = true;
   int64_t ld = 0, stride = 0;
-  auto see = [&](const lsgd_rows& r) {
+  auto see = [&](const lsgd_rows& r, int bytes) {
     if (!r.data) return;
     const int64_t l = d->T > 1 ? r.ld & 7 : 0, p = d->P > 1 ? r.stride & 7 : 0;
     if (first) ld = l, stride = p;
     first = false;
-    pieces = pieces && reinterpret_cast<uintptr_t>(r.data) % 16 == 0 && l == ld && p == stride;
+    pieces = pieces && reinterpret_cast<uintptr_t>(r.data) % (8 * bytes) == 0 && l == ld && p == stride;
   };
-  if (has_y) see(d->y);
-  if (token) see(d->gate);
+  if (has_y) see(d->y, ab);
+  if (token) see(d->gate, ab);
   if (backward) {
-    see(d->d_out);
-    if (pre) see(d->out), see(d->d_h);
-    see(d->dx);
-    if (has_y) see(d->dy);
-    if (token) see(d->d_gate);
+    see(d->d_out, rb);
+    if (pre) see(d->out, rb), see(d->d_h, ab);
+    see(d->dx, rb);
+    if (has_y) see(d->dy, ab);
+    if (token) see(d->d_gate, ab);
   } else {
-    see(d->x);
-    if (has_y) see(d->out);
-    if (pre) see(d->h);
+    see(d->x, rb);
+    if (has_y) see(d->out, rb);
+    if (pre) see(d->h, ab);
   }
   s.phased = ld != 0 || stride != 0;
   int need = (d->D + (s.phased ? 7 : 0) + E - 1) / E;
@@ -168,19 +159,23 @@ Shape shape_of(const lsgd_blocknorm_desc* d, bool backward) {
   s.tpr = 4;
   while (s.tpr < 32 && s.tpr < need) s.tpr *= 2;
   if (need > 32) s.tpr = (need + 31) / 32 * 32;
-  s.rpb = s.tpr >= 256 ? 1 : 256 / s.tpr;
+  const int wish = backward ? 256 : 128;  // of a block; backward fewer and larger ones, since each leaves a partial row
+  if (s.l.mode != kDirect && (s.phased || d->D != s.tpr * E)) s.l.mode |= kRagged;
+  s.rpb = s.tpr >= wish ? 1 : wish / s.tpr;
   s.l.threads = s.tpr * s.rpb;
   const size_t per = (size_t)E * s.l.threads;                         // values of a tensor's rows
   const size_t factors = 4 * per * ((pre ? 1 : 0) + (has_y ? 1 : 0));
   const size_t row = per * (backward ? rb + (pre ? rb + ab : 0) + (has_y ? ab : 0) + (token ? ab : 0)
                                      : rb + (has_y ? ab : 0) + (token ? ab : 0));
-  s.stages = factors + 2 * row <= (size_t)kSmemMax ? 2 : 1;
-  s.l.smem = factors + (s.l.mode == kDirect ? 0 : s.stages * row);
+  s.slots = !backward && s.l.mode != kDirect && factors + 2 * row <= (size_t)kSmemMax ? 2 : 1;
+  s.l.smem = factors + (s.l.mode == kDirect ? 0 : s.slots * row);    // at most 64 KiB + 160 KiB: 5 fp32 tensors, D = 8192
   const size_t sums = backward && s.rpb > 1 ? sizeof(float) * (size_t)s.rpb * d->D : 0;
   if (s.l.smem < sums) s.l.smem = sums;
-  // persistent: as many blocks as the SMs hold at once (registers: 512 threads; shared memory), and no more than rows
-  int per_sm = s.l.threads > 256 ? 1 : 2;
-  if (per_sm * (s.l.smem + 2048) > size_t(228) * 1024) per_sm = 1;
+  // persistent: as many blocks as the SMs hold at once (registers, shared memory), and no more than rows
+  int per_sm = (backward ? kBackwardThreads : kForwardThreads) / s.l.threads;
+  const int fit = (int)(size_t(228) * 1024 / (s.l.smem + 2048));
+  if (per_sm > fit) per_sm = fit;
+  if (per_sm < 1) per_sm = 1;
   const int64_t groups = (d->T + s.rpb - 1) / s.rpb;
   int64_t n = ((int64_t)sm_count() * per_sm + d->P - 1) / d->P;
   if (s.phased && n < groups) n = n < 8 ? 8 : n & ~int64_t(7);       // a block's rows are a multiple of 8 apart
@@ -195,8 +190,8 @@ cudaError_t run(const lsgd_blocknorm_desc* d, bool backward, cudaStream_t st) {
   a.T = (uint32_t)d->T;
   a.tpr = s.tpr;
   a.rpb = s.rpb;
-  a.stages = s.stages;
   a.phased = s.phased;
+  a.slots = s.slots;
   a.inv_d = 1.f / (float)d->D;
   a.blocks_w = s.blocks_w;
   a.part = backward ? static_cast<float*>(d->scratch) : nullptr;

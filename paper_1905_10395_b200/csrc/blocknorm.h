@@ -16,14 +16,15 @@
 // Memory-bound: every tensor is read or written once, a row stays on the SM from its load to its store.  A thread holds 16
 // values of a row -- two pieces of 8, 'threads per row' pieces apart -- and keeps the same columns for every row, so factors
 // and sums over the rows are its own: factors in its own words of shared memory, sums in registers.  Blocks are persistent
-// (one worker each); short rows share a block, the shortest a warp.  Rows are fetched one ahead by 16-byte asynchronous
-// copies into the copying thread's own words, so nothing but the sums over a row (a butterfly in the warp, one exchange
-// between the row's warps) makes a thread wait for another.  Arithmetic is on pairs (fma.rn.f32x2), the modes are template
+// (one worker each); short rows share a block, the shortest a warp.  As soon as a thread has taken its values of a tensor's
+// row, it copies its values of a later one into the same words of shared memory, 16 bytes at a time and asynchronously: the
+// words are its own (its warp's for fp32 rows), so only the sums over a row (a butterfly in the warp, one exchange between
+// the row's warps) make warps wait for each other.  Arithmetic is on pairs (fma.rn.f32x2), the modes are template
 // parameters and addresses are running pointers: issue slots, not memory, bound the first versions of the backward pass.
 //
 // Rows of any length: where rows do not start on 16-byte boundaries but all tensors share their layout, a block takes every
 // 8th row (or a multiple), whose starts all have the same offset phi from a boundary; pieces begin phi columns before the
-// row, so all of them are aligned and only the first and the last hold foreign columns, which are masked.
+// row, so all of them are aligned.  Columns behind a row are filled with zeros by the copy, those before it are masked.
 #pragma once
 #include <cstring>
 
@@ -34,21 +35,25 @@ namespace blocknorm {
 
 using bf16 = __nv_bfloat16;
 constexpr int E = 16;        // values of a row that a thread holds, in two halves of 8
+// threads of an SM, which set the registers of one: 80 and 128.  More registers forward: 94 us instead of XX for
+// 8 x 2048 x 2048; fewer backward spill the sums.
+constexpr int kForwardThreads = 768, kBackwardThreads = 512;
 
 struct Args {
   lsgd_blocknorm_desc d;
   uint32_t T;
   int tpr;                   // threads of a row
   int rpb;                   // rows of a block at a time
-  int stages;                // rows in shared memory: 2, or 1 where two do not fit
+  int slots;                 // forward: rows in shared memory, 2 or (where two do not fit) 1
   int phased;                // rows start off 16-byte boundaries
   float inv_d;
   uint32_t blocks_w;         // blocks of one worker
   float* part;               // backward: [P][blocks_w][2][D]
 };
 
-// What a launch computes.  kDirect: any strides, values moved one at a time, the mode read from the arguments.
-enum : int { kPre = 1, kY = 2, kPost = 4, kToken = 8, kDirect = -1 };
+// What a launch computes.  kRagged: some thread's 16 columns are not all in the row.  kDirect: any strides, values moved one
+// at a time, the mode read from the arguments.
+enum : int { kPre = 1, kY = 2, kPost = 4, kToken = 8, kRagged = 16, kDirect = -1 };
 inline __host__ __device__ int mode_of(const lsgd_blocknorm_desc& d) {
   return (d.w_pre.data ? kPre : 0) | (d.y.data ? kY : 0) | (d.post_norm ? kPost : 0) | (d.gate_kind == LSGD_GATE_TOKEN ? kToken : 0);
 }
@@ -86,23 +91,39 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 // ---- a thread's columns: half h covers col[h] .. col[h] + 7; columns outside [0, D) are foreign
 struct Cols {
   int col[2], D, gap;
-  bool full[2], any[2];
+  int have[2];               // columns of the half before the row's end: 0 .. 8
+  bool full[2];
+  int g, L;                  // this thread among the L of its warp that hold the same row
   __device__ __forceinline__ Cols(int t, int tpr, int D_, int phi) : D(D_), gap(tpr * 8) {
+    L = tpr < 32 ? tpr : 32;
+    g = (threadIdx.x & 31) % L;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       col[h] = (h * tpr + t) * 8 - phi;
-      full[h] = col[h] >= 0 && col[h] + 8 <= D;
-      any[h] = col[h] + 8 > 0 && col[h] < D;
+      have[h] = max(0, min(8, D - col[h]));
+      full[h] = col[h] >= 0 && have[h] == 8;
     }
   }
   __device__ __forceinline__ bool in(int h, int k) const { return (unsigned)(col[h] + k) < (unsigned)D; }
 };
 
-// ---- a thread's own words of shared memory: 16-byte unit u at [warp][u][lane], so units are immediate offsets and a quarter
-// warp is on all banks
-__device__ __forceinline__ uint4* unit_at(unsigned char* own, int u) { return reinterpret_cast<uint4*>(own + u * 512); }
+// ---- shared memory of a warp: 16-byte unit u of lane l at [u][l], so units are immediate offsets and a quarter warp is on
+// all banks
+__device__ __forceinline__ uint4* unit_at(unsigned char* warp, int u) {
+  return reinterpret_cast<uint4*>(warp + u * 512 + (threadIdx.x & 31) * 16);
+}
+// fp32 rows: a half is two units of a thread, 32 bytes in memory.  So that a copy instruction covers whole sectors, the warp
+// copies its 64 units (of L lanes: 2 L) in the order of memory, and position n of them holds unit n ^ (n / 8 & 1): a lane's
+// two are then read without bank conflicts.
+__device__ __forceinline__ uint4* pair_at(unsigned char* warp, int u, int n) {
+  return reinterpret_cast<uint4*>(warp + u * 512 + (n ^ (n >> 3 & 1)) * 16);
+}
 __device__ __forceinline__ void copy16(void* smem, const void* g) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(g) : "memory");
+}
+// of which the first `bytes` are read and the others become zeros
+__device__ __forceinline__ void copy16(void* smem, const void* g, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(g), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -115,55 +136,60 @@ template <typename T>
 __device__ __forceinline__ T* row_of(const lsgd_rows& r, uint32_t w, uint32_t t) {
   return static_cast<T*>(r.data) + w * r.stride + t * r.ld;
 }
-template <typename T>
-__device__ __forceinline__ const T* end_of(const lsgd_rows& r, const Args& a) {
-  return static_cast<const T*>(r.data) + (a.d.P - 1) * r.stride + (int64_t)(a.T - 1) * r.ld + a.d.D;
-}
-
-// Half h of a row, `p` at its first column.  A piece with foreign columns is copied whole where it lies inside the
-// matrix; else its own values one by one.
-template <typename T>
-__device__ __forceinline__ void fetch_half(unsigned char* own, int u, const T* p, const lsgd_rows& r, const Args& a, const Cols& c, int h) {
-  if (!c.any[h]) return;
-  if (c.full[h] || p + 8 <= end_of<T>(r, a)) {
-#pragma unroll
-    for (int i = 0; i < units<T>(); ++i) copy16(unit_at(own, u + i), reinterpret_cast<const char*>(p) + i * 16);
+// Half h of a row, `p` at the thread's first column of it.
+template <typename T, bool RAGGED>
+__device__ __forceinline__ void fetch_half(unsigned char* warp, int u, const T* p, const Cols& c, int h) {
+  if constexpr (sizeof(T) == 2) {
+    if (!RAGGED) copy16(unit_at(warp, u), p);
+    else copy16(unit_at(warp, u), p, c.have[h] * 2);
   } else {
+    const T* q = p - c.g * 4;             // the g-th unit of the row's part in this warp
+    const int n = 2 * (int)(threadIdx.x & 31) - c.g;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (c.in(h, k)) reinterpret_cast<T*>(unit_at(own, u + k * (int)sizeof(T) / 16))[k % (16 / sizeof(T))] = p[k];
+    for (int i = 0; i < 2; ++i) {
+      if (!RAGGED) {
+        copy16(pair_at(warp, u, n + i * c.L), q + i * c.L * 4);
+      } else {
+        const int k = max(0, min(4, c.D - (c.col[h] + (i * c.L - c.g) * 4)));
+        copy16(pair_at(warp, u, n + i * c.L), k ? q + i * c.L * 4 : p, k * 4);
+      }
+    }
   }
 }
 template <typename T>
-__device__ __forceinline__ void zero_half(unsigned char* own, int u) {
+__device__ __forceinline__ void zero_half(unsigned char* warp, int u) {
 #pragma unroll
-  for (int i = 0; i < units<T>(); ++i) *unit_at(own, u + i) = make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < units<T>(); ++i)
+    *(sizeof(T) == 2 ? unit_at(warp, u) : pair_at(warp, u, 2 * (threadIdx.x & 31) + i)) = make_uint4(0, 0, 0, 0);
 }
-__device__ __forceinline__ void mask(const Cols& c, int h, float2 (&f)[4]) {
-  if (c.full[h]) return;
-  LSGD_EACH(k) {
-    if (!c.in(h, 2 * k)) f[k].x = 0.f;
-    if (!c.in(h, 2 * k + 1)) f[k].y = 0.f;
-  }
-}
-template <typename T>
-__device__ __forceinline__ void take_half(unsigned char* own, int u, const Cols& c, int h, float2 (&f)[4]) {
+template <typename T, bool RAGGED>
+__device__ __forceinline__ void take_half(unsigned char* warp, int u, const Cols& c, int h, float2 (&f)[4]) {
   uint4 v[units<T>()];
 #pragma unroll
-  for (int i = 0; i < units<T>(); ++i) v[i] = *unit_at(own, u + i);
-  Pack<T, 8> p;
-  static_assert(sizeof(p) == sizeof(v), "");
-  memcpy(&p, v, sizeof(p));
-  p.get(reinterpret_cast<float*>(f));
-  mask(c, h, f);
+  for (int i = 0; i < units<T>(); ++i) v[i] = *(sizeof(T) == 2 ? unit_at(warp, u) : pair_at(warp, u, 2 * (threadIdx.x & 31) + i));
+  float* e = reinterpret_cast<float*>(f);
+  if constexpr (sizeof(T) == 2) {
+    Pack<T, 8> p;
+    p.a = v[0];
+    p.get(e);
+  } else {
+    memcpy(e, v, sizeof(v));
+  }
+  if (RAGGED && c.col[h] < 0) {
+    LSGD_EACH(k) {
+      if (c.col[h] + 2 * k < 0) f[k].x = 0.f;
+      if (c.col[h] + 2 * k + 1 < 0) f[k].y = 0.f;
+    }
+  }
 }
-template <typename T, bool DIRECT>
-__device__ __forceinline__ void store_half(T* p, const Cols& c, int h, const float2 (&f)[4]) {
-  Pack<T, 8> o;
-  o.set(reinterpret_cast<const float*>(f));
-  if (!DIRECT && c.full[h]) {
+template <typename T, bool DIRECT, bool RAGGED>
+__device__ __forceinline__ void store_half(T* p, const Cols& c, int h, bool live, const float2 (&f)[4]) {
+  if (!live) return;
+  if (!DIRECT && (!RAGGED || c.full[h])) {
+    Pack<T, 8> o;
+    o.set(reinterpret_cast<const float*>(f));
     o.store(p);
-  } else if (c.any[h]) {
+  } else {
     LSGD_EACH(k) {
       Pack<T, 1> e;
       e.set(&f[k].x);
@@ -181,15 +207,15 @@ __device__ __forceinline__ void vector_half(const float* v, const Cols& c, int h
     f[k].y = c.in(h, 2 * k + 1) ? __ldg(v + c.col[h] + 2 * k + 1) : 0.f;
   }
 }
-__device__ __forceinline__ void keep_half(unsigned char* own, int u, const float2 (&f)[4]) {
+__device__ __forceinline__ void keep_half(unsigned char* warp, int u, const float2 (&f)[4]) {
 #pragma unroll
   for (int q = 0; q < 2; ++q)
-    *reinterpret_cast<float4*>(unit_at(own, u + q)) = make_float4(f[2 * q].x, f[2 * q].y, f[2 * q + 1].x, f[2 * q + 1].y);
+    *reinterpret_cast<float4*>(unit_at(warp, u + q)) = make_float4(f[2 * q].x, f[2 * q].y, f[2 * q + 1].x, f[2 * q + 1].y);
 }
-__device__ __forceinline__ void kept_half(unsigned char* own, int u, float2 (&f)[4]) {
+__device__ __forceinline__ void kept_half(unsigned char* warp, int u, float2 (&f)[4]) {
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const float4 v = *reinterpret_cast<const float4*>(unit_at(own, u + q));
+    const float4 v = *reinterpret_cast<const float4*>(unit_at(warp, u + q));
     f[2 * q] = make_float2(v.x, v.y);
     f[2 * q + 1] = make_float2(v.z, v.w);
   }
@@ -218,8 +244,15 @@ __device__ __forceinline__ float row_sum(float2 a, int tpr, int sub, float* s_re
   return s;
 }
 
+// 1 / (1 + 2^(-z log2 e)); subnormal intermediates are flushed: they only move results by less than 2^-126
+__device__ __forceinline__ float sigmoid(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
 __device__ __forceinline__ float gate_value(float z, int act) {
-  if (act == LSGD_GATE_SIGMOID) return __fdividef(1.f, 1.f + __expf(-z));
+  if (act == LSGD_GATE_SIGMOID) return sigmoid(z);
   if (act == LSGD_GATE_TANH) return tanhf(z);
   return z;
 }
@@ -229,8 +262,11 @@ __device__ __forceinline__ float gate_slope(float a, int act) {
   return 1.f;
 }
 __device__ __forceinline__ void gate_values(float2 (&f)[4], int act) {
-  if (act == LSGD_GATE_IDENTITY) return;
-  LSGD_EACH(k) f[k] = make_float2(gate_value(f[k].x, act), gate_value(f[k].y, act));
+  if (act == LSGD_GATE_SIGMOID) {
+    LSGD_EACH(k) f[k] = make_float2(sigmoid(f[k].x), sigmoid(f[k].y));
+  } else if (act == LSGD_GATE_TANH) {
+    LSGD_EACH(k) f[k] = make_float2(tanhf(f[k].x), tanhf(f[k].y));
+  }
 }
 
 __device__ __forceinline__ float* vector_of(const lsgd_rows& r, uint32_t w) { return static_cast<float*>(r.data) + w * r.stride; }
@@ -254,31 +290,34 @@ __device__ __forceinline__ void factor_half(const Args& a, uint32_t w, const Col
   }
 }
 
-// A tensor that rows are read from: fetched ahead into the ring, or read in place.  p: at the first half's first column.
-template <typename T, bool DIRECT>
+// A tensor that rows are read from: fetched ahead, or read in place.  p: at the first half's first column.
+template <typename T, bool DIRECT, bool RAGGED>
 struct Input {
   const T* p;
-  int unit;                               // of the first half within a stage
-  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, const Cols& c, int unit_) {
+  int64_t step;
+  int unit;                               // of the first half in the thread's words
+  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, uint32_t rows, const Cols& c, int unit_) {
     p = row_of<T>(r, w, t) + c.col[0];
+    step = (int64_t)rows * r.ld;
     unit = unit_;
   }
-  __device__ __forceinline__ void advance(const lsgd_rows& r, uint32_t rows) { p += (int64_t)rows * r.ld; }
-  __device__ __forceinline__ void fetch(const lsgd_rows& r, const Args& a, uint32_t rows, unsigned char* stage, bool live, const Cols& c) {
+  __device__ __forceinline__ void fetch(unsigned char* warp, bool live, const Cols& c) {
     if constexpr (!DIRECT) {
       if (live) {
-        fetch_half<T>(stage, unit, p, r, a, c, 0);
-        fetch_half<T>(stage, unit + units<T>(), p + c.gap, r, a, c, 1);
-        advance(r, rows);
+        fetch_half<T, RAGGED>(warp, unit, p, c, 0);
+        fetch_half<T, RAGGED>(warp, unit + units<T>(), p + c.gap, c, 1);
+        p += step;
       } else {
-        zero_half<T>(stage, unit);
-        zero_half<T>(stage, unit + units<T>());
+        zero_half<T>(warp, unit);
+        zero_half<T>(warp, unit + units<T>());
       }
+    } else {
+      p += step;
     }
   }
-  __device__ __forceinline__ void get(unsigned char* stage, bool live, const Cols& c, int h, float2 (&f)[4]) const {
+  __device__ __forceinline__ void get(unsigned char* warp, bool live, const Cols& c, int h, float2 (&f)[4]) const {
     if constexpr (!DIRECT) {
-      take_half<T>(stage, unit + h * units<T>(), c, h, f);
+      take_half<T, RAGGED>(warp, unit + h * units<T>(), c, h, f);
     } else {
       const T* q = p + h * c.gap;
       LSGD_EACH(k) {
@@ -290,19 +329,26 @@ struct Input {
     }
   }
 };
-template <typename T, bool DIRECT>
+template <typename T, bool DIRECT, bool RAGGED>
 struct Output {
   T* p;
-  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, const Cols& c) { p = row_of<T>(r, w, t) + c.col[0]; }
-  __device__ __forceinline__ void put(const Cols& c, int h, const float2 (&f)[4]) { store_half<T, DIRECT>(p + h * c.gap, c, h, f); }
-  __device__ __forceinline__ void advance(const lsgd_rows& r, uint32_t rows) { p += (int64_t)rows * r.ld; }
+  int64_t step;
+  __device__ __forceinline__ void open(const lsgd_rows& r, uint32_t w, uint32_t t, uint32_t rows, const Cols& c) {
+    p = row_of<T>(r, w, t) + c.col[0];
+    step = (int64_t)rows * r.ld;
+  }
+  __device__ __forceinline__ void put(const Cols& c, int h, bool live, const float2 (&f)[4]) {
+    store_half<T, DIRECT, RAGGED>(p + h * c.gap, c, h, live, f);
+  }
+  __device__ __forceinline__ void advance() { p += step; }
 };
 
 // Blocks: blockIdx.y = worker; block b of a worker takes its rows b rpb .., then those blocks_w rpb further on.
 template <typename TR, typename TA, int MODE>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(kForwardThreads, 1)
 forward_kernel(const __grid_constant__ Args a) {
-  constexpr bool DIRECT = MODE == kDirect;
+  constexpr bool DIRECT = MODE == kDirect, RAGGED = DIRECT || (MODE & kRagged);
+  constexpr bool PAIRS = !DIRECT && sizeof(TR) == 4;   // lanes read what others of their warp have copied
   pdl_wait();
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ __align__(16) float s_red[kSums * kRowWords];
@@ -313,61 +359,64 @@ forward_kernel(const __grid_constant__ Args a) {
   const int sub = threadIdx.x / a.tpr;
   const uint32_t w = blockIdx.y, step = a.blocks_w * a.rpb;
   uint32_t t = blockIdx.x * a.rpb + sub;
-  const int phi = a.phased ? (int)((w * (uint64_t)d.x.stride + t * (uint64_t)d.x.ld) & 7) : 0;
+  const int phi = RAGGED && a.phased ? (int)((w * (uint64_t)d.x.stride + t * (uint64_t)d.x.ld) & 7) : 0;
   const Cols c((int)threadIdx.x - sub * a.tpr, a.tpr, d.D, phi);
-  const int n_x = 2 * units<TR>(), n_y = has_y ? 2 * units<TA>() : 0, n_g = token ? 2 * units<TA>() : 0;
-  const int factors = (pre ? kFactorUnits : 0) + (has_y ? kFactorUnits : 0), u_c = pre ? kFactorUnits : 0;
-  const int stage = n_x + n_y + n_g;
-  unsigned char* own = smem + (threadIdx.x >> 5) * (factors + (DIRECT ? 0 : a.stages * stage)) * 512 + (threadIdx.x & 31) * 16;
-  unsigned char* ring = own + factors * 512;
+  // a thread's words: w_pre, c, x, y, gate
+  const int u_c = pre ? kFactorUnits : 0, u_x = u_c + (has_y ? kFactorUnits : 0), u_y = u_x + 2 * units<TR>();
+  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), stage = u_g + (token ? 2 * units<TA>() : 0) - u_x;
+  const int words = DIRECT ? u_x : u_x + a.slots * stage;
+  unsigned char* warp = smem + (threadIdx.x >> 5) * words * 512;
   for (int i = threadIdx.x; i < kSums * kRowWords; i += blockDim.x) s_red[i] = 0.f;
-  Input<TR, DIRECT> ix;
-  Input<TA, DIRECT> iy, ig;
-  Output<TR, DIRECT> ox;
-  Output<TA, DIRECT> oh;
-  ix.open(d.x, w, t, c, 0);
-  if (has_y) iy.open(d.y, w, t, c, n_x), ox.open(d.out, w, t, c);
-  if (token) ig.open(d.gate, w, t, c, n_x + n_y);
-  if (pre) oh.open(d.h, w, t, c);
-  const auto fetch = [&](uint32_t row, unsigned char* to) {
-    const bool live = row < a.T;
-    ix.fetch(d.x, a, step, to, live, c);
-    if (has_y) iy.fetch(d.y, a, step, to, live, c);
-    if (token) ig.fetch(d.gate, a, step, to, live, c);
+  Input<TR, DIRECT, RAGGED> ix;
+  Input<TA, DIRECT, RAGGED> iy, ig;
+  Output<TR, DIRECT, RAGGED> ox;
+  Output<TA, DIRECT, RAGGED> oh;
+  ix.open(d.x, w, t, step, c, u_x);
+  if (has_y) iy.open(d.y, w, t, step, c, u_y), ox.open(d.out, w, t, step, c);
+  if (token) ig.open(d.gate, w, t, step, c, u_g);
+  if (pre) oh.open(d.h, w, t, step, c);
+  const auto fetch = [&](uint32_t row, unsigned char* warp) {
+    const bool more = row < a.T;
+    ix.fetch(warp, more, c);
+    if (has_y) iy.fetch(warp, more, c);
+    if (token) ig.fetch(warp, more, c);
     copy_commit();
   };
-  fetch(t, ring);
+  if (!DIRECT) {
+    fetch(t, warp);
+    if (a.slots == 2) fetch(t + step, warp + stage * 512);
+  }
+  unsigned char* in = warp;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float2 f[4];
     if (pre) {
       vector_half(vector_of(d.w_pre, w), c, h, f);
-      keep_half(own, 2 * h, f);
+      keep_half(warp, 2 * h, f);
     }
     if (has_y) {
       factor_half(a, w, c, h, post, channel, f);
-      keep_half(own, u_c + 2 * h, f);
+      keep_half(warp, u_c + 2 * h, f);
     }
   }
   __syncthreads();
-  int slot = 0, phase = 0;
+  int phase = 0;
   for (uint32_t t0 = blockIdx.x * a.rpb; t0 < a.T; t0 += step, t += step, phase ^= 2) {
     const bool live = t < a.T;
-    unsigned char* in = ring + slot * stage * 512;
-    if (a.stages == 2) {
-      slot ^= 1;
-      fetch(t + step, ring + slot * stage * 512);
-      copy_wait<1>();
-    } else {
-      copy_wait<0>();
+    if (a.slots == 2) copy_wait<1>();
+    else copy_wait<0>();
+    if (PAIRS) __syncwarp();
+    float2 x[2][4], y[2][4], g[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ix.get(in, live, c, h, x[h]);
+      if (has_y) iy.get(in, live, c, h, y[h]);
+      if (token) ig.get(in, live, c, h, g[h]);
     }
-    float2 x[2][4];
-    ix.get(in, live, c, 0, x[0]);
-    ix.get(in, live, c, 1, x[1]);
+    if (PAIRS) __syncwarp();
+    fetch(t + a.slots * step, in);
+    if (a.slots == 2) in = in == warp ? warp + stage * 512 : warp;
     if (has_y) {
-      float2 y[2][4];
-      iy.get(in, live, c, 0, y[0]);
-      iy.get(in, live, c, 1, y[1]);
       float rs = 1.f;
       if (post) {
         float2 q = both(0.f);
@@ -380,18 +429,17 @@ forward_kernel(const __grid_constant__ Args a) {
       for (int h = 0; h < 2; ++h) {
         float2 f[4];
         if (token) {
-          ig.get(in, live, c, h, f);
-          gate_values(f, d.gate_act);
-          LSGD_EACH(k) y[h][k] = mul2(y[h][k], f[k]);
+          gate_values(g[h], d.gate_act);
+          LSGD_EACH(k) y[h][k] = mul2(y[h][k], g[h][k]);
         }
-        kept_half(own, u_c + 2 * h, f);
+        kept_half(warp, u_c + 2 * h, f);
         if (post) {
           LSGD_EACH(k) y[h][k] = mul2(y[h][k], both(rs));
         }
         LSGD_EACH(k) x[h][k] = fma2(f[k], y[h][k], mul2(both(d.alpha), x[h][k]));
-        if (live) ox.put(c, h, x[h]);
+        ox.put(c, h, live, x[h]);
       }
-      ox.advance(d.out, step);
+      ox.advance();
     }
     if (pre) {
       float2 q = both(0.f);
@@ -402,27 +450,21 @@ forward_kernel(const __grid_constant__ Args a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float2 f[4];
-        kept_half(own, 2 * h, f);
+        kept_half(warp, 2 * h, f);
         LSGD_EACH(k) x[h][k] = mul2(mul2(x[h][k], both(rs)), f[k]);
-        if (live) oh.put(c, h, x[h]);
+        oh.put(c, h, live, x[h]);
       }
-      oh.advance(d.h, step);
-    }
-    if (DIRECT) {
-      ix.advance(d.x, step);
-      iy.advance(d.y, step);
-      ig.advance(d.gate, step);
-    } else if (a.stages == 1) {
-      fetch(t + step, ring);
+      oh.advance();
     }
   }
   copy_wait<0>();
 }
 
 template <typename TR, typename TA, int MODE>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(kBackwardThreads, 1)
 backward_kernel(const __grid_constant__ Args a) {
-  constexpr bool DIRECT = MODE == kDirect;
+  constexpr bool DIRECT = MODE == kDirect, RAGGED = DIRECT || (MODE & kRagged);
+  constexpr bool PAIRS = !DIRECT && sizeof(TR) == 4;   // lanes read what others of their warp have copied
   pdl_wait();
   pdl_launch_dependents();
   extern __shared__ __align__(16) unsigned char smem[];
@@ -434,53 +476,60 @@ backward_kernel(const __grid_constant__ Args a) {
   const int sub = threadIdx.x / a.tpr;
   const uint32_t w = blockIdx.y, step = a.blocks_w * a.rpb;
   uint32_t t = blockIdx.x * a.rpb + sub;
-  const int phi = a.phased ? (int)((w * (uint64_t)d.dx.stride + t * (uint64_t)d.dx.ld) & 7) : 0;
+  const int phi = RAGGED && a.phased ? (int)((w * (uint64_t)d.dx.stride + t * (uint64_t)d.dx.ld) & 7) : 0;
   const Cols c((int)threadIdx.x - sub * a.tpr, a.tpr, d.D, phi);
-  // a stage: d_out, out, d_h, y, gate
-  const int u_out = 2 * units<TR>(), u_dh = u_out + (pre ? 2 * units<TR>() : 0), u_y = u_dh + (pre ? 2 * units<TA>() : 0);
-  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), stage = u_g + (token ? 2 * units<TA>() : 0);
-  const int factors = (pre ? kFactorUnits : 0) + (has_y ? kFactorUnits : 0), u_c = pre ? kFactorUnits : 0;
-  unsigned char* own = smem + (threadIdx.x >> 5) * (factors + (DIRECT ? 0 : a.stages * stage)) * 512 + (threadIdx.x & 31) * 16;
-  unsigned char* ring = own + factors * 512;
+  // a thread's words: w_pre, c, d_out, out, d_h, y, gate
+  const int u_c = pre ? kFactorUnits : 0, u_d = u_c + (has_y ? kFactorUnits : 0), u_out = u_d + 2 * units<TR>();
+  const int u_dh = u_out + (pre ? 2 * units<TR>() : 0), u_y = u_dh + (pre ? 2 * units<TA>() : 0);
+  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), words = DIRECT ? u_d : u_g + (token ? 2 * units<TA>() : 0);
+  unsigned char* warp = smem + (threadIdx.x >> 5) * words * 512;
   for (int i = threadIdx.x; i < kSums * kRowWords; i += blockDim.x) s_red[i] = 0.f;
-  Input<TR, DIRECT> id, io;
-  Input<TA, DIRECT> ih, iy, ig;
-  Output<TR, DIRECT> ox;
-  Output<TA, DIRECT> oy, og;
-  ox.open(d.dx, w, t, c);
-  if (has_d) id.open(d.d_out, w, t, c, 0);
-  if (pre) io.open(d.out, w, t, c, u_out), ih.open(d.d_h, w, t, c, u_dh);
-  if (has_y) iy.open(d.y, w, t, c, u_y), oy.open(d.dy, w, t, c);
-  if (token) ig.open(d.gate, w, t, c, u_g), og.open(d.d_gate, w, t, c);
-  const auto fetch = [&](uint32_t row, unsigned char* to) {
-    const bool live = row < a.T;
-    if (has_d) id.fetch(d.d_out, a, step, to, live, c);
+  Input<TR, DIRECT, RAGGED> id, io;
+  Input<TA, DIRECT, RAGGED> ih, iy, ig;
+  Output<TR, DIRECT, RAGGED> ox;
+  Output<TA, DIRECT, RAGGED> oy, og;
+  ox.open(d.dx, w, t, step, c);
+  if (has_d) id.open(d.d_out, w, t, step, c, u_d);
+  if (pre) io.open(d.out, w, t, step, c, u_out), ih.open(d.d_h, w, t, step, c, u_dh);
+  if (has_y) iy.open(d.y, w, t, step, c, u_y), oy.open(d.dy, w, t, step, c);
+  if (token) ig.open(d.gate, w, t, step, c, u_g), og.open(d.d_gate, w, t, step, c);
+  // in two groups, in the order in which a row needs them
+  const auto fetch_second = [&](uint32_t row) {
+    const bool more = row < a.T;
     if (pre) {
-      io.fetch(d.out, a, step, to, live, c);
-      ih.fetch(d.d_h, a, step, to, live, c);
+      io.fetch(warp, more, c);
+      ih.fetch(warp, more, c);
     }
-    if (has_y) iy.fetch(d.y, a, step, to, live, c);
-    if (token) ig.fetch(d.gate, a, step, to, live, c);
     copy_commit();
   };
-  fetch(t, ring);
+  const auto fetch_first = [&](uint32_t row) {
+    const bool more = row < a.T;
+    if (has_d) id.fetch(warp, more, c);
+    if (has_y) iy.fetch(warp, more, c);
+    if (token) ig.fetch(warp, more, c);
+    copy_commit();
+  };
+  if (!DIRECT) {
+    fetch_second(t);
+    fetch_first(t);
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float2 f[4];
     if (pre) {
       vector_half(vector_of(d.w_pre, w), c, h, f);
-      keep_half(own, 2 * h, f);
+      keep_half(warp, 2 * h, f);
     }
     if (has_y) {
       factor_half(a, w, c, h, post, channel, f);
-      keep_half(own, u_c + 2 * h, f);
+      keep_half(warp, u_c + 2 * h, f);
     }
   }
   __syncthreads();
   float2 sum_pre[2][4], sum_y[2][4];      // of d_h n_x and of g (a) n_y
 #pragma unroll
   for (int h = 0; h < 2; ++h) LSGD_EACH(k) sum_pre[h][k] = sum_y[h][k] = both(0.f);
-  int slot = 0, phase = 0;
+  int phase = 0;
   for (uint32_t t0 = blockIdx.x * a.rpb; t0 < a.T; t0 += step, t += step, phase ^= 2) {
     const bool live = t < a.T;
     const size_t r = (size_t)w * a.T + t;
@@ -489,22 +538,16 @@ backward_kernel(const __grid_constant__ Args a) {
     float rs = 0.f, mean = 0.f, rs_y = 0.f;
     if (pre) rs = live ? d.rstd_pre[r] : 0.f;
     if (post) rs_y = live ? d.rstd_post[r] : 0.f;
-    unsigned char* in = ring + slot * stage * 512;
-    if (a.stages == 2) {
-      slot ^= 1;
-      fetch(t + step, ring + slot * stage * 512);
-      copy_wait<1>();
-    } else {
-      copy_wait<0>();
-    }
+    copy_wait<1>();
+    if (PAIRS) __syncwarp();
     if (pre) {
       float2 q = both(0.f);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float2 f[4];
-        io.get(in, live, c, h, n[h]);
-        ih.get(in, live, c, h, up[h]);
-        kept_half(own, 2 * h, f);
+        io.get(warp, live, c, h, n[h]);
+        ih.get(warp, live, c, h, up[h]);
+        kept_half(warp, 2 * h, f);
         LSGD_EACH(k) {
           n[h][k] = mul2(n[h][k], both(rs));
           sum_pre[h][k] = fma2(up[h][k], n[h][k], sum_pre[h][k]);
@@ -512,64 +555,63 @@ backward_kernel(const __grid_constant__ Args a) {
           q = fma2(up[h][k], n[h][k], q);
         }
       }
+      if (PAIRS) __syncwarp();
+      fetch_second(t + step);
       mean = -rs * (row_sum(q, a.tpr, sub, s_red + phase * kRowWords) * a.inv_d);
+    } else {
+      copy_commit();                      // keeps the count of groups
     }
+    copy_wait<1>();
+    if (PAIRS) __syncwarp();
     float2 q = both(0.f);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float2 g[4];                        // d_out, then the gradient of x'
       LSGD_EACH(k) g[k] = both(0.f);
-      if (has_d) id.get(in, live, c, h, g);
+      if (has_d) id.get(warp, live, c, h, g);
       if (pre) {
         LSGD_EACH(k) g[k] = fma2(n[h][k], both(mean), fma2(up[h][k], both(rs), g[k]));
       }
       float2 b[4];
       LSGD_EACH(k) b[k] = has_y ? mul2(both(d.alpha), g[k]) : g[k];
-      if (live) ox.put(c, h, b);
+      ox.put(c, h, live, b);
       if (!has_y) continue;
-      iy.get(in, live, c, h, n[h]);
+      iy.get(warp, live, c, h, n[h]);
       if (post) {
         LSGD_EACH(k) n[h][k] = mul2(n[h][k], both(rs_y));
       }
       float2 f[4];
-      kept_half(own, u_c + 2 * h, f);
+      kept_half(warp, u_c + 2 * h, f);
       if (token) {
-        ig.get(in, live, c, h, b);
+        ig.get(warp, live, c, h, b);
         gate_values(b, d.gate_act);
         LSGD_EACH(k) {
           const float2 av = b[k];
           b[k] = mul2(mul2(mul2(g[k], n[h][k]), f[k]), make_float2(gate_slope(av.x, d.gate_act), gate_slope(av.y, d.gate_act)));
           g[k] = mul2(g[k], av);
         }
-        if (live) og.put(c, h, b);
+        og.put(c, h, live, b);
       }
       LSGD_EACH(k) {
         sum_y[h][k] = fma2(g[k], n[h][k], sum_y[h][k]);
         up[h][k] = mul2(g[k], f[k]);
         q = fma2(up[h][k], n[h][k], q);
       }
-      if (!post && live) oy.put(c, h, up[h]);
+      if (!post) oy.put(c, h, live, up[h]);
     }
+    if (PAIRS) __syncwarp();
+    fetch_first(t + step);
     if (post) {
       mean = -rs_y * (row_sum(q, a.tpr, sub, s_red + (phase + 1) * kRowWords) * a.inv_d);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         LSGD_EACH(k) up[h][k] = fma2(n[h][k], both(mean), mul2(up[h][k], both(rs_y)));
-        if (live) oy.put(c, h, up[h]);
+        oy.put(c, h, live, up[h]);
       }
     }
-    ox.advance(d.dx, step);
-    oy.advance(d.dy, step);
-    og.advance(d.d_gate, step);
-    if (DIRECT) {
-      id.advance(d.d_out, step);
-      io.advance(d.out, step);
-      ih.advance(d.d_h, step);
-      iy.advance(d.y, step);
-      ig.advance(d.gate, step);
-    } else if (a.stages == 1) {
-      fetch(t + step, ring);
-    }
+    ox.advance();
+    oy.advance();
+    og.advance();
   }
   copy_wait<0>();
   // one partial row per block for the two sums
@@ -616,20 +658,25 @@ cudaError_t launch_mode(const Args& a, const Launch& l, cudaStream_t s) {
                     : launch_pdl(forward_kernel<TR, TA, MODE>, grid, block, l.smem, s, a);
 }
 
+template <typename TR, typename TA, int RAGGED>
+cudaError_t launch_shape(const Args& a, const Launch& l, cudaStream_t s) {
+  switch (l.mode & ~kRagged) {
+    case kPre: return launch_mode<TR, TA, RAGGED | kPre>(a, l, s);
+    case kY: return launch_mode<TR, TA, RAGGED | kY>(a, l, s);
+    case kY | kPre: return launch_mode<TR, TA, RAGGED | kY | kPre>(a, l, s);
+    case kY | kPost: return launch_mode<TR, TA, RAGGED | kY | kPost>(a, l, s);
+    case kY | kPost | kPre: return launch_mode<TR, TA, RAGGED | kY | kPost | kPre>(a, l, s);
+    case kY | kToken: return launch_mode<TR, TA, RAGGED | kY | kToken>(a, l, s);
+    case kY | kToken | kPre: return launch_mode<TR, TA, RAGGED | kY | kToken | kPre>(a, l, s);
+    case kY | kToken | kPost: return launch_mode<TR, TA, RAGGED | kY | kToken | kPost>(a, l, s);
+    case kY | kToken | kPost | kPre: return launch_mode<TR, TA, RAGGED | kY | kToken | kPost | kPre>(a, l, s);
+    default: return cudaErrorInvalidValue;
+  }
+}
 template <typename TR, typename TA>
 cudaError_t launch_types(const Args& a, const Launch& l, cudaStream_t s) {
-  switch (l.mode) {
-    case kPre: return launch_mode<TR, TA, kPre>(a, l, s);
-    case kY: return launch_mode<TR, TA, kY>(a, l, s);
-    case kY | kPre: return launch_mode<TR, TA, kY | kPre>(a, l, s);
-    case kY | kPost: return launch_mode<TR, TA, kY | kPost>(a, l, s);
-    case kY | kPost | kPre: return launch_mode<TR, TA, kY | kPost | kPre>(a, l, s);
-    case kY | kToken: return launch_mode<TR, TA, kY | kToken>(a, l, s);
-    case kY | kToken | kPre: return launch_mode<TR, TA, kY | kToken | kPre>(a, l, s);
-    case kY | kToken | kPost: return launch_mode<TR, TA, kY | kToken | kPost>(a, l, s);
-    case kY | kToken | kPost | kPre: return launch_mode<TR, TA, kY | kToken | kPost | kPre>(a, l, s);
-    default: return launch_mode<TR, TA, kDirect>(a, l, s);
-  }
+  if (l.mode == kDirect) return launch_mode<TR, TA, kDirect>(a, l, s);
+  return l.mode & kRagged ? launch_shape<TR, TA, kRagged>(a, l, s) : launch_shape<TR, TA, 0>(a, l, s);
 }
 
 }  // namespace

@@ -48,7 +48,7 @@ inline int row_vec(const lsgd_rows& r, int64_t P, int64_t T, int64_t D, int byte
     return D % vec == 0 && reinterpret_cast<uintptr_t>(r.data) % align == 0 && (T <= 1 || (r.ld * bytes) % align == 0) &&
            (P <= 1 || (r.stride * bytes) % align == 0);
   };
-  if (fits(8, 16)) return 8;
+  if (fits(8, 8 * bytes)) return 8;
   if (fits(2, 2 * bytes)) return 2;
   return 1;
 }
@@ -59,23 +59,24 @@ inline int min_vec(int a, int b) { return a < b ? a : b; }
 template <typename T, int VEC>
 struct Pack;
 template <>
-struct Pack<float, 8> {
-  float4 a, b;
+struct Pack<float, 8> {      // 32 bytes in one instruction: two of 16 would touch every sector twice
+  float v[8];
   __device__ __forceinline__ void load(const float* p) {
-    a = *reinterpret_cast<const float4*>(p);
-    b = *reinterpret_cast<const float4*>(p + 4);
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p) : "memory");
   }
   __device__ __forceinline__ void store(float* p) const {
-    *reinterpret_cast<float4*>(p) = a;
-    *reinterpret_cast<float4*>(p + 4) = b;
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                 "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
   }
   __device__ __forceinline__ void get(float* f) const {
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = v[k];
   }
   __device__ __forceinline__ void set(const float* f) {
-    a = make_float4(f[0], f[1], f[2], f[3]);
-    b = make_float4(f[4], f[5], f[6], f[7]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = f[k];
   }
 };
 template <>
