@@ -167,7 +167,7 @@ Shape shape_of(const lsgd_blocknorm_desc* d, bool backward) {
   const size_t factors = 4 * per * ((pre ? 1 : 0) + (has_y ? 1 : 0));
   const size_t row = per * (backward ? rb + (pre ? rb + ab : 0) + (has_y ? ab : 0) + (token ? ab : 0)
                                      : rb + (has_y ? ab : 0) + (token ? ab : 0));
-  s.slots = !backward && s.l.mode != kDirect && factors + 2 * row <= (size_t)kSmemMax ? 2 : 1;
+  s.slots = s.l.mode != kDirect && factors + 2 * row <= (size_t)kSmemMax ? 2 : 1;
   s.l.smem = factors + (s.l.mode == kDirect ? 0 : s.slots * row);    // at most 64 KiB + 160 KiB: 5 fp32 tensors, D = 8192
   const size_t sums = backward && s.rpb > 1 ? sizeof(float) * (size_t)s.rpb * d->D : 0;
   if (s.l.smem < sums) s.l.smem = sums;

@@ -16,10 +16,10 @@
 // Memory-bound: every tensor is read or written once, a row stays on the SM from its load to its store.  A thread holds 16
 // values of a row -- two pieces of 8, 'threads per row' pieces apart -- and keeps the same columns for every row, so factors
 // and sums over the rows are its own: factors in its own words of shared memory, sums in registers.  Blocks are persistent
-// (one worker each); short rows share a block, the shortest a warp.  As soon as a thread has taken its values of a tensor's
-// row, it copies its values of a later one into the same words of shared memory, 16 bytes at a time and asynchronously: the
-// words are its own (its warp's for fp32 rows), so only the sums over a row (a butterfly in the warp, one exchange between
-// the row's warps) make warps wait for each other.  Arithmetic is on pairs (fma.rn.f32x2), the modes are template
+// (one worker each); short rows share a block, the shortest a warp.  Rows are fetched one
+// ahead into shared memory, 16 bytes at a time and asynchronously, by the thread that reads them (its warp for fp32 rows), so
+// only the sums over a row (a butterfly in the warp, one exchange between the row's warps) make warps wait for each other.
+// Arithmetic is on pairs (fma.rn.f32x2), the modes are template
 // parameters and addresses are running pointers: issue slots, not memory, bound the first versions of the backward pass.
 //
 // Rows of any length: where rows do not start on 16-byte boundaries but all tensors share their layout, a block takes every
@@ -44,7 +44,7 @@ struct Args {
   uint32_t T;
   int tpr;                   // threads of a row
   int rpb;                   // rows of a block at a time
-  int slots;                 // forward: rows in shared memory, 2 or (where two do not fit) 1
+  int slots;                 // rows in shared memory: 2, or (where two do not fit, and for kDirect) 1
   int phased;                // rows start off 16-byte boundaries
   float inv_d;
   uint32_t blocks_w;         // blocks of one worker
@@ -384,7 +384,6 @@ forward_kernel(const __grid_constant__ Args a) {
   };
   if (!DIRECT) {
     fetch(t, warp);
-    if (a.slots == 2) fetch(t + step, warp + stage * 512);
   }
   unsigned char* in = warp;
 #pragma unroll
@@ -403,8 +402,13 @@ forward_kernel(const __grid_constant__ Args a) {
   int phase = 0;
   for (uint32_t t0 = blockIdx.x * a.rpb; t0 < a.T; t0 += step, t += step, phase ^= 2) {
     const bool live = t < a.T;
-    if (a.slots == 2) copy_wait<1>();
-    else copy_wait<0>();
+    unsigned char* next = a.slots == 2 && in == warp ? warp + stage * 512 : warp;
+    if (a.slots == 2) {
+      fetch(t + step, next);
+      copy_wait<1>();
+    } else {
+      copy_wait<0>();
+    }
     if (PAIRS) __syncwarp();
     float2 x[2][4], y[2][4], g[2][4];
 #pragma unroll
@@ -413,9 +417,9 @@ forward_kernel(const __grid_constant__ Args a) {
       if (has_y) iy.get(in, live, c, h, y[h]);
       if (token) ig.get(in, live, c, h, g[h]);
     }
-    if (PAIRS) __syncwarp();
-    fetch(t + a.slots * step, in);
-    if (a.slots == 2) in = in == warp ? warp + stage * 512 : warp;
+    if (PAIRS) __syncwarp();              // the words are free again
+    if (a.slots == 1) fetch(t + step, in);
+    in = next;
     if (has_y) {
       float rs = 1.f;
       if (post) {
@@ -481,7 +485,8 @@ backward_kernel(const __grid_constant__ Args a) {
   // a thread's words: w_pre, c, d_out, out, d_h, y, gate
   const int u_c = pre ? kFactorUnits : 0, u_d = u_c + (has_y ? kFactorUnits : 0), u_out = u_d + 2 * units<TR>();
   const int u_dh = u_out + (pre ? 2 * units<TR>() : 0), u_y = u_dh + (pre ? 2 * units<TA>() : 0);
-  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), words = DIRECT ? u_d : u_g + (token ? 2 * units<TA>() : 0);
+  const int u_g = u_y + (has_y ? 2 * units<TA>() : 0), stage = u_g + (token ? 2 * units<TA>() : 0) - u_d;
+  const int words = DIRECT ? u_d : u_d + a.slots * stage;
   unsigned char* warp = smem + (threadIdx.x >> 5) * words * 512;
   for (int i = threadIdx.x; i < kSums * kRowWords; i += blockDim.x) s_red[i] = 0.f;
   Input<TR, DIRECT, RAGGED> id, io;
@@ -493,26 +498,19 @@ backward_kernel(const __grid_constant__ Args a) {
   if (pre) io.open(d.out, w, t, step, c, u_out), ih.open(d.d_h, w, t, step, c, u_dh);
   if (has_y) iy.open(d.y, w, t, step, c, u_y), oy.open(d.dy, w, t, step, c);
   if (token) ig.open(d.gate, w, t, step, c, u_g), og.open(d.d_gate, w, t, step, c);
-  // in two groups, in the order in which a row needs them
-  const auto fetch_second = [&](uint32_t row) {
+  const auto fetch = [&](uint32_t row, unsigned char* warp) {
     const bool more = row < a.T;
+    if (has_d) id.fetch(warp, more, c);
     if (pre) {
       io.fetch(warp, more, c);
       ih.fetch(warp, more, c);
     }
-    copy_commit();
-  };
-  const auto fetch_first = [&](uint32_t row) {
-    const bool more = row < a.T;
-    if (has_d) id.fetch(warp, more, c);
     if (has_y) iy.fetch(warp, more, c);
     if (token) ig.fetch(warp, more, c);
     copy_commit();
   };
-  if (!DIRECT) {
-    fetch_second(t);
-    fetch_first(t);
-  }
+  if (!DIRECT) fetch(t, warp);
+  unsigned char* in = warp;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float2 f[4];
@@ -538,15 +536,21 @@ backward_kernel(const __grid_constant__ Args a) {
     float rs = 0.f, mean = 0.f, rs_y = 0.f;
     if (pre) rs = live ? d.rstd_pre[r] : 0.f;
     if (post) rs_y = live ? d.rstd_post[r] : 0.f;
-    copy_wait<1>();
+    unsigned char* next = a.slots == 2 && in == warp ? warp + stage * 512 : warp;
+    if (a.slots == 2) {
+      fetch(t + step, next);
+      copy_wait<1>();
+    } else {
+      copy_wait<0>();
+    }
     if (PAIRS) __syncwarp();
     if (pre) {
       float2 q = both(0.f);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float2 f[4];
-        io.get(warp, live, c, h, n[h]);
-        ih.get(warp, live, c, h, up[h]);
+        io.get(in, live, c, h, n[h]);
+        ih.get(in, live, c, h, up[h]);
         kept_half(warp, 2 * h, f);
         LSGD_EACH(k) {
           n[h][k] = mul2(n[h][k], both(rs));
@@ -555,20 +559,14 @@ backward_kernel(const __grid_constant__ Args a) {
           q = fma2(up[h][k], n[h][k], q);
         }
       }
-      if (PAIRS) __syncwarp();
-      fetch_second(t + step);
       mean = -rs * (row_sum(q, a.tpr, sub, s_red + phase * kRowWords) * a.inv_d);
-    } else {
-      copy_commit();                      // keeps the count of groups
     }
-    copy_wait<1>();
-    if (PAIRS) __syncwarp();
     float2 q = both(0.f);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float2 g[4];                        // d_out, then the gradient of x'
       LSGD_EACH(k) g[k] = both(0.f);
-      if (has_d) id.get(warp, live, c, h, g);
+      if (has_d) id.get(in, live, c, h, g);
       if (pre) {
         LSGD_EACH(k) g[k] = fma2(n[h][k], both(mean), fma2(up[h][k], both(rs), g[k]));
       }
@@ -576,14 +574,14 @@ backward_kernel(const __grid_constant__ Args a) {
       LSGD_EACH(k) b[k] = has_y ? mul2(both(d.alpha), g[k]) : g[k];
       ox.put(c, h, live, b);
       if (!has_y) continue;
-      iy.get(warp, live, c, h, n[h]);
+      iy.get(in, live, c, h, n[h]);
       if (post) {
         LSGD_EACH(k) n[h][k] = mul2(n[h][k], both(rs_y));
       }
       float2 f[4];
       kept_half(warp, u_c + 2 * h, f);
       if (token) {
-        ig.get(warp, live, c, h, b);
+        ig.get(in, live, c, h, b);
         gate_values(b, d.gate_act);
         LSGD_EACH(k) {
           const float2 av = b[k];
@@ -599,8 +597,9 @@ backward_kernel(const __grid_constant__ Args a) {
       }
       if (!post) oy.put(c, h, live, up[h]);
     }
-    if (PAIRS) __syncwarp();
-    fetch_first(t + step);
+    if (PAIRS) __syncwarp();              // the words are free again
+    if (a.slots == 1) fetch(t + step, in);
+    in = next;
     if (post) {
       mean = -rs_y * (row_sum(q, a.tpr, sub, s_red + (phase + 1) * kRowWords) * a.inv_d);
 #pragma unroll
