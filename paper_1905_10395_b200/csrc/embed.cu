@@ -8,8 +8,9 @@
 // The gradient must not depend on timing, so no row is added with atomics.  Two ways to the same sums:
 //   few tokens   one launch.  The block of position i leaves if an earlier position holds the same token; otherwise it
 //                finds the later ones by comparing all tokens, and adds their rows in order.
-//   many tokens  positions are sorted by (worker, token) with a stable radix sort of at most kDigitBits bits a pass
-//                (a histogram and a scatter launch per pass); a warp then walks a piece of the sorted list, adding rows
+//   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 65536 positions in the shared
+//                memory of one cluster, in one launch, more with a histogram and a scatter launch per pass; a warp then
+//                walks a piece of the sorted list, adding rows
 //                while the token stays the same.  A token that lies within one piece is written at once; pieces of a
 //                token that crosses piece ends leave fp32 partial rows, which a last launch adds in order.  Work is
 //                split by positions, never by token, so it stays even however often one token occurs.
@@ -235,6 +236,17 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
 }
 
 // ------------------------------------------------------------------------------------------------ sort
+// The lanes whose digit is this lane's: one vote per bit.  (A match instruction takes as many rounds as there are different
+// digits, 32 as a rule: the cluster sort of 65536 tokens takes XX us with it, XX us so.)
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool live, int bits) {
+  uint32_t same = __ballot_sync(0xFFFFFFFFu, live);
+  for (int b = 0; b < bits; ++b) {
+    const uint32_t one = __ballot_sync(0xFFFFFFFFu, d >> b & 1);
+    same &= d >> b & 1 ? one : ~one;
+  }
+  return same;
+}
+
 constexpr int kDigitBits = 10;
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
@@ -331,13 +343,14 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
 #pragma unroll
     for (int q = 0; q < kSortItems; ++q) {
       const uint32_t i = s + warp * (32 * kSortItems) + q * 32 + lane;
-      const uint32_t d = i < i1 ? (key[q] >> a.shift) & (bins - 1) : kNone;
-      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+      const uint32_t d = (key[q] >> a.shift) & (bins - 1);
+      const bool live = i < i1;
+      const uint32_t same = same_digit(d, live, a.bits);
       uint32_t prev = 0;
-      if (d != kNone) prev = cnt[d];
+      if (live) prev = cnt[d];
       rank[q] = prev + __popc(same & ((1u << lane) - 1));
       __syncwarp();
-      if (d != kNone && (same >> lane) == 1u) cnt[d] = (uint16_t)(prev + __popc(same));   // the last lane of the group
+      if (live && (same >> lane) == 1u) cnt[d] = (uint16_t)(prev + __popc(same));   // the last lane of the group
       __syncwarp();
     }
     __syncthreads();
@@ -368,6 +381,183 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
   }
 }
 
+// ---- up to kClusterKeys keys: the whole sort in the shared memory of one cluster.  A block holds kBlockKeys consecutive
+// places.  A pass orders the block's own keys by digit in its shared memory, adds up the blocks' digit counts through
+// distributed shared memory, and copies the keys to their places in whichever block holds them: in the order of the digits,
+// so that a warp's stores to another block are runs of consecutive places.  Two cluster barriers a pass instead of two
+// launches.
+constexpr int kClusterThreads = 1024;
+constexpr int kClusterWarps = kClusterThreads / 32;
+constexpr int kClusterItems = 8;
+constexpr int kBlockKeys = kClusterThreads * kClusterItems;    // 8192
+constexpr int kClusterBlocks = 8;                              // the portable cluster size
+constexpr int kClusterKeys = kBlockKeys * kClusterBlocks;      // 65536
+constexpr int kClusterBits = 9;
+constexpr int kClusterBins = 1 << kClusterBits;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote(const void* smem, uint32_t block) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(smem)), "r"(block));
+  return r;
+}
+__device__ __forceinline__ uint32_t load_remote(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_remote(uint32_t a, uint2 v) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(v.x), "r"(v.y) : "memory");
+}
+
+struct ClusterSort {
+  uint32_t *key_out, *pos_out;
+  uint8_t* touched;           // nullptr: not wanted
+  uint32_t N, none_key, rows;
+  int bits, passes, blocks;
+};
+struct ClusterMemory {
+  uint2 stage[kBlockKeys];    // (key, position): this block's keys in the order of their digits
+  uint2 place[kBlockKeys];    // what the blocks have put in this block's places
+  uint32_t count[kClusterBins];                    // this block's digits; read by all blocks
+  uint32_t base[kClusterBins];                     // first place of this block's digit
+  uint32_t local[kClusterBins];                    // first place of the digit in `stage`
+  uint16_t warp[kClusterWarps][kClusterBins];
+  uint32_t scan[2][kClusterWarps];
+};
+
+// Sum of the values of the threads before this one, of the whole block.
+__device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* s_scan) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += n;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  uint32_t sums = lane < warp ? s_scan[lane] : 0;
+  sums = __reduce_add_sync(0xFFFFFFFFu, sums);
+  return sums + incl - v;
+}
+
+__global__ void __launch_bounds__(kClusterThreads, 1)
+embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ uint32_t smem[];
+  ClusterMemory& s = *reinterpret_cast<ClusterMemory*>(smem);
+  const uint32_t bins = 1u << a.bits;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t me = cluster_rank();
+  const uint32_t first = me * kBlockKeys;
+  const uint32_t n = a.N > first ? min(a.N - first, (uint32_t)kBlockKeys) : 0;   // places of this block
+  const uint32_t at = warp * (32 * kClusterItems) + lane;                     // of the thread's first key; 32 apart
+
+  uint2 item[kClusterItems];
+#pragma unroll
+  for (int q = 0; q < kClusterItems; ++q) {
+    item[q] = make_uint2(0, first + at + q * 32);
+    if (at + q * 32 < n) {
+      item[q].x = tok.key(item[q].y);
+      if (item[q].x == kNone) item[q].x = a.none_key;
+    }
+  }
+  if (a.touched)
+    for (uint32_t i = (me * kClusterThreads + threadIdx.x) * 16; i < a.rows; i += a.blocks * kClusterThreads * 16)
+      *reinterpret_cast<uint4*>(a.touched + i) = make_uint4(0, 0, 0, 0);      // the buffer is a multiple of 256 bytes
+
+  for (int pass = 0; pass < a.passes; ++pass) {
+    const int shift = pass * a.bits;
+    const uint32_t mask = bins - 1;
+    for (uint32_t b = lane; b < bins; b += 32) s.warp[warp][b] = 0;
+    __syncwarp();
+    uint16_t* cnt = s.warp[warp];
+    uint32_t rank[kClusterItems];
+#pragma unroll
+    for (int q = 0; q < kClusterItems; ++q) {
+      const uint32_t d = (item[q].x >> shift) & mask;
+      const bool live = at + q * 32 < n;
+      const uint32_t same = same_digit(d, live, a.bits);
+      uint32_t prev = 0;
+      if (live) prev = cnt[d];
+      rank[q] = prev + __popc(same & ((1u << lane) - 1));
+      __syncwarp();
+      if (live && (same >> lane) == 1u) cnt[d] = (uint16_t)(prev + __popc(same));
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t mine = 0;
+    if (threadIdx.x < bins) {
+      uint32_t c[kClusterWarps];
+#pragma unroll
+      for (int w = 0; w < kClusterWarps; ++w) c[w] = s.warp[w][threadIdx.x];
+#pragma unroll
+      for (int w = 0; w < kClusterWarps; ++w) {
+        s.warp[w][threadIdx.x] = (uint16_t)mine;
+        mine += c[w];
+      }
+      s.count[threadIdx.x] = mine;
+    }
+    const uint32_t local = scan_before(mine, s.scan[0]);
+    if (threadIdx.x < bins) s.local[threadIdx.x] = local;
+    cluster_sync();                        // every block's counts are there; its keys are in registers
+    uint32_t total = 0, before = 0;
+    if (threadIdx.x < bins) {
+#pragma unroll
+      for (int r = 0; r < kClusterBlocks; ++r) {
+        const uint32_t c = r < a.blocks ? load_remote(remote(&s.count[threadIdx.x], r)) : 0;
+        total += c;
+        before += r < (int)me ? c : 0;
+      }
+    }
+    const uint32_t start = scan_before(total, s.scan[1]);
+    if (threadIdx.x < bins) s.base[threadIdx.x] = start + before;
+#pragma unroll
+    for (int q = 0; q < kClusterItems; ++q) {
+      if (at + q * 32 < n) {
+        const uint32_t d = (item[q].x >> shift) & mask;
+        s.stage[s.local[d] + cnt[d] + rank[q]] = item[q];
+        if (pass == 0 && a.touched && item[q].x != a.none_key) a.touched[item[q].x] = 1;   // cleared before the barrier
+      }
+    }
+    __syncthreads();
+    if (a.blocks > 1) {
+#pragma unroll
+      for (int q = 0; q < kClusterItems; ++q) {
+        const uint32_t i = threadIdx.x + q * kClusterThreads;
+        if (i < n) {
+          const uint2 v = s.stage[i];
+          const uint32_t d = (v.x >> shift) & mask;
+          const uint32_t to = s.base[d] + (i - s.local[d]);                   // < N
+          store_remote(remote(&s.place[to % kBlockKeys], to / kBlockKeys), v);
+        }
+      }
+      cluster_sync();                      // every key is in its place
+    }
+    const uint2* from = a.blocks > 1 ? s.place : s.stage;
+#pragma unroll
+    for (int q = 0; q < kClusterItems; ++q)
+      if (at + q * 32 < n) item[q] = from[at + q * 32];
+    __syncthreads();                       // the digit tables are written again
+  }
+#pragma unroll
+  for (int q = 0; q < kClusterItems; ++q) {
+    if (at + q * 32 < n) {
+      a.key_out[first + at + q * 32] = item[q].x;
+      a.pos_out[first + at + q * 32] = item[q].y;
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ sums over the sorted list
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
@@ -393,9 +583,13 @@ embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
   if (blockIdx.x >= a.sum_blocks) {      // rows of absent tokens: zeros
     const uint32_t r0 = (blockIdx.x - a.sum_blocks) * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
     const float zero[8] = {};
-    for (uint32_t i = warp; i < (r1 - r0) * a.slabs; i += kSumWarps) {
-      const uint32_t r = r0 + i / a.slabs;
-      if (!a.touched[r]) write_row<TG, VEC>(grad.row(r), (int)(i % a.slabs), lane, a.D, zero, 0.f, false);
+    for (uint32_t r = r0; r < r1; r += 32) {
+      const uint32_t absent = __ballot_sync(0xFFFFFFFFu, r + lane < r1 && !a.touched[min(r + lane, r1 - 1)]);
+      const uint32_t items = min(32u, r1 - r) * a.slabs;
+      for (uint32_t i = warp; i < items; i += kSumWarps) {
+        const uint32_t k = i / a.slabs;
+        if (absent >> k & 1) write_row<TG, VEC>(grad.row(r + k), (int)(i - k * a.slabs), lane, a.D, zero, 0.f, false);
+      }
     }
     return;
   }
@@ -467,19 +661,19 @@ embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
   else write_row<TG, VEC>(grad.row(cur), slab, lane, a.D, acc, a.scale, a.add);
 }
 
-// One block per (piece, slab): if a token begins in the piece and goes on in the next ones, its partial rows are added in
-// order -- each warp a run of pieces, then the runs.
+// Block (piece, group of slabs): if a token begins in the piece and goes on in the next ones, its partial rows are added in
+// order.  Few: a warp adds a slab's alone; many: each warp a run of them, then the runs.
+constexpr int kJoinFew = 8;
+
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(kSumThreads)
 embed_join_kernel(SumArgs a, GradRows<TG> grad) {
   pdl_wait();
-  const uint32_t c = blockIdx.x / a.slabs;
-  const int slab = blockIdx.x - c * a.slabs;
+  const uint32_t c = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t next = (c + 1) * a.piece;           // < N: the last piece has no block
-  const uint32_t k = a.key[next];
-  if (k == a.none_key || a.key[next - 1] != k) return;
-  if (c > 0 && a.key[c * a.piece - 1] == k) return;  // it began earlier
+  const uint32_t k = a.key[next], mine = a.key[next - 1], before = c > 0 ? a.key[c * a.piece - 1] : ~k;
+  if (k == a.none_key || mine != k || before == k) return;   // nothing goes on, or it began earlier
   uint32_t last = c + 1;                             // last piece that begins with the token
   for (;;) {
     const uint32_t q = last + 1 + lane;
@@ -488,37 +682,50 @@ embed_join_kernel(SumArgs a, GradRows<TG> grad) {
     last += bits == 0xFFFFFFFFu ? 32 : __ffs(~bits) - 1;
     if (bits != 0xFFFFFFFFu) break;
   }
-  __shared__ float s_part[kSumWarps][kSlab];
-  const uint32_t n = last - c + 1;                   // partial rows
-  const uint32_t per = (n + kSumWarps - 1) / kSumWarps;
-  const float* src = a.part + (size_t)slab * kSlab + lane;
+  const uint32_t n = last - c + 1;                   // partial rows: the first piece's end, then whole beginnings
   const size_t row = (size_t)a.slabs * kSlab;
-  float acc[8] = {};
-  const uint32_t j1 = min(n, (warp + 1) * per);
+  const auto add = [&](int slab, uint32_t j0, uint32_t j1, float (&acc)[8]) {
+    const float* src = a.part + (size_t)slab * kSlab + lane;
 #pragma unroll 4
-  for (uint32_t j = warp * per; j < j1; ++j) {
-    const float* p = src + ((size_t)(c + j) * 2 + (j == 0)) * row;   // the first piece's end, then whole beginnings
+    for (uint32_t j = j0; j < j1; ++j) {
+      const float* p = src + ((size_t)(c + j) * 2 + (j == 0)) * row;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) acc[q] += p[q * 32];
+      for (int q = 0; q < 8; ++q) acc[q] += p[q * 32];
+    }
+  };
+  if (n <= kJoinFew) {
+    for (int slab = blockIdx.y + warp * gridDim.y; slab < (int)a.slabs; slab += kSumWarps * gridDim.y) {
+      float acc[8] = {};
+      add(slab, 0, n, acc);
+      write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
+    }
+    return;
   }
+  __shared__ float s_part[kSumWarps][kSlab];
+  const uint32_t per = (n + kSumWarps - 1) / kSumWarps, used = (n + per - 1) / per;
+  for (int slab = blockIdx.y; slab < (int)a.slabs; slab += gridDim.y) {
+    float acc[8] = {};
+    add(slab, min(n, warp * per), min(n, (warp + 1) * per), acc);
+    __syncthreads();
 #pragma unroll
-  for (int q = 0; q < 8; ++q) s_part[warp][q * 32 + lane] = acc[q];
-  __syncthreads();
-  if (warp != 0) return;
-  const uint32_t used = (n + per - 1) / per;
+    for (int q = 0; q < 8; ++q) s_part[warp][q * 32 + lane] = acc[q];
+    __syncthreads();
+    if (warp != 0) continue;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    float s = 0.f;
-    for (uint32_t w = 0; w < used; ++w) s += s_part[w][q * 32 + lane];
-    acc[q] = s;
+    for (int q = 0; q < 8; ++q) {
+      float s = 0.f;
+      for (uint32_t w = 0; w < used; ++w) s += s_part[w][q * 32 + lane];
+      acc[q] = s;
+    }
+    write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
   }
-  write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
 }
 
 // ------------------------------------------------------------------------------------------------ host
 struct SortPlan {
   uint32_t N, rows, piece, pieces, slabs, per_tile;
   int passes, bits, tiles;
+  bool cluster;
   size_t o_touched, o_key[2], o_pos[2], o_counts, o_part, bytes;
 };
 
@@ -528,23 +735,25 @@ SortPlan sort_plan(uint32_t N, uint32_t rows, int D) {
   s.rows = rows;
   int need = 1;
   while ((rows >> need) != 0) ++need;      // keys 0 .. rows (rows: no row)
-  s.passes = (need + kDigitBits - 1) / kDigitBits;
+  s.cluster = N <= kClusterKeys;
+  s.passes = s.cluster ? (need + kClusterBits - 1) / kClusterBits : (need + kDigitBits - 1) / kDigitBits;
   s.bits = (need + s.passes - 1) / s.passes;
   const uint32_t sub = (N + kSortTile - 1) / kSortTile;
   s.per_tile = ((sub + kMaxTiles - 1) / kMaxTiles) * kSortTile;
   s.tiles = (int)((N + s.per_tile - 1) / s.per_tile);
   s.slabs = (uint32_t)((D + kSlab - 1) / kSlab);
-  s.piece = 32;
-  while (s.piece < 128 && (uint64_t)(N / (2 * s.piece)) * s.slabs >= 8192) s.piece *= 2;
+  // pieces as long as there are still enough of them to fill the machine: every piece end can cost two partial rows
+  s.piece = 8;
+  while (s.piece < 128 && (uint64_t)(N / (2 * s.piece)) * s.slabs >= 4096) s.piece *= 2;
   s.pieces = (N + s.piece - 1) / s.piece;
   size_t off = 0;
   auto take = [&](size_t b) { size_t o = off; off += (b + 255) & ~size_t(255); return o; };
   s.o_touched = take(rows);
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < (s.cluster ? 1 : 2); ++i) {
     s.o_key[i] = take(sizeof(uint32_t) * (size_t)N);
     s.o_pos[i] = take(sizeof(uint32_t) * (size_t)N);
   }
-  s.o_counts = take(sizeof(uint32_t) * ((size_t)s.tiles << s.bits));
+  if (!s.cluster) s.o_counts = take(sizeof(uint32_t) * ((size_t)s.tiles << s.bits));
   s.o_part = take(sizeof(float) * 2 * (size_t)s.pieces * s.slabs * kSlab);
   s.bytes = off;
   return s;
@@ -604,6 +813,40 @@ cudaError_t launch_lookup(const lsgd_embed_desc* e, cudaStream_t s) {
                     rows_of<const TT>(e->table), rows_of<TA>(e->out), nvec, tx, e->scale);
 }
 
+cudaError_t launch_cluster_sort(const SortPlan& p, const Tokens& tok, char* w, uint8_t* touched, cudaStream_t s) {
+  static OncePerDevice once;
+  if (!once.here()) {
+    const cudaError_t e = cudaFuncSetAttribute(embed_cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sizeof(ClusterMemory));
+    if (e != cudaSuccess) return e;
+    once.here() = true;
+  }
+  ClusterSort a{};
+  a.key_out = reinterpret_cast<uint32_t*>(w + p.o_key[0]);
+  a.pos_out = reinterpret_cast<uint32_t*>(w + p.o_pos[0]);
+  a.touched = touched;
+  a.N = p.N;
+  a.none_key = a.rows = p.rows;
+  a.bits = p.bits;
+  a.passes = p.passes;
+  a.blocks = 1;
+  while ((uint32_t)a.blocks * kBlockKeys < p.N) a.blocks *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.blocks);
+  cfg.blockDim = dim3(kClusterThreads);
+  cfg.dynamicSmemBytes = sizeof(ClusterMemory);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = a.blocks;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = LSGD_NO_PDL ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, embed_cluster_sort_kernel, tok, a);
+}
+
 template <typename TG, typename TA, int VEC>
 cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   const bool shared = shared_grad(e);
@@ -629,9 +872,10 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   char* w = static_cast<char*>(e->scratch);
   uint8_t* touched = add ? nullptr : reinterpret_cast<uint8_t*>(w + p.o_touched);
   cudaError_t err;
-  if (touched && (err = cudaMemsetAsync(touched, 0, rows, s)) != cudaSuccess) return err;
+  if (p.cluster && (err = launch_cluster_sort(p, tok, w, touched, s)) != cudaSuccess) return err;
+  if (!p.cluster && touched && (err = cudaMemsetAsync(touched, 0, rows, s)) != cudaSuccess) return err;
   const size_t bins = size_t(1) << p.bits;
-  for (int i = 0; i < p.passes; ++i) {
+  for (int i = 0; i < (p.cluster ? 0 : p.passes); ++i) {
     SortPass a{};
     a.key_in = i ? reinterpret_cast<uint32_t*>(w + p.o_key[(i - 1) & 1]) : nullptr;
     a.pos_in = i ? reinterpret_cast<uint32_t*>(w + p.o_pos[(i - 1) & 1]) : nullptr;
@@ -652,8 +896,9 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
       return err;
   }
   SumArgs a{};
-  a.key = reinterpret_cast<uint32_t*>(w + p.o_key[(p.passes - 1) & 1]);
-  a.pos = reinterpret_cast<uint32_t*>(w + p.o_pos[(p.passes - 1) & 1]);
+  const int last = p.cluster ? 0 : (p.passes - 1) & 1;
+  a.key = reinterpret_cast<uint32_t*>(w + p.o_key[last]);
+  a.pos = reinterpret_cast<uint32_t*>(w + p.o_pos[last]);
   a.touched = touched;
   a.part = reinterpret_cast<float*>(w + p.o_part);
   a.N = p.N;
@@ -672,7 +917,7 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   if ((err = launch_pdl(embed_sum_kernel<TG, TA, VEC>, dim3(a.sum_blocks + zero_blocks), dim3(kSumThreads), 0, s, a, d_out, grad)) != cudaSuccess)
     return err;
   if (p.pieces > 1)
-    return launch_pdl(embed_join_kernel<TG, VEC>, dim3((p.pieces - 1) * slabs), dim3(kSumThreads), 0, s, a, grad);
+    return launch_pdl(embed_join_kernel<TG, VEC>, dim3(p.pieces - 1, slabs < 4 ? slabs : 4), dim3(kSumThreads), 0, s, a, grad);
   return cudaSuccess;
 }
 

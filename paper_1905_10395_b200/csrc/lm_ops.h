@@ -29,11 +29,11 @@ inline lsgd_status check_rows(const lsgd_rows& r, int64_t P, int64_t T, int64_t 
   if (reinterpret_cast<uintptr_t>(r.data) % bytes) return LSGD_ERR_ALIGNMENT;
   const int64_t lim = int64_t(1) << 56;
   if ((T > 1 && r.ld > lim / T) || (P > 1 && r.stride > lim / P)) return LSGD_ERR_TOO_LARGE;
-  if (written) {
+  if (written && T > 0) {
     const bool many_t = T > 1, many_p = P > 1 && !(shared_ok && r.stride == 0);
     if (many_t && r.ld < D) return LSGD_ERR_INVALID_ARG;
     if (many_p) {
-      const bool worker_major = r.stride >= (T > 0 ? (T - 1) * (many_t ? r.ld : 0) : 0) + D;
+      const bool worker_major = r.stride >= (many_t ? (T - 1) * r.ld : 0) + D;
       const bool row_major = r.stride >= D && (!many_t || r.ld >= (P - 1) * r.stride + D);
       if (!worker_major && !row_major) return LSGD_ERR_INVALID_ARG;
     }
