@@ -37,8 +37,10 @@ struct Tokens {
   }
   // (worker, token) as one number, or kNone
   __device__ __forceinline__ uint32_t key(uint32_t pos) const {
-    const uint32_t w = pos / T, t = pos - w * T;
-    const int64_t v = token(w, t);
+    const uint32_t w = pos / T;
+    return key_of(w, token(w, pos - w * T));
+  }
+  __device__ __forceinline__ uint32_t key_of(uint32_t w, int64_t v) const {
     if (v < 0 || v >= V) {
       atomicOr(&g_embed_status, FLAG_BAD_INDEX);
       return kNone;
@@ -236,13 +238,14 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
 }
 
 // ------------------------------------------------------------------------------------------------ sort
-// The lanes whose digit is this lane's: one vote per bit.  (A match instruction takes as many rounds as there are different
-// digits, 32 as a rule: the cluster sort of 65536 tokens takes XX us with it, XX us so.)
-__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool live, int bits) {
+// The lanes whose digit is this lane's: one vote per bit.
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool live) {
   uint32_t same = __ballot_sync(0xFFFFFFFFu, live);
-  for (int b = 0; b < bits; ++b) {
-    const uint32_t one = __ballot_sync(0xFFFFFFFFu, d >> b & 1);
-    same &= d >> b & 1 ? one : ~one;
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const int one = (int)(d << (31 - b)) >> 31;                // all bits are bit b
+    same &= ~(__ballot_sync(0xFFFFFFFFu, one) ^ (uint32_t)one);
   }
   return same;
 }
@@ -345,7 +348,7 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
       const uint32_t i = s + warp * (32 * kSortItems) + q * 32 + lane;
       const uint32_t d = (key[q] >> a.shift) & (bins - 1);
       const bool live = i < i1;
-      const uint32_t same = same_digit(d, live, a.bits);
+      const uint32_t same = same_digit<kDigitBits>(d, live);
       uint32_t prev = 0;
       if (live) prev = cnt[d];
       rank[q] = prev + __popc(same & ((1u << lane) - 1));
@@ -463,12 +466,19 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
   const uint32_t at = warp * (32 * kClusterItems) + lane;                     // of the thread's first key; 32 apart
 
   uint2 item[kClusterItems];
+  int64_t token[kClusterItems];            // all of them before the first is looked at
 #pragma unroll
   for (int q = 0; q < kClusterItems; ++q) {
-    item[q] = make_uint2(0, first + at + q * 32);
+    const uint32_t pos = first + at + q * 32, w = pos / tok.T;
+    item[q].y = pos;
+    token[q] = at + q * 32 < n ? tok.token(w, pos - w * tok.T) : 0;
+  }
+#pragma unroll
+  for (int q = 0; q < kClusterItems; ++q) {
+    item[q].x = a.none_key;
     if (at + q * 32 < n) {
-      item[q].x = tok.key(item[q].y);
-      if (item[q].x == kNone) item[q].x = a.none_key;
+      const uint32_t k = tok.key_of(item[q].y / tok.T, token[q]);
+      if (k != kNone) item[q].x = k;
     }
   }
   if (a.touched)
@@ -484,9 +494,11 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
     uint32_t rank[kClusterItems];
 #pragma unroll
     for (int q = 0; q < kClusterItems; ++q) {
+      rank[q] = 0;
+      if (warp * (32 * kClusterItems) + q * 32 >= n) break;                   // the whole warp
       const uint32_t d = (item[q].x >> shift) & mask;
       const bool live = at + q * 32 < n;
-      const uint32_t same = same_digit(d, live, a.bits);
+      const uint32_t same = same_digit<kClusterBits>(d, live);
       uint32_t prev = 0;
       if (live) prev = cnt[d];
       rank[q] = prev + __popc(same & ((1u << lane) - 1));
@@ -526,7 +538,6 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
       if (at + q * 32 < n) {
         const uint32_t d = (item[q].x >> shift) & mask;
         s.stage[s.local[d] + cnt[d] + rank[q]] = item[q];
-        if (pass == 0 && a.touched && item[q].x != a.none_key) a.touched[item[q].x] = 1;   // cleared before the barrier
       }
     }
     __syncthreads();
@@ -547,14 +558,19 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
 #pragma unroll
     for (int q = 0; q < kClusterItems; ++q)
       if (at + q * 32 < n) item[q] = from[at + q * 32];
-    __syncthreads();                       // the digit tables are written again
-  }
+    if (pass + 1 == a.passes) {
 #pragma unroll
-  for (int q = 0; q < kClusterItems; ++q) {
-    if (at + q * 32 < n) {
-      a.key_out[first + at + q * 32] = item[q].x;
-      a.pos_out[first + at + q * 32] = item[q].y;
+      for (int q = 0; q < kClusterItems; ++q) {
+        const uint32_t i = at + q * 32;
+        if (i < n) {
+          a.key_out[first + i] = item[q].x;
+          a.pos_out[first + i] = item[q].y;
+          // a row's first place marks it (flags were cleared before the cluster barriers)
+          if (a.touched && item[q].x != a.none_key && (i == 0 || from[i - 1].x != item[q].x)) a.touched[item[q].x] = 1;
+        }
+      }
     }
+    __syncthreads();                       // the digit tables are written again
   }
 }
 
