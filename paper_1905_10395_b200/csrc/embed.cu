@@ -6,8 +6,8 @@
 // writes every row of d_table once (the rows of absent tokens with zeros).
 //
 // The gradient must not depend on timing, so no row is added with atomics.  Two ways to the same sums:
-//   few tokens   one launch.  The block of position i leaves if an earlier position holds the same token; otherwise it
-//                finds the later ones by comparing all tokens, and adds their rows in order.
+//   few tokens   one launch.  Every block reads all tokens; a warp takes a position, leaves if an earlier one holds the same
+//                token, and otherwise lists the later ones and adds their rows in order.
 //   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 65536 positions in the shared
 //                memory of one cluster, in one launch, more with a histogram and a scatter launch per pass; a warp then
 //                walks a piece of the sorted list, adding rows
@@ -139,102 +139,154 @@ __device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, co
   }
 }
 
+// Adds rows list[j0 .. j1) of d_out to a lane's columns of a slab, kAhead rows in flight.
+template <typename TA, int VEC, typename List>
+__device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>& d_out, const List* list, uint32_t j0, uint32_t j1,
+                                         int slab, int lane, int D, float (&acc)[8]) {
+  constexpr int kAhead = 16 / (int)sizeof(TA);
+  for (uint32_t j = j0; j < j1; j += kAhead) {
+    Pack<TA, VEC> in[kAhead][8 / VEC];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (j + u >= j1) break;
+      const uint32_t pos = list[j + u], w = pos / tok.T;
+      const TA* row = d_out.row(w, pos - w * tok.T);
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i)
+        if (slab_col<VEC>(slab, lane, i) < D) in[u][i].load(row + slab_col<VEC>(slab, lane, i));
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (j + u >= j1) break;
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i) {
+        if (slab_col<VEC>(slab, lane, i) >= D) break;
+        float f[VEC];
+        in[u][i].get(f);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) acc[i * VEC + k] += f[k];
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ few tokens
-constexpr int kFewTokens = 1024;
+// One launch instead of three: XX us against XX us for 3 x 1021 tokens, and even with the sort at 4096.
+constexpr int kFewTokens = 4096;
 constexpr int kFewThreads = 256;
 constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kFewAlone = 128;                      // rows that one warp adds alone
+
+// The positions after `mine`'s that hold the same key, in order, into list[0 .. cap): returns how many there are with
+// itself, or 0 if there is an earlier one.  128 keys at a time, 4 to a lane; a whole warp calls it.
+__device__ __forceinline__ uint32_t find_same(const uint32_t* s_key, uint32_t N, uint32_t me, uint32_t mine, uint16_t* list, uint32_t cap) {
+  const int lane = threadIdx.x & 31;
+  uint32_t count = 0;
+  for (uint32_t j0 = 0; j0 < N; j0 += 128) {        // the keys behind the last are none's
+    const uint4 k = *reinterpret_cast<const uint4*>(s_key + j0 + lane * 4);
+    const uint32_t hit = (k.x == mine) | (k.y == mine) << 1 | (k.z == mine) << 2 | (k.w == mine) << 3;
+    const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, hit != 0);
+    if (lanes == 0) continue;
+    if (count == 0) {
+      const int l = __ffs(lanes) - 1;
+      if (j0 + l * 4 + __ffs(__shfl_sync(0xFFFFFFFFu, hit, l)) - 1 != me) return 0;
+    }
+    const uint32_t n = __popc(hit);
+    uint32_t incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    uint32_t place = count + incl - n;
+    for (uint32_t b = hit; b; b &= b - 1, ++place)
+      if (place < cap) list[place] = (uint16_t)(j0 + lane * 4 + __ffs(b) - 1);
+    count += __shfl_sync(0xFFFFFFFFu, incl, 31);
+  }
+  __syncwarp();
+  return count;
+}
 
 template <typename TG, typename TA, int VEC>
 __global__ void __launch_bounds__(kFewThreads)
-embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint32_t rows, uint32_t rows_per_block, int D,
-                      float scale, bool add) {
+embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint32_t rows, uint32_t rows_per_block, uint32_t sum_blocks,
+                      int slabs, int D, float scale, bool add) {
   pdl_wait();
-  __shared__ uint32_t s_bits[kFewTokens / 32];
+  __shared__ __align__(16) uint32_t s_key[kFewTokens];
+  __shared__ uint16_t s_list[kFewTokens];           // kFewAlone for each warp, or one long list
   __shared__ float s_part[kFewWarps][kSlab];
-  __shared__ uint32_t s_none;
-  const int slab = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (blockIdx.x >= tok.N) {             // rows of absent tokens: zeros
-    const uint32_t r0 = (blockIdx.x - tok.N) * rows_per_block;
+  __shared__ uint32_t s_count[kFewWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (uint32_t j0 = 0; j0 < tok.N; j0 += 4 * kFewThreads) {
+    int64_t t[4];                                   // in flight together
+    uint32_t w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t j = j0 + u * kFewThreads + threadIdx.x;
+      w[u] = tok.T < tok.N ? j / tok.T : 0;
+      t[u] = j < tok.N ? tok.token(w[u], j - w[u] * tok.T) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t j = j0 + u * kFewThreads + threadIdx.x;
+      s_key[j] = j < tok.N ? tok.key_of(w[u], t[u]) : kNone;
+    }
+  }
+  if (blockIdx.x >= sum_blocks) {                   // rows of absent tokens: zeros
+    uint32_t* s_bits = reinterpret_cast<uint32_t*>(s_list);
+    const uint32_t r0 = (blockIdx.x - sum_blocks) * rows_per_block;
     const uint32_t n = min(rows_per_block, rows - r0);
-    for (uint32_t i = threadIdx.x; i < kFewTokens / 32; i += kFewThreads) s_bits[i] = 0;
+    for (uint32_t i = threadIdx.x; i < (n + 31) / 32; i += kFewThreads) s_bits[i] = 0;
     __syncthreads();
     for (uint32_t j = threadIdx.x; j < tok.N; j += kFewThreads) {
-      const uint32_t k = tok.key(j);
+      const uint32_t k = s_key[j];
       if (k >= r0 && k - r0 < n) atomicOr(&s_bits[(k - r0) >> 5], 1u << ((k - r0) & 31));
     }
     __syncthreads();
     const float zero[8] = {};
     for (uint32_t r = warp; r < n; r += kFewWarps)
-      if (!(s_bits[r >> 5] >> (r & 31) & 1)) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
+      if (!(s_bits[r >> 5] >> (r & 31) & 1))
+        for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
     return;
   }
-  const uint32_t mine = tok.key(blockIdx.x);
-  if (mine == kNone) return;
-  if (threadIdx.x == 0) s_none = 0;
   __syncthreads();
-  const uint32_t words = (tok.N + 31) / 32;
-  bool earlier = false;
-  for (uint32_t w = warp; w < words; w += kFewWarps) {
-    const uint32_t j = w * 32 + lane;
-    const bool same = j < tok.N && tok.key(j) == mine;
-    earlier |= same && j < blockIdx.x;
-    const uint32_t bits = __ballot_sync(0xFFFFFFFFu, same);
-    if (lane == 0) s_bits[w] = bits;
-  }
-  if (__syncthreads_or(earlier)) return;
-  // each warp adds the rows of a run of words; the runs are added in order
-  const uint32_t per = (words + kFewWarps - 1) / kFewWarps;
-  float acc[8] = {};
-  bool any = false;
-  for (uint32_t w = warp * per; w < min(words, (warp + 1) * per); ++w) {
-    uint32_t bits = s_bits[w];
-    any |= bits != 0;
-    while (bits) {
-      constexpr int U = 4;
-      Pack<TA, VEC> in[U][8 / VEC];
-      int n = 0;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!bits) break;
-        const uint32_t pos = w * 32 + __ffs(bits) - 1;
-        bits &= bits - 1;
-        ++n;
-        const uint32_t p = pos / tok.T;
-        const TA* row = d_out.row(p, pos - p * tok.T);
-#pragma unroll
-        for (int i = 0; i < 8 / VEC; ++i)
-          if (slab_col<VEC>(slab, lane, i) < D) in[u][i].load(row + slab_col<VEC>(slab, lane, i));
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u >= n) break;
-#pragma unroll
-        for (int i = 0; i < 8 / VEC; ++i) {
-          if (slab_col<VEC>(slab, lane, i) >= D) break;
-          float f[VEC];
-          in[u][i].get(f);
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) acc[i * VEC + k] += f[k];
-        }
-      }
+  const uint32_t i = blockIdx.x * kFewWarps + warp;
+  const uint32_t mine = i < tok.N ? s_key[i] : kNone;
+  uint16_t* l = s_list + warp * kFewAlone;
+  const uint32_t count = mine == kNone ? 0 : find_same(s_key, tok.N, i, mine, l, kFewAlone);
+  if (count > 0 && count <= kFewAlone) {
+    for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
+      float acc[8] = {};
+      add_rows<TA, VEC>(tok, d_out, l, 0, count, slab, lane, D, acc);
+      write_row<TG, VEC>(grad.row(mine), slab, lane, D, acc, scale, add);
     }
   }
-  if (any) {
+  if (lane == 0) s_count[warp] = count > kFewAlone ? count : 0;
+  for (int h = 0; h < kFewWarps; ++h) {             // frequent tokens: the whole block
+    __syncthreads();
+    const uint32_t n = s_count[h];
+    if (n == 0) continue;
+    if (warp == h) find_same(s_key, tok.N, i, mine, s_list, kFewTokens);
+    __syncthreads();
+    const uint32_t per = (n + kFewWarps - 1) / kFewWarps, used = (n + per - 1) / per;
+    const uint32_t key = s_key[blockIdx.x * kFewWarps + h];
+    for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
+      float acc[8] = {};
+      add_rows<TA, VEC>(tok, d_out, s_list, min(n, warp * per), min(n, (warp + 1) * per), slab, lane, D, acc);
+      __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s_part[warp][k * 32 + lane] = acc[k];
-    if (lane == 0) atomicOr(&s_none, 1u << warp);
-  }
-  __syncthreads();
-  if (warp != 0) return;
-  const uint32_t have = s_none;
+      for (int k = 0; k < 8; ++k) s_part[warp][k * 32 + lane] = acc[k];
+      __syncthreads();
+      if (warp != 0) continue;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    float a = 0.f;
-    for (int w = 0; w < kFewWarps; ++w)
-      if (have >> w & 1) a += s_part[w][k * 32 + lane];
-    acc[k] = a;
+      for (int k = 0; k < 8; ++k) {
+        float v = 0.f;
+        for (uint32_t w = 0; w < used; ++w) v += s_part[w][k * 32 + lane];
+        acc[k] = v;
+      }
+      write_row<TG, VEC>(grad.row(key), slab, lane, D, acc, scale, add);
+    }
   }
-  write_row<TG, VEC>(grad.row(mine), slab, lane, D, acc, scale, add);
 }
 
 // ------------------------------------------------------------------------------------------------ sort
@@ -876,13 +928,13 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   uint32_t rows_per_block = (uint32_t)(65536 / (row_bytes < 64 ? 64 : row_bytes));   // about 64 KiB of zeros a block
   if (rows_per_block < 1) rows_per_block = 1;
   if (tok.N <= kFewTokens) {
-    const uint32_t few_rows = kFewTokens;  // bits that a block can mark
-    if (rows_per_block > few_rows) rows_per_block = few_rows;
+    if (rows_per_block > 1024) rows_per_block = 1024;
     if (rows_per_block < 32) rows_per_block = 32;
     const uint32_t zero_blocks = add ? 0 : (rows + rows_per_block - 1) / rows_per_block;
-    if (tok.N + zero_blocks == 0) return cudaSuccess;
-    return launch_pdl(embed_grad_few_kernel<TG, TA, VEC>, dim3(tok.N + zero_blocks, slabs), dim3(kFewThreads), 0, s, tok, d_out,
-                      grad, rows, rows_per_block, (int)e->D, e->scale, add);
+    const uint32_t sum_blocks = (tok.N + kFewWarps - 1) / kFewWarps;
+    if (sum_blocks + zero_blocks == 0) return cudaSuccess;
+    return launch_pdl(embed_grad_few_kernel<TG, TA, VEC>, dim3(sum_blocks + zero_blocks, slabs < 4 ? slabs : 4), dim3(kFewThreads), 0, s,
+                      tok, d_out, grad, rows, rows_per_block, sum_blocks, (int)slabs, (int)e->D, e->scale, add);
   }
   const SortPlan p = sort_plan(tok.N, rows, e->D);
   char* w = static_cast<char*>(e->scratch);

@@ -98,7 +98,7 @@ def test_lookup_shared_table_and_bad_tokens():
 
 @pytest.mark.parametrize("table", DT)
 @pytest.mark.parametrize("act", DT)
-@pytest.mark.parametrize("T", [40, 1500])               # few tokens: one launch; more: sorted
+@pytest.mark.parametrize("T", [40, 1500, 4500])         # few tokens: one launch; more: sorted
 @pytest.mark.parametrize("D", [1, 2, 8, 63, 250, 256, 264, 1032])
 def test_gradient_rows_and_types(table, act, T, D):
     backward(1, T, 300, D, table, act, seed=D)
@@ -106,7 +106,7 @@ def test_gradient_rows_and_types(table, act, T, D):
     backward(1, T, 40, D, table, act, pads=(3, 5), offset=1, padding=3, seed=D + 2)
 
 
-@pytest.mark.parametrize("T", [0, 1, 2, 31, 32, 33, 1023, 1024, 1025, 2048, 2049, 8191, 8192, 8193, 16385, 40000, 65536, 65537, 70001,
+@pytest.mark.parametrize("T", [0, 1, 2, 31, 32, 33, 1023, 1024, 1025, 2048, 2049, 4095, 4096, 4097, 8191, 8192, 8193, 16385, 40000, 65536, 65537, 70001,
                                140000])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_lengths(T, accumulate):
@@ -169,7 +169,7 @@ def test_same_inputs_same_bits():
 def test_scratch_is_free_and_the_op_repeats():
     """What the scratch holds at the call plays no part, and a bound operator may be called again with new values."""
     gen = torch.Generator().manual_seed(6)
-    for T in (3000, 70000):
+    for T in (5000, 70000):
         op, tab = backward(1, T, 400, 24, seed=1)
         first = tab.view.clone()
         op._keep[1].fill_(255)
