@@ -526,7 +526,7 @@ LSGD_API lsgd_status lsgd_blocknorm_backward(const lsgd_blocknorm_desc* desc, vo
  *                    whose change per step is smaller than a code's spacing would otherwise never move.  The random bits
  *                    are a hash of (seed, t, position), so a run can be repeated bit for bit.  A second moment that is not
  *                    zero is never rounded to zero.  A block that holds a moment that is not finite reads as NaN.
- * lsgd_adamw_create copies the HOST arrays and builds a table of the tensors on the current device (16 bytes per 4096
+ * lsgd_adamw_create copies the HOST arrays and builds a table of the tensors on the current device (40 bytes per 4096
  * parameters; the only allocation).  The gradients' addresses are fixed too: keep the buffers from step to step.
  * The step counter lives on the device, so captured steps replay correctly from a CUDA graph (lr is frozen in it). */
 typedef struct lsgd_adamw_ctx* lsgd_adamw_handle;
@@ -549,7 +549,7 @@ typedef struct {
   float* m_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   float* v_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   double beta1, beta2;       /* in [0, 1)                                                                      */
-  double eps;                /* > 0                                                                            */
+  double eps;                /* > 0 as a normal fp32 number                                                    */
   uint32_t seed;             /* LSGD_STATE_8BIT: of the random rounding                                        */
   void* stream;              /* cudaStream_t; NULL = the legacy default stream                                 */
 } lsgd_adamw_desc;

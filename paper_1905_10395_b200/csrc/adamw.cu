@@ -5,7 +5,8 @@
 // Bound by memory: per parameter 4 + 4 bytes of p, 4 or 2 of g, 2 of the copy and 16 bytes (fp32 moments) or 4 (8-bit ones)
 // of state.  A warp owns a block of 256 values, 8 a lane, so that the scales of the 8-bit moments (the largest magnitude of a
 // block) are one warp reduction and nothing is read twice.  The tensors are cut into chunks of 16 blocks; a persistent grid
-// walks the table of chunks, so tensors of every size are one launch.
+// walks the table of chunks (the next one's entry is on its way while one is computed), so tensors of every size are one
+// launch.
 //
 // An 8-bit code c stands for bits(c << 20) * 2^s * scale: c's bits become exponent and fraction of a small fp32 number
 // (exponent field from 0, so the lowest codes are fp32 subnormals, which the hardware multiplies at full speed), and the
@@ -32,27 +33,23 @@ constexpr int kBlock = 256;               // values that share a scale
 constexpr int kWarps = 8;
 constexpr int kChunk = kBlock * 2 * kWarps;
 
-struct Tensor {                           // one entry per tensor, device memory
-  float* p;
-  const void* g;
-  uint16_t* copy;
-  int64_t n;                              // values
-  int64_t at;                             // first value of its moments
-  float wd;
-  int32_t wide;                           // every pointer is aligned to 8 of its values
-};
 struct Counter {                          // steps taken; the running powers of beta1 and beta2
   double b1t, b2t;
   int64_t t;
   uint32_t done;                          // blocks of the running launch that have ended
 };
-struct Chunk {
-  int32_t tensor;
-  uint32_t index;                         // of the tensor's chunks
+struct Chunk {                            // 4096 values of a tensor, or what is left of it
+  float* p;
+  const void* g;
+  uint16_t* copy;
+  uint32_t block;                         // of the moments, the chunk's first
+  int32_t n;                              // values
+  float wd;
+  int32_t wide;                           // every pointer is aligned to 8 of its values
 };
+constexpr int kChunkWords = sizeof(Chunk) / 4;
 
 struct StepArgs {
-  const Tensor* tensors;
   const Chunk* chunks;
   Counter* counter;
   uint32_t n_chunks;
@@ -81,167 +78,273 @@ __device__ __forceinline__ uint32_t mix(uint32_t h) {
   return h ^ (h >> 13);
 }
 
-__device__ __forceinline__ float decode_m(uint32_t c, float scale) {
-  const float a = __fmul_rn(__fmul_rn(__uint_as_float((c & 127u) << 20), pow2(kShiftM)), scale);
-  return c & 128u ? -a : a;
+// Codes lie at the top of a word (byte 3) on their way: there they are 4 bits away from the float's bits.
+template <int K>
+__device__ __forceinline__ uint32_t top_byte(uint32_t w) { return __byte_perm(w, 0, 0x0444 | K << 12); }
+
+// 8 codes times their scale.  2^s scale is one factor where it is finite (FOLD): the same product, rounded once.
+template <bool SIGNED, bool FOLD>
+__device__ __forceinline__ void decode8(uint2 c, float scale, float2 (&f)[4]) {
+  constexpr float kPow = pow2(SIGNED ? kShiftM : kShiftV);
+  const float factor = FOLD ? __fmul_rn(scale, kPow) : scale;
+  uint32_t w[8] = {top_byte<0>(c.x), top_byte<1>(c.x), top_byte<2>(c.x), top_byte<3>(c.x),
+                   top_byte<0>(c.y), top_byte<1>(c.y), top_byte<2>(c.y), top_byte<3>(c.y)};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    uint32_t bits = w[k] >> 4;
+    if (SIGNED) bits = (bits & 0x07F00000u) | (w[k] & 0x80000000u);
+    (k & 1 ? f[k >> 1].y : f[k >> 1].x) = __uint_as_float(bits);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (!FOLD) f[k] = mul2(f[k], both(kPow));
+    f[k] = mul2(f[k], both(factor));
+  }
 }
-__device__ __forceinline__ float decode_v(uint32_t c, float scale) {
-  return __fmul_rn(__fmul_rn(__uint_as_float(c << 20), pow2(kShiftV)), scale);
-}
-// scale of a block from its largest magnitude, and the reciprocal that codes are made with.  A magnitude that is not finite
-// stays in the scale, so the block reads as NaN.
-__device__ __forceinline__ float block_scale(uint32_t top_bits, float& inv) {
+// Scales below this are folded into the powers of two, up and (as reciprocals) down, without overflow or loss.
+constexpr float kFoldBelow = 16384.f;
+
+// Scale of a block from its largest magnitude.  A magnitude that is not finite stays in the scale, so the block reads as NaN.
+__device__ __forceinline__ float block_scale(uint32_t top_bits) {
   const float top = __uint_as_float(top_bits);
-  const float scale = top < kTiny ? 0.f : __fmul_rn(top, kTop);
-  inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
-  return scale;
+  return top < kTiny ? 0.f : __fmul_rn(top, kTop);
 }
-__device__ __forceinline__ uint32_t encode_m(float z, float inv, uint32_t rnd16) {
-  const uint32_t bits = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(z), inv), pow2(-kShiftM)));
-  const uint32_t c = min((bits + (rnd16 << 4)) >> 20, 127u);
-  return c | (z < 0.f ? 128u : 0u);
-}
-__device__ __forceinline__ uint32_t encode_v(float z, float inv, uint32_t rnd16) {
-  const uint32_t bits = __float_as_uint(__fmul_rn(__fmul_rn(z, inv), pow2(-kShiftV)));
-  const uint32_t c = min((bits + (rnd16 << 4)) >> 20, 255u);
-  return bits ? max(c, 1u) : c;           // a second moment that is not zero keeps a denominator
+// 8 values as codes.  rnd: their hashes; the low half rounds m, the high half v.  The sum of a value's bits and 16 random ones
+// below the code is formed 4 bits to the left, so that the code is byte 3 and a sign has left the word.  No code overflows:
+// the largest value is at most 4 units in its last place above 1.875, and 15 and the largest random number do not carry.
+template <bool SIGNED, bool FOLD>
+__device__ __forceinline__ uint2 encode8(const float2 (&z)[4], float scale, const uint32_t (&rnd)[8]) {
+  constexpr float kPow = pow2(SIGNED ? -kShiftM : -kShiftV);
+  float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  if (FOLD) inv = __fmul_rn(inv, kPow);
+  uint32_t w[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float2 q = mul2(z[k], both(inv));
+    if (!FOLD) q = mul2(q, both(kPow));
+    w[2 * k] = __float_as_uint(q.x);
+    w[2 * k + 1] = __float_as_uint(q.y);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (!SIGNED && w[k] != 0) w[k] = max(w[k], 0x00100000u);     // a second moment that is not zero keeps a denominator
+    w[k] = (w[k] << 4) + __byte_perm(rnd[k], 0, SIGNED ? 0x4104 : 0x4324);
+    if (SIGNED) w[k] = (w[k] & 0x7FFFFFFFu) | (__float_as_uint(k & 1 ? z[k >> 1].y : z[k >> 1].x) & 0x80000000u);
+  }
+  uint2 c;
+  c.x = __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
+  c.y = __byte_perm(__byte_perm(w[4], w[5], 0x0073), __byte_perm(w[6], w[7], 0x0073), 0x5410);
+  return c;
 }
 
-__device__ __forceinline__ float approx_sqrt(float x) {
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+// Largest magnitude of a block, as bits (NaN is largest); a whole warp calls it.
+__device__ __forceinline__ uint32_t block_top(const float2 (&z)[4]) {
+  float top = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(z[k].x)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(z[k].y)));
+  }
+  return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top));
+}
+
+// 1 / (sqrt(v) root + eps).  Subnormal intermediates are flushed: eps is not below 2^-126.
+__device__ __forceinline__ float reciprocal_root(float v, float root, float eps) {
+  float s, r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(v));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(s, root, eps)));
   return r;
 }
 
+// A sum of products that are rounded first: as a pair the addition would be fused with one of them.
+__device__ __forceinline__ float2 sum(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+
+struct Scalars {
+  float step, root, gs;
+  uint32_t key;
+};
+
+// A lane's 8 values of a block as they lie in memory.
 template <typename TG, bool BYTES>
-__global__ void __launch_bounds__(kWarps * 32)
-adamw_step_kernel(const __grid_constant__ StepArgs a) {
-  pdl_wait();
-  __shared__ float s_k[2];
-  __shared__ uint32_t s_key;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) {
-    const double c1 = 1.0 - a.counter->b1t * a.beta1, c2 = 1.0 - a.counter->b2t * a.beta2;
-    s_k[0] = (float)(a.lr / c1);
-    s_k[1] = (float)(1.0 / sqrt(c2));
-    s_key = mix(mix(a.seed) ^ (uint32_t)(a.counter->t + 1));
+struct Lane8 {
+  Pack<float, 8> p;
+  Pack<TG, 8> g;
+  uint2 cm, cv;
+  float sm, sv;
+  Pack<float, 8> m, v;
+  __device__ __forceinline__ void load(const StepArgs& a, const Chunk& c, int j0, uint32_t block, int lane) {
+    p.load(c.p + j0);
+    g.load(static_cast<const TG*>(c.g) + j0);
+    load_moments(a, block, lane);
   }
-  __syncthreads();
-  const float step = s_k[0], root = s_k[1];
-  const uint32_t key = s_key;
-  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  for (uint32_t i = blockIdx.x; i < a.n_chunks; i += gridDim.x) {
-    const Chunk ch = a.chunks[i];
-    const Tensor t = a.tensors[ch.tensor];
-    const float keep = (float)(1.0 - a.lr * (double)t.wd);
+  __device__ __forceinline__ void load_moments(const StepArgs& a, uint32_t block, int lane) {
+    const size_t s0 = (size_t)block * kBlock + lane * 8;
+    if (BYTES) {
+      cm = *reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.m) + s0);
+      cv = *reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.v) + s0);
+      sm = a.m_scale[block];
+      sv = a.v_scale[block];
+    } else {
+      m.load(static_cast<float*>(a.m) + s0);
+      v.load(static_cast<float*>(a.v) + s0);
+    }
+  }
+};
+
+template <bool SIGNED>
+__device__ __forceinline__ void decode_block(uint2 c, float scale, float2 (&f)[4]) {
+  if (scale < kFoldBelow) decode8<SIGNED, true>(c, scale, f);
+  else decode8<SIGNED, false>(c, scale, f);
+}
+template <bool SIGNED>
+__device__ __forceinline__ uint2 encode_block(const float2 (&z)[4], float scale, const uint32_t (&rnd)[8]) {
+  return scale < kFoldBelow ? encode8<SIGNED, true>(z, scale, rnd) : encode8<SIGNED, false>(z, scale, rnd);
+}
+
+// The step of 8 values of one block in each lane; `have` of them are the tensor's.
+template <typename TG, bool BYTES>
+__device__ __forceinline__ void step8(const StepArgs& a, const Scalars& k_, const Chunk& c, const Lane8<TG, BYTES>& in, int j0, uint32_t block,
+                                      int lane, int have, bool wide) {
+  float2 p[4], g[4], m[4], v[4];
+  in.p.get(reinterpret_cast<float*>(p));
+  in.g.get(reinterpret_cast<float*>(g));
+  if (a.grad_scale) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int64_t j0 = (int64_t)ch.index * kChunk + (half * kWarps + warp) * kBlock + lane * 8;
-      const int64_t b0 = j0 - lane * 8;
-      if (b0 >= t.n) continue;            // whole warp
-      const int have = t.n - j0 >= 8 ? 8 : t.n - j0 > 0 ? (int)(t.n - j0) : 0;
-      const bool wide = t.wide && have == 8;
-      const int64_t s0 = t.at + j0;       // moments
-      float p[8], g[8], m[8], v[8];
-      if (wide) {
-        Pack<float, 8> pp;
-        pp.load(t.p + j0);
-        pp.get(p);
-        Pack<TG, 8> pg;
-        pg.load(static_cast<const TG*>(t.g) + j0);
-        pg.get(g);
-      } else {
+    for (int k = 0; k < 4; ++k) g[k] = mul2(g[k], both(k_.gs));
+  }
+  if (BYTES) {
+    decode_block<true>(in.cm, in.sm, m);
+    decode_block<false>(in.cv, in.sv, v);
+  } else {
+    in.m.get(reinterpret_cast<float*>(m));
+    in.v.get(reinterpret_cast<float*>(v));
+  }
+  const float decay = -(float)a.lr * c.wd;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          p[k] = k < have ? t.p[j0 + k] : 0.f;
-          g[k] = k < have ? (float)static_cast<const TG*>(t.g)[j0 + k] : 0.f;
-        }
-      }
-      if (a.grad_scale) {
+  for (int k = 0; k < 4; ++k) {           // every product and sum rounded by itself: the moments' bits do not depend on the code
+    m[k] = sum(mul2(m[k], both(a.b1)), mul2(g[k], both(a.omb1)));
+    v[k] = sum(mul2(v[k], both(a.b2)), mul2(mul2(g[k], both(a.omb2)), g[k]));
+    const float2 r = make_float2(reciprocal_root(v[k].x, k_.root, a.eps), reciprocal_root(v[k].y, k_.root, a.eps));
+    p[k] = fma2(mul2(m[k], r), both(-k_.step), fma2(p[k], both(decay), p[k]));   // two roundings of p's size
+  }
+  if (wide) {
+    Pack<float, 8> pp;
+    pp.set(reinterpret_cast<const float*>(p));
+    pp.store(c.p + j0);
+    if (c.copy) {
+      Pack<__nv_bfloat16, 8> pc;
+      pc.set(reinterpret_cast<const float*>(p));
+      pc.store(reinterpret_cast<__nv_bfloat16*>(c.copy) + j0);
+    }
+  } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) g[k] = __fmul_rn(g[k], gs);
-      }
-      if (BYTES) {
-        const uint2 cm = *reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.m) + s0);
-        const uint2 cv = *reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.v) + s0);
-        const float sm = a.m_scale[s0 / kBlock], sv = a.v_scale[s0 / kBlock];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          m[k] = decode_m((k < 4 ? cm.x : cm.y) >> (8 * (k & 3)) & 255u, sm);
-          v[k] = decode_v((k < 4 ? cv.x : cv.y) >> (8 * (k & 3)) & 255u, sv);
-        }
-      } else {
-        Pack<float, 8> q;
-        q.load(static_cast<float*>(a.m) + s0);
-        q.get(m);
-        q.load(static_cast<float*>(a.v) + s0);
-        q.get(v);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        m[k] = __fadd_rn(__fmul_rn(m[k], a.b1), __fmul_rn(g[k], a.omb1));
-        v[k] = __fadd_rn(__fmul_rn(v[k], a.b2), __fmul_rn(__fmul_rn(g[k], a.omb2), g[k]));
-        p[k] = p[k] * keep - step * __fdividef(m[k], fmaf(approx_sqrt(v[k]), root, a.eps));
-      }
-      if (wide) {
-        Pack<float, 8> pp;
-        pp.set(p);
-        pp.store(t.p + j0);
-        if (t.copy) {
-          Pack<__nv_bfloat16, 8> pc;
-          pc.set(p);
-          pc.store(reinterpret_cast<__nv_bfloat16*>(t.copy) + j0);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < have) {
-            t.p[j0 + k] = p[k];
-            if (t.copy) reinterpret_cast<__nv_bfloat16*>(t.copy)[j0 + k] = __float2bfloat16_rn(p[k]);
-          }
-      }
-      if (BYTES) {
-        uint32_t tm = 0, tv = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (k >= have) m[k] = v[k] = 0.f;
-          tm = max(tm, __float_as_uint(m[k]) & 0x7FFFFFFFu);
-          tv = max(tv, __float_as_uint(v[k]) & 0x7FFFFFFFu);
-        }
-        tm = __reduce_max_sync(0xFFFFFFFFu, tm);
-        tv = __reduce_max_sync(0xFFFFFFFFu, tv);
-        float im, iv;
-        const float sm = block_scale(tm, im), sv = block_scale(tv, iv);
-        uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t h = mix((uint32_t)(s0 + k) ^ key);
-          wm[k >> 2] |= encode_m(m[k], im, h & 0xFFFFu) << (8 * (k & 3));
-          wv[k >> 2] |= encode_v(v[k], iv, h >> 16) << (8 * (k & 3));
-        }
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s0) = make_uint2(wm[0], wm[1]);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s0) = make_uint2(wv[0], wv[1]);
-        if (lane == 0) {
-          a.m_scale[s0 / kBlock] = sm;
-          a.v_scale[s0 / kBlock] = sv;
-        }
-      } else if (have == 8) {
-        Pack<float, 8> q;
-        q.set(m);
-        q.store(static_cast<float*>(a.m) + s0);
-        q.set(v);
-        q.store(static_cast<float*>(a.v) + s0);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < have) {
-            static_cast<float*>(a.m)[s0 + k] = m[k];
-            static_cast<float*>(a.v)[s0 + k] = v[k];
-          }
+    for (int k = 0; k < 8; ++k) {
+      const float x = k & 1 ? p[k >> 1].y : p[k >> 1].x;
+      if (k < have) {
+        c.p[j0 + k] = x;
+        if (c.copy) reinterpret_cast<__nv_bfloat16*>(c.copy)[j0 + k] = __float2bfloat16_rn(x);
       }
     }
   }
+  const size_t s0 = (size_t)block * kBlock + lane * 8;
+  if (BYTES) {
+    if (have < 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k >= have) (k & 1 ? m[k >> 1].y : m[k >> 1].x) = (k & 1 ? v[k >> 1].y : v[k >> 1].x) = 0.f;
+    }
+    const float sm = block_scale(block_top(m)), sv = block_scale(block_top(v));
+    uint32_t rnd[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) rnd[k] = mix(((uint32_t)s0 + k) ^ k_.key);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s0) = encode_block<true>(m, sm, rnd);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s0) = encode_block<false>(v, sv, rnd);
+    if (lane == 0) {
+      a.m_scale[block] = sm;
+      a.v_scale[block] = sv;
+    }
+  } else if (have == 8) {
+    Pack<float, 8> q;
+    q.set(reinterpret_cast<const float*>(m));
+    q.store(static_cast<float*>(a.m) + s0);
+    q.set(reinterpret_cast<const float*>(v));
+    q.store(static_cast<float*>(a.v) + s0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < have) {
+        static_cast<float*>(a.m)[s0 + k] = k & 1 ? m[k >> 1].y : m[k >> 1].x;
+        static_cast<float*>(a.v)[s0 + k] = k & 1 ? v[k >> 1].y : v[k >> 1].x;
+      }
+  }
+}
+
+template <typename TG, bool BYTES>
+__global__ void __launch_bounds__(kWarps * 32, 3)
+adamw_step_kernel(const __grid_constant__ StepArgs a) {
+  pdl_wait();
+  __shared__ Scalars s_k;
+  __shared__ __align__(16) uint32_t s_chunk[2][kChunkWords];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const auto chunk_word = [&](uint32_t i) {
+    return i < a.n_chunks && threadIdx.x < kChunkWords ? reinterpret_cast<const uint32_t*>(a.chunks + i)[threadIdx.x] : 0;
+  };
+  const uint32_t word = chunk_word(blockIdx.x);
+  if (threadIdx.x < kChunkWords) s_chunk[0][threadIdx.x] = word;
+  if (threadIdx.x == 32) {
+    const double c1 = 1.0 - a.counter->b1t * a.beta1, c2 = 1.0 - a.counter->b2t * a.beta2;
+    s_k.step = (float)(a.lr / c1);
+    s_k.root = (float)(1.0 / sqrt(c2));
+    s_k.key = mix(mix(a.seed) ^ (uint32_t)(a.counter->t + 1));
+    s_k.gs = a.grad_scale ? *a.grad_scale : 1.f;
+  }
   __syncthreads();
+  const Scalars k = s_k;
+  int turn = 0;
+  for (uint32_t i = blockIdx.x; i < a.n_chunks; i += gridDim.x) {
+    const uint32_t next = chunk_word(i + gridDim.x);           // i + gridDim.x < 2^32: there are less than 2^31 chunks
+    const Chunk& c = *reinterpret_cast<const Chunk*>(s_chunk[turn]);
+    if (c.wide && c.n == kChunk) {
+      Lane8<TG, BYTES> in[2];
+      constexpr int kAhead = BYTES ? 2 : 1;                    // blocks whose loads are in flight before the first is computed
+#pragma unroll
+      for (int h = 0; h < 2; h += kAhead) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const int b = warp + (h + q) * kWarps;
+          in[q].load(a, c, b * kBlock + lane * 8, c.block + b, lane);
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const int b = warp + (h + q) * kWarps;
+          step8<TG, BYTES>(a, k, c, in[q], b * kBlock + lane * 8, c.block + b, lane, 8, true);
+        }
+      }
+    } else {
+      for (int b = warp; b * kBlock < c.n; b += kWarps) {      // whole warps
+        const int j0 = b * kBlock + lane * 8, have = max(0, min(8, c.n - j0));
+        const bool wide = c.wide && have == 8;
+        Lane8<TG, BYTES> in;
+        if (wide) {
+          in.load(a, c, j0, c.block + b, lane);
+        } else {
+          float f[8], h[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            f[q] = q < have ? c.p[j0 + q] : 0.f;
+            h[q] = q < have ? (float)static_cast<const TG*>(c.g)[j0 + q] : 0.f;
+          }
+          in.p.set(f);
+          in.g.set(h);
+          in.load_moments(a, c.block + b, lane);
+        }
+        step8<TG, BYTES>(a, k, c, in, j0, c.block + b, lane, have, wide);
+      }
+    }
+    turn ^= 1;
+    if (threadIdx.x < kChunkWords) s_chunk[turn][threadIdx.x] = next;
+    __syncthreads();
+  }
   if (threadIdx.x == 0) {                 // every block has read the counter by the time the last one moves it on
     __threadfence();
     if (atomicAdd(&a.counter->done, 1u) == gridDim.x - 1) {
@@ -253,27 +356,40 @@ adamw_step_kernel(const __grid_constant__ StepArgs a) {
   }
 }
 
+// A warp reads out kReadBlocks blocks at a time.
+constexpr int kReadBlocks = 4;
 __global__ void __launch_bounds__(256)
 adamw_moments_kernel(const uint8_t* m, const uint8_t* v, const float* m_scale, const float* v_scale, float* m_out, float* v_out,
-                     int64_t values) {
+                     uint32_t blocks) {
   pdl_wait();
-  const int64_t stride = (int64_t)gridDim.x * blockDim.x * 8;
-  for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 8; i < values; i += stride) {
+  const int lane = threadIdx.x & 31;
+  const uint64_t step = (uint64_t)gridDim.x * 8 * kReadBlocks;
+  for (uint64_t b0 = ((uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * kReadBlocks; b0 < blocks; b0 += step) {
+    uint2 cm[kReadBlocks], cv[kReadBlocks];
+    float sm[kReadBlocks], sv[kReadBlocks];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      float* out = which ? v_out : m_out;
-      if (!out) continue;
-      const uint2 c = *reinterpret_cast<const uint2*>((which ? v : m) + i);
-      const float s = (which ? v_scale : m_scale)[i / kBlock];
-      float f[8];
+    for (int q = 0; q < kReadBlocks; ++q) {
+      if (b0 + q >= blocks) break;
+      cm[q] = *reinterpret_cast<const uint2*>(m + (b0 + q) * kBlock + lane * 8);
+      cv[q] = *reinterpret_cast<const uint2*>(v + (b0 + q) * kBlock + lane * 8);
+      sm[q] = m_scale[b0 + q];
+      sv[q] = v_scale[b0 + q];
+    }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t b = (k < 4 ? c.x : c.y) >> (8 * (k & 3)) & 255u;
-        f[k] = which ? decode_v(b, s) : decode_m(b, s);
-      }
+    for (int q = 0; q < kReadBlocks; ++q) {
+      if (b0 + q >= blocks) break;
+      float2 f[4];
       Pack<float, 8> o;
-      o.set(f);
-      o.store(out + i);
+      if (m_out) {
+        decode_block<true>(cm[q], sm[q], f);
+        o.set(reinterpret_cast<const float*>(f));
+        o.store(m_out + (b0 + q) * kBlock + lane * 8);
+      }
+      if (v_out) {
+        decode_block<false>(cv[q], sv[q], f);
+        o.set(reinterpret_cast<const float*>(f));
+        o.store(v_out + (b0 + q) * kBlock + lane * 8);
+      }
     }
   }
 }
@@ -299,7 +415,7 @@ lsgd_status check_adamw(const lsgd_adamw_desc* d) {
   if (d->grad_dtype < LSGD_F32 || d->grad_dtype > LSGD_BF16 || d->state_dtype < LSGD_STATE_F32 || d->state_dtype > LSGD_STATE_8BIT)
     return LSGD_ERR_INVALID_ARG;
   if (!(d->beta1 >= 0 && d->beta1 < 1) || !(d->beta2 >= 0 && d->beta2 < 1) || !(d->eps > 0) || !std::isfinite((float)d->eps) ||
-      !((float)d->eps > 0))
+      !((float)d->eps >= 1.1754944e-38f))
     return LSGD_ERR_INVALID_ARG;
   const int64_t values = lsgd_adamw_state_values(d->n_tensors, d->sizes);
   if (values < 0) return LSGD_ERR_INVALID_ARG;
@@ -322,12 +438,11 @@ lsgd_status check_adamw(const lsgd_adamw_desc* d) {
 }
 
 Counter* counter_of(const lsgd_adamw_ctx* h) { return static_cast<Counter*>(h->slab); }
-Tensor* tensors_of(const lsgd_adamw_ctx* h) { return reinterpret_cast<Tensor*>(static_cast<char*>(h->slab) + 256); }
-Chunk* chunks_of(const lsgd_adamw_ctx* h) { return reinterpret_cast<Chunk*>(tensors_of(h) + h->d.n_tensors); }
+Chunk* chunks_of(const lsgd_adamw_ctx* h) { return reinterpret_cast<Chunk*>(static_cast<char*>(h->slab) + 256); }
 
 template <typename TG, bool BYTES>
 cudaError_t launch_step(const StepArgs& a, cudaStream_t s) {
-  const uint32_t cap = (uint32_t)sm_count() * 4;
+  const uint32_t cap = (uint32_t)sm_count() * 3;
   const uint32_t grid = a.n_chunks < 1 ? 1 : a.n_chunks < cap ? a.n_chunks : cap;   // one block even with nothing to do: it counts the step
   return launch_pdl(adamw_step_kernel<TG, BYTES>, dim3(grid), dim3(kWarps * 32), 0, s, a);
 }
@@ -366,7 +481,7 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* ou
   const int n = desc->n_tensors;
   uint64_t chunks = 0;
   for (int i = 0; i < n; ++i) chunks += (uint64_t)((desc->sizes[i] + kChunk - 1) / kChunk);
-  const size_t bytes = 256 + sizeof(Tensor) * (size_t)n + sizeof(Chunk) * (size_t)chunks;
+  const size_t bytes = 256 + sizeof(Chunk) * (size_t)chunks;
   char* host = new (std::nothrow) char[bytes]();
   if (!host) {
     delete h;
@@ -374,21 +489,22 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* ou
   }
   Counter* counter = reinterpret_cast<Counter*>(host);
   counter->b1t = counter->b2t = 1.0;
-  Tensor* t = reinterpret_cast<Tensor*>(host + 256);
-  Chunk* c = reinterpret_cast<Chunk*>(t + n);
+  Chunk* c = reinterpret_cast<Chunk*>(host + 256);
   const size_t gb = elem_bytes(desc->grad_dtype);
   int64_t at = 0;
   for (int i = 0; i < n; ++i) {
-    t[i].p = desc->params[i];
-    t[i].g = desc->grads[i];
-    t[i].copy = desc->copies ? desc->copies[i] : nullptr;
-    t[i].n = desc->sizes[i];
-    t[i].at = at;
-    t[i].wd = desc->weight_decay[i];
-    t[i].wide = aligned(t[i].p, 32) && aligned(t[i].g, 8 * gb) && aligned(t[i].copy, 16);
-    at += padded(t[i].n);
-    const uint64_t k = (uint64_t)((t[i].n + kChunk - 1) / kChunk);
-    for (uint64_t q = 0; q < k; ++q) *c++ = Chunk{i, (uint32_t)q};
+    uint16_t* copy = desc->copies ? desc->copies[i] : nullptr;
+    const bool wide = aligned(desc->params[i], 32) && aligned(desc->grads[i], 8 * gb) && aligned(copy, 16);
+    for (int64_t j = 0; j < desc->sizes[i]; j += kChunk, ++c) {
+      c->p = desc->params[i] + j;
+      c->g = static_cast<const char*>(desc->grads[i]) + j * gb;
+      c->copy = copy ? copy + j : nullptr;
+      c->block = (uint32_t)((at + j) / kBlock);
+      c->n = (int32_t)(desc->sizes[i] - j < kChunk ? desc->sizes[i] - j : kChunk);
+      c->wd = desc->weight_decay[i];
+      c->wide = wide;
+    }
+    at += padded(desc->sizes[i]);
   }
   h->values = at;
   h->chunks = (uint32_t)chunks;
@@ -416,7 +532,6 @@ lsgd_status lsgd_adamw_step(lsgd_adamw_handle h, double lr, const float* grad_sc
   if (!aligned(grad_scale, 4)) return LSGD_ERR_ALIGNMENT;
   if (!on_own_device(h)) return LSGD_ERR_STATE;
   StepArgs a{};
-  a.tensors = tensors_of(h);
   a.chunks = chunks_of(h);
   a.counter = counter_of(h);
   a.n_chunks = h->chunks;
@@ -453,10 +568,11 @@ lsgd_status lsgd_adamw_moments(lsgd_adamw_handle h, float* m_out, float* v_out) 
     if (v_out && cudaMemcpyAsync(v_out, h->d.v, n, cudaMemcpyDeviceToDevice, h->stream) != cudaSuccess) return LSGD_ERR_CUDA;
     return LSGD_OK;
   }
-  const int64_t blocks = (h->values / 8 + 255) / 256, cap = (int64_t)sm_count() * 8;
-  return launch_pdl(adamw_moments_kernel, dim3((unsigned)(blocks < cap ? blocks : cap)), dim3(256), 0, h->stream,
+  const uint32_t blocks = (uint32_t)(h->values / kBlock);
+  const int64_t want = ((int64_t)blocks + 8 * kReadBlocks - 1) / (8 * kReadBlocks), cap = (int64_t)sm_count() * 8;
+  return launch_pdl(adamw_moments_kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(256), 0, h->stream,
                     static_cast<const uint8_t*>(h->d.m), static_cast<const uint8_t*>(h->d.v), h->d.m_scale, h->d.v_scale, m_out,
-                    v_out, h->values) == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
+                    v_out, blocks) == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
 }
 
 lsgd_status lsgd_adamw_get_step(lsgd_adamw_handle h, int64_t* n) {

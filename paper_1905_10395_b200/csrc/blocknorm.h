@@ -72,20 +72,6 @@ constexpr int kSmemMax = 224 * 1024;      // dynamic shared memory of a block at
 #if defined(LSGD_BLOCKNORM_KERNELS)
 namespace {
 
-// ---- pairs of fp32
-__device__ __forceinline__ unsigned long long bits2(float2 a) { return *reinterpret_cast<unsigned long long*>(&a); }
-__device__ __forceinline__ float2 pair(unsigned long long u) { return *reinterpret_cast<float2*>(&u); }
-__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-  return pair(r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-  return pair(r);
-}
 #define LSGD_EACH(k) _Pragma("unroll") for (int k = 0; k < 4; ++k)
 
 // ---- a thread's columns: half h covers col[h] .. col[h] + 7; columns outside [0, D) are foreign

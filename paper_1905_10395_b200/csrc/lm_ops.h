@@ -130,6 +130,21 @@ struct Pack<__nv_bfloat16, 1> {
   __device__ __forceinline__ void get(float* f) const { f[0] = __bfloat162float(a); }
   __device__ __forceinline__ void set(const float* f) { a = __float2bfloat16_rn(f[0]); }
 };
+
+// Pairs of fp32, one instruction for both.
+__device__ __forceinline__ unsigned long long bits2(float2 a) { return *reinterpret_cast<unsigned long long*>(&a); }
+__device__ __forceinline__ float2 pair(unsigned long long u) { return *reinterpret_cast<float2*>(&u); }
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return pair(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return pair(r);
+}
 #endif  // __CUDACC__
 
 }  // namespace lsgd
