@@ -143,7 +143,7 @@ __device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, co
 template <typename TA, int VEC, typename List>
 __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>& d_out, const List* list, uint32_t j0, uint32_t j1,
                                          int slab, int lane, int D, float (&acc)[8]) {
-  constexpr int kAhead = 16 / (int)sizeof(TA);
+  constexpr int kAhead = VEC < 8 ? 3 : sizeof(TA) == 2 ? 8 : 4;   // what the registers of 4 blocks an SM hold
   for (uint32_t j = j0; j < j1; j += kAhead) {
     Pack<TA, VEC> in[kAhead][8 / VEC];
 #pragma unroll
@@ -175,16 +175,24 @@ __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>
 constexpr int kFewTokens = 4096;
 constexpr int kFewThreads = 256;
 constexpr int kFewWarps = kFewThreads / 32;
-constexpr int kFewAlone = 128;                      // rows that one warp adds alone
+constexpr int kFewLoads = 8;                        // tokens that a thread loads together; divides kFewTokens / kFewThreads
+constexpr int kFewAlone = 32;                       // rows that one warp adds alone
 
 // The positions after `mine`'s that hold the same key, in order, into list[0 .. cap): returns how many there are with
 // itself, or 0 if there is an earlier one.  128 keys at a time, 4 to a lane; a whole warp calls it.
 __device__ __forceinline__ uint32_t find_same(const uint32_t* s_key, uint32_t N, uint32_t me, uint32_t mine, uint16_t* list, uint32_t cap) {
   const int lane = threadIdx.x & 31;
   uint32_t count = 0;
-  for (uint32_t j0 = 0; j0 < N; j0 += 128) {        // the keys behind the last are none's
-    const uint4 k = *reinterpret_cast<const uint4*>(s_key + j0 + lane * 4);
-    const uint32_t hit = (k.x == mine) | (k.y == mine) << 1 | (k.z == mine) << 2 | (k.w == mine) << 3;
+  for (uint32_t j = 0; j < N; j += 512) {           // the keys behind the last are none's
+   uint32_t hits = 0;
+#pragma unroll
+   for (int u = 0; u < 4; ++u) {
+    const uint4 k = *reinterpret_cast<const uint4*>(s_key + j + u * 128 + lane * 4);
+    hits |= ((k.x == mine) | (k.y == mine) << 1 | (k.z == mine) << 2 | (k.w == mine) << 3) << (4 * u);
+   }
+   if (!__any_sync(0xFFFFFFFFu, hits)) continue;
+   for (int u = 0; u < 4; ++u) {
+    const uint32_t j0 = j + u * 128, hit = hits >> (4 * u) & 15u;
     const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, hit != 0);
     if (lanes == 0) continue;
     if (count == 0) {
@@ -202,13 +210,14 @@ __device__ __forceinline__ uint32_t find_same(const uint32_t* s_key, uint32_t N,
     for (uint32_t b = hit; b; b &= b - 1, ++place)
       if (place < cap) list[place] = (uint16_t)(j0 + lane * 4 + __ffs(b) - 1);
     count += __shfl_sync(0xFFFFFFFFu, incl, 31);
+   }
   }
   __syncwarp();
   return count;
 }
 
 template <typename TG, typename TA, int VEC>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, 4)
 embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint32_t rows, uint32_t rows_per_block, uint32_t sum_blocks,
                       int slabs, int D, float scale, bool add) {
   pdl_wait();
@@ -217,17 +226,17 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
   __shared__ float s_part[kFewWarps][kSlab];
   __shared__ uint32_t s_count[kFewWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (uint32_t j0 = 0; j0 < tok.N; j0 += 4 * kFewThreads) {
-    int64_t t[4];                                   // in flight together
-    uint32_t w[4];
+  for (uint32_t j0 = 0; j0 < tok.N; j0 += kFewLoads * kFewThreads) {
+    int64_t t[kFewLoads];                           // in flight together
+    uint32_t w[kFewLoads];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kFewLoads; ++u) {
       const uint32_t j = j0 + u * kFewThreads + threadIdx.x;
       w[u] = tok.T < tok.N ? j / tok.T : 0;
       t[u] = j < tok.N ? tok.token(w[u], j - w[u] * tok.T) : 0;
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kFewLoads; ++u) {
       const uint32_t j = j0 + u * kFewThreads + threadIdx.x;
       s_key[j] = j < tok.N ? tok.key_of(w[u], t[u]) : kNone;
     }
@@ -250,7 +259,7 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
     return;
   }
   __syncthreads();
-  const uint32_t i = blockIdx.x * kFewWarps + warp;
+  const uint32_t i = blockIdx.x + warp * sum_blocks;   // frequent tokens have their first position early: spread over the blocks
   const uint32_t mine = i < tok.N ? s_key[i] : kNone;
   uint16_t* l = s_list + warp * kFewAlone;
   const uint32_t count = mine == kNone ? 0 : find_same(s_key, tok.N, i, mine, l, kFewAlone);
@@ -269,7 +278,7 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
     if (warp == h) find_same(s_key, tok.N, i, mine, s_list, kFewTokens);
     __syncthreads();
     const uint32_t per = (n + kFewWarps - 1) / kFewWarps, used = (n + per - 1) / per;
-    const uint32_t key = s_key[blockIdx.x * kFewWarps + h];
+    const uint32_t key = s_key[blockIdx.x + h * sum_blocks];
     for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
       float acc[8] = {};
       add_rows<TA, VEC>(tok, d_out, s_list, min(n, warp * per), min(n, (warp + 1) * per), slab, lane, D, acc);
