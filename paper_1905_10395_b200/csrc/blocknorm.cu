@@ -12,50 +12,52 @@ __device__ __forceinline__ float gate_at(float z, int act, float& slope) {
   return v;
 }
 
-// Adds the blocks' partial rows in order.  Block: 32 columns of one of the three sums of one worker (of all workers where
-// they share the vector); each warp adds a run of rows, then the runs are added.
-constexpr int kJoinWarps = 32;
-constexpr int kJoinThreads = kJoinWarps * 32;
-__global__ void __launch_bounds__(kJoinThreads)
-blocknorm_join_kernel(const __grid_constant__ Args a) {
+// Adds the blocks' partial rows in order: columns of one of the three sums of one worker (of all workers where they share the
+// vector).  `split` warps share 32 columns, each adding a run of rows, then the runs are added.
+constexpr int kJoinMaxSplit = 32;
+struct Join {
+  int which[3];              // of the sums, per blockIdx.y
+  int split;
+};
+__global__ void __launch_bounds__(1024)
+blocknorm_join_kernel(const __grid_constant__ Args a, const __grid_constant__ Join join) {
   pdl_wait();
   const lsgd_blocknorm_desc& d = a.d;
-  const int j = blockIdx.y;              // 0: w_pre, 1: w_post, 2: channel gate -- the last two from the same sums
+  const int j = join.which[blockIdx.y];  // 0: w_pre, 1: w_post, 2: channel gate -- the last two from the same sums
   const lsgd_rows& o = j == 0 ? d.d_w_pre : j == 1 ? d.d_w_post : d.d_gate;
   const bool channel = d.gate_kind == LSGD_GATE_CHANNEL;
-  if (!o.data || (j == 0 && !d.w_pre.data) || (j == 1 && !d.post_norm) || (j == 2 && !channel)) return;
   const bool shared = d.P > 1 && o.stride == 0;
   if (shared && blockIdx.z > 0) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
-  __shared__ float s[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % join.split, group = warp / join.split;
+  const int col = (blockIdx.x * (blockDim.x / (32 * join.split)) + group) * 32 + lane;
+  __shared__ float s[kJoinMaxSplit][32];
   float total = 0.f;
+  const uint32_t per = (a.blocks_w + join.split - 1) / join.split, i0 = min(a.blocks_w, sub * per), i1 = min(a.blocks_w, i0 + per);
   for (uint32_t w = shared ? 0 : blockIdx.z, last = shared ? d.P - 1 : w; w <= last; ++w) {
-    const float* src = a.part + ((size_t)w * a.blocks_w * 2 + (j > 0)) * d.D + col;
-    const uint32_t per = (a.blocks_w + kJoinWarps - 1) / kJoinWarps, i1 = min(a.blocks_w, (warp + 1) * per);
-    float acc = 0.f;
-    if (col < d.D)
+    float v = 0.f;
+    if (col < d.D) {
+      const float* src = a.part + ((size_t)w * a.blocks_w * 2 + (j > 0)) * d.D + col;
 #pragma unroll 8
-      for (uint32_t i = warp * per; i < i1; ++i) acc += src[(size_t)i * 2 * d.D];
-    __syncthreads();
-    s[warp][lane] = acc;
-    __syncthreads();
-    if (warp == 0 && col < d.D) {
-      float v = 0.f;
-#pragma unroll
-      for (int q = 0; q < kJoinWarps; ++q) v += s[q][lane];
-      if (j > 0) {
-        float ga = 1.f, slope = 1.f;
-        if (channel) {
-          ga = gate_at(static_cast<const float*>(d.gate.data)[w * d.gate.stride + col], d.gate_act, slope);
-        }
-        v *= d.beta;
-        if (j == 1) v *= ga;
-        else v *= slope * (d.post_norm ? static_cast<const float*>(d.w_post.data)[w * d.w_post.stride + col] : 1.f);
-      }
-      total += v;
+      for (uint32_t i = i0; i < i1; ++i) v += src[(size_t)i * 2 * d.D];
     }
+    if (join.split > 1) {
+      __syncthreads();
+      s[warp][lane] = v;
+      __syncthreads();
+      v = 0.f;
+      if (sub == 0)
+        for (int q = 0; q < join.split; ++q) v += s[warp + q][lane];
+    }
+    if (sub == 0 && col < d.D && j > 0) {
+      float ga = 1.f, slope = 1.f;
+      if (channel) ga = gate_at(static_cast<const float*>(d.gate.data)[w * d.gate.stride + col], d.gate_act, slope);
+      v *= d.beta;
+      if (j == 1) v *= ga;
+      else v *= slope * (d.post_norm ? static_cast<const float*>(d.w_post.data)[w * d.w_post.stride + col] : 1.f);
+    }
+    total += v;
   }
-  if (warp != 0 || col >= d.D) return;
+  if (sub != 0 || col >= d.D) return;
   float* dst = static_cast<float*>(o.data) + (shared ? 0 : blockIdx.z) * o.stride + col;
   *dst = d.accumulate ? *dst + total : total;
 }
@@ -200,10 +202,15 @@ cudaError_t run(const lsgd_blocknorm_desc* d, bool backward, cudaStream_t st) {
     e = d->resid_dtype == LSGD_BF16 ? launch_bf16_bf16(a, s.l, st)
         : d->act_dtype == LSGD_BF16 ? launch_f32_bf16(a, s.l, st) : launch_f32_f32(a, s.l, st);
   if (e != cudaSuccess || !backward) return e;
-  const bool sums = (d->w_pre.data && d->d_w_pre.data) || (d->post_norm && d->d_w_post.data) ||
-                    (d->gate_kind == LSGD_GATE_CHANNEL && d->d_gate.data);
-  if (!sums) return cudaSuccess;
-  return launch_pdl(blocknorm_join_kernel, dim3((d->D + 31) / 32, 3, d->P), dim3(kJoinThreads), 0, st, a);
+  Join join{};
+  int n = 0;
+  if (d->w_pre.data && d->d_w_pre.data) join.which[n++] = 0;
+  if (d->post_norm && d->d_w_post.data) join.which[n++] = 1;
+  if (d->gate_kind == LSGD_GATE_CHANNEL && d->d_gate.data) join.which[n++] = 2;
+  if (n == 0) return cudaSuccess;
+  join.split = s.blocks_w <= 16 ? 1 : s.blocks_w <= 64 ? 8 : kJoinMaxSplit;
+  const int threads = join.split == kJoinMaxSplit ? 1024 : 256, cols = threads / join.split;
+  return launch_pdl(blocknorm_join_kernel, dim3((d->D + cols - 1) / cols, n, d->P), dim3(threads), 0, st, a, join);
 }
 
 }  // namespace

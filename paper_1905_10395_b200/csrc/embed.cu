@@ -8,7 +8,7 @@
 // The gradient must not depend on timing, so no row is added with atomics.  Two ways to the same sums:
 //   few tokens   one launch.  Every block reads all tokens; a warp takes a position, leaves if an earlier one holds the same
 //                token, and otherwise lists the later ones and adds their rows in order.
-//   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 65536 positions in the shared
+//   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 131072 positions in the shared
 //                memory of one cluster, in one launch, more with a histogram and a scatter launch per pass; a warp then
 //                walks a piece of the sorted list, adding rows
 //                while the token stays the same.  A token that lies within one piece is written at once; pieces of a
@@ -75,25 +75,34 @@ embed_lookup_kernel(Tokens tok, Rows<const TT> table, Rows<TA> out, uint32_t nve
       else if (cx == 0 && blockIdx.y == 0) atomicOr(&g_embed_status, FLAG_BAD_INDEX);
     }
   }
-  for (uint32_t c = blockIdx.y * tx + cx; c < nvec; c += gridDim.y * tx) {
-    Pack<TT, VEC> in[kLookupRows];
+  constexpr int kPieces = VEC == 8 ? 1 : 4;      // narrow pieces: several in flight
+  for (uint32_t c0 = blockIdx.y * tx + cx; c0 < nvec; c0 += kPieces * gridDim.y * tx) {
+    Pack<TT, VEC> in[kPieces][kLookupRows];
 #pragma unroll
-    for (int u = 0; u < kLookupRows; ++u)
-      if (src[u]) in[u].load(src[u] + (int64_t)c * VEC);
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t c = c0 + i * gridDim.y * tx;
 #pragma unroll
-    for (int u = 0; u < kLookupRows; ++u) {
-      if (!dst[u]) continue;
-      float f[VEC];
+      for (int u = 0; u < kLookupRows; ++u)
+        if (src[u] && c < nvec) in[i][u].load(src[u] + (int64_t)c * VEC);
+    }
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) f[k] = 0.f;
-      if (src[u]) {
-        in[u].get(f);
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t c = c0 + i * gridDim.y * tx;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) f[k] *= scale;
+      for (int u = 0; u < kLookupRows; ++u) {
+        if (!dst[u] || c >= nvec) continue;
+        float f[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] = 0.f;
+        if (src[u]) {
+          in[i][u].get(f);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) f[k] *= scale;
+        }
+        Pack<TA, VEC> o;
+        o.set(f);
+        o.store(dst[u] + (int64_t)c * VEC);
       }
-      Pack<TA, VEC> o;
-      o.set(f);
-      o.store(dst[u] + (int64_t)c * VEC);
     }
   }
 }
@@ -226,6 +235,7 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
   __shared__ float s_part[kFewWarps][kSlab];
   __shared__ uint32_t s_count[kFewWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x >= sum_blocks && blockIdx.y > 0) return;
   for (uint32_t j0 = 0; j0 < tok.N; j0 += kFewLoads * kFewThreads) {
     int64_t t[kFewLoads];                           // in flight together
     uint32_t w[kFewLoads];
@@ -255,7 +265,7 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
     const float zero[8] = {};
     for (uint32_t r = warp; r < n; r += kFewWarps)
       if (!(s_bits[r >> 5] >> (r & 31) & 1))
-        for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
+        for (int slab = 0; slab < slabs; ++slab) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
     return;
   }
   __syncthreads();
@@ -369,6 +379,7 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
   for (uint32_t q = 0; q < per; ++q) {
     const uint32_t b = threadIdx.x * per + q;
     if (b < bins) {
+#pragma unroll 16
       for (int t = 0; t < a.tiles; ++t) {
         const uint32_t n = a.counts[(size_t)t * bins + b];
         total[q] += n;
@@ -445,17 +456,16 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
   }
 }
 
-// ---- up to kClusterKeys keys: the whole sort in the shared memory of one cluster.  A block holds kBlockKeys consecutive
+// ---- up to kClusterKeys keys: the whole sort in the shared memory of one cluster.  A block holds 1024 ITEMS consecutive
 // places.  A pass orders the block's own keys by digit in its shared memory, adds up the blocks' digit counts through
 // distributed shared memory, and copies the keys to their places in whichever block holds them: in the order of the digits,
 // so that a warp's stores to another block are runs of consecutive places.  Two cluster barriers a pass instead of two
 // launches.
 constexpr int kClusterThreads = 1024;
 constexpr int kClusterWarps = kClusterThreads / 32;
-constexpr int kClusterItems = 4;
-constexpr int kBlockKeys = kClusterThreads * kClusterItems;    // 4096
 constexpr int kClusterBlocks = 16;                             // 8 (the portable size) of twice the keys: 30 us instead of 20 for 65536
-constexpr int kClusterKeys = kBlockKeys * kClusterBlocks;      // 65536
+constexpr int kClusterItems = 8;                               // keys of a thread: 4, or 8 beyond 65536
+constexpr int kClusterKeys = kClusterThreads * kClusterItems * kClusterBlocks;
 constexpr int kClusterBits = 9;
 constexpr int kClusterBins = 1 << kClusterBits;
 
@@ -487,9 +497,10 @@ struct ClusterSort {
   uint32_t N, none_key, rows;
   int bits, passes, blocks;
 };
+template <int ITEMS>
 struct ClusterMemory {
-  uint2 stage[kBlockKeys];    // (key, position): this block's keys in the order of their digits
-  uint2 place[kBlockKeys];    // what the blocks have put in this block's places
+  uint2 stage[kClusterThreads * ITEMS];    // (key, position): this block's keys in the order of their digits
+  uint2 place[kClusterThreads * ITEMS];    // what the blocks have put in this block's places
   uint32_t count[kClusterBins];                    // this block's digits; read by all blocks
   uint32_t base[kClusterBins];                     // first place of this block's digit
   uint32_t local[kClusterBins];                    // first place of the digit in `stage`
@@ -513,29 +524,31 @@ __device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* s_scan) {
   return sums + incl - v;
 }
 
+template <int ITEMS>
 __global__ void __launch_bounds__(kClusterThreads, 1)
 embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
   pdl_wait();
   pdl_launch_dependents();
   extern __shared__ uint32_t smem[];
-  ClusterMemory& s = *reinterpret_cast<ClusterMemory*>(smem);
+  constexpr uint32_t kBlockKeys = kClusterThreads * ITEMS;
+  ClusterMemory<ITEMS>& s = *reinterpret_cast<ClusterMemory<ITEMS>*>(smem);
   const uint32_t bins = 1u << a.bits;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t me = cluster_rank();
   const uint32_t first = me * kBlockKeys;
   const uint32_t n = a.N > first ? min(a.N - first, (uint32_t)kBlockKeys) : 0;   // places of this block
-  const uint32_t at = warp * (32 * kClusterItems) + lane;                     // of the thread's first key; 32 apart
+  const uint32_t at = warp * (32 * ITEMS) + lane;                     // of the thread's first key; 32 apart
 
-  uint2 item[kClusterItems];
-  int64_t token[kClusterItems];            // all of them before the first is looked at
+  uint2 item[ITEMS];
+  int64_t token[ITEMS];            // all of them before the first is looked at
 #pragma unroll
-  for (int q = 0; q < kClusterItems; ++q) {
+  for (int q = 0; q < ITEMS; ++q) {
     const uint32_t pos = first + at + q * 32, w = pos / tok.T;
     item[q].y = pos;
     token[q] = at + q * 32 < n ? tok.token(w, pos - w * tok.T) : 0;
   }
 #pragma unroll
-  for (int q = 0; q < kClusterItems; ++q) {
+  for (int q = 0; q < ITEMS; ++q) {
     item[q].x = a.none_key;
     if (at + q * 32 < n) {
       const uint32_t k = tok.key_of(item[q].y / tok.T, token[q]);
@@ -552,11 +565,11 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
     for (uint32_t b = lane; b < bins; b += 32) s.warp[warp][b] = 0;
     __syncwarp();
     uint16_t* cnt = s.warp[warp];
-    uint32_t rank[kClusterItems];
+    uint32_t rank[ITEMS];
 #pragma unroll
-    for (int q = 0; q < kClusterItems; ++q) {
+    for (int q = 0; q < ITEMS; ++q) {
       rank[q] = 0;
-      if (warp * (32 * kClusterItems) + q * 32 >= n) break;                   // the whole warp
+      if (warp * (32 * ITEMS) + q * 32 >= n) break;                   // the whole warp
       const uint32_t d = (item[q].x >> shift) & mask;
       const bool live = at + q * 32 < n;
       const uint32_t same = same_digit<kClusterBits>(d, live);
@@ -595,7 +608,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
     const uint32_t start = scan_before(total, s.scan[1]);
     if (threadIdx.x < bins) s.base[threadIdx.x] = start + before;
 #pragma unroll
-    for (int q = 0; q < kClusterItems; ++q) {
+    for (int q = 0; q < ITEMS; ++q) {
       if (at + q * 32 < n) {
         const uint32_t d = (item[q].x >> shift) & mask;
         s.stage[s.local[d] + cnt[d] + rank[q]] = item[q];
@@ -604,7 +617,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
     __syncthreads();
     if (a.blocks > 1) {
 #pragma unroll
-      for (int q = 0; q < kClusterItems; ++q) {
+      for (int q = 0; q < ITEMS; ++q) {
         const uint32_t i = threadIdx.x + q * kClusterThreads;
         if (i < n) {
           const uint2 v = s.stage[i];
@@ -617,11 +630,11 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
     }
     const uint2* from = a.blocks > 1 ? s.place : s.stage;
 #pragma unroll
-    for (int q = 0; q < kClusterItems; ++q)
+    for (int q = 0; q < ITEMS; ++q)
       if (at + q * 32 < n) item[q] = from[at + q * 32];
     if (pass + 1 == a.passes) {
 #pragma unroll
-      for (int q = 0; q < kClusterItems; ++q) {
+      for (int q = 0; q < ITEMS; ++q) {
         const uint32_t i = at + q * 32;
         if (i < n) {
           a.key_out[first + i] = item[q].x;
@@ -638,6 +651,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
 // ------------------------------------------------------------------------------------------------ sums over the sorted list
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
+constexpr uint32_t kMaxPiece = 64;
 
 struct SumArgs {
   const uint32_t *key, *pos;  // sorted
@@ -680,9 +694,11 @@ embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
   float* part = a.part + ((size_t)c * 2 * a.slabs + slab) * kSlab;
   float acc[8] = {};
   const auto to_part = [&](int which) {
-    float* o = part + (size_t)which * a.slabs * kSlab;
+    float* o = part + (size_t)which * a.slabs * kSlab + lane * 8;
+    Pack<float, 8> v;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k * 32 + lane] = acc[k];
+    for (int k = 0; k < 8; ++k) v.v[k] = acc[k];
+    v.store(o);
   };
   constexpr int U = 4;
   for (uint32_t i = i0; i < i1; i += 32) {
@@ -738,63 +754,84 @@ embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
   else write_row<TG, VEC>(grad.row(cur), slab, lane, a.D, acc, a.scale, a.add);
 }
 
-// Block (piece, group of slabs): if a token begins in the piece and goes on in the next ones, its partial rows are added in
-// order.  Few: a warp adds a slab's alone; many: each warp a run of them, then the runs.
-constexpr int kJoinFew = 8;
+// A warp takes a piece: if a token begins in it and goes on in the next ones, its partial rows are added in order.  Few: by
+// the warp alone; many: by the block, each warp a run of them, then the runs.
+constexpr uint32_t kJoinFew = 16;
 
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(kSumThreads)
 embed_join_kernel(SumArgs a, GradRows<TG> grad) {
   pdl_wait();
-  const uint32_t c = blockIdx.x;
+  __shared__ uint32_t s_n[kSumWarps], s_key[kSumWarps];
+  __shared__ float s_part[kSumWarps][kSlab];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t next = (c + 1) * a.piece;           // < N: the last piece has no block
-  const uint32_t k = a.key[next], mine = a.key[next - 1], before = c > 0 ? a.key[c * a.piece - 1] : ~k;
-  if (k == a.none_key || mine != k || before == k) return;   // nothing goes on, or it began earlier
-  uint32_t last = c + 1;                             // last piece that begins with the token
-  for (;;) {
-    const uint32_t q = last + 1 + lane;
-    const bool same = q < a.pieces && a.key[q * a.piece] == k;
-    const uint32_t bits = __ballot_sync(0xFFFFFFFFu, same);
-    last += bits == 0xFFFFFFFFu ? 32 : __ffs(~bits) - 1;
-    if (bits != 0xFFFFFFFFu) break;
+  const uint32_t c = blockIdx.x + warp * gridDim.x;  // spread: a long token's pieces are neighbours
+  uint32_t n = 0, k = 0;                             // partial rows: the first piece's end, then whole beginnings
+  if (c + 1 < a.pieces) {
+    const uint32_t next = (c + 1) * a.piece;
+    k = a.key[next];
+    const uint32_t mine = a.key[next - 1], before = c > 0 ? a.key[c * a.piece - 1] : ~k;
+    if (k != a.none_key && mine == k && before != k) {
+      uint32_t last = c + 1;                         // last piece that begins with the token
+      for (;;) {
+        const uint32_t q = last + 1 + lane;
+        const bool same = q < a.pieces && a.key[q * a.piece] == k;
+        const uint32_t bits = __ballot_sync(0xFFFFFFFFu, same);
+        last += bits == 0xFFFFFFFFu ? 32 : __ffs(~bits) - 1;
+        if (bits != 0xFFFFFFFFu) break;
+      }
+      n = last - c + 1;
+    }
   }
-  const uint32_t n = last - c + 1;                   // partial rows: the first piece's end, then whole beginnings
   const size_t row = (size_t)a.slabs * kSlab;
-  const auto add = [&](int slab, uint32_t j0, uint32_t j1, float (&acc)[8]) {
-    const float* src = a.part + (size_t)slab * kSlab + lane;
-#pragma unroll 4
-    for (uint32_t j = j0; j < j1; ++j) {
-      const float* p = src + ((size_t)(c + j) * 2 + (j == 0)) * row;
+  const auto add = [&](uint32_t first, int slab, uint32_t j0, uint32_t j1, float (&acc)[8]) {
+    const float* src = a.part + (size_t)slab * kSlab + lane * 8;
+    constexpr int kAhead = 4;
+    for (uint32_t j = j0; j < j1; j += kAhead) {
+      Pack<float, 8> v[kAhead];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) acc[q] += p[q * 32];
+      for (int u = 0; u < kAhead; ++u)
+        if (j + u < j1) v[u].load(src + ((size_t)(first + j + u) * 2 + (j + u == 0)) * row);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (j + u >= j1) break;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) acc[q] += v[u].v[q];
+      }
     }
   };
-  if (n <= kJoinFew) {
-    for (int slab = blockIdx.y + warp * gridDim.y; slab < (int)a.slabs; slab += kSumWarps * gridDim.y) {
+  if (n > 0 && n <= kJoinFew) {
+    for (int slab = blockIdx.y; slab < (int)a.slabs; slab += gridDim.y) {
       float acc[8] = {};
-      add(slab, 0, n, acc);
+      add(c, slab, 0, n, acc);
       write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
     }
-    return;
   }
-  __shared__ float s_part[kSumWarps][kSlab];
-  const uint32_t per = (n + kSumWarps - 1) / kSumWarps, used = (n + per - 1) / per;
-  for (int slab = blockIdx.y; slab < (int)a.slabs; slab += gridDim.y) {
-    float acc[8] = {};
-    add(slab, min(n, warp * per), min(n, (warp + 1) * per), acc);
-    __syncthreads();
+  if (lane == 0) {
+    s_n[warp] = n > kJoinFew ? n : 0;
+    s_key[warp] = k;
+  }
+  __syncthreads();
+  for (int h = 0; h < kSumWarps; ++h) {
+    const uint32_t m = s_n[h];
+    if (m == 0) continue;                            // the same for the whole block
+    const uint32_t per = (m + kSumWarps - 1) / kSumWarps, used = (m + per - 1) / per, first = blockIdx.x + h * gridDim.x;
+    for (int slab = blockIdx.y; slab < (int)a.slabs; slab += gridDim.y) {
+      float acc[8] = {};
+      add(first, slab, min(m, warp * per), min(m, (warp + 1) * per), acc);
+      __syncthreads();
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s_part[warp][q * 32 + lane] = acc[q];
-    __syncthreads();
-    if (warp != 0) continue;
+      for (int q = 0; q < 8; ++q) s_part[warp][q * 32 + lane] = acc[q];
+      __syncthreads();
+      if (warp != 0) continue;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      float s = 0.f;
-      for (uint32_t w = 0; w < used; ++w) s += s_part[w][q * 32 + lane];
-      acc[q] = s;
+      for (int q = 0; q < 8; ++q) {
+        float v = 0.f;
+        for (uint32_t w = 0; w < used; ++w) v += s_part[w][q * 32 + lane];
+        acc[q] = v;
+      }
+      write_row<TG, VEC>(grad.row(s_key[h]), slab, lane, a.D, acc, a.scale, a.add);
     }
-    write_row<TG, VEC>(grad.row(k), slab, lane, a.D, acc, a.scale, a.add);
   }
 }
 
@@ -806,11 +843,12 @@ struct SortPlan {
   size_t o_touched, o_key[2], o_pos[2], o_counts, o_part, bytes;
 };
 
+template <int ITEMS>
 cudaLaunchConfig_t cluster_config(int blocks, cudaStream_t s, cudaLaunchAttribute (&at)[2]) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(kClusterThreads);
-  cfg.dynamicSmemBytes = sizeof(ClusterMemory);
+  cfg.dynamicSmemBytes = sizeof(ClusterMemory<ITEMS>);
   cfg.stream = s;
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = blocks;
@@ -823,18 +861,18 @@ cudaLaunchConfig_t cluster_config(int blocks, cudaStream_t s, cudaLaunchAttribut
 }
 
 // Whether the device can hold a cluster of kClusterBlocks (16 is more than the portable 8).  Looked up once per device.
+template <int ITEMS>
 bool cluster_fits() {
   static OncePerDevice once, fits;
   if (!once.here()) {
     int n = 0;
     cudaLaunchAttribute at[2];
-    cudaLaunchConfig_t cfg = cluster_config(kClusterBlocks, nullptr, at);
+    cudaLaunchConfig_t cfg = cluster_config<ITEMS>(kClusterBlocks, nullptr, at);
     cfg.numAttrs = 1;
-    fits.here() =
-        cudaFuncSetAttribute(embed_cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ClusterMemory)) ==
-            cudaSuccess &&
-        cudaFuncSetAttribute(embed_cluster_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-        cudaOccupancyMaxActiveClusters(&n, embed_cluster_sort_kernel, &cfg) == cudaSuccess && n > 0;
+    const auto kernel = embed_cluster_sort_kernel<ITEMS>;
+    fits.here() = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) == cudaSuccess &&
+                  cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
     if (!fits.here()) (void)cudaGetLastError();
     once.here() = true;
   }
@@ -847,7 +885,7 @@ SortPlan sort_plan(uint32_t N, uint32_t rows, int D) {
   s.rows = rows;
   int need = 1;
   while ((rows >> need) != 0) ++need;      // keys 0 .. rows (rows: no row)
-  s.cluster = N <= kClusterKeys && cluster_fits();
+  s.cluster = N <= kClusterKeys / 2 ? cluster_fits<4>() : N <= kClusterKeys && cluster_fits<8>();
   s.passes = s.cluster ? (need + kClusterBits - 1) / kClusterBits : (need + kDigitBits - 1) / kDigitBits;
   s.bits = (need + s.passes - 1) / s.passes;
   const uint32_t sub = (N + kSortTile - 1) / kSortTile;
@@ -856,7 +894,7 @@ SortPlan sort_plan(uint32_t N, uint32_t rows, int D) {
   s.slabs = (uint32_t)((D + kSlab - 1) / kSlab);
   // pieces as long as there are still enough of them to fill the machine: every piece end can cost two partial rows
   s.piece = 8;
-  while (s.piece < 128 && (uint64_t)(N / (2 * s.piece)) * s.slabs >= 4096) s.piece *= 2;
+  while (s.piece < kMaxPiece && (uint64_t)(N / (2 * s.piece)) * s.slabs >= 4096) s.piece *= 2;
   s.pieces = (N + s.piece - 1) / s.piece;
   size_t off = 0;
   auto take = [&](size_t b) { size_t o = off; off += (b + 255) & ~size_t(255); return o; };
@@ -919,12 +957,13 @@ cudaError_t launch_lookup(const lsgd_embed_desc* e, cudaStream_t s) {
   const uint32_t rows_per_block = kLookupThreads / tx * kLookupRows;
   const uint32_t gx = (tok.N + rows_per_block - 1) / rows_per_block;
   uint32_t gy = (nvec + tx - 1) / tx;      // wide rows: column groups side by side while rows alone do not fill the machine
-  if (gx >= (uint32_t)sm_count() * 8) gy = 1;
-  if (gy > 65535) gy = 65535;
+  const uint32_t most = ((uint32_t)sm_count() * 8 + gx - 1) / gx;
+  if (gy > most) gy = most;
   return launch_pdl(embed_lookup_kernel<TT, TA, VEC>, dim3(gx, gy), dim3(kLookupThreads), 0, s, tok,
                     rows_of<const TT>(e->table), rows_of<TA>(e->out), nvec, tx, e->scale);
 }
 
+template <int ITEMS>
 cudaError_t launch_cluster_sort(const SortPlan& p, const Tokens& tok, char* w, uint8_t* touched, cudaStream_t s) {
   ClusterSort a{};
   a.key_out = reinterpret_cast<uint32_t*>(w + p.o_key[0]);
@@ -935,10 +974,10 @@ cudaError_t launch_cluster_sort(const SortPlan& p, const Tokens& tok, char* w, u
   a.bits = p.bits;
   a.passes = p.passes;
   a.blocks = 1;
-  while ((uint32_t)a.blocks * kBlockKeys < p.N) a.blocks *= 2;
+  while ((uint32_t)a.blocks * kClusterThreads * ITEMS < p.N) a.blocks *= 2;
   cudaLaunchAttribute at[2];
-  const cudaLaunchConfig_t cfg = cluster_config(a.blocks, s, at);
-  return cudaLaunchKernelEx(&cfg, embed_cluster_sort_kernel, tok, a);
+  const cudaLaunchConfig_t cfg = cluster_config<ITEMS>(a.blocks, s, at);
+  return cudaLaunchKernelEx(&cfg, embed_cluster_sort_kernel<ITEMS>, tok, a);
 }
 
 template <typename TG, typename TA, int VEC>
@@ -954,8 +993,11 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   uint32_t rows_per_block = (uint32_t)(65536 / (row_bytes < 64 ? 64 : row_bytes));   // about 64 KiB of zeros a block
   if (rows_per_block < 1) rows_per_block = 1;
   if (tok.N <= kFewTokens) {
-    if (rows_per_block > 1024) rows_per_block = 1024;
+    // each block reads all tokens first: two blocks an SM where the rows are many, at least 32 rows and 64 KiB a block
+    const uint32_t even = (rows + 2 * sm_count() - 1) / (2 * sm_count());
+    if (rows_per_block < even) rows_per_block = even;
     if (rows_per_block < 32) rows_per_block = 32;
+    if (rows_per_block > kFewTokens * 16) rows_per_block = kFewTokens * 16;      // bits in s_list
     const uint32_t zero_blocks = add ? 0 : (rows + rows_per_block - 1) / rows_per_block;
     const uint32_t sum_blocks = (tok.N + kFewWarps - 1) / kFewWarps;
     if (sum_blocks + zero_blocks == 0) return cudaSuccess;
@@ -966,7 +1008,10 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   char* w = static_cast<char*>(e->scratch);
   uint8_t* touched = add ? nullptr : reinterpret_cast<uint8_t*>(w + p.o_touched);
   cudaError_t err;
-  if (p.cluster && (err = launch_cluster_sort(p, tok, w, touched, s)) != cudaSuccess) return err;
+  if (p.cluster) {
+    err = p.N <= kClusterKeys / 2 ? launch_cluster_sort<4>(p, tok, w, touched, s) : launch_cluster_sort<8>(p, tok, w, touched, s);
+    if (err != cudaSuccess) return err;
+  }
   if (!p.cluster && touched && (err = cudaMemsetAsync(touched, 0, rows, s)) != cudaSuccess) return err;
   const size_t bins = size_t(1) << p.bits;
   for (int i = 0; i < (p.cluster ? 0 : p.passes); ++i) {
@@ -1011,7 +1056,7 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   if ((err = launch_pdl(embed_sum_kernel<TG, TA, VEC>, dim3(a.sum_blocks + zero_blocks), dim3(kSumThreads), 0, s, a, d_out, grad)) != cudaSuccess)
     return err;
   if (p.pieces > 1)
-    return launch_pdl(embed_join_kernel<TG, VEC>, dim3(p.pieces - 1, slabs < 4 ? slabs : 4), dim3(kSumThreads), 0, s, a, grad);
+    return launch_pdl(embed_join_kernel<TG, VEC>, dim3((p.pieces - 1 + kSumWarps - 1) / kSumWarps, slabs < 8 ? slabs : 8), dim3(kSumThreads), 0, s, a, grad);
   return cudaSuccess;
 }
 
