@@ -651,7 +651,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a) {
 // ------------------------------------------------------------------------------------------------ sums over the sorted list
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
-constexpr uint32_t kMaxPiece = 64;
+constexpr uint32_t kMaxPiece = 128;
 
 struct SumArgs {
   const uint32_t *key, *pos;  // sorted
