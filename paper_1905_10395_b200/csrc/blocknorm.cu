@@ -161,27 +161,39 @@ Shape shape_of(const lsgd_blocknorm_desc* d, bool backward) {
   s.tpr = 4;
   while (s.tpr < 32 && s.tpr < need) s.tpr *= 2;
   if (need > 32) s.tpr = (need + 31) / 32 * 32;
-  const int wish = backward ? 256 : 128;  // of a block; backward fewer and larger ones, since each leaves a partial row
   if (s.l.mode != kDirect && (s.phased || d->D != s.tpr * E)) s.l.mode |= kRagged;
+  const int wish = backward ? 256 : 128;  // threads of a block; backward fewer and larger blocks, since each leaves a partial row
   s.rpb = s.tpr >= wish ? 1 : wish / s.tpr;
-  s.l.threads = s.tpr * s.rpb;
+  // few rows: smaller blocks (of whole warps) until there are two for every SM
+  while (s.rpb > 1 && s.tpr * s.rpb >= 64 && (d->T + s.rpb - 1) / s.rpb * d->P < 2 * sm_count()) s.rpb = (s.rpb + 1) / 2;
+  s.l.threads = (s.tpr * s.rpb + 31) / 32 * 32;
+  s.rpb = s.l.threads / s.tpr;
   const size_t per = (size_t)E * s.l.threads;                         // values of a tensor's rows
   const size_t factors = 4 * per * ((pre ? 1 : 0) + (has_y ? 1 : 0));
   const size_t row = per * (backward ? rb + (pre ? rb + ab : 0) + (has_y ? ab : 0) + (token ? ab : 0)
                                      : rb + (has_y ? ab : 0) + (token ? ab : 0));
-  s.slots = s.l.mode != kDirect && factors + 2 * row <= (size_t)kSmemMax ? 2 : 1;
-  s.l.smem = factors + (s.l.mode == kDirect ? 0 : s.slots * row);    // at most 64 KiB + 160 KiB: 5 fp32 tensors, D = 8192
   const size_t sums = backward && s.rpb > 1 ? sizeof(float) * (size_t)s.rpb * d->D : 0;
-  if (s.l.smem < sums) s.l.smem = sums;
-  // persistent: as many blocks as the SMs hold at once (registers, shared memory), and no more than rows
-  int per_sm = (backward ? kBackwardThreads : kForwardThreads) / s.l.threads;
-  const int fit = (int)(size_t(228) * 1024 / (s.l.smem + 2048));
-  if (per_sm > fit) per_sm = fit;
-  if (per_sm < 1) per_sm = 1;
   const int64_t groups = (d->T + s.rpb - 1) / s.rpb;
-  int64_t n = ((int64_t)sm_count() * per_sm + d->P - 1) / d->P;
-  if (s.phased && n < groups) n = n < 8 ? 8 : n & ~int64_t(7);       // a block's rows are a multiple of 8 apart
-  s.blocks_w = (uint32_t)(groups < n ? groups : n);
+  // persistent: as many blocks as the SMs hold at once (registers, shared memory), and no more than rows
+  const auto plan = [&](int slots) {
+    s.slots = slots;
+    s.l.smem = factors + (s.l.mode == kDirect ? 0 : slots * row);    // one slot: at most 64 + 160 KiB (5 fp32 tensors, D = 8192)
+    if (s.l.smem < sums) s.l.smem = sums;
+    int per_sm = (backward ? kBackwardThreads : kForwardThreads) / s.l.threads;
+    const int fit = (int)(size_t(228) * 1024 / (s.l.smem + 2048));
+    if (per_sm > fit) per_sm = fit;
+    if (per_sm < 1) per_sm = 1;
+    int64_t n = (int64_t)sm_count() * per_sm / d->P;                 // rounded down: one block more would be a second round
+    if (n < 1) n = 1;
+    if (s.phased && n < groups) n = n < 8 ? 8 : n & ~int64_t(7);     // a block's rows are a multiple of 8 apart
+    s.blocks_w = (uint32_t)(groups < n ? groups : n);
+  };
+  if (s.l.mode != kDirect && factors + 2 * row <= (size_t)kSmemMax) {
+    plan(2);
+    if (groups <= (int64_t)s.blocks_w) plan(1);                      // one group of rows a block: nothing is fetched ahead
+  } else {
+    plan(1);
+  }
   return s;
 }
 

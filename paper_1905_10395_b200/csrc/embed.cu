@@ -148,6 +148,21 @@ __device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, co
   }
 }
 
+// A row of zeros, by a warp: single values up to a 16-byte boundary and behind the last, 16 bytes at a time between, so that
+// rows of odd length are cleared as fast as others (3 x 32698 rows of 1019 bf16 values: XX us, XX us value by value).
+template <typename TG>
+__device__ __forceinline__ void clear_row(TG* row, int lane, int D) {
+  constexpr int n = 16 / (int)sizeof(TG);
+  const int head = min(D, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(TG));
+  const int body = (D - head) / n;
+  TG zero{};
+  if (lane < head) row[lane] = zero;
+  uint4* wide = reinterpret_cast<uint4*>(row + head);
+  for (int i = lane; i < body; i += 32) wide[i] = make_uint4(0, 0, 0, 0);
+  const int tail = head + body * n;
+  if (lane < D - tail) row[tail + lane] = zero;
+}
+
 // Adds rows list[j0 .. j1) of d_out to a lane's columns of a slab, kAhead rows in flight.
 template <typename TA, int VEC, typename List>
 __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>& d_out, const List* list, uint32_t j0, uint32_t j1,
@@ -262,10 +277,8 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
       if (k >= r0 && k - r0 < n) atomicOr(&s_bits[(k - r0) >> 5], 1u << ((k - r0) & 31));
     }
     __syncthreads();
-    const float zero[8] = {};
     for (uint32_t r = warp; r < n; r += kFewWarps)
-      if (!(s_bits[r >> 5] >> (r & 31) & 1))
-        for (int slab = 0; slab < slabs; ++slab) write_row<TG, VEC>(grad.row(r0 + r), slab, lane, D, zero, 0.f, false);
+      if (!(s_bits[r >> 5] >> (r & 31) & 1)) clear_row(grad.row(r0 + r), lane, D);
     return;
   }
   __syncthreads();
@@ -673,14 +686,10 @@ embed_sum_kernel(SumArgs a, Rows<const TA> d_out, GradRows<TG> grad) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (blockIdx.x >= a.sum_blocks) {      // rows of absent tokens: zeros
     const uint32_t r0 = (blockIdx.x - a.sum_blocks) * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-    const float zero[8] = {};
     for (uint32_t r = r0; r < r1; r += 32) {
       const uint32_t absent = __ballot_sync(0xFFFFFFFFu, r + lane < r1 && !a.touched[min(r + lane, r1 - 1)]);
-      const uint32_t items = min(32u, r1 - r) * a.slabs;
-      for (uint32_t i = warp; i < items; i += kSumWarps) {
-        const uint32_t k = i / a.slabs;
-        if (absent >> k & 1) write_row<TG, VEC>(grad.row(r + k), (int)(i - k * a.slabs), lane, a.D, zero, 0.f, false);
-      }
+      for (uint32_t k = warp; k < min(32u, r1 - r); k += kSumWarps)
+        if (absent >> k & 1) clear_row(grad.row(r + k), lane, a.D);
     }
     return;
   }
