@@ -1002,8 +1002,10 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   uint32_t rows_per_block = (uint32_t)(65536 / (row_bytes < 64 ? 64 : row_bytes));   // about 64 KiB of zeros a block
   if (rows_per_block < 1) rows_per_block = 1;
   if (tok.N <= kFewTokens) {
-    // each block reads all tokens first: two blocks an SM where the rows are many, at least 32 rows and 64 KiB a block
-    const uint32_t even = (rows + 2 * sm_count() - 1) / (2 * sm_count());
+    // each block reads all tokens first: one block an SM beside those that add rows (four are resident), two where there is
+    // more to clear than to add, and at least 32 rows and 64 KiB a block
+    const uint32_t blocks = (uint32_t)sm_count() * ((uint64_t)rows * row_bytes > (64u << 20) ? 2 : 1);
+    const uint32_t even = (rows + blocks - 1) / blocks;
     if (rows_per_block < even) rows_per_block = even;
     if (rows_per_block < 32) rows_per_block = 32;
     if (rows_per_block > kFewTokens * 16) rows_per_block = kFewTokens * 16;      // bits in s_list
