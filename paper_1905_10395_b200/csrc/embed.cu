@@ -50,6 +50,10 @@ struct Tokens {
 };
 
 // ------------------------------------------------------------------------------------------------ lookup
+// A block copies kLookupRows rows for each group of tx threads.  8 x 4096 rows of 1024 fp32 values into bf16: 27 us.  HBM gives
+// the 57 MB of distinct rows and takes part of the 67 MB written; what bounds it is that every token's row crosses from L2 to
+// an SM, 134 MB in and 67 MB out at 7.5 TB/s: 1, 2 or 4 rows a thread, 3 to 8 blocks an SM and a persistent form with the
+// tokens ahead measured 27 to 30 us.
 constexpr int kLookupThreads = 256;
 constexpr int kLookupRows = 4;           // rows whose loads a thread issues before the first store
 
@@ -149,7 +153,8 @@ __device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, co
 }
 
 // A row of zeros, by a warp: single values up to a 16-byte boundary and behind the last, 16 bytes at a time between, so that
-// rows of odd length are cleared as fast as others (3 x 32698 rows of 1019 bf16 values: XX us, XX us value by value).
+// rows of odd length are cleared as fast as others (gradient of 3 tables of 32698 x 1019 bf16 values from 480 tokens: 51 us, 70
+// value by value).
 template <typename TG>
 __device__ __forceinline__ void clear_row(TG* row, int lane, int D) {
   constexpr int n = 16 / (int)sizeof(TG);
@@ -195,7 +200,8 @@ __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// One launch instead of three: 15 us against 23 us for 3 x 1021 tokens of 250 values.
+// One launch instead of three: 15 us against 23 us for 3 x 1021 tokens of 250 values.  It is a chain of latencies (tokens, the
+// search for equal ones, rows, the write), so blocks are small enough for all of them to be resident.
 constexpr int kFewTokens = 4096;
 constexpr int kFewThreads = 256;
 constexpr int kFewWarps = kFewThreads / 32;
@@ -666,6 +672,8 @@ constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr uint32_t kMaxPiece = 128;
 
+// A warp carries 256 columns of a piece.  65536 tokens of 2048 bf16 values into a table of 50000 fp32 rows: 104 us for the
+// 652 MB of rows read and written, 6.3 TB/s or 0.96 of the measured copy bandwidth; sort and join add 20 and 8 us of latency.
 struct SumArgs {
   const uint32_t *key, *pos;  // sorted
   const uint8_t* touched;     // nullptr: rows of absent tokens are left alone
