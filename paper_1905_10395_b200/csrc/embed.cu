@@ -131,23 +131,30 @@ __device__ __forceinline__ int slab_col(int slab, int lane, int i) { return slab
 
 template <typename TG, int VEC>
 __device__ __forceinline__ void write_row(TG* row, int slab, int lane, int D, const float* acc, float scale, bool add) {
+  constexpr int N = 8 / VEC;
+  float f[8];
 #pragma unroll
-  for (int i = 0; i < 8 / VEC; ++i) {
+  for (int k = 0; k < 8; ++k) f[k] = acc[k] * scale;
+  if (add) {                             // all of what is there before the first is written: the stores would hold the loads up
+    Pack<TG, VEC> o[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (slab_col<VEC>(slab, lane, i) < D) o[i].load(row + slab_col<VEC>(slab, lane, i));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (slab_col<VEC>(slab, lane, i) >= D) break;
+      float e[VEC];
+      o[i].get(e);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f[i * VEC + k] += e[k];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
     const int col = slab_col<VEC>(slab, lane, i);
     if (col >= D) break;
-    float f[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) f[k] = acc[i * VEC + k] * scale;
-    if (add) {
-      Pack<TG, VEC> o;
-      o.load(row + col);
-      float e[VEC];
-      o.get(e);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) f[k] += e[k];
-    }
     Pack<TG, VEC> o;
-    o.set(f);
+    o.set(f + i * VEC);
     o.store(row + col);
   }
 }
@@ -483,7 +490,7 @@ embed_scatter_kernel(Tokens tok, SortPass a) {
 constexpr int kClusterThreads = 1024;
 constexpr int kClusterWarps = kClusterThreads / 32;
 constexpr int kClusterBlocks = 16;                             // 8 (the portable size) of twice the keys: 30 us instead of 20 for 65536
-constexpr int kClusterItems = 8;                               // keys of a thread: 4, or 8 beyond 65536
+constexpr int kClusterItems = 8;                               // keys of a thread: 1, 2, 4 or 8, the fewest that 16 blocks hold
 constexpr int kClusterKeys = kClusterThreads * kClusterItems * kClusterBlocks;
 constexpr int kClusterBits = 9;
 constexpr int kClearBlocks = 112;                              // blocks of all clusters where some of them clear rows
@@ -868,7 +875,7 @@ embed_join_kernel(SumArgs a, GradRows<TG> grad) {
 // ------------------------------------------------------------------------------------------------ host
 struct SortPlan {
   uint32_t N, rows, piece, pieces, slabs, per_tile;
-  int passes, bits, tiles;
+  int passes, bits, tiles, items;
   bool cluster;
   size_t o_touched, o_key[2], o_pos[2], o_counts, o_part, bytes;
 };
@@ -915,8 +922,12 @@ SortPlan sort_plan(uint32_t N, uint32_t rows, int D) {
   s.rows = rows;
   int need = 1;
   while ((rows >> need) != 0) ++need;      // keys 0 .. rows (rows: no row)
-  s.cluster = N <= kClusterKeys / 2 ? (cluster_fits<4, float>() && cluster_fits<4, __nv_bfloat16>())
-                                    : N <= kClusterKeys && cluster_fits<8, float>() && cluster_fits<8, __nv_bfloat16>();
+  s.items = 1;
+  while (s.items < kClusterItems && (uint32_t)(kClusterThreads * kClusterBlocks * s.items) < N) s.items *= 2;
+  s.cluster = N <= kClusterKeys && (s.items == 1   ? cluster_fits<1, float>() && cluster_fits<1, __nv_bfloat16>()
+                                    : s.items == 2 ? cluster_fits<2, float>() && cluster_fits<2, __nv_bfloat16>()
+                                    : s.items == 4 ? cluster_fits<4, float>() && cluster_fits<4, __nv_bfloat16>()
+                                                   : cluster_fits<8, float>() && cluster_fits<8, __nv_bfloat16>());
   s.passes = s.cluster ? (need + kClusterBits - 1) / kClusterBits : (need + kDigitBits - 1) / kDigitBits;
   s.bits = (need + s.passes - 1) / s.passes;
   const uint32_t sub = (N + kSortTile - 1) / kSortTile;
@@ -1054,8 +1065,10 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   }
   if (cleared == rows) touched = nullptr;  // nothing is left to be cleared
   if (p.cluster) {
-    err = p.N <= kClusterKeys / 2 ? launch_cluster_sort<4>(p, tok, w, touched, cleared, grad, (int)e->D, s)
-                                  : launch_cluster_sort<8>(p, tok, w, touched, cleared, grad, (int)e->D, s);
+    const auto sort = p.items == 1   ? launch_cluster_sort<1, TG>
+                      : p.items == 2 ? launch_cluster_sort<2, TG>
+                      : p.items == 4 ? launch_cluster_sort<4, TG> : launch_cluster_sort<8, TG>;
+    err = sort(p, tok, w, touched, cleared, grad, (int)e->D, s);
     if (err != cudaSuccess) return err;
   }
   if (!p.cluster && touched && (err = cudaMemsetAsync(touched, 0, rows, s)) != cudaSuccess) return err;
