@@ -237,11 +237,6 @@ __device__ __forceinline__ float sigmoid(float z) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
-__device__ __forceinline__ float gate_value(float z, int act) {
-  if (act == LSGD_GATE_SIGMOID) return sigmoid(z);
-  if (act == LSGD_GATE_TANH) return tanhf(z);
-  return z;
-}
 __device__ __forceinline__ float gate_slope(float a, int act) {
   if (act == LSGD_GATE_SIGMOID) return a * (1.f - a);
   if (act == LSGD_GATE_TANH) return 1.f - a * a;

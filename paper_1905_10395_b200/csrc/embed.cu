@@ -10,8 +10,7 @@
 //                token, and otherwise lists the later ones and adds their rows in order.
 //   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 131072 positions in the shared
 //                memory of one cluster, in one launch, more with a histogram and a scatter launch per pass; a warp then
-//                walks a piece of the sorted list, adding rows
-//                while the token stays the same.  A token that lies within one piece is written at once; pieces of a
+//                walks a piece of the sorted list, adding rows while the token stays the same.  A token that lies within one piece is written at once; pieces of a
 //                token that crosses piece ends leave fp32 partial rows, which a last launch adds in order.  Work is
 //                split by positions, never by token, so it stays even however often one token occurs.
 #include "lm_ops.h"
@@ -691,8 +690,9 @@ constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr uint32_t kMaxPiece = 128;
 
-// A warp carries 256 columns of a piece.  65536 tokens of 2048 bf16 values into a table of 50000 fp32 rows: 104 us for the
-// 652 MB of rows read and written, 6.3 TB/s or 0.96 of the measured copy bandwidth; sort and join add 20 and 8 us of latency.
+// A warp carries 256 columns of a piece.  65536 tokens of 2048 bf16 values into a table of 50000 fp32 rows: 104 us for all 652 MB
+// of rows read and written, 6.3 TB/s or 0.96 of the measured copy bandwidth, and so many fewer as the sort's launch has
+// cleared rows; sort and join add 20 and 8 us of latency.
 struct SumArgs {
   const uint32_t *key, *pos;  // sorted
   const uint8_t* touched;     // nullptr: rows of absent tokens are left alone

@@ -85,9 +85,11 @@ class _Bound:
         self._forward, self._backward = getattr(L, f"lsgd_{name}_forward"), getattr(L, f"lsgd_{name}_backward")
         self._name, self.desc, self._ref = name, desc, C.byref(desc)
         if scratch:
-            n = int(getattr(L, f"lsgd_{name}_scratch_bytes")(self._ref))
+            with torch.cuda.device(device):
+                n = int(getattr(L, f"lsgd_{name}_scratch_bytes")(self._ref))
             if n:
-                buf = torch.empty(n, dtype=torch.uint8, device=device)
+                with torch.cuda.stream(stream):      # the allocator's order of use is the operator's
+                    buf = torch.empty(n, dtype=torch.uint8, device=device)
                 desc.scratch, desc.scratch_bytes = buf.data_ptr(), n
                 self._keep.append(buf)
 
@@ -182,7 +184,8 @@ class BlockNorm(_Bound):
         stats = {}
         for name, t, used in (("rstd_post", rstd_post, post_norm), ("rstd_pre", rstd_pre, w_pre is not None)):
             if t is None and used:
-                t = torch.empty((P, T), dtype=torch.float32, device=device)
+                with torch.cuda.stream(stream):
+                    t = torch.empty((P, T), dtype=torch.float32, device=device)
             if t is not None and (t.dtype != torch.float32 or t.numel() != P * T or not t.is_contiguous()):
                 _fail(f"{name}: fp32 [P, T], contiguous")
             stats[name] = t
@@ -234,7 +237,8 @@ class AdamW:
 
         def buffer(name, t, count, dtype):
             if t is None:
-                return torch.zeros(count, dtype=dtype, device=device)
+                with torch.cuda.stream(stream):      # cleared before the first step, on its stream
+                    return torch.zeros(count, dtype=dtype, device=device)
             if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
                 _fail(f"{name}: {count} contiguous values of {dtype}")
             return t
@@ -265,7 +269,7 @@ class AdamW:
             raise api.LsgdError(s, "lsgd_adamw_create")
         self.h = h
         self._step = api.lib().lsgd_adamw_step
-        self._read = None
+        self._read, self._torch_stream = None, stream
         if step:
             self.set_step(step)
 
@@ -280,7 +284,8 @@ class AdamW:
     def moments(self):
         """The moments as the fp32 values that they stand for, flat, in buffers that the next call overwrites."""
         if self._read is None:
-            self._read = [torch.empty(self.values, dtype=torch.float32, device=self.device) for _ in range(2)]
+            with torch.cuda.stream(self._torch_stream):
+                self._read = [torch.empty(self.values, dtype=torch.float32, device=self.device) for _ in range(2)]
         m, v = self._read
         s = api.lib().lsgd_adamw_moments(self.h, m.data_ptr(), v.data_ptr())
         if s:

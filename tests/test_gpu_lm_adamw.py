@@ -256,3 +256,22 @@ def test_captured_in_a_graph():
     torch.cuda.synchronize()
     assert a.t() == b.t() == 6
     assert all(torch.equal(x.view, y.view) for x, y in zip(p, q)) and torch.equal(a.m, b.m) and torch.equal(a.v, b.v)
+
+
+def test_moments_of_its_own_on_another_stream():
+    """Moments that the binding allocates are cleared on the step's stream: no order with the current one is needed for them."""
+    from paper_1905_10395_b200 import lm
+    n = 1 << 22
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    p, g = torch.randn(n, generator=gen, device="cuda"), torch.randn(n, generator=gen, device="cuda")
+    got = []
+    for stream in (None, torch.cuda.Stream()):
+        x = p.clone()
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)                 # the current stream is busy for about 10 ms
+        opt = lm.AdamW([x], [g], state="8bit", stream=stream)
+        for _ in range(2):
+            opt.step(1e-2)
+        torch.cuda.synchronize()
+        got.append((x, opt.m.clone(), opt.v.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
