@@ -206,7 +206,7 @@ __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// One launch instead of three: 15 us against 23 us for 3 x 1021 tokens of 250 values.  It is a chain of latencies (tokens, the
+// One launch instead of three: 17 us against 23 us for 3 x 1021 tokens of 250 values.  It is a chain of latencies (tokens, the
 // search for equal ones, rows, the write), so blocks are small enough for all of them to be resident.
 constexpr int kFewTokens = 4096;
 constexpr int kFewThreads = 256;
