@@ -527,7 +527,8 @@ LSGD_API lsgd_status lsgd_blocknorm_backward(const lsgd_blocknorm_desc* desc, vo
  *                    are a hash of (seed, t, position), so a run can be repeated bit for bit.  A second moment that is not
  *                    zero is never rounded to zero.  A block that holds a moment that is not finite reads as NaN.
  * lsgd_adamw_create copies the HOST arrays and builds a table of the tensors on the current device (40 bytes per 4096
- * parameters; the only allocation).  The gradients' addresses are fixed too: keep the buffers from step to step.
+ * parameters; the only allocation), copied on `stream`, which it synchronises.  The gradients' addresses are fixed too:
+ * keep the buffers from step to step.
  * The step counter lives on the device, so captured steps replay correctly from a CUDA graph (lr is frozen in it). */
 typedef struct lsgd_adamw_ctx* lsgd_adamw_handle;
 typedef enum {

@@ -520,7 +520,10 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_desc* desc, lsgd_adamw_handle* ou
   h->d.weight_decay = nullptr;
   bool ok = cudaMalloc(&h->slab, bytes) == cudaSuccess;
   if (!ok) h->slab = nullptr;
-  ok = ok && cudaMemcpy(h->slab, host, bytes, cudaMemcpyHostToDevice) == cudaSuccess;
+  // ordered before the first step: a blocking copy from pageable memory may return before its last piece has arrived, and
+  // nothing orders a non-blocking stream behind the legacy one.  `host` dies here, so the copy is drained.
+  ok = ok && cudaMemcpyAsync(h->slab, host, bytes, cudaMemcpyHostToDevice, h->stream) == cudaSuccess;
+  ok = ok && cudaStreamSynchronize(h->stream) == cudaSuccess;
   delete[] host;
   if (!ok) {
     if (h->slab) cudaFree(h->slab);
