@@ -412,7 +412,9 @@ LSGD_API lsgd_status lsgd_bgemm_check_device(uint32_t* flag_out /* HOST, may be 
  * The matrix products between them are lsgd_bgemm_bf16's; the leaders' election and pulls are lsgd_elect's and
  * lsgd_step's (objective EXTERNAL).  Each operator works on all P workers in one call: worker p's token t is
  * row (p, t).  Conventions as above; the descriptors are HOST structs read during the call, all buffers in them
- * are DEVICE and the caller's, and work is enqueued on `stream` without synchronising.
+ * are DEVICE and the caller's, and work is enqueued on `stream` without synchronising.  The buffers and the stream are those
+ * of the device that is current at the call (scratch sizes too); an AdamW handle belongs to the device that was current at
+ * its creation, and its calls return LSGD_ERR_STATE under another one (destroy is legal under any).
  * ------------------------------------------------------------------------------------------------------ */
 typedef enum {
   LSGD_F32 = 0,

@@ -586,6 +586,7 @@ lsgd_status lsgd_adamw_moments(lsgd_adamw_handle h, float* m_out, float* v_out) 
 lsgd_status lsgd_adamw_get_step(lsgd_adamw_handle h, int64_t* n) {
   using namespace lsgd;
   if (!h || !n) return LSGD_ERR_INVALID_ARG;
+  if (!on_own_device(h)) return LSGD_ERR_STATE;
   Counter c{};
   if (cudaMemcpyAsync(&c, h->slab, sizeof(c), cudaMemcpyDeviceToHost, h->stream) != cudaSuccess) return LSGD_ERR_CUDA;
   if (cudaStreamSynchronize(h->stream) != cudaSuccess) return LSGD_ERR_CUDA;
@@ -603,8 +604,11 @@ lsgd_status lsgd_adamw_set_step(lsgd_adamw_handle h, int64_t n) {
 
 lsgd_status lsgd_adamw_destroy(lsgd_adamw_handle h) {
   if (!h) return LSGD_OK;
+  int was = h->device;                    // a NULL stream is that of the current device
+  const bool moved = cudaGetDevice(&was) == cudaSuccess && was != h->device && cudaSetDevice(h->device) == cudaSuccess;
   cudaStreamSynchronize(h->stream);
   const cudaError_t e = cudaFree(h->slab);
+  if (moved) cudaSetDevice(was);
   delete h;
   return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
 }

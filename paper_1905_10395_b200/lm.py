@@ -3,7 +3,8 @@
 Each class takes the buffers that its operator works on once, checks them, and keeps the descriptor: a call afterwards is
 one call of the C ABI, with no allocation and no synchronisation, so it can be captured in a CUDA graph.  The tensors must
 outlive the object.  Work is enqueued on the stream given at construction (default: torch's current one at that time); a
-tensor last used on another stream has to be ordered with it by the caller.  There is no CPU path.
+tensor last used on another stream has to be ordered with it by the caller.  The tensors' device has to be the current one at
+every call (ERR_STATE otherwise).  There is no CPU path.
 
 Rows are [P, T, D] (worker, token, channel) with a channel stride of 1 and any row and worker stride; one worker's may be
 given as [T, D].  Vectors are [P, D] or [D].  An input that is expanded over the workers (stride 0) is shared by them."""
@@ -18,6 +19,7 @@ import torch
 from . import api
 
 _DTYPES = {torch.float32: api.F32, torch.bfloat16: api.BF16}
+_current_device = torch._C._cuda_getDevice      # torch.cuda.current_device() without its check for initialisation: half the time
 _GATE_ACTS = {"identity": api.GATE_IDENTITY, "sigmoid": api.GATE_SIGMOID, "tanh": api.GATE_TANH}
 
 
@@ -26,7 +28,11 @@ def _fail(what: str) -> None:
 
 
 def _stream(stream, device: torch.device) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        _fail(f"a stream of {device}, got one of {stream.device}")
+    return stream.cuda_stream
 
 
 def _dtype(name: str, *tensors) -> int:
@@ -79,7 +85,7 @@ class _Bound:
     """A descriptor with its stream and what it points to."""
 
     def _bind(self, name, desc, device, stream, keep, scratch):
-        self.device, self._keep = device, [keep]
+        self.device, self._index, self._keep = device, device.index, [keep]
         self._stream = _stream(stream, device)
         L = api.lib()
         self._forward, self._backward = getattr(L, f"lsgd_{name}_forward"), getattr(L, f"lsgd_{name}_backward")
@@ -93,12 +99,19 @@ class _Bound:
                 desc.scratch, desc.scratch_bytes = buf.data_ptr(), n
                 self._keep.append(buf)
 
+    def _other_device(self) -> None:
+        raise api.LsgdError(api.ERR_STATE, f"lsgd_{self._name}: device {_current_device()} is current, the tensors are on {self.device}")
+
     def forward(self) -> None:
+        if _current_device() != self._index:     # the default stream would be the other device's, and so would the plan
+            self._other_device()
         s = self._forward(self._ref, self._stream)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_forward")
 
     def backward(self) -> None:
+        if _current_device() != self._index:
+            self._other_device()
         s = self._backward(self._ref, self._stream)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_backward")
@@ -271,7 +284,8 @@ class AdamW:
         self._step = api.lib().lsgd_adamw_step
         self._read, self._torch_stream = None, stream
         if step:
-            self.set_step(step)
+            with torch.cuda.device(device):
+                self.set_step(step)
 
     def step(self, lr: float, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step.  grad_scale: a device fp32 scalar that the gradients are multiplied by first."""
