@@ -27,12 +27,13 @@ def _fail(what: str) -> None:
     raise api.LsgdError(api.ERR_INVALID_ARG, what)
 
 
-def _stream(stream, device: torch.device) -> int:
+def _stream(stream, device: torch.device):
+    """The stream that an operator keeps, for its calls and for the buffers that it allocates."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
+        return torch.cuda.current_stream(device)
+    if stream.device != device:
         _fail(f"a stream of {device}, got one of {stream.device}")
-    return stream.cuda_stream
+    return stream
 
 
 def _dtype(name: str, *tensors) -> int:
@@ -86,7 +87,7 @@ class _Bound:
 
     def _bind(self, name, desc, device, stream, keep, scratch):
         self.device, self._index, self._keep = device, device.index, [keep]
-        self._stream = _stream(stream, device)
+        self._stream = stream.cuda_stream
         L = api.lib()
         self._forward, self._backward = getattr(L, f"lsgd_{name}_forward"), getattr(L, f"lsgd_{name}_backward")
         self._name, self.desc, self._ref = name, desc, C.byref(desc)
@@ -136,6 +137,7 @@ class Embedding(_Bound):
         if not tables or (table is None) != (out is None) or (d_table is None) != (d_out is None):
             _fail("Embedding: table and out, or d_out and d_table, or all four")
         device = _same_device(tokens, *tables, *acts)
+        stream = _stream(stream, device)
         P, T = tok.shape
         V, D = tables[0].shape[-2:]
         e = api.EmbedDesc()
@@ -178,6 +180,7 @@ class BlockNorm(_Bound):
         token_gate = None if channel else gate
         keep = [x, y, gate, w_post, w_pre, out, h, rstd_post, rstd_pre, d_out, d_h, dx, dy, d_gate, dw_post, dw_pre]
         device = _same_device(*keep)
+        stream = _stream(stream, device)
         d = api.BlocknormDesc()
         d.struct_size = C.sizeof(api.BlocknormDesc)
         d.P, d.T, d.D = P, T, D
@@ -240,6 +243,7 @@ class AdamW:
                 _fail(f"AdamW: tensor {i} is not contiguous")
         grad_dtype = _dtype("grads", *grads)
         self.device = device = _same_device(*params, *grads, *[c for c in copies or [] if c is not None], m, v, m_scale, v_scale)
+        self._stream = stream = _stream(stream, device)
         if state is None:
             state = "8bit" if m is not None and m.dtype == torch.uint8 else "f32"
         if state not in ("f32", "8bit"):
@@ -272,7 +276,7 @@ class AdamW:
         if state == "8bit":
             d.m_scale, d.v_scale = self.m_scale.data_ptr(), self.v_scale.data_ptr()
         d.beta1, d.beta2, d.eps, d.seed = float(beta1), float(beta2), float(eps), int(seed) & 0xFFFFFFFF
-        d.stream = _stream(stream, device) or None
+        d.stream = stream.cuda_stream or None
         self.state = state
         self._keep = (params, grads, copies)
         h = C.c_void_p()
@@ -282,7 +286,7 @@ class AdamW:
             raise api.LsgdError(s, "lsgd_adamw_create")
         self.h = h
         self._step = api.lib().lsgd_adamw_step
-        self._read, self._torch_stream = None, stream
+        self._read = None
         if step:
             with torch.cuda.device(device):
                 self.set_step(step)
@@ -298,7 +302,7 @@ class AdamW:
     def moments(self):
         """The moments as the fp32 values that they stand for, flat, in buffers that the next call overwrites."""
         if self._read is None:
-            with torch.cuda.stream(self._torch_stream):
+            with torch.cuda.stream(self._stream):
                 self._read = [torch.empty(self.values, dtype=torch.float32, device=self.device) for _ in range(2)]
         m, v = self._read
         s = api.lib().lsgd_adamw_moments(self.h, m.data_ptr(), v.data_ptr())
