@@ -119,6 +119,7 @@ template <bool SIGNED, bool FOLD>
 __device__ __forceinline__ uint2 encode8(const float2 (&z)[4], float scale, const uint32_t (&rnd)[8]) {
   constexpr float kPow = pow2(SIGNED ? -kShiftM : -kShiftV);
   float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  const uint32_t least = inv > 0.f ? 0x00100000u : 0u;         // code 1
   if (FOLD) inv = __fmul_rn(inv, kPow);
   uint32_t w[8];
 #pragma unroll
@@ -130,7 +131,8 @@ __device__ __forceinline__ uint2 encode8(const float2 (&z)[4], float scale, cons
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    if (!SIGNED && w[k] != 0) w[k] = max(w[k], 0x00100000u);     // a second moment that is not zero keeps a denominator
+    // a second moment that is not zero keeps a denominator, also where it is so far below the block's that w is 0
+    if (!SIGNED && (k & 1 ? z[k >> 1].y : z[k >> 1].x) > 0.f) w[k] = max(w[k], least);
     w[k] = (w[k] << 4) + __byte_perm(rnd[k], 0, SIGNED ? 0x4104 : 0x4324);
     if (SIGNED) w[k] = (w[k] & 0x7FFFFFFFu) | (__float_as_uint(k & 1 ? z[k >> 1].y : z[k >> 1].x) & 0x80000000u);
   }

@@ -1,0 +1,64 @@
+"""GPU check of the AdamW step at the ends of its range: moments of very different sizes in one block."""
+import pytest
+import torch
+
+from tests import test_gpu_lm_adamw as base
+
+pytestmark = pytest.mark.gpu
+
+B = base.B
+
+
+def encode_by_contract(z, rnd16, signed):
+    """As the header has it: a second moment above zero has a code above zero, however small it is in its block."""
+    code, scale = base_encode(z, rnd16, signed)
+    if not signed:
+        code = torch.where((z > 0) & (scale > 0)[:, None], code.clamp(min=1), code)
+    return code, scale
+
+
+base_encode = base.encode
+
+
+def test_small_second_moments_beside_a_large_one(monkeypatch):
+    """One gradient of 1 in every block, the others 2^-28, for 30 steps: v of the others is 2^-56 of the block's.
+
+    Their bound.  From the second step on a stored m is at most its smallest code, 2^-17 scale, and a stored v at least its
+    smallest, 2^-33 scale, with scale = (1 - b^t) / 1.875 for a largest gradient of 1.  So the step is at most
+    0.9 2^-17 / 1.875 / sqrt(0.95 2^-33 / 1.875) = 0.477 lr, and less at small t (m's factor (1 - b1^(t-1)) / (1 - b1^t) is the
+    smaller one); the first is 2^-28 / (2^-28 + 1e-8) = 0.27 lr."""
+    monkeypatch.setattr(base, "encode", encode_by_contract)
+    n = 64 * B
+    opt, model, p, g, c, _ = base.build([n], "8bit", "f32", False, seed=21, wd=[0.0])
+    gr = torch.full((n,), 2.0 ** -28)
+    gr[::B] = 1.0
+    g[0].view.copy_(gr)
+    small = gr < 1
+    last = p[0].view.cpu().clone()
+    p[0].view.zero_()
+    model.x[0] = torch.zeros(n)
+    last.zero_()
+    for _ in range(30):
+        opt.step(1.0)
+        model.step([gr], 1.0)
+        base.check(opt, model, p, g, c)
+        now = p[0].view.cpu()
+        step = (now - last).abs()
+        last = now.clone()
+        assert step[small].max() <= 0.48 and 0.8 <= step[~small].min() and step[~small].max() <= 1.2
+        assert (opt.v.cpu() > 0).all()
+        p[0].view.zero_()
+        model.x[0].zero_()
+        last.zero_()
+
+
+def test_far_apart_values_keep_their_codes(monkeypatch):
+    """Gradients over 40 binades in every block, fresh ones every step: codes, scales, moments and parameters."""
+    monkeypatch.setattr(base, "encode", encode_by_contract)
+    opt, model, p, g, c, gen = base.build([5000, 300], "8bit", "f32", False, seed=22)
+    for _ in range(4):
+        for b in g:
+            b.view.copy_(torch.randn(b.view.shape, generator=gen) * torch.exp2(-40 * torch.rand(b.view.shape, generator=gen)))
+        opt.step(1e-2)
+        model.step([b.view.cpu() for b in g], 1e-2)
+        base.check(opt, model, p, g, c)
