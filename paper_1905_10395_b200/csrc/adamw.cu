@@ -107,10 +107,10 @@ __device__ __forceinline__ void decode8(uint2 c, float scale, float2 (&f)[4]) {
 // Scales below this are folded into the powers of two, up and (as reciprocals) down, without overflow or loss.
 constexpr float kFoldBelow = 16384.f;
 
-// Scale of a block from its largest magnitude.  A magnitude that is not finite stays in the scale, so the block reads as NaN.
+// Scale of a block from its largest magnitude: NaN if that is not finite (top - top), so the whole block reads as NaN.
 __device__ __forceinline__ float block_scale(uint32_t top_bits) {
   const float top = __uint_as_float(top_bits);
-  return top < kTiny ? 0.f : __fmul_rn(top, kTop);
+  return top < kTiny ? 0.f : __fmaf_rn(top, kTop, top - top);
 }
 // 8 values as codes.  rnd: their hashes; the low half rounds m, the high half v.  The sum of a value's bits and 16 random ones
 // below the code is formed 4 bits to the left, so that the code is byte 3 and a sign has left the word.  No code overflows:

@@ -62,3 +62,20 @@ def test_far_apart_values_keep_their_codes(monkeypatch):
         opt.step(1e-2)
         model.step([b.view.cpu() for b in g], 1e-2)
         base.check(opt, model, p, g, c)
+
+
+@pytest.mark.parametrize("moment", ["m", "v"])
+def test_an_infinity_whose_rounding_adds_nothing(moment):
+    """A block with an infinite moment reads as NaN whatever random bits its values get: here those of the infinity are 0."""
+    n, seed = 1 << 18, 23
+    h = base.mix(torch.arange(n) ^ base.mix(base.mix(seed + 77) ^ 1))
+    at = int(torch.nonzero((h & 0xFFFF if moment == "m" else h >> 16) == 0)[0])
+    opt, _, p, g, _, _ = base.build([n], "8bit", "f32", False, seed=seed)
+    g[0].view[at] = float("inf")
+    opt.step(1e-2)
+    m, v = opt.moments()
+    torch.cuda.synchronize()
+    lost = torch.zeros(n, dtype=torch.bool, device="cuda")
+    lost[at // B * B:at // B * B + B] = True
+    for t in (m, v):
+        assert torch.isnan(t[lost]).all() and torch.isfinite(t[~lost]).all()
