@@ -527,7 +527,10 @@ LSGD_API lsgd_status lsgd_blocknorm_backward(const lsgd_blocknorm_desc* desc, vo
  *                    same range.  Moments are rounded up or down at random with the right mean: a moving average
  *                    whose change per step is smaller than a code's spacing would otherwise never move.  The random bits
  *                    are a hash of (seed, t, position), so a run can be repeated bit for bit.  A second moment that is not
- *                    zero is never rounded to zero.  A block that holds a moment that is not finite reads as NaN.
+ *                    zero is never rounded to zero, except in a block whose largest one is below 2^-100 (gradients of about
+ *                    4e-15 at beta2 = 0.95): a block whose largest moment is below 2^-100 is stored as zeros.  eps has to be
+ *                    at least 2^-50, what such a second moment's root is below, so a step of such a block is at most about
+ *                    lr / sqrt(1 - beta2).  A block that holds a moment that is not finite reads as NaN.
  * lsgd_adamw_create copies the HOST arrays and builds a table of the tensors on the current device (40 bytes per 4096
  * parameters; the only allocation), copied on `stream`, which it synchronises.  The gradients' addresses are fixed too:
  * keep the buffers from step to step.
@@ -552,7 +555,7 @@ typedef struct {
   float* m_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   float* v_scale;            /* DEVICE, LSGD_STATE_8BIT only                                                   */
   double beta1, beta2;       /* in [0, 1)                                                                      */
-  double eps;                /* > 0 as a normal fp32 number                                                    */
+  double eps;                /* > 0 as a normal fp32 number; LSGD_STATE_8BIT: >= 2^-50                         */
   uint32_t seed;             /* LSGD_STATE_8BIT: of the random rounding                                        */
   void* stream;              /* cudaStream_t; NULL = the legacy default stream                                 */
 } lsgd_adamw_desc;

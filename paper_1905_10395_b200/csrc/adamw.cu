@@ -65,7 +65,10 @@ struct StepArgs {
 };
 
 constexpr float kTop = 0.53333336f;       // 1 / 1.875: a block's largest magnitude is code 1.875
-constexpr float kTiny = 7.8886091e-31f;   // 2^-100: blocks below it are zero
+// 2^-100: blocks below it are stored as zeros, since the least code (2^-33 of a scale) has to be a number and a reciprocal of
+// the scale finite.  What m / sqrt(v) loses with them, sqrt(v) < 2^-50, eps replaces.
+constexpr float kTiny = 7.8886091e-31f;
+constexpr double kLeastEps8 = 8.8817841970012523e-16;   // 2^-50
 
 __host__ __device__ constexpr float pow2(int e) {
   float r = 1.f;
@@ -424,6 +427,7 @@ lsgd_status check_adamw(const lsgd_adamw_desc* d) {
   if (!(d->beta1 >= 0 && d->beta1 < 1) || !(d->beta2 >= 0 && d->beta2 < 1) || !(d->eps > 0) || !std::isfinite((float)d->eps) ||
       !((float)d->eps >= 1.1754944e-38f))
     return LSGD_ERR_INVALID_ARG;
+  if (d->state_dtype == LSGD_STATE_8BIT && d->eps < kLeastEps8) return LSGD_ERR_INVALID_ARG;
   const int64_t values = lsgd_adamw_state_values(d->n_tensors, d->sizes);
   if (values < 0) return LSGD_ERR_INVALID_ARG;
   if (values / kBlock >= int64_t(1) << 32) return LSGD_ERR_TOO_LARGE;

@@ -218,7 +218,7 @@ class AdamW:
     state "f32" or "8bit".  The moments m, v (and, for 8 bits, their block scales) are zeros unless given: flat buffers in
     which every tensor begins at a multiple of 256 values (`api.adamw_state_values` is their length; m, v fp32 or uint8,
     m_scale, v_scale fp32 of a 256th of it).  weight_decay: one number, or one for each tensor.  seed: of the random rounding
-    of the 8-bit moments.  step: steps already taken (a restored run)."""
+    of the 8-bit moments, which need an eps of at least 2^-50.  step: steps already taken (a restored run)."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, state: Optional[str] = None,
                  m: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, m_scale: Optional[torch.Tensor] = None,

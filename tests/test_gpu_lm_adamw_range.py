@@ -79,3 +79,17 @@ def test_an_infinity_whose_rounding_adds_nothing(moment):
     lost[at // B * B:at // B * B + B] = True
     for t in (m, v):
         assert torch.isnan(t[lost]).all() and torch.isfinite(t[~lost]).all()
+
+
+@pytest.mark.parametrize("size", [1e-14, 4e-15, 1e-15, 1e-20])
+def test_blocks_below_the_least_scale(size):
+    """Blocks whose second moments are stored as zeros, at the least eps: m^ is at most 2^-50 / sqrt(1 - b2) there, so a step is at
+    most lr / sqrt(1 - b2).  A gradient of 1e-14 keeps its v: m^ / sqrt(v^) = 1, and a code of v is within a factor of 9 / 8."""
+    from paper_1905_10395_b200 import lm
+    x, g = torch.zeros(B, device="cuda"), torch.full((B,), size, device="cuda")
+    opt = lm.AdamW([x], [g], state="8bit", beta1=base.B1, beta2=base.B2, eps=2.0 ** -50)
+    bound = 9 / 8 if size == 1e-14 else (1 - base.B2) ** -0.5
+    for _ in range(40):
+        x.zero_()
+        opt.step(1.0)
+        assert 0 <= float(-x.max()) and float(x.abs().max()) <= bound * 1.001

@@ -150,3 +150,23 @@ def test_an_adamw_handle_belongs_to_its_device(lm, tmp_path):
     subprocess.run(["gcc", "-shared", "-fPIC", str(src), "-o", str(so)], check=True)
     r = subprocess.run([sys.executable, "-c", PROGRAM, str(so), ROOT], env={**os.environ, "LD_PRELOAD": str(so)}, capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "done", r.stderr[-2000:]
+
+
+def test_the_least_eps_of_8_bit_moments(lm):
+    """sqrt of the largest second moment that is stored as zero is 2^-50: eps is not below it.  fp32 moments take any normal eps."""
+    import ctypes as C
+
+    import numpy as np
+    api = lm.api
+    size, ptr, wd = np.array([10], dtype=np.int64), np.array([8192], dtype=np.uint64), np.zeros(1, dtype=np.float32)
+    for state, eps, refused in ((1, 2.0 ** -51, True), (1, 1e-30, True), (1, 2.0 ** -50, False), (1, 1e-8, False), (0, 2.0 ** -51, False),
+                                (0, 1e-30, False), (0, 1e-39, True)):
+        d = api.AdamwDesc()
+        d.struct_size, d.n_tensors = C.sizeof(d), 1
+        d.sizes, d.params, d.grads, d.weight_decay = (a.ctypes.data for a in (size, ptr, ptr, wd))
+        d.state_dtype, d.m, d.v, d.m_scale, d.v_scale, d.beta1, d.beta2, d.eps = state, 8192, 8192, 8192, 8192, 0.9, 0.99, eps
+        h = C.c_void_p()
+        status = api.lib().lsgd_adamw_create(C.byref(d), C.byref(h))
+        assert (status == api.ERR_INVALID_ARG) == refused, (state, eps, status)
+        if status == 0:
+            api.lib().lsgd_adamw_destroy(h)
