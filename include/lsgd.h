@@ -520,7 +520,7 @@ LSGD_API lsgd_status lsgd_blocknorm_backward(const lsgd_blocknorm_desc* desc, vo
  * Parameters are fp32, as everywhere in this library, with an optional bf16 copy for the matrix products.
  * Moments live in one buffer each, tensor after tensor, every tensor begun at a multiple of 256 values (its "blocks");
  * lsgd_adamw_state_values() is their length.  A fresh run starts from zeroed buffers.
- *   LSGD_STATE_F32   m, v: float[values]
+ *   LSGD_STATE_F32   m, v: float[values], subnormal second moments (gradients of about 1e-19) included
  *   LSGD_STATE_8BIT  m, v: uint8[values], m_scale, v_scale: float[values / 256], one scale per block.  A code's value is
  *                    a small float times its block's scale: m has a sign, 4 exponent and 3 fraction bits, v has 5 exponent
  *                    and 3 fraction bits and no sign (1.875 is the largest, subnormals included), so m / sqrt(v) keeps the

@@ -156,13 +156,22 @@ __device__ __forceinline__ uint32_t block_top(const float2 (&z)[4]) {
   return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top));
 }
 
-// 1 / (sqrt(v) root + eps).  Subnormal intermediates are flushed: eps is not below 2^-126.
+// 1 / (sqrt(v) root + eps).  eps is not below 2^-126, so the reciprocal's argument is normal; a subnormal v would count as zero,
+// so where its root matters beside eps (LOW) a small v is lifted by 2^64 first and its root lowered by 2^32.
+template <bool LOW>
 __device__ __forceinline__ float reciprocal_root(float v, float root, float eps) {
   float s, r;
+  if (LOW && v < 5.421010862427522e-20f) {                     // 2^-64
+    v *= 18446744073709551616.f;
+    root *= 2.3283064365386963e-10f;
+  }
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(v));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(s, root, eps)));
   return r;
 }
+// A root that is taken as zero is below 2^-63, and root is at most 1 / sqrt(1 - beta2) (the first step's): from this eps on
+// it is below 2^-22 eps, as the approximations are.
+bool low_eps(const lsgd_adamw_desc& d) { return d.eps * std::sqrt(1.0 - d.beta2) < 4.547473508864641e-13; }   // 2^-41
 
 // A sum of products that are rounded first: as a pair the addition would be fused with one of them.
 __device__ __forceinline__ float2 sum(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
@@ -212,7 +221,7 @@ __device__ __forceinline__ uint2 encode_block(const float2 (&z)[4], float scale,
 // The step of 8 values of one block in each lane (32 classifiers of 1.86 million parameters, bf16 gradients, 8-bit moments, bf16
 // copies: 163 us for 954 MB, 5.9 TB/s or 0.89 of the measured copy bandwidth; with scalar arithmetic and codes taken apart bit
 // by bit it was bound by issue slots, 296 us); `have` of them are the tensor's.
-template <typename TG, bool BYTES>
+template <typename TG, bool BYTES, bool LOW>
 __device__ __forceinline__ void step8(const StepArgs& a, const Scalars& k_, const Chunk& c, const Lane8<TG, BYTES>& in, int j0, uint32_t block,
                                       int lane, int have, bool wide) {
   float2 p[4], g[4], m[4], v[4];
@@ -234,7 +243,7 @@ __device__ __forceinline__ void step8(const StepArgs& a, const Scalars& k_, cons
   for (int k = 0; k < 4; ++k) {           // every product and sum rounded by itself: the moments' bits do not depend on the code
     m[k] = sum(mul2(m[k], both(a.b1)), mul2(g[k], both(a.omb1)));
     v[k] = sum(mul2(v[k], both(a.b2)), mul2(mul2(g[k], both(a.omb2)), g[k]));
-    const float2 r = make_float2(reciprocal_root(v[k].x, k_.root, a.eps), reciprocal_root(v[k].y, k_.root, a.eps));
+    const float2 r = make_float2(reciprocal_root<LOW>(v[k].x, k_.root, a.eps), reciprocal_root<LOW>(v[k].y, k_.root, a.eps));
     p[k] = fma2(mul2(m[k], r), both(-k_.step), fma2(p[k], both(decay), p[k]));   // two roundings of p's size
   }
   if (wide) {
@@ -289,7 +298,7 @@ __device__ __forceinline__ void step8(const StepArgs& a, const Scalars& k_, cons
   }
 }
 
-template <typename TG, bool BYTES>
+template <typename TG, bool BYTES, bool LOW>
 __global__ void __launch_bounds__(kWarps * 32, BYTES ? kBlocksBytes : kBlocksF32)
 adamw_step_kernel(const __grid_constant__ StepArgs a) {
   pdl_wait();
@@ -327,7 +336,7 @@ adamw_step_kernel(const __grid_constant__ StepArgs a) {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
           const int b = warp + (h + q) * kWarps;
-          step8<TG, BYTES>(a, k, c, in[q], b * kBlock + lane * 8, c.block + b, lane, 8, true);
+          step8<TG, BYTES, LOW>(a, k, c, in[q], b * kBlock + lane * 8, c.block + b, lane, 8, true);
         }
       }
     } else {
@@ -348,7 +357,7 @@ adamw_step_kernel(const __grid_constant__ StepArgs a) {
           in.g.set(h);
           in.load_moments(a, c.block + b, lane);
         }
-        step8<TG, BYTES>(a, k, c, in, j0, c.block + b, lane, have, wide);
+        step8<TG, BYTES, LOW>(a, k, c, in, j0, c.block + b, lane, have, wide);
       }
     }
     turn ^= 1;
@@ -452,10 +461,11 @@ Counter* counter_of(const lsgd_adamw_ctx* h) { return static_cast<Counter*>(h->s
 Chunk* chunks_of(const lsgd_adamw_ctx* h) { return reinterpret_cast<Chunk*>(static_cast<char*>(h->slab) + 256); }
 
 template <typename TG, bool BYTES>
-cudaError_t launch_step(const StepArgs& a, cudaStream_t s) {
+cudaError_t launch_step(const StepArgs& a, bool low, cudaStream_t s) {
   const uint32_t cap = (uint32_t)sm_count() * (BYTES ? kBlocksBytes : kBlocksF32);
   const uint32_t grid = a.n_chunks < 1 ? 1 : a.n_chunks < cap ? a.n_chunks : cap;   // one block even with nothing to do: it counts the step
-  return launch_pdl(adamw_step_kernel<TG, BYTES>, dim3(grid), dim3(kWarps * 32), 0, s, a);
+  return low ? launch_pdl(adamw_step_kernel<TG, BYTES, true>, dim3(grid), dim3(kWarps * 32), 0, s, a)
+             : launch_pdl(adamw_step_kernel<TG, BYTES, false>, dim3(grid), dim3(kWarps * 32), 0, s, a);
 }
 
 }  // namespace
@@ -563,10 +573,11 @@ lsgd_status lsgd_adamw_step(lsgd_adamw_handle h, double lr, const float* grad_sc
   a.omb2 = (float)(1.0 - h->d.beta2);
   a.eps = (float)h->d.eps;
   a.seed = h->d.seed;
-  const bool bytes = h->d.state_dtype == LSGD_STATE_8BIT;
-  const cudaError_t e = h->d.grad_dtype == LSGD_BF16
-                            ? (bytes ? launch_step<__nv_bfloat16, true>(a, h->stream) : launch_step<__nv_bfloat16, false>(a, h->stream))
-                            : (bytes ? launch_step<float, true>(a, h->stream) : launch_step<float, false>(a, h->stream));
+  const bool bytes = h->d.state_dtype == LSGD_STATE_8BIT, low = low_eps(h->d);
+  const cudaError_t e =
+      h->d.grad_dtype == LSGD_BF16
+          ? (bytes ? launch_step<__nv_bfloat16, true>(a, low, h->stream) : launch_step<__nv_bfloat16, false>(a, low, h->stream))
+          : (bytes ? launch_step<float, true>(a, low, h->stream) : launch_step<float, false>(a, low, h->stream));
   return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
 }
 

@@ -93,3 +93,38 @@ def test_blocks_below_the_least_scale(size):
         x.zero_()
         opt.step(1.0)
         assert 0 <= float(-x.max()) and float(x.abs().max()) <= bound * 1.001
+
+
+@pytest.mark.parametrize("eps", [1.2e-38, 1e-30, 1e-20, 1e-16, 1e-13, 1e-11, 1e-8])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_roots_of_small_second_moments(eps, grad):
+    """fp32 moments down to subnormal ones, against the step of the moments as they are stored: 2^-20 of it, as in the other tests
+    (approximate root and reciprocal, within 2^-22 each, and four roundings).  Sizes from 1 to 1e-21, tensors off 32 bytes too."""
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator(device="cuda").manual_seed(24)
+    n, dtype = 6000, {"f32": torch.float32, "bf16": torch.bfloat16}[grad]
+    for offset in (0, 1):
+        buf = [torch.zeros(n + 1, device="cuda", dtype=t)[offset:offset + n] for t in (torch.float32, dtype)]
+        x, g = buf
+        sizes = torch.logspace(-21, 0, n, dtype=torch.float64, device="cuda")
+        opt = lm.AdamW([x], [g], beta1=base.B1, beta2=base.B2, eps=eps)
+        for t in range(1, 4):
+            g.copy_(torch.randn(n, generator=gen, device="cuda").double() * sizes)
+            x.zero_()
+            opt.step(1.0)
+            m, v = (z[:n].double() for z in opt.moments())
+            want = (m / (1 - base.B1 ** t)) / (torch.sqrt(v / (1 - base.B2 ** t)) + eps)
+            assert (((-x).double() - want).abs() <= 2.0 ** -20 * want.abs() + 1e-37).all(), (offset, t)
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+@pytest.mark.parametrize("scale", [1e-25, 1e-16, 1e-12, 1.0, 1e12])
+def test_steps_with_a_small_eps(state, scale, monkeypatch):
+    """The whole step of every type at an eps whose kernels lift small roots."""
+    monkeypatch.setattr(base, "EPS", 2.0 ** -50)
+    for grad, offset in (("f32", 0), ("bf16", 1)):
+        opt, model, p, g, c, gen = base.build([3000, 4096, 5], state, grad, True, offset, seed=25, scale=scale)
+        for _ in range(3):
+            opt.step(1e-2)
+            model.step([b.view.cpu() for b in g], 1e-2)
+            base.check(opt, model, p, g, c)
