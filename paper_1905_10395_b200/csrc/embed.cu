@@ -258,7 +258,7 @@ embed_grad_few_kernel(Tokens tok, Rows<const TA> d_out, GradRows<TG> grad, uint3
                       int slabs, int D, float scale, bool add) {
   pdl_wait();
   __shared__ __align__(16) uint32_t s_key[kFewTokens];
-  __shared__ uint16_t s_list[kFewTokens];           // kFewAlone for each warp, or one long list
+  __shared__ __align__(16) uint16_t s_list[kFewTokens];   // kFewAlone for each warp, or one long list; or words of row bits
   __shared__ float s_part[kFewWarps][kSlab];
   __shared__ uint32_t s_count[kFewWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kSortThreads)
 embed_scatter_kernel(Tokens tok, SortPass a) {
   pdl_wait();
   pdl_launch_dependents();
-  extern __shared__ uint32_t smem[];
+  extern __shared__ __align__(16) uint32_t smem[];
   const uint32_t bins = 1u << a.bits;
   uint32_t* s_base = smem;                                                   // [bins] next place of each digit
   uint16_t* s_cnt = reinterpret_cast<uint16_t*>(smem + bins);                // [warps][bins]
@@ -566,7 +566,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a, GradRows<TG> grad) {
       clear_row(grad.row(r), threadIdx.x & 31, a.D);
     return;
   }
-  extern __shared__ uint32_t smem[];
+  extern __shared__ __align__(16) uint32_t smem[];
   constexpr uint32_t kBlockKeys = kClusterThreads * ITEMS;
   ClusterMemory<ITEMS>& s = *reinterpret_cast<ClusterMemory<ITEMS>*>(smem);
   const uint32_t bins = 1u << a.bits;
