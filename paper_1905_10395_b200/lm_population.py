@@ -10,6 +10,7 @@ every tau steps the workers' losses elect the leaders and lsgd_step pulls every 
 update is the two pulls alone)."""
 from __future__ import annotations
 
+from contextlib import contextmanager
 from typing import List, Optional, Tuple
 
 import numpy as np
@@ -42,6 +43,7 @@ class LmPopulation:
         self.P, self.V, self.D, self.F, self.L, self.T, self.lr, self.tau = P, V, D, F, L, T, lr, tau
         dev = torch.device(device)
         torch.cuda.set_device(dev)
+        self.stream = torch.cuda.current_stream(dev)      # of all work, whatever stream is current at a call
         self.segs, self.ld = layout(V, D, F, L)
         gen = torch.Generator().manual_seed(seed)
         x = torch.zeros(P, self.ld)
@@ -88,7 +90,7 @@ class LmPopulation:
                             weight_decay=[0.1 if d else 0.0 for _ in range(P) for _, _, _, d in self.segs])
         group_of = np.arange(P) * G // P
         cfg, keep = api.make_config(P=P, G=G, group_of=group_of, d=self.ld, ld=self.ld, eta=1.0, lambda_l=pull, lambda_g=pull / 2, tau=1,
-                                    objective=api.OBJ_EXTERNAL, x=self.x, g=self.zero, stream=torch.cuda.current_stream(dev).cuda_stream)
+                                    objective=api.OBJ_EXTERNAL, x=self.x, g=self.zero, stream=self.stream.cuda_stream)
         self.lsgd = api.Lsgd(cfg, keep)
         self.t = 0
 
@@ -111,10 +113,32 @@ class LmPopulation:
             d.bias, d.stride_bias = bias.data_ptr(), bias.stride(0)
         if mask is not None:
             d.mask, d.ld_mask, d.stride_mask = mask.data_ptr(), mask.stride(1), mask.stride(0)
-        api.lsgd_bgemm_bf16(d, torch.cuda.current_stream().cuda_stream)
+        api.lsgd_bgemm_bf16(d, self.stream.cuda_stream)
+
+    @contextmanager
+    def _in_order(self, *inputs: torch.Tensor):
+        """The population's stream as the current one, behind the caller's and with the caller's behind it."""
+        caller = torch.cuda.current_stream(self.x.device)
+        if caller == self.stream:
+            yield
+            return
+        self.stream.wait_stream(caller)
+        for t in inputs:
+            if t.is_cuda:
+                t.record_stream(self.stream)
+        with torch.cuda.stream(self.stream):
+            yield
+        caller.wait_stream(self.stream)
 
     def forward(self, tokens: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
         """Mean next-token loss of every worker, [P]."""
+        caller = torch.cuda.current_stream(self.x.device)
+        with self._in_order(tokens, target):
+            loss = self._forward(tokens, target)
+        loss.record_stream(caller)
+        return loss
+
+    def _forward(self, tokens: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
         D, W, X = self.D, lambda n: self._view(self.copy, n), lambda n: self._view(self.x, n)
         self.tokens.copy_(tokens)
         self.target.copy_(target)
@@ -134,6 +158,10 @@ class LmPopulation:
 
     def backward(self) -> None:
         """Gradients of every worker's loss into g."""
+        with self._in_order():
+            self._backward()
+
+    def _backward(self) -> None:
         D, W, Gv = self.D, lambda n: self._view(self.copy, n), lambda n: self._view(self.g, n)
         d_logits = self.logp.exp()
         d_logits.scatter_add_(2, self.target[..., None], torch.full_like(self.target[..., None], -1, dtype=torch.float32))
@@ -155,13 +183,14 @@ class LmPopulation:
 
     def step(self, tokens: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
         loss = self.forward(tokens, target)
-        self.backward()
-        self.opt.step(self.lr)
-        self.t += 1
-        if self.t % self.tau == 0:
-            self.lsgd.elect(loss)
-            self.lsgd.step()
-            self.copy.copy_(self.x)          # the pulls moved the parameters: the products' copies follow
+        with self._in_order():
+            self._backward()
+            self.opt.step(self.lr)
+            self.t += 1
+            if self.t % self.tau == 0:
+                self.lsgd.elect(loss)
+                self.lsgd.step()
+                self.copy.copy_(self.x)          # the pulls moved the parameters: the products' copies follow
         return loss
 
     def close(self) -> None:

@@ -47,3 +47,27 @@ def test_the_readout_buffers_are_the_steps_streams(given):
     torch.cuda.synchronize()
     assert torch.isfinite(m).all() and (m != 0).any() and (v > 0).any()
     assert [t.data_ptr() for t in opt.moments()] == [m.data_ptr(), v.data_ptr()]
+
+
+def test_the_population_steps_under_any_stream():
+    """A population built under one stream and stepped under another, busy ones: the same bits as one that is alone."""
+    from paper_1905_10395_b200.lm_population import LmPopulation, markov_tokens
+    make = lambda: LmPopulation(3, 1, V=64, D=32, F=64, L=2, T=128, tau=2, seed=3)  # noqa: E731
+    gen = torch.Generator().manual_seed(4)
+    batches = [markov_tokens(3, 128, 64, gen) for _ in range(4)]
+    alone = make()
+    want = [alone.step(a.cuda(), b.cuda()).cpu() for a, b in batches]
+    torch.cuda.synchronize()
+    pop, s = make(), torch.cuda.Stream()
+    got = []
+    for a, b in batches:
+        torch.cuda._sleep(BUSY // 10)
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(BUSY // 10)
+            loss = pop.step(a.cuda(), b.cuda())
+            got.append(loss.clone())
+    torch.cuda.synchronize()
+    assert all(torch.equal(u, v.cpu()) for u, v in zip(want, got))
+    assert torch.equal(pop.x, alone.x) and torch.equal(pop.copy, alone.copy)
+    for q in (pop, alone):
+        q.close()
