@@ -2,8 +2,10 @@
 
 Each class takes the buffers that its operator works on once, checks them, and keeps the descriptor: a call afterwards is
 one call of the C ABI, with no allocation and no synchronisation, so it can be captured in a CUDA graph.  The tensors must
-outlive the object.  Work is enqueued on the stream given at construction (default: torch's current one at that time); a
-tensor last used on another stream has to be ordered with it by the caller.  The tensors' device has to be the current one at
+outlive the object.  Work is enqueued on the stream given at construction (default: torch's current one at that time), not on
+the one that is current at the call; a tensor last used on another stream has to be ordered with it by the caller.  An operator
+that is to be captured is given the capture's stream: under a capture that its stream is not part of, a call is refused
+(ERR_STATE).  The tensors' device has to be the current one at
 every call (ERR_STATE otherwise).  There is no CPU path.
 
 Rows are [P, T, D] (worker, token, channel) with a channel stride of 1 and any row and worker stride; one worker's may be
@@ -20,6 +22,7 @@ from . import api
 
 _DTYPES = {torch.float32: api.F32, torch.bfloat16: api.BF16}
 _current_device = torch._C._cuda_getDevice      # torch.cuda.current_device() without its check for initialisation: half the time
+_current_stream = torch._C._cuda_getCurrentRawStream
 _GATE_ACTS = {"identity": api.GATE_IDENTITY, "sigmoid": api.GATE_SIGMOID, "tanh": api.GATE_TANH}
 
 
@@ -34,6 +37,17 @@ def _stream(stream, device: torch.device):
     if stream.device != device:
         _fail(f"a stream of {device}, got one of {stream.device}")
     return stream
+
+
+def _not_left_out(stream, name: str) -> None:
+    """Refuses a call under a capture that `stream` is not part of: the call would run at once and be missing from the graph."""
+    if not torch.cuda.is_current_stream_capturing():
+        return
+    if stream.cuda_stream:                       # the default stream cannot be captured
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                return
+    raise api.LsgdError(api.ERR_STATE, f"{name}: a capture is under way that the operator's stream is not part of")
 
 
 def _dtype(name: str, *tensors) -> int:
@@ -87,7 +101,7 @@ class _Bound:
 
     def _bind(self, name, desc, device, stream, keep, scratch):
         self.device, self._index, self._keep = device, device.index, [keep]
-        self._stream = stream.cuda_stream
+        self._stream, self._torch_stream = stream.cuda_stream, stream
         L = api.lib()
         self._forward, self._backward = getattr(L, f"lsgd_{name}_forward"), getattr(L, f"lsgd_{name}_backward")
         self._name, self.desc, self._ref = name, desc, C.byref(desc)
@@ -106,6 +120,8 @@ class _Bound:
     def forward(self) -> None:
         if _current_device() != self._index:     # the default stream would be the other device's, and so would the plan
             self._other_device()
+        if _current_stream(self._index) != self._stream:
+            _not_left_out(self._torch_stream, f"lsgd_{self._name}")
         s = self._forward(self._ref, self._stream)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_forward")
@@ -113,6 +129,8 @@ class _Bound:
     def backward(self) -> None:
         if _current_device() != self._index:
             self._other_device()
+        if _current_stream(self._index) != self._stream:
+            _not_left_out(self._torch_stream, f"lsgd_{self._name}")
         s = self._backward(self._ref, self._stream)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_backward")
@@ -291,16 +309,22 @@ class AdamW:
             with torch.cuda.device(device):
                 self.set_step(step)
 
+    def _ready(self, name: str) -> None:
+        if _current_stream(self.device.index) != self._stream.cuda_stream:
+            _not_left_out(self._stream, name)
+
     def step(self, lr: float, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step.  grad_scale: a device fp32 scalar that the gradients are multiplied by first."""
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.device):
             _fail("grad_scale: one fp32 value on the tensors' device")
+        self._ready("lsgd_adamw_step")
         s = self._step(self.h, lr, grad_scale.data_ptr() if grad_scale is not None else None)
         if s:
             raise api.LsgdError(s, "lsgd_adamw_step")
 
     def moments(self):
         """The moments as the fp32 values that they stand for, flat, in buffers that the next call overwrites."""
+        self._ready("lsgd_adamw_moments")
         if self._read is None:
             with torch.cuda.stream(self._stream):
                 self._read = [torch.empty(self.values, dtype=torch.float32, device=self.device) for _ in range(2)]
@@ -318,6 +342,7 @@ class AdamW:
         return n.value
 
     def set_step(self, n: int) -> None:
+        self._ready("lsgd_adamw_set_step")
         s = api.lib().lsgd_adamw_set_step(self.h, int(n))
         if s:
             raise api.LsgdError(s, "lsgd_adamw_set_step")

@@ -71,3 +71,60 @@ def test_the_population_steps_under_any_stream():
     assert torch.equal(pop.x, alone.x) and torch.equal(pop.copy, alone.copy)
     for q in (pop, alone):
         q.close()
+
+
+def _bound(stream=None):
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    table, d_table, rows = mk(1, 40, 64), torch.zeros(1, 40, 64, device="cuda"), [mk(1, 30, 64) for _ in range(6)]
+    tok = torch.randint(0, 40, (1, 30), generator=gen, device="cuda")
+    e = lm.Embedding(tok, table=table, out=rows[0], d_out=rows[1], d_table=d_table, stream=stream)
+    n = lm.BlockNorm(x=rows[0], out=rows[0], h=rows[2], w_pre=mk(1, 64), d_out=rows[3], d_h=rows[4], dx=rows[5], stream=stream)
+    p = mk(1000)
+    a = lm.AdamW([p], [mk(1000)], state="8bit", stream=stream)
+    a.step(1e-2)
+    a.moments()
+    torch.cuda.synchronize()
+    return e, n, a, (rows, d_table, p)
+
+
+def test_a_call_is_not_left_out_of_a_capture():
+    """Operators of the default stream under a capture of another: refused, nothing is launched, and the capture goes on."""
+    from paper_1905_10395_b200 import api
+    e, n, a, (rows, d_table, p) = _bound()
+    before = [t.clone() for t in (*rows, d_table, p)]
+    graph, count = torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        count += 1
+        for call in (e.forward, e.backward, n.forward, n.backward, lambda: a.step(1e-2), a.moments, lambda: a.set_step(3)):
+            with pytest.raises(api.LsgdError) as err:
+                call()
+            assert err.value.status == api.ERR_STATE
+        count += 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert count.item() == 2 and a.t() == 1
+    assert all(torch.equal(u, v) for u, v in zip(before, (*rows, d_table, p)))
+
+
+def test_a_stream_that_the_capture_has_been_forked_to():
+    """The operators' stream joins the capture through an event: their calls are captured, whatever stream is current."""
+    side = torch.cuda.Stream()
+    e, n, a, (rows, d_table, p) = _bound(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        e.forward()
+        n.forward()
+        a.step(1e-2)
+        torch.cuda.current_stream().wait_stream(side)
+    x = p.clone()
+    rows[0].zero_()
+    rows[2].zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert not torch.equal(p, x) and a.t() == 4
+    assert (rows[0].abs().sum(-1) > 0).all() and (rows[2].abs().sum(-1) > 0).all()

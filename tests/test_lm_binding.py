@@ -28,6 +28,8 @@ class Devices:
 
         monkeypatch.setattr(lm, "_same_device", lambda *t: torch.device("cuda:1"))
         monkeypatch.setattr(lm, "_current_device", lambda: self.current, raising=False)
+        monkeypatch.setattr(lm, "_current_stream", lambda index: 0, raising=False)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
         monkeypatch.setattr(torch.cuda, "device", device)
         monkeypatch.setattr(torch.cuda, "current_device", lambda: self.current)
         monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: Stream(torch.device(d), 0))
