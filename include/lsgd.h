@@ -473,7 +473,8 @@ LSGD_API lsgd_status lsgd_embed_check_device(uint32_t* flag_out /* HOST, may be 
  * fp32; out and h are each rounded once (h from the unrounded x').  The forward pass stores 1 / sqrt(...) of both norms
  * for the backward pass, which reads x' as stored in `out` (with y absent: give x itself as `out`):
  *   dx' = d_out + d norm / dx' (d_h w_pre),  dx = alpha dx',  dy, d_gate, d_w_post, d_w_pre by the chain rule.
- * d_out absent counts as zeros.  A weight gradient that is absent is not computed; given with stride 0 and P > 1 it is the
+ * d_out absent counts as zeros.  A weight gradient that is absent is not computed; given without its weight (or h, d_h without
+ * w_pre, d_gate without a gate, dy without y) it is refused, LSGD_ERR_INVALID_ARG; given with stride 0 and P > 1 it is the
  * sum over the workers (one gain shared by all).  Sums over rows are fp32 in a fixed order.
  * out may be x and dx may be d_out (same strides): every value is read before it is overwritten.                */
 typedef enum {

@@ -80,6 +80,10 @@ lsgd_status check_norm(const lsgd_blocknorm_desc* d, bool backward) {
   const bool has_y = d->y.data != nullptr, pre = d->w_pre.data != nullptr, rows = d->T > 0;
   const bool gated = d->gate_kind != LSGD_GATE_NONE, channel = d->gate_kind == LSGD_GATE_CHANNEL;
   if (!has_y && rows && (d->post_norm || gated || !pre)) return LSGD_ERR_INVALID_ARG;
+  // what would be left unwritten, or unread, for want of the operand it belongs to
+  if (!pre && (backward ? d->d_w_pre.data || d->d_h.data : d->h.data != nullptr)) return LSGD_ERR_INVALID_ARG;
+  if (backward && ((!d->post_norm && d->d_w_post.data) || (!gated && d->d_gate.data) || (!has_y && rows && d->dy.data)))
+    return LSGD_ERR_INVALID_ARG;
   const int rb = elem_bytes(d->resid_dtype), ab = elem_bytes(d->act_dtype);
   const int64_t P = d->P, T = d->T, D = d->D;
   if (d->post_norm && (!d->w_post.data || (rows && !d->rstd_post))) return LSGD_ERR_INVALID_ARG;

@@ -194,6 +194,10 @@ class BlockNorm(_Bound):
         if gate_act not in _GATE_ACTS:
             _fail(f"gate_act: one of {sorted(_GATE_ACTS)}")
         post_norm = bool(post_norm) and y is not None
+        for given, of, names in (((h, d_h, dw_pre), w_pre, "h, d_h and dw_pre need w_pre"), ((d_gate,), gate, "d_gate needs a gate"),
+                                 ((dy,), y, "dy needs y"), ((dw_post,), y if post_norm else None, "dw_post needs a norm of y")):
+            if of is None and any(t is not None for t in given):
+                _fail(f"BlockNorm: {names}")
         channel = gate is not None and gate.dim() == (2 if like.dim() == 3 else 1)
         token_gate = None if channel else gate
         keep = [x, y, gate, w_post, w_pre, out, h, rstd_post, rstd_pre, d_out, d_h, dx, dy, d_gate, dw_post, dw_pre]

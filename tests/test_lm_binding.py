@@ -172,3 +172,24 @@ def test_the_least_eps_of_8_bit_moments(lm):
         assert (status == api.ERR_INVALID_ARG) == refused, (state, eps, status)
         if status == 0:
             api.lib().lsgd_adamw_destroy(h)
+
+
+def test_results_without_their_operand_are_refused(lm, devices):
+    """A gradient, or h, whose operand is absent would stay unwritten: the library and the binding refuse it."""
+    from tests.test_lm_boundary import _norm
+    api = lm.api
+    none = api.Rows(None, 0, 0)
+    fwd, bwd = api.lib().lsgd_blocknorm_forward, api.lib().lsgd_blocknorm_backward
+    import ctypes as C
+    assert fwd(C.byref(_norm(api, w_pre=none)), None) == api.ERR_INVALID_ARG                         # h
+    for over in (dict(w_pre=none, d_h=none), dict(w_pre=none, d_w_pre=none), dict(post_norm=0), dict(gate_kind=0),
+                 dict(y=none, post_norm=0, gate_kind=0, d_w_post=none, d_gate=none)):
+        scratch = dict(scratch=8192, scratch_bytes=1 << 40)
+        assert bwd(C.byref(_norm(api, **scratch, **over)), None) == api.ERR_INVALID_ARG, over
+    t, w = torch.zeros(1, 4, 8), torch.ones(1, 8)
+    for kw in (dict(y=t, out=t, h=t, w_post=w), dict(y=t, out=t, d_h=t, w_post=w), dict(y=t, out=t, w_post=w, dw_pre=w),
+               dict(y=t, out=t, post_norm=False, dw_post=w), dict(h=t, w_pre=w, dw_post=w), dict(y=t, out=t, w_post=w, d_gate=t),
+               dict(h=t, w_pre=w, dy=t)):
+        with pytest.raises(api.LsgdError) as e:
+            lm.BlockNorm(x=t, **kw)
+        assert e.value.status == api.ERR_INVALID_ARG, kw
