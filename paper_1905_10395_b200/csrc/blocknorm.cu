@@ -99,7 +99,7 @@ lsgd_status check_norm(const lsgd_blocknorm_desc* d, bool backward) {
   LSGD_ROWS(d->gate, channel ? 1 : T, channel ? 4 : ab, false, false);
   LSGD_ROWS(d->w_post, 1, 4, false, false);
   LSGD_ROWS(d->w_pre, 1, 4, false, false);
-  LSGD_ROWS(d->out, T, rb, !backward, false);
+  LSGD_ROWS(d->out, T, rb, !backward && has_y, false);      // without y it is only the backward pass's input
   if (!backward) {
     if (rows && (!d->x.data || (has_y && !d->out.data) || (pre && !d->h.data))) return LSGD_ERR_INVALID_ARG;
     LSGD_ROWS(d->x, T, rb, false, false);
