@@ -76,7 +76,8 @@ class LmPopulation:
         self.embed = lm.Embedding(self.tokens, table=view(self.x, "table"), out=self.res[0], d_out=self.d_res[0],
                                   d_table=view(self.g, "table"), scale=scale, accumulate=True)
         # boundary 0 normalises the embedded tokens; boundary i + 1 closes block i and opens the next
-        self.boundary = [lm.BlockNorm(x=self.res[0], h=self.h[0], out=self.res[0], w_pre=view(self.x, "w_pre0"), d_out=self.d_res[0],
+        self.boundary = [lm.BlockNorm(x=self.res[0], h=self.h[0], out=self.res[0], w_pre=view(self.x, "w_pre0"),
+                                      d_out=self.d_res[0] if L else None,
                                       d_h=self.d_h[0], dx=self.d_res[0], dw_pre=view(self.g, "w_pre0"))]
         for i in range(L):
             last = i + 1 == L

@@ -67,3 +67,23 @@ def test_training_with_leaders(state):
     assert losses[0].mean() > 3.5 and losses[-1].mean() < 1.2, (losses[0], losses[-1])     # log 64 = 4.16; the source has 0.69
     assert pop.opt.t() == 80
     pop.close()
+
+
+def test_a_population_without_blocks():
+    """L = 0: the embedded tokens' norm and the output layer alone.  Nothing is read that no kernel has written (10 % of a tensor's
+    gradient as in the other tests of whole models: bf16 operands)."""
+    from paper_1905_10395_b200.lm_population import LmPopulation, markov_tokens
+    pop = LmPopulation(2, 1, V=64, D=32, F=64, L=0, T=100, seed=4)
+    for t in (*pop.res, *pop.d_res, *pop.h, *pop.d_h, pop.logits):
+        t.fill_(float("nan"))
+    tok, target = (t.cuda() for t in markov_tokens(2, 100, 64, torch.Generator().manual_seed(5)))
+    loss = pop.forward(tok, target)
+    pop.backward()
+    torch.cuda.synchronize()
+    for p in range(2):
+        want, grads = _model(pop, p, tok[p], target[p])
+        assert abs(loss[p].item() - want) <= 2e-2 * abs(want)
+        for name, g in grads.items():
+            mine = pop._view(pop.g, name)[p]
+            assert (mine - g).norm() <= 0.1 * g.norm() + 1e-6, (p, name)
+    pop.close()
