@@ -652,23 +652,20 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a, GradRows<TG> grad) {
       }
     }
     __syncthreads();
-    if (a.blocks > 1) {
 #pragma unroll
-      for (int q = 0; q < ITEMS; ++q) {
-        const uint32_t i = threadIdx.x + q * kClusterThreads;
-        if (i < n) {
-          const uint2 v = s.stage[i];
-          const uint32_t d = (v.x >> shift) & mask;
-          const uint32_t to = s.base[d] + (i - s.local[d]);                   // < N
-          store_remote(remote(&s.place[to % kBlockKeys], to / kBlockKeys), v);
-        }
+    for (int q = 0; q < ITEMS; ++q) {
+      const uint32_t i = threadIdx.x + q * kClusterThreads;
+      if (i < n) {
+        const uint2 v = s.stage[i];
+        const uint32_t d = (v.x >> shift) & mask;
+        const uint32_t to = s.base[d] + (i - s.local[d]);                     // < N
+        store_remote(remote(&s.place[to % kBlockKeys], to / kBlockKeys), v);
       }
-      cluster_sync();                      // every key is in its place
     }
-    const uint2* from = a.blocks > 1 ? s.place : s.stage;
+    cluster_sync();                        // every key is in its place
 #pragma unroll
     for (int q = 0; q < ITEMS; ++q)
-      if (at + q * 32 < n) item[q] = from[at + q * 32];
+      if (at + q * 32 < n) item[q] = s.place[at + q * 32];
     if (pass + 1 == a.passes) {
 #pragma unroll
       for (int q = 0; q < ITEMS; ++q) {
@@ -677,7 +674,7 @@ embed_cluster_sort_kernel(Tokens tok, ClusterSort a, GradRows<TG> grad) {
           a.key_out[first + i] = item[q].x;
           a.pos_out[first + i] = item[q].y;
           // a row's first place marks it (flags were cleared before the cluster barriers)
-          if (a.touched && item[q].x != a.none_key && (i == 0 || from[i - 1].x != item[q].x)) a.touched[item[q].x] = 1;
+          if (a.touched && item[q].x != a.none_key && (i == 0 || s.place[i - 1].x != item[q].x)) a.touched[item[q].x] = 1;
         }
       }
     }
@@ -697,7 +694,7 @@ struct SumArgs {
   const uint32_t *key, *pos;  // sorted
   const uint8_t* touched;     // nullptr: rows of absent tokens are left alone
   float* part;                // [pieces][2][slabs * 256]
-  uint32_t N, T, none_key, rows;
+  uint32_t N, T, none_key;
   uint32_t piece, pieces, slabs;
   uint32_t sum_blocks, rows_per_block;
   uint32_t clear_rows;        // the absent ones of the first clear_rows rows are cleared here
@@ -1017,7 +1014,7 @@ cudaError_t launch_cluster_sort(const SortPlan& p, const Tokens& tok, char* w, u
   a.none_key = a.rows = p.rows;
   a.bits = p.bits;
   a.passes = p.passes;
-  a.blocks = 1;
+  a.blocks = kClusterBlocks / 2;             // the fewest that more than kFewTokens positions take
   while ((uint32_t)a.blocks * kClusterThreads * ITEMS < p.N) a.blocks *= 2;
   a.clear_from = p.rows - cleared;
   a.D = D;
@@ -1102,7 +1099,6 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   a.N = p.N;
   a.T = tok.T;
   a.none_key = rows;
-  a.rows = rows;
   a.piece = p.piece;
   a.pieces = p.pieces;
   a.slabs = slabs;
@@ -1115,9 +1111,8 @@ cudaError_t launch_grad(const lsgd_embed_desc* e, cudaStream_t s) {
   const uint32_t zero_blocks = (a.clear_rows + rows_per_block - 1) / rows_per_block;
   if ((err = launch_pdl(embed_sum_kernel<TG, TA, VEC>, dim3(a.sum_blocks + zero_blocks), dim3(kSumThreads), 0, s, a, d_out, grad)) != cudaSuccess)
     return err;
-  if (p.pieces > 1)
-    return launch_pdl(embed_join_kernel<TG, VEC>, dim3((p.pieces - 1 + kSumWarps - 1) / kSumWarps, slabs < 8 ? slabs : 8), dim3(kSumThreads), 0, s, a, grad);
-  return cudaSuccess;
+  return launch_pdl(embed_join_kernel<TG, VEC>, dim3((p.pieces - 1 + kSumWarps - 1) / kSumWarps, slabs < 8 ? slabs : 8), dim3(kSumThreads), 0, s,
+                    a, grad);                // more than kFewTokens positions are many pieces
 }
 
 template <int VEC>
