@@ -3,16 +3,18 @@
 //     out[p][t] = scale * table[p][token]          d_table[p][v] = scale * sum_{t: token = v} d_out[p][t]
 //
 // Both only move rows: the lookup reads and writes each value once, the gradient reads every row of d_out once and
-// writes every row of d_table once (the rows of absent tokens with zeros).
+// writes every row of d_table, the rows of absent tokens with zeros.  A row is written once, except for the last rows of a
+// table whose tokens are sorted by a cluster: those are cleared during the sort, before it is known which of them have a token.
 //
 // The gradient must not depend on timing, so no row is added with atomics.  Two ways to the same sums:
 //   few tokens   one launch.  Every block reads all tokens; a warp takes a position, leaves if an earlier one holds the same
 //                token, and otherwise lists the later ones and adds their rows in order.
 //   many tokens  positions are sorted by (worker, token) with a stable radix sort -- up to 131072 positions in the shared
 //                memory of one cluster, in one launch, more with a histogram and a scatter launch per pass; a warp then
-//                walks a piece of the sorted list, adding rows while the token stays the same.  A token that lies within one piece is written at once; pieces of a
-//                token that crosses piece ends leave fp32 partial rows, which a last launch adds in order.  Work is
-//                split by positions, never by token, so it stays even however often one token occurs.
+//                walks a piece of the sorted list, adding rows while the token stays the same.  A token that lies within
+//                one piece is written at once; pieces of a token that crosses piece ends leave fp32 partial rows, which a
+//                last launch adds in order.  Work is split by positions, never by token, so it stays even however often
+//                one token occurs.
 #include "lm_ops.h"
 
 namespace lsgd {
@@ -215,38 +217,38 @@ constexpr int kFewLoads = 8;                        // tokens that a thread load
 constexpr int kFewAlone = 32;                       // rows that one warp adds alone
 
 // The positions after `mine`'s that hold the same key, in order, into list[0 .. cap): returns how many there are with
-// itself, or 0 if there is an earlier one.  128 keys at a time, 4 to a lane; a whole warp calls it.
+// itself, or 0 if there is an earlier one.  512 keys at a time, 4 times 4 to a lane; a whole warp calls it.
 __device__ __forceinline__ uint32_t find_same(const uint32_t* s_key, uint32_t N, uint32_t me, uint32_t mine, uint16_t* list, uint32_t cap) {
   const int lane = threadIdx.x & 31;
   uint32_t count = 0;
   for (uint32_t j = 0; j < N; j += 512) {           // the keys behind the last are none's
-   uint32_t hits = 0;
+    uint32_t hits = 0;
 #pragma unroll
-   for (int u = 0; u < 4; ++u) {
-    const uint4 k = *reinterpret_cast<const uint4*>(s_key + j + u * 128 + lane * 4);
-    hits |= ((k.x == mine) | (k.y == mine) << 1 | (k.z == mine) << 2 | (k.w == mine) << 3) << (4 * u);
-   }
-   if (!__any_sync(0xFFFFFFFFu, hits)) continue;
-   for (int u = 0; u < 4; ++u) {
-    const uint32_t j0 = j + u * 128, hit = hits >> (4 * u) & 15u;
-    const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, hit != 0);
-    if (lanes == 0) continue;
-    if (count == 0) {
-      const int l = __ffs(lanes) - 1;
-      if (j0 + l * 4 + __ffs(__shfl_sync(0xFFFFFFFFu, hit, l)) - 1 != me) return 0;
+    for (int u = 0; u < 4; ++u) {
+      const uint4 k = *reinterpret_cast<const uint4*>(s_key + j + u * 128 + lane * 4);
+      hits |= ((k.x == mine) | (k.y == mine) << 1 | (k.z == mine) << 2 | (k.w == mine) << 3) << (4 * u);
     }
-    const uint32_t n = __popc(hit);
-    uint32_t incl = n;
+    if (!__any_sync(0xFFFFFFFFu, hits)) continue;
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t j0 = j + u * 128, hit = hits >> (4 * u) & 15u;
+      const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, hit != 0);
+      if (lanes == 0) continue;
+      if (count == 0) {
+        const int l = __ffs(lanes) - 1;
+        if (j0 + l * 4 + __ffs(__shfl_sync(0xFFFFFFFFu, hit, l)) - 1 != me) return 0;
+      }
+      const uint32_t n = __popc(hit);
+      uint32_t incl = n;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += v;
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      uint32_t place = count + incl - n;
+      for (uint32_t b = hit; b; b &= b - 1, ++place)
+        if (place < cap) list[place] = (uint16_t)(j0 + lane * 4 + __ffs(b) - 1);
+      count += __shfl_sync(0xFFFFFFFFu, incl, 31);
     }
-    uint32_t place = count + incl - n;
-    for (uint32_t b = hit; b; b &= b - 1, ++place)
-      if (place < cap) list[place] = (uint16_t)(j0 + lane * 4 + __ffs(b) - 1);
-    count += __shfl_sync(0xFFFFFFFFu, incl, 31);
-   }
   }
   __syncwarp();
   return count;
