@@ -237,7 +237,7 @@ class AdamW:
     """One AdamW step over many tensors, in one launch.  params fp32, grads fp32 or bf16 (all of one type), each of them
     contiguous; copies: bf16 copies of the parameters (entries may be None), rewritten by every step.
 
-    state "f32" or "8bit".  The moments m, v (and, for 8 bits, their block scales) are zeros unless given: flat buffers in
+    state "f32" or "8bit".  The moments m, v (and, for 8 bits, their block scales) are zeros, or given all together: flat buffers in
     which every tensor begins at a multiple of 256 values (`api.adamw_state_values` is their length; m, v fp32 or uint8,
     m_scale, v_scale fp32 of a 256th of it).  weight_decay: one number, or one for each tensor.  seed: of the random rounding
     of the 8-bit moments, which need an eps of at least 2^-50.  step: steps already taken (a restored run)."""
@@ -282,6 +282,11 @@ class AdamW:
                 _fail(f"{name}: {count} contiguous values of {dtype}")
             return t
 
+        parts = (m, v, m_scale, v_scale) if state == "8bit" else (m, v)
+        if any(t is not None for t in parts) and any(t is None for t in parts):
+            _fail("AdamW: a state is given whole (m, v and, for 8 bits, m_scale and v_scale) or not at all")
+        if state == "f32" and (m_scale is not None or v_scale is not None):
+            _fail("AdamW: scales belong to 8-bit moments")
         self.m, self.v = buffer("m", m, values, kind), buffer("v", v, values, kind)
         self.m_scale = self.v_scale = None
         if state == "8bit":

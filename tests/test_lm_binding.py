@@ -193,3 +193,24 @@ def test_results_without_their_operand_are_refused(lm, devices):
         with pytest.raises(api.LsgdError) as e:
             lm.BlockNorm(x=t, **kw)
         assert e.value.status == api.ERR_INVALID_ARG, kw
+
+
+def test_a_state_is_given_whole(lm, devices, monkeypatch):
+    """Codes without their scales would read as zeros, and one moment without the other is no state."""
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: b"" if name == "lsgd_status_string" else 0
+
+    x, f = torch.zeros(256), torch.zeros(256)
+    b, s = torch.zeros(256, dtype=torch.uint8), torch.zeros(1)
+    monkeypatch.setattr(lm.api, "adamw_state_values", lambda sizes: 256)
+    monkeypatch.setattr(lm.api, "lib", lambda: Library())
+    for kw in (dict(m=f), dict(v=f), dict(m=b, v=b), dict(m=b, v=b, m_scale=s), dict(m=b, m_scale=s, state="8bit"),
+               dict(v=b, v_scale=s, state="8bit"), dict(m_scale=s, v_scale=s, state="8bit"), dict(m=f, v=f, m_scale=s, v_scale=s)):
+        with pytest.raises(lm.api.LsgdError) as e:
+            lm.AdamW([x], [x], **kw)
+        assert e.value.status == lm.api.ERR_INVALID_ARG, kw
+    for kw in (dict(m=f, v=f), dict(m=b, v=b, m_scale=s, v_scale=s)):
+        opt = lm.AdamW([x], [x], **kw)
+        assert opt.m is kw["m"] and opt.v is kw["v"]
+        opt.h = None
