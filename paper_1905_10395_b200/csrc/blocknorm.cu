@@ -5,13 +5,6 @@ namespace lsgd {
 namespace blocknorm {
 namespace {
 
-// a(z) and its derivative
-__device__ __forceinline__ float gate_at(float z, int act, float& slope) {
-  const float v = act == LSGD_GATE_SIGMOID ? 1.f / (1.f + __expf(-z)) : act == LSGD_GATE_TANH ? tanhf(z) : z;
-  slope = act == LSGD_GATE_SIGMOID ? v * (1.f - v) : act == LSGD_GATE_TANH ? 1.f - v * v : 1.f;
-  return v;
-}
-
 // Adds the blocks' partial rows in order: columns of one of the three sums of one worker (of all workers where they share the
 // vector).  `split` warps share 32 columns, each adding a run of rows, then the runs are added.
 constexpr int kJoinMaxSplit = 32;
@@ -49,11 +42,10 @@ blocknorm_join_kernel(const __grid_constant__ Args a, const __grid_constant__ Jo
         for (int q = 0; q < join.split; ++q) v += s[warp + q][lane];
     }
     if (sub == 0 && col < d.D && j > 0) {
-      float ga = 1.f, slope = 1.f;
-      if (channel) ga = gate_at(static_cast<const float*>(d.gate.data)[w * d.gate.stride + col], d.gate_act, slope);
+      const float ga = channel ? gate_value(static_cast<const float*>(d.gate.data)[w * d.gate.stride + col], d.gate_act) : 1.f;
       v *= d.beta;
       if (j == 1) v *= ga;
-      else v *= slope * (d.post_norm ? static_cast<const float*>(d.w_post.data)[w * d.w_post.stride + col] : 1.f);
+      else v *= gate_slope(ga, d.gate_act) * (d.post_norm ? static_cast<const float*>(d.w_post.data)[w * d.w_post.stride + col] : 1.f);
     }
     total += v;
   }

@@ -69,6 +69,25 @@ cudaError_t launch_f32_bf16(const Args& a, const Launch& l, cudaStream_t s);
 cudaError_t launch_bf16_bf16(const Args& a, const Launch& l, cudaStream_t s);
 constexpr int kSmemMax = 224 * 1024;      // dynamic shared memory of a block at most
 
+#if defined(__CUDACC__)
+// ---- the gate, for the kernels of the rows and of the last sums alike
+// 1 / (1 + 2^(-z log2 e)); subnormal intermediates are flushed: they only move results by less than 2^-126
+__device__ __forceinline__ float sigmoid(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+__device__ __forceinline__ float gate_slope(float a, int act) {
+  if (act == LSGD_GATE_SIGMOID) return a * (1.f - a);
+  if (act == LSGD_GATE_TANH) return 1.f - a * a;
+  return 1.f;
+}
+__device__ __forceinline__ float gate_value(float z, int act) {
+  return act == LSGD_GATE_SIGMOID ? sigmoid(z) : act == LSGD_GATE_TANH ? tanhf(z) : z;
+}
+#endif
+
 #if defined(LSGD_BLOCKNORM_KERNELS)
 namespace {
 
@@ -230,18 +249,6 @@ __device__ __forceinline__ float row_sum(float2 a, int tpr, int sub, float* s_re
   return s;
 }
 
-// 1 / (1 + 2^(-z log2 e)); subnormal intermediates are flushed: they only move results by less than 2^-126
-__device__ __forceinline__ float sigmoid(float z) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-  return r;
-}
-__device__ __forceinline__ float gate_slope(float a, int act) {
-  if (act == LSGD_GATE_SIGMOID) return a * (1.f - a);
-  if (act == LSGD_GATE_TANH) return 1.f - a * a;
-  return 1.f;
-}
 __device__ __forceinline__ void gate_values(float2 (&f)[4], int act) {
   if (act == LSGD_GATE_SIGMOID) {
     LSGD_EACH(k) f[k] = make_float2(sigmoid(f[k].x), sigmoid(f[k].y));
