@@ -102,6 +102,7 @@ class _Bound:
     def _bind(self, name, desc, device, stream, keep, scratch):
         self.device, self._index, self._keep = device, device.index, [keep]
         self._stream, self._torch_stream = stream.cuda_stream, stream
+        self._arg = stream.cuda_stream or None           # as the library gets it (None is passed on faster than 0)
         L = api.lib()
         self._forward, self._backward = getattr(L, f"lsgd_{name}_forward"), getattr(L, f"lsgd_{name}_backward")
         self._name, self.desc, self._ref = name, desc, C.byref(desc)
@@ -122,7 +123,7 @@ class _Bound:
             self._other_device()
         if _current_stream(self._index) != self._stream:
             _not_left_out(self._torch_stream, f"lsgd_{self._name}")
-        s = self._forward(self._ref, self._stream)
+        s = self._forward(self._ref, self._arg)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_forward")
 
@@ -131,7 +132,7 @@ class _Bound:
             self._other_device()
         if _current_stream(self._index) != self._stream:
             _not_left_out(self._torch_stream, f"lsgd_{self._name}")
-        s = self._backward(self._ref, self._stream)
+        s = self._backward(self._ref, self._arg)
         if s:
             raise api.LsgdError(s, f"lsgd_{self._name}_backward")
 
