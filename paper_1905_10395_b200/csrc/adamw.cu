@@ -77,6 +77,7 @@ __host__ __device__ constexpr float pow2(int e) {
 }
 constexpr int kShiftM = 112, kShiftV = 96;
 
+// Random bits of a number: the multipliers and the first two shifts of the final mixing of xxHash (Y. Collet, 32-bit variant).
 __device__ __forceinline__ uint32_t mix(uint32_t h) {
   h *= 0x9E3779B1u;
   h ^= h >> 15;

@@ -35,8 +35,10 @@ namespace blocknorm {
 
 using bf16 = __nv_bfloat16;
 constexpr int E = 16;        // values of a row that a thread holds, in two halves of 8
-// threads of an SM, which set the registers of one: 80 and 128.  With 896 threads forward 8 x 2048 x 2048 takes 98 us instead
-// of 85, with 640 as long; fewer registers backward spill the sums.
+// Threads of an SM, which set the registers of one: 80 and 128.  Rows that fill their threads: forward 8 x 2048 x 2048 takes 80
+// us, 98 with 896 threads and as long with 640; fewer registers backward spill the sums.  The ragged kernels' extra addresses
+// and masks do not all fit: with a gate for each value they spill up to 344 bytes a thread forward and 180 backward (fp32
+// activations; 176 and 220 with bf16 ones beside an fp32 residual, at most 20 with a bf16 residual).
 constexpr int kForwardThreads = 768, kBackwardThreads = 512;
 
 struct Args {
@@ -71,7 +73,8 @@ constexpr int kSmemMax = 224 * 1024;      // dynamic shared memory of a block at
 
 #if defined(__CUDACC__)
 // ---- the gate, for the kernels of the rows and of the last sums alike
-// 1 / (1 + 2^(-z log2 e)); subnormal intermediates are flushed: they only move results by less than 2^-126
+// 1 / (1 + 2^(-z log2 e)) with the approximate power and reciprocal, each within about 2^-22; the product's rounding adds |z| 2^-24
+// to the power.  Subnormal intermediates are flushed: they only move results by less than 2^-126.
 __device__ __forceinline__ float sigmoid(float z) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
@@ -331,8 +334,8 @@ struct Output {
   __device__ __forceinline__ void advance() { p += step; }
 };
 
-// 8 x 2048 rows of 2048 values, fp32 residual, a sigmoid gate for each value: 80 us for 470 MB, 5.9 TB/s or 0.90 of the measured
-// copy bandwidth.
+// 8 x 2048 rows of 2048 values, fp32 residual, a sigmoid gate for each value: 80 to 83 us for 470 MB (two devices), 5.9 to 5.7
+// TB/s or 0.90 to 0.87 of the measured copy bandwidth.
 // Blocks: blockIdx.y = worker; block b of a worker takes its rows b rpb .., then those blocks_w rpb further on.
 template <typename TR, typename TA, int MODE>
 __global__ void __launch_bounds__(kForwardThreads, 1)

@@ -51,10 +51,11 @@ struct Tokens {
 };
 
 // ------------------------------------------------------------------------------------------------ lookup
-// A block copies kLookupRows rows for each group of tx threads.  8 x 4096 rows of 1024 fp32 values into bf16: 27 us.  HBM gives
-// the 57 MB of distinct rows and takes part of the 67 MB written; what bounds it is that every token's row crosses from L2 to
-// an SM, 134 MB in and 67 MB out at 7.5 TB/s: 1, 2 or 4 rows a thread, 3 to 8 blocks an SM and a persistent form with the
-// tokens ahead measured 27 to 30 us.
+// A block copies kLookupRows rows for each group of tx threads.  8 x 4096 rows of 1024 fp32 values into bf16: 27 us, 1.4 times
+// what the 124 MB of distinct rows and outputs take at the measured copy bandwidth.  No unit is at its limit (DRAM 35 %, L2
+// 30 %, issue 47 %): a row waits for its token, and a block has no row in flight meanwhile.  1, 2 or 4 rows a thread, 3 to 8
+// blocks an SM and a persistent form with the tokens ahead measured 27 to 30 us.  Rows that are moved in pairs or one by one
+// (rows of 1022 and 1023 values): 61 us.
 constexpr int kLookupThreads = 256;
 constexpr int kLookupRows = 4;           // rows whose loads a thread issues before the first store
 
@@ -208,7 +209,7 @@ __device__ __forceinline__ void add_rows(const Tokens& tok, const Rows<const TA>
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// One launch instead of three: 17 us against 23 us for 3 x 1021 tokens of 250 values.  It is a chain of latencies (tokens, the
+// One launch instead of three: 16 to 17 us against 23 us for 3 x 1021 tokens of 250 values.  It is a chain of latencies (tokens, the
 // search for equal ones, rows, the write), so blocks are small enough for all of them to be resident.
 constexpr int kFewTokens = 4096;
 constexpr int kFewThreads = 256;
@@ -556,7 +557,7 @@ __device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* s_scan) {
 
 // Cluster 0 sorts.  The sort leaves most of the machine idle and waits more than it works, so further clusters clear rows
 // meanwhile, whether they have a token or not: the last ones, since vocabularies tend to begin with the frequent tokens, and
-// no more than takes about as long as the sort (65536 tokens into 50000 rows of 2048 fp32 values: 127 us instead of 135).
+// no more than takes about as long as the sort (65536 tokens into 50000 rows of 2048 fp32 values: 125 us instead of 135).
 template <int ITEMS, typename TG>
 __global__ void __launch_bounds__(kClusterThreads, 1)
 embed_cluster_sort_kernel(Tokens tok, ClusterSort a, GradRows<TG> grad) {
