@@ -155,6 +155,8 @@ class Embedding(_Bound):
         tables, acts = [t for t in (table, d_table) if t is not None], [t for t in (out, d_out) if t is not None]
         if not tables or (table is None) != (out is None) or (d_table is None) != (d_out is None):
             _fail("Embedding: table and out, or d_out and d_table, or all four")
+        if any(t.dim() not in (2, 3) for t in tables):
+            _fail("Embedding: tables of [P, V, D] or [V, D]")
         device = _same_device(tokens, *tables, *acts)
         stream = _stream(stream, device)
         P, T = tok.shape

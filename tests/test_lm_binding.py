@@ -214,3 +214,11 @@ def test_a_state_is_given_whole(lm, devices, monkeypatch):
         opt = lm.AdamW([x], [x], **kw)
         assert opt.m is kw["m"] and opt.v is kw["v"]
         opt.h = None
+
+
+def test_tables_of_one_dimension(lm, devices):
+    tok, row = torch.zeros(4, dtype=torch.int64), torch.zeros(8)
+    for kw in (dict(table=row, out=torch.zeros(4, 8)), dict(d_table=row, d_out=torch.zeros(4, 8))):
+        with pytest.raises(lm.api.LsgdError) as e:
+            lm.Embedding(tok, **kw)
+        assert e.value.status == lm.api.ERR_INVALID_ARG
