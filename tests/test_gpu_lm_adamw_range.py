@@ -1,4 +1,5 @@
-"""GPU check of the AdamW step at the ends of its range: moments of very different sizes in one block."""
+"""GPU check of the AdamW step at the ends of its range: moments of very different sizes in one block, tiny and infinite ones, and an
+eps that does not hide them."""
 import pytest
 import torch
 
