@@ -573,6 +573,93 @@ LSGD_API lsgd_status lsgd_adamw_get_step(lsgd_adamw_handle h, int64_t* n);
 LSGD_API lsgd_status lsgd_adamw_set_step(lsgd_adamw_handle h, int64_t n);
 LSGD_API lsgd_status lsgd_adamw_destroy(lsgd_adamw_handle h);   /* NULL is accepted                              */
 
+/* ---- Sequences -----------------------------------------------------------------------------------------
+ * The operators below run along the sequences that a worker's T rows hold one behind another.  starts: DEVICE int32, S + 1
+ * ascending rows a worker (sequence i is the rows starts[i] .. starts[i + 1] - 1; it may be empty; the last entry is the end of
+ * all), `stride` apart (0: all workers have the same).  Rows in front of the first and behind the last sequence are neither read
+ * nor written.  NULL: S equal parts of the T rows (T % S == 0).  Entries outside [0, T] act as the nearest of the two; where
+ * they descend, results are undefined (no access leaves the buffers).                                     */
+typedef struct {
+  const int32_t* starts;
+  int64_t stride;
+  int32_t S;                 /* >= 1                                                                         */
+} lsgd_sequences;
+
+/* ---- Causal convolution -----------------------------------------------------------------------------------
+ * pre[p][t][d] = bias[p][d] + sum_j w[p][d][j] x[p][t - W + 1 + j][d],  out = act(pre), act the identity or pre sigmoid(pre),
+ * over the rows of t's own sequence; in front of its first row the inputs are the state's (oldest first) or, without one, zeros.
+ *   forward    out; state, where given, is replaced by the last W - 1 inputs of its sequence (an empty one keeps its state).
+ *   backward   for sequences without a state (it is refused):  d = d_out act'(pre),  dx[t] = sum_k w[W - 1 - k] d[t + k],
+ *              dw[d][j] = sum_t d[t] x[t - W + 1 + j],  d_bias[d] = sum_t d[t]
+ * with all arithmetic in fp32 and each output rounded once.  x, out, d_out, dx: P x T rows of D values of act_dtype; outputs
+ * overlap no input.  w, dw: P x D rows of W values, fp32; bias, d_bias: P rows of D values, fp32.  dw and d_bias with a
+ * worker stride of 0 are summed over the workers.  accumulate: they are added to what their buffers hold.
+ * The backward pass, and both passes of sequences given by starts, need scratch (lsgd_conv_scratch_bytes(d, backward),
+ * 256-byte aligned), whose contents are not kept between calls; so calls that share it are ordered by the caller.    */
+typedef enum {
+  LSGD_CONV_IDENTITY = 0,
+  LSGD_CONV_SILU = 1
+} lsgd_conv_act;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_conv_desc)                                                       */
+  int32_t P;                 /* >= 1                                                                          */
+  int64_t T;                 /* >= 0, P * T < 2^31 - 4096                                                     */
+  int32_t D, W;              /* D in [1, 65536], W in [1, 4]                                                  */
+  int32_t act_dtype;         /* lsgd_dtype                                                                    */
+  int32_t act;               /* lsgd_conv_act                                                                 */
+  int32_t accumulate;
+  lsgd_sequences seq;
+  lsgd_rows x, w, bias;      /* bias may be absent (data NULL)                                                */
+  lsgd_rows out;             /* forward                                                                       */
+  void* state;               /* forward, may be NULL: DEVICE act_dtype [P][S][W - 1][D], contiguous             */
+  lsgd_rows d_out, dx, dw, d_bias; /* backward                                                                */
+  void* scratch;
+  uint64_t scratch_bytes;
+} lsgd_conv_desc;
+LSGD_API uint64_t lsgd_conv_scratch_bytes(const lsgd_conv_desc* desc, int32_t backward);
+LSGD_API lsgd_status lsgd_conv_forward(const lsgd_conv_desc* desc, void* stream);
+LSGD_API lsgd_status lsgd_conv_backward(const lsgd_conv_desc* desc, void* stream);
+
+/* ---- Selective state space scan -----------------------------------------------------------------------------
+ * Every channel d has N states, which its time step delta moves:
+ *   delta[t] = softplus(dt[t][d] + dt_bias[d]),   A[n] = -exp(a_log[d][n]),
+ *   h[t][n]  = exp(delta[t] A[n]) h[t - 1][n] + delta[t] x[t][d] b[t][n],
+ *   y[t]     = sum_n c[t][n] h[t][n] + skip[d] x[t][d],       out[t][d] = y[t] z sigmoid(z),  z = z[t][d]  (without z: y)
+ * with h[-1] of a sequence from `state`, or zero without one.
+ *   forward    out; state, where given, is replaced by its sequence's last h (an empty one keeps its state); saved, where
+ *              given (for the backward pass): the states in front of every 8th row, fp32 [P][ceil(T / 8)][D][N].
+ *   backward   for sequences without a state (it is refused), from the saved states of the forward pass of the same inputs:
+ *              d = d_out z sigmoid(z),  g[t] = d[t] c[t] + exp(delta[t + 1] A) g[t + 1],  q[t] = exp(delta[t] A) g[t] h[t - 1],
+ *              dx = delta sum_n g b + skip d,   d_delta = x sum_n g b + sum_n q A,   d_dt = d_delta sigmoid(dt + dt_bias),
+ *              db[t][n] = sum_d g delta x,   dc[t][n] = sum_d d h,   dz = d_out y (z sigmoid(z))',
+ *              d_a_log[d][n] = A sum_t q delta,   d_skip[d] = sum_t d x,   d_dt_bias[d] = sum_t d_dt
+ * with states, sums and arithmetic in fp32 and each output rounded once.  x, dt, z, out and their gradients: P x T rows of D
+ * values; b, c and theirs: P x T rows of N values; all of act_dtype.  a_log, d_a_log: P x D rows of N values, fp32; skip, dt_bias
+ * and theirs: P rows of D values, fp32; with a worker stride of 0 these gradients are summed over the workers.  accumulate: they
+ * are added to what their buffers hold.  Outputs overlap no input.  z, skip and dt_bias may be absent, and their gradients
+ * are given with them.  Rows of one token each (S = T equal sequences) take a form of their own, as a loop of single tokens does.
+ * Scratch: lsgd_scan_scratch_bytes(d, backward), which may be 0, 256-byte aligned; as for the convolution.           */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_scan_desc)                                                       */
+  int32_t P;                 /* >= 1                                                                          */
+  int64_t T;                 /* >= 0, P * T < 2^31 - 4096                                                     */
+  int32_t D, N;              /* D in [1, 65536], N in [1, 64]                                                  */
+  int32_t act_dtype;         /* lsgd_dtype                                                                    */
+  int32_t accumulate;
+  lsgd_sequences seq;
+  lsgd_rows x, dt, b, c, z;
+  lsgd_rows a_log, skip, dt_bias;
+  lsgd_rows out;             /* forward                                                                       */
+  float* state;              /* forward, may be NULL: DEVICE [P][S][D][N], 16-byte aligned                      */
+  float* saved;              /* written by forward (may be NULL), read by backward; 16-byte aligned             */
+  lsgd_rows d_out, dx, d_dt, db, dc, dz, d_a_log, d_skip, d_dt_bias; /* backward                               */
+  void* scratch;
+  uint64_t scratch_bytes;
+} lsgd_scan_desc;
+LSGD_API uint64_t lsgd_scan_scratch_bytes(const lsgd_scan_desc* desc, int32_t backward);
+LSGD_API lsgd_status lsgd_scan_forward(const lsgd_scan_desc* desc, void* stream);
+LSGD_API lsgd_status lsgd_scan_backward(const lsgd_scan_desc* desc, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -64,6 +64,8 @@ F32, BF16 = range(2)
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN = range(3)
 GATE_IDENTITY, GATE_SIGMOID, GATE_TANH = range(3)
 STATE_F32, STATE_8BIT = range(2)
+CONV_IDENTITY, CONV_SILU = range(2)      # lsgd_conv_act
+SAVED_EVERY = 8                          # rows between the scan's saved states
 
 
 class Rows(C.Structure):
@@ -94,6 +96,26 @@ class AdamwDesc(C.Structure):
                 ("state_dtype", C.c_int32), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("seed", C.c_uint32), ("stream", C.c_void_p)]
+
+
+class Sequences(C.Structure):
+    _fields_ = [("starts", C.c_void_p), ("stride", C.c_int64), ("S", C.c_int32)]
+
+
+class ConvDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("T", C.c_int64), ("D", C.c_int32), ("W", C.c_int32),
+                ("act_dtype", C.c_int32), ("act", C.c_int32), ("accumulate", C.c_int32), ("seq", Sequences), ("x", Rows),
+                ("w", Rows), ("bias", Rows), ("out", Rows), ("state", C.c_void_p), ("d_out", Rows), ("dx", Rows), ("dw", Rows),
+                ("d_bias", Rows), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
+class ScanDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("T", C.c_int64), ("D", C.c_int32), ("N", C.c_int32),
+                ("act_dtype", C.c_int32), ("accumulate", C.c_int32), ("seq", Sequences), ("x", Rows), ("dt", Rows), ("b", Rows),
+                ("c", Rows), ("z", Rows), ("a_log", Rows), ("skip", Rows), ("dt_bias", Rows), ("out", Rows),
+                ("state", C.c_void_p), ("saved", C.c_void_p), ("d_out", Rows), ("dx", Rows), ("d_dt", Rows), ("db", Rows),
+                ("dc", Rows), ("dz", Rows), ("d_a_log", Rows), ("d_skip", Rows), ("d_dt_bias", Rows), ("scratch", C.c_void_p),
+                ("scratch_bytes", C.c_uint64)]
 
 
 class Config(C.Structure):
@@ -166,6 +188,12 @@ def lib() -> C.CDLL:
         for name, desc in (("embed", EmbedDesc), ("blocknorm", BlocknormDesc)):
             f = getattr(L, f"lsgd_{name}_scratch_bytes")
             f.argtypes, f.restype = [C.POINTER(desc)], C.c_uint64
+            for direction in ("forward", "backward"):
+                f = getattr(L, f"lsgd_{name}_{direction}")
+                f.argtypes, f.restype = [C.POINTER(desc), C.c_void_p], C.c_int
+        for name, desc in (("conv", ConvDesc), ("scan", ScanDesc)):
+            f = getattr(L, f"lsgd_{name}_scratch_bytes")
+            f.argtypes, f.restype = [C.POINTER(desc), C.c_int32], C.c_uint64
             for direction in ("forward", "backward"):
                 f = getattr(L, f"lsgd_{name}_{direction}")
                 f.argtypes, f.restype = [C.POINTER(desc), C.c_void_p], C.c_int

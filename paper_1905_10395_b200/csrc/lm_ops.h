@@ -80,6 +80,14 @@ struct Pack<float, 8> {      // 32 bytes in one instruction: two of 16 would tou
   }
 };
 template <>
+struct Pack<float, 4> {
+  float4 a;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = a; }
+  __device__ __forceinline__ void get(float* f) const { f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; }
+  __device__ __forceinline__ void set(const float* f) { a = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <>
 struct Pack<float, 2> {
   float2 a;
   __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float2*>(p); }
@@ -113,6 +121,14 @@ struct Pack<__nv_bfloat16, 8> {
   __device__ __forceinline__ void set(const float* f) {
     a = make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
   }
+};
+template <>
+struct Pack<__nv_bfloat16, 4> {
+  uint2 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint2*>(p) = a; }
+  __device__ __forceinline__ void get(float* f) const { f[0] = bf16_lo(a.x); f[1] = bf16_hi(a.x); f[2] = bf16_lo(a.y); f[3] = bf16_hi(a.y); }
+  __device__ __forceinline__ void set(const float* f) { a = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3])); }
 };
 template <>
 struct Pack<__nv_bfloat16, 2> {

@@ -1,0 +1,249 @@
+// Host side of the selective state space scan, and the passes over its chains; the mathematics and the kernels are in scan.h.
+#include "scan.h"
+
+namespace lsgd {
+namespace scan {
+namespace {
+
+// What a chain starts from: a thread takes one state of a channel through the chains of its worker.
+template <bool REVERSE>
+__global__ void __launch_bounds__(256) chain_kernel(const __grid_constant__ Args a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t n = (int64_t)a.d.D * a.d.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int p = blockIdx.y;
+  if (i >= n) return;
+  const int ch = (int)(i / a.d.N), st = (int)(i % a.d.N);
+  const float A2 = -expf(static_cast<const float*>(a.d.a_log.data)[p * a.d.a_log.stride + ch * a.d.a_log.ld + st]) * kLog2e;
+  float* ends = a.ends + (int64_t)p * a.chains * n + i;
+  const float* sums = a.sums + (int64_t)p * a.chains * a.d.D + ch;
+  float carry = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < a.chains; ++k) {
+    const int c = REVERSE ? a.chains - 1 - k : k;
+    const float e = ends[c * n], s = sums[(int64_t)c * a.d.D];
+    ends[c * n] = carry;
+    carry = s < 0.f ? e : fmaf(ex2(s * A2), carry, e);
+  }
+}
+
+// Gradients of a_log, skip and dt_bias: the chains' sums in order (of all workers where they share the vector).  Columns of a
+// worker: D x N of a_log, D of skip, D of dt_bias.
+__global__ void __launch_bounds__(256) join_params_kernel(const __grid_constant__ Args a) {
+  pdl_wait();
+  const int64_t n = (int64_t)a.d.D * a.d.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n + 2 * a.d.D) return;
+  const int which = i < n ? 0 : i < n + a.d.D ? 1 : 2;
+  const lsgd_rows& o = which == 0 ? a.d.d_a_log : which == 1 ? a.d.d_skip : a.d.d_dt_bias;
+  const bool shared = a.d.P > 1 && o.stride == 0;
+  if (!o.data || (shared && blockIdx.y > 0)) return;
+  const int64_t width = which == 0 ? n : 2 * a.d.D;
+  const float* src = (which == 0 ? a.part_a + i : a.part_v + (i - n));
+  float total = 0.f;
+  const int p0 = shared ? 0 : blockIdx.y, p1 = shared ? a.d.P : p0 + 1;
+  for (int p = p0; p < p1; ++p) {
+    const float* s = src + (int64_t)p * a.chains * width;
+#pragma unroll 8
+    for (int c = 0; c < a.chains; ++c) total += s[c * width];
+  }
+  const int64_t col = which == 0 ? i / a.d.N * o.ld + i % a.d.N : i - n - (which == 1 ? 0 : a.d.D);
+  float* dst = static_cast<float*>(o.data) + (shared ? 0 : blockIdx.y * o.stride) + col;
+  *dst = a.d.accumulate ? *dst + total : total;
+}
+
+// ------------------------------------------------------------------------------------------------ host
+lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
+  if (!d || d->struct_size != sizeof(lsgd_scan_desc)) return LSGD_ERR_INVALID_ARG;
+  if (d->P < 1 || d->T < 0 || d->D < 1 || d->N < 1) return LSGD_ERR_INVALID_ARG;
+  if (d->act_dtype < LSGD_F32 || d->act_dtype > LSGD_BF16) return LSGD_ERR_INVALID_ARG;
+  if (d->D > 65536 || d->N > 64 || d->P > 65535) return LSGD_ERR_UNSUPPORTED;
+  if (d->T >= kMaxRows / d->P) return LSGD_ERR_TOO_LARGE;
+  lsgd_status st;
+  if ((st = check_sequences(d->seq, d->P, d->T)) != LSGD_OK) return st;
+  if ((int64_t)d->seq.S * d->P >= int64_t(1) << 31) return LSGD_ERR_TOO_LARGE;
+  const int64_t P = d->P, T = d->T, D = d->D, N = d->N;
+  const int ab = elem_bytes(d->act_dtype);
+  const bool rows = T > 0;
+  if (!d->a_log.data || (rows && (!d->x.data || !d->dt.data || !d->b.data || !d->c.data))) return LSGD_ERR_INVALID_ARG;
+#define LSGD_ROWS(r, t, w, bytes, written, shared)                                                 \
+  do {                                                                                            \
+    if ((r).data && (st = check_rows(r, P, t, w, bytes, written, shared)) != LSGD_OK) return st;  \
+  } while (0)
+  LSGD_ROWS(d->x, T, D, ab, false, false);
+  LSGD_ROWS(d->dt, T, D, ab, false, false);
+  LSGD_ROWS(d->z, T, D, ab, false, false);
+  LSGD_ROWS(d->b, T, N, ab, false, false);
+  LSGD_ROWS(d->c, T, N, ab, false, false);
+  LSGD_ROWS(d->a_log, D, N, 4, false, false);
+  LSGD_ROWS(d->skip, 1, D, 4, false, false);
+  LSGD_ROWS(d->dt_bias, 1, D, 4, false, false);
+  if ((reinterpret_cast<uintptr_t>(d->state) | reinterpret_cast<uintptr_t>(d->saved)) % 16) return LSGD_ERR_ALIGNMENT;
+  if (!backward) {
+    const void* o = d->out.data;
+    if (rows && (!o || o == d->x.data || o == d->dt.data || o == d->z.data || o == d->b.data || o == d->c.data)) return LSGD_ERR_INVALID_ARG;
+    LSGD_ROWS(d->out, T, D, ab, true, false);
+    return LSGD_OK;
+  }
+  if (d->state || (rows && (!d->saved || !d->d_out.data || !d->dx.data || !d->d_dt.data || !d->db.data || !d->dc.data))) return LSGD_ERR_INVALID_ARG;
+  if (!d->d_a_log.data) return LSGD_ERR_INVALID_ARG;
+  if ((rows && (d->z.data != nullptr) != (d->dz.data != nullptr)) || (d->skip.data != nullptr) != (d->d_skip.data != nullptr) ||
+      (d->dt_bias.data != nullptr) != (d->d_dt_bias.data != nullptr))
+    return LSGD_ERR_INVALID_ARG;
+  const void* ins[] = {d->x.data, d->dt.data, d->z.data, d->b.data, d->c.data, d->d_out.data};
+  const void* outs[] = {d->dx.data, d->d_dt.data, d->dz.data, d->db.data, d->dc.data};
+  for (int i = 0; i < 5; ++i) {
+    for (const void* in : ins)
+      if (outs[i] && outs[i] == in) return LSGD_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return LSGD_ERR_INVALID_ARG;
+  }
+  LSGD_ROWS(d->d_out, T, D, ab, false, false);
+  LSGD_ROWS(d->dx, T, D, ab, true, false);
+  LSGD_ROWS(d->d_dt, T, D, ab, true, false);
+  LSGD_ROWS(d->dz, T, D, ab, true, false);
+  LSGD_ROWS(d->db, T, N, ab, true, false);
+  LSGD_ROWS(d->dc, T, N, ab, true, false);
+  LSGD_ROWS(d->d_a_log, D, N, 4, true, true);
+  LSGD_ROWS(d->d_skip, 1, D, 4, true, true);
+  LSGD_ROWS(d->d_dt_bias, 1, D, 4, true, true);
+#undef LSGD_ROWS
+  return LSGD_OK;
+}
+
+struct Plan {
+  Launch l;
+  int32_t chains, per, split, wide;
+  uint32_t tiles;
+  uint64_t codes, ends, sums, old_state, part_bc, part_a, part_v, total;   // offsets in the scratch
+};
+
+Plan plan_of(const lsgd_scan_desc* d, bool backward) {
+  Plan m{};
+  const int64_t P = d->P, T = d->T, D = d->D, N = d->N, S = d->seq.S;
+  m.l.L = N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16;
+  const int ch = kThreads / m.l.L, rows = m.l.L == 2 ? 16 : 32;
+  m.tiles = (uint32_t)((D + ch - 1) / ch);
+  const int ab = elem_bytes(d->act_dtype);
+  auto fits = [&](const lsgd_rows& r) { return row_vec(r, P, T, D, ab) == 8; };
+  m.wide = fits(d->x) && fits(d->dt) && fits(d->z) &&
+           (backward ? fits(d->d_out) && fits(d->dx) && fits(d->d_dt) && fits(d->dz) : fits(d->out));
+  const bool equal = !d->seq.starts;
+  m.l.single = !backward && equal && S == T && !d->saved;
+  // Chains: whole sequences where that gives every SM a block; else equal runs of rows, four blocks an SM.
+  const int64_t columns = P * m.tiles, sms = sm_count();
+  int64_t chains;
+  if (columns >= sms) {
+    chains = 1;
+    m.per = (int32_t)S;
+  } else if (equal && columns * S >= sms) {
+    int64_t want = (4 * sms + columns - 1) / columns;
+    if (want > S) want = S;
+    m.per = (int32_t)((S + want - 1) / want);
+    chains = (S + m.per - 1) / m.per;
+  } else {
+    m.split = 1;
+    const int64_t want = (4 * sms + columns - 1) / columns;
+    int64_t per = (T + want - 1) / want;
+    per = (per + rows - 1) / rows * rows;
+    if (per < 2 * rows) per = 2 * rows;
+    if (per > T) per = (T + rows - 1) / rows * rows;
+    m.per = (int32_t)(per < 1 ? 1 : per);
+    chains = T > 0 ? (T + m.per - 1) / m.per : 1;
+    if (chains <= 1) {       // one chain is a run of all sequences
+      chains = 1;
+      m.split = 0;
+      m.per = (int32_t)S;
+    }
+  }
+  m.chains = (int32_t)chains;
+  m.l.grid = dim3(m.tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
+  uint64_t at = codes_bytes(d->seq, P, T);
+  auto take = [&](uint64_t floats) {
+    const uint64_t here = at;
+    at += align256(sizeof(float) * floats);
+    return here;
+  };
+  if (m.split) {
+    m.ends = take((uint64_t)P * chains * D * N);
+    m.sums = take((uint64_t)P * chains * D);
+    if (d->state) m.old_state = take((uint64_t)P * S * D * N);
+  }
+  if (backward) {
+    m.part_bc = take((uint64_t)P * m.tiles * T * 2 * N);
+    m.part_a = take((uint64_t)P * chains * D * N);
+    m.part_v = take((uint64_t)P * chains * 2 * D);
+  }
+  m.total = at;
+  return m;
+}
+
+lsgd_status run_scan(const lsgd_scan_desc* d, bool backward, cudaStream_t s) {
+  const Plan m = plan_of(d, backward);
+  char* scratch = static_cast<char*>(d->scratch);
+  Args a{};
+  a.d = *d;
+  a.q = seq_view(d->seq, d->T, reinterpret_cast<int32_t*>(scratch));
+  a.chains = m.chains;
+  a.per = m.per;
+  a.split = m.split;
+  a.wide = m.wide;
+  a.tiles = m.tiles;
+  auto at = [&](uint64_t offset) { return reinterpret_cast<float*>(scratch + offset); };
+  a.ends = at(m.ends);
+  a.sums = at(m.sums);
+  a.old_state = at(m.old_state);
+  a.part_bc = at(m.part_bc);
+  a.part_a = at(m.part_a);
+  a.part_v = at(m.part_v);
+  cudaError_t e = cudaSuccess;
+  if (d->T > 0) {
+    if (d->seq.starts) e = launch_codes(a.q, reinterpret_cast<int32_t*>(scratch), d->P, s);
+    const bool f32 = d->act_dtype == LSGD_F32;
+    if (e == cudaSuccess)
+      e = backward ? (f32 ? launch_backward_f32(a, m.l, s) : launch_backward_bf16(a, m.l, s))
+                   : (f32 ? launch_forward_f32(a, m.l, s) : launch_forward_bf16(a, m.l, s));
+  }
+  if (e == cudaSuccess && backward) {
+    if (d->T == 0) a.chains = 0;
+    const int64_t cols = (int64_t)d->D * (d->N + 2);
+    e = launch_pdl(join_params_kernel, dim3((unsigned)((cols + 255) / 256), d->P), dim3(256), 0, s, a);
+  }
+  return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
+}
+
+}  // namespace
+
+cudaError_t launch_chain_join(const Args& a, bool reverse, cudaStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)a.d.D * a.d.N + 255) / 256), a.d.P);
+  return reverse ? launch_pdl(chain_kernel<true>, grid, dim3(256), 0, s, a) : launch_pdl(chain_kernel<false>, grid, dim3(256), 0, s, a);
+}
+
+}  // namespace scan
+}  // namespace lsgd
+
+extern "C" {
+
+uint64_t lsgd_scan_scratch_bytes(const lsgd_scan_desc* d, int32_t backward) {
+  using namespace lsgd;
+  using namespace lsgd::scan;
+  if (!d || d->struct_size != sizeof(lsgd_scan_desc) || d->P < 1 || d->T < 0 || d->D < 1 || d->D > 65536 || d->N < 1 || d->N > 64 ||
+      d->seq.S < 1 || d->act_dtype < LSGD_F32 || d->act_dtype > LSGD_BF16 || d->T >= kMaxRows / d->P)
+    return 0;
+  return plan_of(d, backward).total;
+}
+
+#define LSGD_SCAN_CALL(name, backward)                                                            \
+  lsgd_status name(const lsgd_scan_desc* d, void* stream) {                                       \
+    using namespace lsgd;                                                                         \
+    const lsgd_status st = scan::check_scan(d, backward);                                         \
+    if (st != LSGD_OK) return st;                                                                 \
+    const uint64_t need = lsgd_scan_scratch_bytes(d, backward);                                   \
+    if (need && (!d->scratch || d->scratch_bytes < need)) return LSGD_ERR_INVALID_ARG;            \
+    if (need && reinterpret_cast<uintptr_t>(d->scratch) % 256) return LSGD_ERR_ALIGNMENT;         \
+    return scan::run_scan(d, backward, static_cast<cudaStream_t>(stream));                        \
+  }
+LSGD_SCAN_CALL(lsgd_scan_forward, false)
+LSGD_SCAN_CALL(lsgd_scan_backward, true)
+#undef LSGD_SCAN_CALL
+
+}  // extern "C"

@@ -1,0 +1,47 @@
+// Sequences in a worker's rows, for the operators that run along them (conv.cu, scan*.cu): which sequence a row belongs to.
+#pragma once
+#include "lm_ops.h"
+
+namespace lsgd {
+
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;      // of all workers; a tile behind the last row still has a row number
+
+// Sequences given by their starts are looked up once: codes[p][t] is the sequence of row t, -1 in front of the first and behind
+// the last.  A row begins a sequence where its code differs from the row's before it (an empty sequence has no row).  Equal parts
+// need no table.
+struct SeqView {
+  const int32_t* starts;     // NULL: equal parts of `len` rows
+  int64_t stride;
+  const int32_t* codes;      // [P][T], with starts
+  int32_t S, T, len;
+
+  __device__ __forceinline__ int code(int p, int t) const {
+    if ((unsigned)t >= (unsigned)T) return -1;
+    return starts ? codes[(int64_t)p * T + t] : t / len;
+  }
+  __device__ __forceinline__ int edge(int p, int s) const {      // first row of sequence s (s == S: the end of all)
+    if (!starts) return s * len;
+    const int v = starts[p * stride + s];
+    return v < 0 ? 0 : v > T ? T : v;
+  }
+};
+
+inline lsgd_status check_sequences(const lsgd_sequences& q, int64_t P, int64_t T) {
+  if (q.S < 1) return LSGD_ERR_INVALID_ARG;
+  if (!q.starts) return T % q.S == 0 ? LSGD_OK : LSGD_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(q.starts) % 4) return LSGD_ERR_ALIGNMENT;
+  if (q.stride < 0 || (q.stride > 0 && q.stride < q.S + 1 && P > 1)) return LSGD_ERR_INVALID_ARG;
+  if (P > 1 && q.stride > (int64_t(1) << 56) / P) return LSGD_ERR_TOO_LARGE;
+  return LSGD_OK;
+}
+inline SeqView seq_view(const lsgd_sequences& q, int64_t T, const int32_t* codes) {
+  return SeqView{q.starts, q.stride, codes, q.S, (int32_t)T, q.starts ? 0 : (int32_t)(T / q.S)};
+}
+inline uint64_t align256(uint64_t n) { return (n + 255) & ~uint64_t(255); }
+inline uint64_t codes_bytes(const lsgd_sequences& q, int64_t P, int64_t T) {
+  return q.starts ? align256(sizeof(int32_t) * (uint64_t)(P * T)) : 0;
+}
+// Fills the table (conv.cu).
+cudaError_t launch_codes(const SeqView& q, int32_t* codes, int32_t P, cudaStream_t s);
+
+}  // namespace lsgd

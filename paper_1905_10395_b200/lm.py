@@ -99,7 +99,8 @@ def _vector(name: str, t: Optional[torch.Tensor], P: int, D: int) -> api.Rows:
 class _Bound:
     """A descriptor with its stream and what it points to."""
 
-    def _bind(self, name, desc, device, stream, keep, scratch):
+    def _bind(self, name, desc, device, stream, keep, scratch, *passes):
+        """scratch: whether the operator needs any; passes: the directions whose sizes the library is asked for."""
         self.device, self._index, self._keep = device, device.index, [keep]
         self._stream, self._torch_stream = stream.cuda_stream, stream
         self._arg = stream.cuda_stream or None           # as the library gets it (None is passed on faster than 0)
@@ -108,7 +109,8 @@ class _Bound:
         self._name, self.desc, self._ref = name, desc, C.byref(desc)
         if scratch:
             with torch.cuda.device(device):
-                n = int(getattr(L, f"lsgd_{name}_scratch_bytes")(self._ref))
+                size = getattr(L, f"lsgd_{name}_scratch_bytes")
+                n = max((int(size(self._ref, back)) for back in passes), default=0) if passes else int(size(self._ref))
             if n:
                 with torch.cuda.stream(stream):      # the allocator's order of use is the operator's
                     buf = torch.empty(n, dtype=torch.uint8, device=device)
@@ -234,6 +236,148 @@ class BlockNorm(_Bound):
         self.rstd_post, self.rstd_pre = stats["rstd_post"], stats["rstd_pre"]
         keep += list(stats.values())
         self._bind("blocknorm", d, device, stream, keep, dx is not None)
+
+
+def _given_rows(name: str, t: torch.Tensor):
+    """[P, T, D] from a tensor of [P, T, D] or, for one worker, [T, D]."""
+    if t.dim() not in (2, 3):
+        _fail(f"{name}: [P, T, D] or [T, D]")
+    return t if t.dim() == 3 else t.unsqueeze(0)
+
+
+def _sequences(sequences: Optional[int], starts: Optional[torch.Tensor], P: int, T: int, device: torch.device) -> api.Sequences:
+    if starts is None:
+        S = 1 if sequences is None else int(sequences)
+        if S < 1 or T % S:
+            _fail(f"sequences: {S} equal parts of {T} rows")
+        return api.Sequences(None, 0, S)
+    if sequences is not None:
+        _fail("sequences or starts, not both")
+    if starts.dtype != torch.int32:
+        raise api.LsgdError(api.ERR_UNSUPPORTED, f"starts: {starts.dtype}")
+    if starts.device != device:
+        _fail(f"starts: a tensor of {device}, got one of {starts.device}")
+    if starts.dim() not in (1, 2) or starts.shape[-1] < 2 or (starts.dim() == 2 and starts.shape[0] != P) or starts.stride(-1) != 1:
+        _fail("starts: [S + 1] or [P, S + 1], a worker's contiguous")
+    return api.Sequences(starts.data_ptr(), starts.stride(0) if starts.dim() == 2 and P > 1 else 0, starts.shape[-1] - 1)
+
+
+def _table(name: str, t: Optional[torch.Tensor], P: int, rows: int, cols: int) -> api.Rows:
+    """A [P, rows, cols] (or, for one worker, [rows, cols]) fp32 tensor as lsgd_rows."""
+    if t is not None and t.dtype != torch.float32:
+        raise api.LsgdError(api.ERR_UNSUPPORTED, f"{name}: {t.dtype}")
+    return _rows(name, t, (P, rows, cols))
+
+
+def _state(name: str, t: Optional[torch.Tensor], shape, dtype) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise api.LsgdError(api.ERR_UNSUPPORTED, f"{name}: {t.dtype}, expected {dtype}")
+    if t.dim() == len(shape) - 1 and shape[0] == 1:
+        t = t.unsqueeze(0)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _fail(f"{name}: contiguous {tuple(shape)}")
+    return t.data_ptr() or None
+
+
+class CausalConv(_Bound):
+    """out[t] = act(bias + sum_j w[:, j] x[t - W + 1 + j]) along the sequences of every worker's rows, and its gradient.
+
+    x, out, d_out, dx [P, T, D]; w, dw [P, D, W] and bias, d_bias [P, D], fp32 (gradients expanded over the workers are summed
+    over them).  The T rows hold `sequences` sequences of equal length (default 1), or those whose first rows `starts` gives:
+    int32 [S + 1] or [P, S + 1] on the device, ascending, the last entry the end of all; rows outside them are not touched.
+    state [P, S, W - 1, D] of x's type: the inputs in front of every sequence, replaced by its last ones (forward only).
+    act "silu" or "identity".  accumulate: dw and d_bias are added to."""
+
+    def __init__(self, x: torch.Tensor, w: torch.Tensor, *, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 state: Optional[torch.Tensor] = None, d_out: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                 dw: Optional[torch.Tensor] = None, d_bias: Optional[torch.Tensor] = None, sequences: Optional[int] = None,
+                 starts: Optional[torch.Tensor] = None, act: str = "silu", accumulate: bool = False, stream=None):
+        if act not in ("silu", "identity"):
+            _fail("act: silu or identity")
+        device = _same_device(x, w, bias, out, state, d_out, dx, dw, d_bias)
+        stream = _stream(stream, device)
+        P, T, D = _given_rows("x", x).shape
+        grads = any(t is not None for t in (d_out, dx, dw, d_bias))
+        if grads and (d_out is None or dx is None or dw is None or (bias is None) != (d_bias is None)):
+            _fail("CausalConv: the backward pass needs d_out, dx, dw and, with a bias, d_bias")
+        if grads and state is not None:
+            _fail("CausalConv: no gradient through a state")
+        if out is None and not grads:
+            _fail("CausalConv: out, or the tensors of the backward pass, or both")
+        d = api.ConvDesc()
+        d.struct_size = C.sizeof(api.ConvDesc)
+        d.P, d.T, d.D, d.W = P, T, D, w.shape[-1]
+        d.act_dtype = _dtype("x", x, out, d_out, dx)
+        d.act, d.accumulate = (api.CONV_SILU if act == "silu" else api.CONV_IDENTITY), int(accumulate)
+        d.seq = _sequences(sequences, starts, P, T, device)
+        for name, t in (("x", x), ("out", out), ("d_out", d_out), ("dx", dx)):
+            setattr(d, name, _rows(name, t, (P, T, D)))
+        d.w, d.dw = _table("w", w, P, D, d.W), _table("dw", dw, P, D, d.W)
+        d.bias, d.d_bias = _vector("bias", bias, P, D), _vector("d_bias", d_bias, P, D)
+        d.state = _state("state", state, (P, d.seq.S, d.W - 1, D), x.dtype)
+        passes = ([0] if out is not None else []) + ([1] if grads else [])
+        self._bind("conv", d, device, stream, (x, w, bias, out, state, d_out, dx, dw, d_bias, starts), True, *passes)
+
+
+class SelectiveScan(_Bound):
+    """h[t] = exp(delta A) h[t - 1] + delta x[t] b[t],  y[t] = c[t] . h[t] + skip x[t],  out = y silu(z), with N states a channel,
+    delta = softplus(dt + dt_bias) and A = -exp(a_log), along the sequences of every worker's rows; and its gradient.
+
+    x, dt, z, out and their gradients [P, T, D]; b, c, d_b, d_c [P, T, N], all of one type; a_log, d_a_log [P, D, N] and skip,
+    dt_bias and theirs [P, D], fp32 (gradients expanded over the workers are summed over them).  z, skip and dt_bias may be
+    absent.  sequences / starts as for CausalConv.  state [P, S, D, N] fp32: what every sequence starts from, replaced by what it
+    ends with (forward only; zeros without it).  saved [P, ceil(T / 8), D, N] fp32, written by forward and read by backward
+    (allocated when not given).  accumulate: d_a_log, d_skip and d_dt_bias are added to."""
+
+    def __init__(self, x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, b: torch.Tensor, c: torch.Tensor, *,
+                 z: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
+                 d_out: Optional[torch.Tensor] = None, d_x: Optional[torch.Tensor] = None, d_dt: Optional[torch.Tensor] = None,
+                 d_a_log: Optional[torch.Tensor] = None, d_b: Optional[torch.Tensor] = None, d_c: Optional[torch.Tensor] = None,
+                 d_z: Optional[torch.Tensor] = None, d_skip: Optional[torch.Tensor] = None,
+                 d_dt_bias: Optional[torch.Tensor] = None, sequences: Optional[int] = None, starts: Optional[torch.Tensor] = None,
+                 accumulate: bool = False, stream=None):
+        keep = [x, dt, a_log, b, c, z, skip, dt_bias, out, state, saved, d_out, d_x, d_dt, d_a_log, d_b, d_c, d_z, d_skip, d_dt_bias]
+        device = _same_device(*keep)
+        stream = _stream(stream, device)
+        P, T, D = _given_rows("x", x).shape
+        N = a_log.shape[-1]
+        grads = any(t is not None for t in (d_out, d_x, d_dt, d_a_log, d_b, d_c, d_z, d_skip, d_dt_bias))
+        if grads:
+            if any(t is None for t in (d_out, d_x, d_dt, d_a_log, d_b, d_c)):
+                _fail("SelectiveScan: the backward pass needs d_out, d_x, d_dt, d_a_log, d_b and d_c")
+            for name, t, g in (("z", z, d_z), ("skip", skip, d_skip), ("dt_bias", dt_bias, d_dt_bias)):
+                if (t is None) != (g is None):
+                    _fail(f"SelectiveScan: {name} and its gradient are given together")
+            if state is not None:
+                _fail("SelectiveScan: no gradient through a state")
+        if out is None and not grads:
+            _fail("SelectiveScan: out, or the tensors of the backward pass, or both")
+        d = api.ScanDesc()
+        d.struct_size = C.sizeof(api.ScanDesc)
+        d.P, d.T, d.D, d.N = P, T, D, N
+        d.act_dtype = _dtype("x", x, dt, b, c, z, out, d_out, d_x, d_dt, d_b, d_c, d_z)
+        d.accumulate = int(accumulate)
+        d.seq = _sequences(sequences, starts, P, T, device)
+        for name, field, t in (("x", "x", x), ("dt", "dt", dt), ("z", "z", z), ("out", "out", out), ("d_out", "d_out", d_out),
+                               ("d_x", "dx", d_x), ("d_dt", "d_dt", d_dt), ("d_z", "dz", d_z)):
+            setattr(d, field, _rows(name, t, (P, T, D)))
+        for name, field, t in (("b", "b", b), ("c", "c", c), ("d_b", "db", d_b), ("d_c", "dc", d_c)):
+            setattr(d, field, _rows(name, t, (P, T, N)))
+        d.a_log, d.d_a_log = _table("a_log", a_log, P, D, N), _table("d_a_log", d_a_log, P, D, N)
+        for name, t in (("skip", skip), ("dt_bias", dt_bias), ("d_skip", d_skip), ("d_dt_bias", d_dt_bias)):
+            setattr(d, name, _vector(name, t, P, D))
+        d.state = _state("state", state, (P, d.seq.S, D, N), torch.float32)
+        shape = (P, (T + api.SAVED_EVERY - 1) // api.SAVED_EVERY, D, N)
+        if saved is None and grads:
+            with torch.cuda.stream(stream):
+                saved = torch.empty(shape, dtype=torch.float32, device=device)
+        d.saved = _state("saved", saved, shape, torch.float32)
+        self.saved = saved
+        passes = ([0] if out is not None else []) + ([1] if grads else [])
+        self._bind("scan", d, device, stream, (*keep, saved, starts), True, *passes)
 
 
 class AdamW:
