@@ -660,6 +660,37 @@ LSGD_API uint64_t lsgd_scan_scratch_bytes(const lsgd_scan_desc* desc, int32_t ba
 LSGD_API lsgd_status lsgd_scan_forward(const lsgd_scan_desc* desc, void* stream);
 LSGD_API lsgd_status lsgd_scan_backward(const lsgd_scan_desc* desc, void* stream);
 
+/* ---- Orthogonalised updates -------------------------------------------------------------------------------
+ * For every worker's m x n matrix: U = grad, or with a momentum  M <- mu M + grad,  U = M (nesterov: grad + mu M);
+ *   X = U / (|U| + eps), |U| the root of the sum of squares;   `steps` times  X <- a X + (b G + c G G) X,  G = X X^T
+ * (of X^T where m > n: the smaller side's products);   out = scale X.  Each step maps every singular value v to
+ * a v + b v^3 + c v^5; with the usual (3.4445, -4.7750, 2.0315) five steps bring all that are not tiny to about one.
+ * The products' operands are fp16 with a power-of-two scale (11 significant bits; X, G and the polynomial are bounded by about 4,
+ * which bf16's wider range would only pay for with three bits less), sums are fp32.  grad: P x m rows of n values
+ * of grad_dtype; momentum: the same in fp32, updated in place; out: P x m rows of n values, bf16.  A zero matrix gives zeros; one with a
+ * value that is not finite gives NaN.  Coefficients that let singular values pass 16 are out of range: the result is then not
+ * finite, or saturated.  Scratch: lsgd_ortho_scratch_bytes(d), 256-byte aligned; as for the convolution.         */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(lsgd_ortho_desc)                                                      */
+  int32_t P;                 /* [1, 65535]                                                                    */
+  int32_t m, n;              /* [1, 65536], m n < 2^31                                                        */
+  int32_t grad_dtype;        /* lsgd_dtype                                                                    */
+  int32_t steps;             /* [0, 32]                                                                       */
+  int32_t nesterov;          /* with momentum                                                                 */
+  float a, b, c;             /* |.| <= 16                                                                     */
+  float mu;                  /* [0, 1)                                                                        */
+  float eps;                 /* >= 0                                                                          */
+  float scale;               /* of out                                                                        */
+  lsgd_rows grad, momentum, out; /* momentum may be absent                                                    */
+  void* scratch;
+  uint64_t scratch_bytes;
+} lsgd_ortho_desc;
+LSGD_API uint64_t lsgd_ortho_scratch_bytes(const lsgd_ortho_desc* desc);
+LSGD_API lsgd_status lsgd_ortho(const lsgd_ortho_desc* desc, void* stream);
+/* Synchronises the current device, then reads and clears the status word of lsgd_ortho on it (its products' bounded waits record
+ * LSGD_DEVFLAG_WAIT_TIMEOUT there): LSGD_ERR_DEVICE_FLAG if it was set.                                         */
+LSGD_API lsgd_status lsgd_ortho_check_device(uint32_t* flag_out /* HOST, may be NULL */);
+
 #ifdef __cplusplus
 }
 #endif

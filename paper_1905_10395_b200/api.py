@@ -118,6 +118,13 @@ class ScanDesc(C.Structure):
                 ("scratch_bytes", C.c_uint64)]
 
 
+class OrthoDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("m", C.c_int32), ("n", C.c_int32), ("grad_dtype", C.c_int32),
+                ("steps", C.c_int32), ("nesterov", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float),
+                ("mu", C.c_float), ("eps", C.c_float), ("scale", C.c_float), ("grad", Rows), ("momentum", Rows), ("out", Rows),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
 class Config(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("P", C.c_int32), ("G", C.c_int32), ("group_of", C.c_void_p),
                 ("d", C.c_int64), ("ld", C.c_int64), ("eta", C.c_float), ("lambda_l", C.c_float),
@@ -197,6 +204,9 @@ def lib() -> C.CDLL:
             for direction in ("forward", "backward"):
                 f = getattr(L, f"lsgd_{name}_{direction}")
                 f.argtypes, f.restype = [C.POINTER(desc), C.c_void_p], C.c_int
+        L.lsgd_ortho_scratch_bytes.argtypes, L.lsgd_ortho_scratch_bytes.restype = [C.POINTER(OrthoDesc)], C.c_uint64
+        L.lsgd_ortho.argtypes, L.lsgd_ortho.restype = [C.POINTER(OrthoDesc), C.c_void_p], C.c_int
+        L.lsgd_ortho_check_device.argtypes, L.lsgd_ortho_check_device.restype = [C.POINTER(C.c_uint32)], C.c_int
         L.lsgd_embed_check_device.argtypes = [C.POINTER(C.c_uint32)]
         L.lsgd_embed_check_device.restype = C.c_int
         L.lsgd_adamw_state_values.argtypes = [C.c_int32, C.c_void_p]

@@ -1,0 +1,573 @@
+// Orthogonalised updates (include/lsgd.h): momentum and norm, then Newton-Schulz steps on the 5th-generation tensor cores.
+//
+//   G = X X^T,   Q = b G + c G G,   X <- a X + Q X        (X is the smaller side by the larger: rows r <= columns)
+//
+// Three batched products a step, with the sums of the polynomial in their epilogues.  G and Q are symmetric: only tiles on and
+// above the diagonal are computed, each stored twice, the second time transposed, so a step costs 3 r r n + r r r
+// multiply-adds instead of 4 r r n + 2 r r r.
+//
+// Operands are fp16 times 2^10, sums fp32.  Entries of X and G are below 2 (singular values stay below 1.3 with the usual
+// coefficients) and those that matter are not below 2^-13 of their matrix's largest, so fp16's range holds them and its 11 bits
+// leave a third of the error that bf16's 8 would: the whole chain loses about what the last rounding to bf16 does.
+//
+// product_kernel is a persistent kernel of one CTA an SM on 128 x 128 tiles with three roles, as the batched product of gemm_tc.cu:
+// one thread fetches operands (and the tile that is added) by tiled bulk copies into a ring, one issues tcgen05.mma into one of
+// two accumulators in tensor memory, eight warps run the epilogue.  Every wait is bounded by a clock budget; on expiry the kernel
+// raises a status bit, drains its copies, frees tensor memory and returns.
+#include <cuda_fp16.h>
+
+#include "seq.h"
+#include "tc.h"
+
+namespace lsgd {
+namespace ortho {
+using namespace tc;
+namespace {
+
+__device__ uint32_t g_status;                    // of the device
+
+constexpr float kScale = 1024.f;                 // of X, G and Q as stored
+constexpr int BM = 128, BN = 128, BK = 64, kStages = 5;
+constexpr int kBoxBytes = 64 * 64 * 2, kStageBytes = (BM + BN) * BK * 2, kTileBytes = BM * BN * 2;
+constexpr int kSmemBytes = kStages * kStageBytes + 2 * kTileBytes + 1024;
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+
+// ------------------------------------------------------------------------------------------------ momentum and norm
+struct Prep {
+  lsgd_ortho_desc d;
+  double* part;              // [P][blocks] sums of squares
+  uint32_t blocks;
+  __half* x;                 // [P][r][ld]
+  int32_t r, n, tall;        // rows and columns of X; tall: X is the matrix transposed
+  int64_t ld, stride;
+};
+
+template <typename T, int VEC>
+__device__ __forceinline__ void update_of(const Prep& a, int p, int row, int col, bool write, float (&u)[VEC]) {
+  Pack<T, VEC> g;
+  g.load(Rows<T>{static_cast<T*>(a.d.grad.data), a.d.grad.ld, a.d.grad.stride}.row(p, row) + col);
+  g.get(u);
+  if (!a.d.momentum.data) return;
+  float* at = Rows<float>{static_cast<float*>(a.d.momentum.data), a.d.momentum.ld, a.d.momentum.stride}.row(p, row) + col;
+  Pack<float, VEC> k;
+  float m[VEC];
+  k.load(at);
+  k.get(m);
+  if (write) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) m[v] = fmaf(a.d.mu, m[v], u[v]);
+    k.set(m);
+    k.store(at);
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) u[v] = a.d.nesterov ? fmaf(a.d.mu, m[v], u[v]) : m[v];
+}
+
+// The momentum's step, and every block's sum of squares of the update: in 64 bits, since squares of small gradients leave fp32's range.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prep a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int p = blockIdx.y;
+  const uint32_t per = (a.d.n + VEC - 1) / VEC;
+  const int64_t pieces = (int64_t)a.d.m * per;
+  double s = 0.0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+    const int row = (int)((uint32_t)i / per), col = (int)((uint32_t)i % per) * VEC;
+    float u[VEC];
+    update_of<T, VEC>(a, p, row, col, true, u);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) s = fma((double)u[v], (double)u[v], s);
+  }
+  __shared__ double warps[8];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double t = 0.0;
+    for (int w = 0; w < 8; ++w) t += warps[w];
+    a.part[(int64_t)p * a.blocks + blockIdx.x] = t;
+  }
+}
+
+// 1 / (|U| + eps); 0 for a zero matrix, NaN where a value is not finite.
+__device__ __forceinline__ float inverse_norm(const Prep& a, int p) {
+  __shared__ float s;
+  if (threadIdx.x < 32) {
+    const double t = sqrt(warp_sum_fixed(a.part + (int64_t)p * a.blocks, a.blocks)) + (double)a.d.eps;
+    if (threadIdx.x == 0) s = t > 0.0 && t < 1e300 ? (float)fmin(1.0 / t, 3e38) : t == 0.0 ? 0.f : __int_as_float(0x7FC00000);
+  }
+  __syncthreads();
+  return s;
+}
+
+// X as fp16, transposed where the matrix is tall: tiles of 64 x 64 through shared memory.  Without steps: out itself.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int p = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;       // of the matrix as given
+  const float inv = inverse_norm(a, p);
+  __shared__ float tile[64][65];
+  for (int i = threadIdx.x; i < 64 * (64 / VEC); i += 256) {
+    const int row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
+    float u[VEC] = {};
+    if (r0 + row < a.d.m && c0 + col < a.d.n) update_of<T, VEC>(a, p, r0 + row, c0 + col, false, u);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) tile[row][col + v] = u[v] * inv;
+  }
+  __syncthreads();
+  if (a.d.steps == 0) {
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.d.out.data) + p * a.d.out.stride;
+    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
+      const int row = i / 64, col = i % 64;
+      if (r0 + row < a.d.m && c0 + col < a.d.n) out[(r0 + row) * a.d.out.ld + c0 + col] = __float2bfloat16_rn(a.d.scale * tile[row][col]);
+    }
+    return;
+  }
+  __half* x = a.x + p * a.stride;
+  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+    const int row = i / 8, col = i % 8 * 8;                                  // of X within its tile
+    const int xr = (a.tall ? c0 : r0) + row, xc = (a.tall ? r0 : c0) + col;
+    if (xr >= a.r || xc >= a.ld) continue;
+    uint4 w;
+    __half2* h = reinterpret_cast<__half2*>(&w);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float f0 = a.tall ? tile[col + 2 * v][row] : tile[row][col + 2 * v];
+      const float f1 = a.tall ? tile[col + 2 * v + 1][row] : tile[row][col + 2 * v + 1];
+      h[v] = __floats2half2_rn(f0 * kScale, f1 * kScale);
+    }
+    *reinterpret_cast<uint4*>(x + xr * a.ld + xc) = w;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ products
+struct Product {
+  int M, N, K, batch;
+  int b_mn;                  // B is stored [K][N] (else [N][K])
+  int symmetric;             // square: tiles on and above the diagonal, stored twice
+  int add;                   // C = alpha acc + beta D
+  float alpha, beta;
+  __nv_bfloat16* out;        // last product: bf16 rows instead of C, times scale
+  int64_t out_ld, out_stride;
+  int out_transposed, out_wide;
+  float scale;
+};
+
+struct Tile {
+  int z, m0, n0;
+};
+// Tile number t: all of a row of tiles, or those from the diagonal on.
+__device__ __forceinline__ Tile tile_of(const Product& p, int t, int mt, int nt, int per) {
+  Tile q;
+  q.z = t / per;
+  t -= q.z * per;
+  int i = 0;
+  if (p.symmetric) {
+    while (t >= nt - i) t -= nt - i++;
+    q.m0 = i * BM;
+    q.n0 = (i + t) * BN;
+  } else {
+    q.m0 = t / nt * BM;
+    q.n0 = t % nt * BN;
+  }
+  return q;
+}
+
+__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); }
+
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+  __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ Product p) {
+  constexpr uint32_t kTmemCols = 2 * BN;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* buf = smem + kStages * kStageBytes;   // the tile: D in, C out; two boxes of [128][64]
+  uint8_t* mirror = buf + kTileBytes;            // C transposed
+  __shared__ uint64_t full_bar[kStages], empty_bar[kStages], acc_full[2], acc_empty[2], in_full, in_free;
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int mt = (p.M + BM - 1) / BM, nt = (p.N + BN - 1) / BN, per = p.symmetric ? nt * (nt + 1) / 2 : mt * nt;
+  const int n_tiles = per * p.batch, nk = (p.K + BK - 1) / BK;
+  uint32_t* status = &g_status;
+  if (threadIdx.x == 0) {
+    abort_s = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full_bar[s], 1);
+      mbar_init(&empty_bar[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], kEpiWarps);
+    }
+    mbar_init(&in_full, 1);
+    mbar_init(&in_free, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_c) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_d) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = tmem_base_s;
+  volatile int* abort_flag = &abort_s;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == 0 && lane == 0) {
+    // ---------------------------------------------------------------- producer
+    uint32_t it = 0;
+    int local = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++local) {
+      const Tile q = tile_of(p, t, mt, nt, per);
+      for (int kt = 0; kt < nk; ++kt, ++it) {
+        const int s = it % kStages;
+        ok = mbar_wait(&empty_bar[s], ((it / kStages) & 1) ^ 1, abort_flag, status);
+        if (!ok) break;
+        uint8_t* sa = smem + s * kStageBytes;
+        uint8_t* sb = sa + BM * BK * 2;
+        mbar_expect_tx(&full_bar[s], kStageBytes);
+        const int k0 = kt * BK;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          tma_load_3d(sa + j * kBoxBytes, &map_a, &full_bar[s], k0, q.m0 + 64 * j, q.z);
+          if (p.b_mn) tma_load_3d(sb + j * kBoxBytes, &map_b, &full_bar[s], q.n0 + 64 * j, k0, q.z);
+          else tma_load_3d(sb + j * kBoxBytes, &map_b, &full_bar[s], k0, q.n0 + 64 * j, q.z);
+        }
+      }
+      if (ok && p.add) {
+        ok = mbar_wait(&in_free, (local & 1) ^ 1, abort_flag, status);
+        if (!ok) break;
+        mbar_expect_tx(&in_full, kTileBytes);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) tma_load_3d(buf + j * 2 * kBoxBytes, &map_d, &in_full, q.n0 + 64 * j, q.m0, q.z);
+      }
+    }
+    if (!ok) {       // copies in flight land before the CTA leaves (bounded again: an aborted wait returns at its first failure)
+      const long long t0 = clock64();
+      for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
+        while (!mbar_try(&full_bar[j % kStages], (j / kStages) & 1) && clock64() - t0 < kWaitBudgetCycles / 4) {
+        }
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---------------------------------------------------------------- products
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(p.b_mn ? 1 : 0) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+    uint32_t it = 0;
+    int local = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++local) {
+      const int b = local & 1;
+      ok = mbar_wait(&acc_empty[b], ((local >> 1) & 1) ^ 1, abort_flag, status);
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t tacc = tmem_base + (uint32_t)(b * BN);
+      for (int kt = 0; kt < nk; ++kt, ++it) {
+        const int s = it % kStages;
+        ok = mbar_wait(&full_bar[s], (it / kStages) & 1, abort_flag, status);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t sa = smem_u32(smem + s * kStageBytes), sb = sa + BM * BK * 2;
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) {
+          const uint64_t da = smem_desc(sa + k * 32, 16, 1024);
+          const uint64_t db = p.b_mn ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024);
+          mma_bf16(tacc, da, db, idesc, (kt | k) != 0 ? 1u : 0u);
+        }
+        mma_commit(&empty_bar[s]);
+      }
+      if (ok) mma_commit(&acc_full[b]);
+    }
+  } else if (warp >= 2) {
+    // ---------------------------------------------------------------- epilogue
+    const int q4 = warp & 3, part = (warp - 2) >> 2, row = q4 * 32 + lane;
+    const bool leader = threadIdx.x == 64;
+    int local = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++local) {
+      const Tile q = tile_of(p, t, mt, nt, per);
+      const int b = local & 1;
+      ok = mbar_wait(&acc_full[b], (local >> 1) & 1, abort_flag, status);
+      if (ok && p.add) ok = mbar_wait(&in_full, local & 1, abort_flag, status);
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t tacc = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * BN);
+      const bool twice = p.symmetric && q.m0 != q.n0;
+#pragma unroll 1
+      for (int c = 2 * part; c < 2 * part + 2; ++c) {
+        if (q.n0 + c * 32 >= p.N) break;
+        uint32_t r[32];
+        tmem_ld32(tacc + (uint32_t)(c * 32), r);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        uint8_t* box = buf + (c >> 1) * 2 * kBoxBytes;
+        const int u0 = (c & 1) * 4;
+        float v[32];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (p.add) w = *reinterpret_cast<const uint4*>(box + swz(row, u0 + u));
+          const __half2* h = reinterpret_cast<const __half2*>(&w);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = __half22float2(h[j]);
+            v[8 * u + 2 * j] = fmaf(p.alpha, __uint_as_float(r[8 * u + 2 * j]), p.beta * f.x);
+            v[8 * u + 2 * j + 1] = fmaf(p.alpha, __uint_as_float(r[8 * u + 2 * j + 1]), p.beta * f.y);
+          }
+        }
+        if (p.out) {
+          const int gr = q.m0 + row, gc = q.n0 + c * 32;
+          if (gr < p.M) {
+            __nv_bfloat16* o = p.out + q.z * p.out_stride;
+            if (p.out_transposed) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (gc + j < p.N) o[(gc + j) * p.out_ld + gr] = __float2bfloat16_rn(v[j] * p.scale);
+            } else if (p.out_wide) {
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                if (gc + 8 * u < p.N) {
+                  float f[8];
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) f[j] = v[8 * u + j] * p.scale;
+                  Pack<__nv_bfloat16, 8> k;
+                  k.set(f);
+                  k.store(o + gr * p.out_ld + gc + 8 * u);
+                }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (gc + j < p.N) o[gr * p.out_ld + gc + j] = __float2bfloat16_rn(v[j] * p.scale);
+            }
+          }
+          continue;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<uint4*>(box + swz(row, u0 + u)) =
+              make_uint4(half_pair(v[8 * u], v[8 * u + 1]), half_pair(v[8 * u + 2], v[8 * u + 3]),
+                         half_pair(v[8 * u + 4], v[8 * u + 5]), half_pair(v[8 * u + 6], v[8 * u + 7]));
+        if (twice) {
+          uint8_t* mbox = mirror + (row >> 6) * 2 * kBoxBytes;
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            *reinterpret_cast<__half*>(mbox + swz(c * 32 + j, (row & 63) >> 3) + (row & 7) * 2) = __float2half_rn(v[j]);
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[b]);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      epi_barrier();
+      if (leader) {
+        if (!p.out) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (q.n0 + 64 * j < p.N) tma_store_3d(buf + j * 2 * kBoxBytes, &map_c, q.n0 + 64 * j, q.m0, q.z);
+          if (twice) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              if (q.m0 + 64 * j < p.M) tma_store_3d(mirror + j * 2 * kBoxBytes, &map_c, q.m0 + 64 * j, q.n0, q.z);
+          }
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+        if (p.add) mbar_arrive(&in_free);
+      }
+      epi_barrier();
+    }
+    if (leader) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+lsgd_status check_ortho(const lsgd_ortho_desc* d) {
+  if (!d || d->struct_size != sizeof(lsgd_ortho_desc)) return LSGD_ERR_INVALID_ARG;
+  if (d->P < 1 || d->m < 1 || d->n < 1 || d->steps < 0) return LSGD_ERR_INVALID_ARG;
+  if (d->P > 65535 || d->m > 65536 || d->n > 65536 || d->steps > 32) return LSGD_ERR_UNSUPPORTED;
+  if ((int64_t)d->m * d->n >= int64_t(1) << 31) return LSGD_ERR_TOO_LARGE;
+  if (d->grad_dtype < LSGD_F32 || d->grad_dtype > LSGD_BF16) return LSGD_ERR_INVALID_ARG;
+  if (!(fabsf(d->a) <= 16.f) || !(fabsf(d->b) <= 16.f) || !(fabsf(d->c) <= 16.f)) return LSGD_ERR_INVALID_ARG;
+  if (!(d->mu >= 0.f && d->mu < 1.f) || !(d->eps >= 0.f && d->eps < 1e30f) || !(d->scale - d->scale == 0.f)) return LSGD_ERR_INVALID_ARG;
+  if (!d->grad.data || !d->out.data || d->out.data == d->grad.data || d->momentum.data == d->grad.data || d->out.data == d->momentum.data)
+    return LSGD_ERR_INVALID_ARG;
+  lsgd_status st;
+  if ((st = check_rows(d->grad, d->P, d->m, d->n, elem_bytes(d->grad_dtype), false)) != LSGD_OK) return st;
+  if (d->momentum.data && (st = check_rows(d->momentum, d->P, d->m, d->n, 4, true)) != LSGD_OK) return st;
+  return check_rows(d->out, d->P, d->m, d->n, 2, true);
+}
+
+struct Plan {
+  int r, n;                  // rows and columns of X
+  int64_t ldx, ldg;
+  uint32_t blocks;
+  uint64_t part, x0, x1, g, q, total;
+};
+Plan plan_of(const lsgd_ortho_desc* d) {
+  Plan m{};
+  m.r = d->m < d->n ? d->m : d->n;
+  m.n = d->m < d->n ? d->n : d->m;
+  m.ldx = (m.n + 7) / 8 * 8;
+  m.ldg = (m.r + 7) / 8 * 8;
+  const int64_t want = ((int64_t)d->m * d->n + 4095) / 4096, cap = (4 * (int64_t)sm_count() + d->P - 1) / d->P;
+  m.blocks = (uint32_t)(want < cap ? want : cap);
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 255) & ~uint64_t(255);
+    return here;
+  };
+  m.part = take(sizeof(double) * (uint64_t)d->P * m.blocks);
+  if (d->steps > 0) {
+    const uint64_t x = 2 * (uint64_t)d->P * m.r * m.ldx, g = 2 * (uint64_t)d->P * m.r * m.ldg;
+    m.x0 = take(x);
+    if (d->steps > 1) m.x1 = take(x);
+    m.g = take(g);
+    m.q = take(g);
+  }
+  m.total = at;
+  return m;
+}
+
+bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int64_t P) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, 64);
+}
+bool tile_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int64_t P) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, 128);
+}
+
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, cudaStream_t s) {
+  static OncePerDevice attr;
+  if (!attr.here()) {
+    const cudaError_t e = cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    attr.here() = true;
+  }
+  const int64_t mt = (p.M + BM - 1) / BM, nt = (p.N + BN - 1) / BN, tiles = (p.symmetric ? nt * (nt + 1) / 2 : mt * nt) * p.batch;
+  if (tiles >= int64_t(1) << 31) return cudaErrorInvalidValue;
+  const unsigned grid = (unsigned)(tiles < sm_count() ? tiles : sm_count());
+  return launch_pdl(product_kernel, dim3(grid), dim3(kThreads), kSmemBytes, s, a, b, c, d, p);
+}
+
+template <typename T>
+cudaError_t launch_prep(const Prep& a, int vec, cudaStream_t s) {
+  const dim3 norm(a.blocks, a.d.P), tiles((a.d.n + 63) / 64, (a.d.m + 63) / 64, a.d.P);
+  cudaError_t e = vec == 4 ? launch_pdl(norm_kernel<T, 4>, norm, dim3(256), 0, s, a) : launch_pdl(norm_kernel<T, 1>, norm, dim3(256), 0, s, a);
+  if (e != cudaSuccess) return e;
+  return vec == 4 ? launch_pdl(scale_kernel<T, 4>, tiles, dim3(256), 0, s, a) : launch_pdl(scale_kernel<T, 1>, tiles, dim3(256), 0, s, a);
+}
+
+lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
+  const Plan m = plan_of(d);
+  char* scratch = static_cast<char*>(d->scratch);
+  Prep a{};
+  a.d = *d;
+  a.part = reinterpret_cast<double*>(scratch + m.part);
+  a.blocks = m.blocks;
+  a.x = reinterpret_cast<__half*>(scratch + m.x0);
+  a.r = m.r;
+  a.n = m.n;
+  a.tall = d->m > d->n;
+  a.ld = m.ldx;
+  a.stride = m.ldx * m.r;
+  const int gb = elem_bytes(d->grad_dtype);
+  auto fits = [&](const lsgd_rows& r, int bytes) {
+    return !r.data || (d->n % 4 == 0 && reinterpret_cast<uintptr_t>(r.data) % (4 * bytes) == 0 && (d->m <= 1 || r.ld % 4 == 0) && (d->P <= 1 || r.stride % 4 == 0));
+  };
+  const int vec = fits(d->grad, gb) && fits(d->momentum, 4) ? 4 : 1;
+  cudaError_t e = d->grad_dtype == LSGD_BF16 ? launch_prep<__nv_bfloat16>(a, vec, s) : launch_prep<float>(a, vec, s);
+  if (e != cudaSuccess) return LSGD_ERR_CUDA;
+  void* x[2] = {scratch + m.x0, scratch + m.x1};
+  void *g = scratch + m.g, *q = scratch + m.q;
+  const float down = 1.f / kScale;
+  for (int step = 0; step < d->steps; ++step) {
+    const void* from = x[step & 1];
+    void* to = x[(step & 1) ^ 1];
+    const bool last = step + 1 == d->steps;
+    CUtensorMap x_op, g_op, q_op, g_tile, q_tile, x_tile, to_tile;
+    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
+        !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) ||
+        !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P) || !tile_map(&x_tile, from, m.n, m.r, m.ldx, d->P) ||
+        !tile_map(&to_tile, last ? from : to, m.n, m.r, m.ldx, d->P))
+      return LSGD_ERR_CUDA;
+    Product p{};
+    p.batch = d->P;
+    p.M = p.N = m.r;
+    p.K = m.n;
+    p.symmetric = 1;
+    p.alpha = down;
+    if (launch_product(x_op, x_op, g_tile, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    p.K = m.r;
+    p.add = 1;
+    p.alpha = d->c * down;
+    p.beta = d->b;
+    if (launch_product(g_op, g_op, q_tile, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    p.N = m.n;
+    p.symmetric = 0;
+    p.b_mn = 1;
+    p.alpha = down;
+    p.beta = d->a;
+    if (last) {
+      p.out = static_cast<__nv_bfloat16*>(d->out.data);
+      p.out_ld = d->out.ld;
+      p.out_stride = d->out.stride;
+      p.out_transposed = a.tall;
+      p.out_wide = row_vec(d->out, d->P, d->m, d->n, 2) == 8;
+      p.scale = d->scale * down;
+    }
+    if (launch_product(q_op, x_op, to_tile, x_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+  }
+  return LSGD_OK;
+}
+
+}  // namespace
+}  // namespace ortho
+}  // namespace lsgd
+
+extern "C" {
+
+uint64_t lsgd_ortho_scratch_bytes(const lsgd_ortho_desc* d) {
+  using namespace lsgd::ortho;
+  if (!d || d->struct_size != sizeof(lsgd_ortho_desc) || d->P < 1 || d->P > 65535 || d->m < 1 || d->m > 65536 || d->n < 1 || d->n > 65536 || d->steps < 0) return 0;
+  return plan_of(d).total;
+}
+
+lsgd_status lsgd_ortho(const lsgd_ortho_desc* d, void* stream) {
+  using namespace lsgd::ortho;
+  const lsgd_status st = check_ortho(d);
+  if (st != LSGD_OK) return st;
+  const uint64_t need = lsgd_ortho_scratch_bytes(d);
+  if (need && (!d->scratch || d->scratch_bytes < need)) return LSGD_ERR_INVALID_ARG;
+  if (need && reinterpret_cast<uintptr_t>(d->scratch) % 256) return LSGD_ERR_ALIGNMENT;
+  return run_ortho(d, static_cast<cudaStream_t>(stream));
+}
+
+lsgd_status lsgd_ortho_check_device(uint32_t* flag_out) {
+  uint32_t f = 0;
+  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&f, lsgd::ortho::g_status, sizeof(f)) != cudaSuccess) return LSGD_ERR_CUDA;
+  const uint32_t zero = 0;
+  if (f && cudaMemcpyToSymbol(lsgd::ortho::g_status, &zero, sizeof(zero)) != cudaSuccess) return LSGD_ERR_CUDA;
+  if (flag_out) *flag_out = f;
+  return f ? LSGD_ERR_DEVICE_FLAG : LSGD_OK;
+}
+
+}  // extern "C"

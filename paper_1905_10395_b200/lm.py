@@ -380,6 +380,55 @@ class SelectiveScan(_Bound):
         self._bind("scan", d, device, stream, (*keep, saved, starts), True, *passes)
 
 
+class Orthogonalize:
+    """out = scale X, X the update of every worker's m x n matrix brought near an orthogonal one by Newton-Schulz products:
+    X = U / (|U| + eps), then `steps` times X <- a X + (b G + c G G) X with G = X X^T.
+
+    grad [P, m, n] (or [m, n]) fp32 or bf16; out the same in bf16.  momentum, fp32: M <- mu M + grad, in place, and U = M, or
+    grad + mu M with nesterov; without it U = grad.  The products run on fp16 operands with a power-of-two scale: a result is within
+    about 2^-9 of its matrix's norm of the exact one, as its rounding to bf16 is."""
+
+    def __init__(self, grad: torch.Tensor, out: torch.Tensor, *, momentum: Optional[torch.Tensor] = None, mu: float = 0.95,
+                 nesterov: bool = True, steps: int = 5, coefficients: Sequence[float] = (3.4445, -4.7750, 2.0315),
+                 scale: float = 1.0, eps: float = 1e-7, stream=None):
+        device = _same_device(grad, out, momentum)
+        stream = _stream(stream, device)
+        P, m, n = _given_rows("grad", grad).shape
+        if out.dtype != torch.bfloat16:
+            raise api.LsgdError(api.ERR_UNSUPPORTED, f"out: {out.dtype}")
+        if len(coefficients) != 3:
+            _fail("coefficients: a, b, c")
+        d = api.OrthoDesc()
+        d.struct_size = C.sizeof(api.OrthoDesc)
+        d.P, d.m, d.n, d.steps, d.nesterov = P, m, n, int(steps), int(nesterov)
+        d.grad_dtype = _dtype("grad", grad)
+        d.a, d.b, d.c = (float(v) for v in coefficients)
+        d.mu, d.eps, d.scale = float(mu), float(eps), float(scale)
+        d.grad, d.out = _rows("grad", grad, (P, m, n)), _rows("out", out, (P, m, n))
+        d.momentum = _table("momentum", momentum, P, m, n)
+        L = api.lib()
+        self.device, self._index, self._keep = device, device.index, [grad, out, momentum]
+        self._stream, self._torch_stream = stream.cuda_stream, stream
+        self._arg = stream.cuda_stream or None
+        self.desc, self._ref, self._call = d, C.byref(d), L.lsgd_ortho
+        with torch.cuda.device(device):
+            size = int(L.lsgd_ortho_scratch_bytes(self._ref))
+        if size:
+            with torch.cuda.stream(stream):          # the allocator's order of use is the operator's
+                buf = torch.empty(size, dtype=torch.uint8, device=device)
+            d.scratch, d.scratch_bytes = buf.data_ptr(), size
+            self._keep.append(buf)
+
+    def forward(self) -> None:
+        if _current_device() != self._index:
+            raise api.LsgdError(api.ERR_STATE, f"lsgd_ortho: device {_current_device()} is current, the tensors are on {self.device}")
+        if _current_stream(self._index) != self._stream:
+            _not_left_out(self._torch_stream, "lsgd_ortho")
+        s = self._call(self._ref, self._arg)
+        if s:
+            raise api.LsgdError(s, "lsgd_ortho")
+
+
 class AdamW:
     """One AdamW step over many tensors, in one launch.  params fp32, grads fp32 or bf16 (all of one type), each of them
     contiguous; copies: bf16 copies of the parameters (entries may be None), rewritten by every step.
