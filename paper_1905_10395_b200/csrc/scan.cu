@@ -18,12 +18,23 @@ __global__ void __launch_bounds__(256) chain_kernel(const __grid_constant__ Args
   float* ends = a.ends + (int64_t)p * a.chains * n + i;
   const float* sums = a.sums + (int64_t)p * a.chains * a.d.D + ch;
   float carry = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < a.chains; ++k) {
-    const int c = REVERSE ? a.chains - 1 - k : k;
-    const float e = ends[c * n], s = sums[(int64_t)c * a.d.D];
-    ends[c * n] = carry;
-    carry = s < 0.f ? e : fmaf(ex2(s * A2), carry, e);
+  constexpr int kTake = 16;                      // chains fetched before the first is used
+  for (int k0 = 0; k0 < a.chains; k0 += kTake) {
+    float e[kTake], s[kTake];
+#pragma unroll
+    for (int k = 0; k < kTake; ++k) {
+      if (k0 + k >= a.chains) break;
+      const int c = REVERSE ? a.chains - 1 - k0 - k : k0 + k;
+      e[k] = ends[c * n];
+      s[k] = sums[(int64_t)c * a.d.D];
+    }
+#pragma unroll
+    for (int k = 0; k < kTake; ++k) {
+      if (k0 + k >= a.chains) break;
+      const int c = REVERSE ? a.chains - 1 - k0 - k : k0 + k;
+      ends[c * n] = carry;
+      carry = s[k] < 0.f ? e[k] : fmaf(ex2(s[k] * A2), carry, e[k]);
+    }
   }
 }
 
@@ -110,9 +121,13 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   return LSGD_OK;
 }
 
+bool row_vec4(const lsgd_rows& r, int64_t P, int64_t T, int bytes) {
+  return reinterpret_cast<uintptr_t>(r.data) % (4 * bytes) == 0 && (T <= 1 || r.ld % 4 == 0) && (P <= 1 || r.stride % 4 == 0);
+}
+
 struct Plan {
   Launch l;
-  int32_t chains, per, split, wide;
+  int32_t chains, per, split, wide, wide_bc;
   uint32_t tiles;
   uint64_t codes, ends, sums, old_state, part_bc, part_a, part_v, total;   // offsets in the scratch
 };
@@ -121,8 +136,9 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
   Plan m{};
   const int64_t P = d->P, T = d->T, D = d->D, N = d->N, S = d->seq.S;
   m.l.L = N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16;
-  const int ch = kThreads / m.l.L, rows = m.l.L == 2 ? 16 : 32;
-  m.tiles = (uint32_t)((D + ch - 1) / ch);
+  const int ch = kThreads / m.l.L, rows = 32;              // channels of a block with one a thread; a chain's rows are a multiple of any tile's
+  const uint32_t tiles = (uint32_t)((D + ch - 1) / ch);
+  m.tiles = (uint32_t)((D + 2 * ch - 1) / (2 * ch));
   const int ab = elem_bytes(d->act_dtype);
   auto fits = [&](const lsgd_rows& r) { return row_vec(r, P, T, D, ab) == 8; };
   m.wide = fits(d->x) && fits(d->dt) && fits(d->z) &&
@@ -130,6 +146,7 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
   const bool equal = !d->seq.starts;
   m.l.single = !backward && equal && S == T && !d->saved;
   // Chains: whole sequences where that gives every SM a block; else equal runs of rows, four blocks an SM.
+  m.wide_bc = N % 4 == 0 && row_vec4(d->b, P, T, ab) && row_vec4(d->c, P, T, ab);
   const int64_t columns = P * m.tiles, sms = sm_count();
   int64_t chains;
   if (columns >= sms) {
@@ -156,7 +173,8 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
     }
   }
   m.chains = (int32_t)chains;
-  m.l.grid = dim3(m.tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
+  m.l.back = dim3(m.tiles, (unsigned)chains, (unsigned)P);
+  m.l.grid = dim3(tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
   uint64_t at = codes_bytes(d->seq, P, T);
   auto take = [&](uint64_t floats) {
     const uint64_t here = at;
@@ -187,6 +205,7 @@ lsgd_status run_scan(const lsgd_scan_desc* d, bool backward, cudaStream_t s) {
   a.per = m.per;
   a.split = m.split;
   a.wide = m.wide;
+  a.wide_bc = m.wide_bc;
   a.tiles = m.tiles;
   auto at = [&](uint64_t offset) { return reinterpret_cast<float*>(scratch + offset); };
   a.ends = at(m.ends);
