@@ -136,9 +136,8 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
   Plan m{};
   const int64_t P = d->P, T = d->T, D = d->D, N = d->N, S = d->seq.S;
   m.l.L = N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16;
-  const int ch = kThreads / m.l.L, rows = 32;              // channels of a block with one a thread; a chain's rows are a multiple of any tile's
-  const uint32_t tiles = (uint32_t)((D + ch - 1) / ch);
-  m.tiles = (uint32_t)((D + 2 * ch - 1) / (2 * ch));
+  const int ch = kThreads / m.l.L, rows = 32;              // channels of a block; a chain's rows are a multiple of any tile's
+  m.tiles = (uint32_t)((D + ch - 1) / ch);
   const int ab = elem_bytes(d->act_dtype);
   auto fits = [&](const lsgd_rows& r) { return row_vec(r, P, T, D, ab) == 8; };
   m.wide = fits(d->x) && fits(d->dt) && fits(d->z) &&
@@ -173,8 +172,7 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
     }
   }
   m.chains = (int32_t)chains;
-  m.l.back = dim3(m.tiles, (unsigned)chains, (unsigned)P);
-  m.l.grid = dim3(tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
+  m.l.grid = dim3(m.tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
   uint64_t at = codes_bytes(d->seq, P, T);
   auto take = [&](uint64_t floats) {
     const uint64_t here = at;

@@ -19,8 +19,8 @@
 // Gradient.  The forward pass saves the state in front of every 8th row.  A chain goes backwards in groups of 8 rows: it recomputes
 // the group's states from the saved one, keeps them and the decays in registers, and runs the adjoint
 //   g_t = d_t C_t + a_(t+1) g_(t+1)
-// back through them.  dB and dC are sums over channels: over a thread's two, over the warp's by exchanges that halve the number of
-// values at each step, over the warps in shared memory, over the blocks by a second kernel; all in a fixed order.
+// back through them.  dB and dC are sums over channels: over a warp's by exchanges that halve the number of values at
+// each step, over the warps in shared memory, over the blocks by a second kernel; all in a fixed order.
 #pragma once
 #include <type_traits>
 
@@ -30,9 +30,9 @@ namespace lsgd {
 namespace scan {
 
 constexpr int kThreads = 128, kQuad = 4, kGroup = 8;
-// CH channels of a block, rows of a tile; at most one piece of 8 channels of a row a thread.
-template <int L, int KD> struct Tile {
-  static constexpr int kCh = KD * kThreads / L;
+// Channels of a block, rows of a tile; at most one piece of 8 channels of a row a thread.
+template <int L> struct Tile {
+  static constexpr int kCh = kThreads / L;
   static constexpr int kFull = kThreads * 8 / kCh;                 // rows that give every thread a piece
   static constexpr int kRows = kFull > 32 ? 32 : kFull;
   static constexpr int kN = kQuad * L;                             // states, padded
@@ -70,18 +70,37 @@ __device__ __forceinline__ float ex2(float v) {
   return r;
 }
 __device__ __forceinline__ float2 ex2(float2 v) { return make_float2(ex2(v.x), ex2(v.y)); }
-// softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) <= 1; log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by its series.
-__device__ __forceinline__ float softplus(float v, float& e) {
-  e = ex2(-kLog2e * fabsf(v));
-  const float s = __fdividef(e, 2.f + e), s2 = s * s;
-  float r = fmaf(s2, 1.f / 13, 1.f / 11);
-  r = fmaf(s2, r, 1.f / 9);
-  r = fmaf(s2, r, 1.f / 7);
-  r = fmaf(s2, r, 1.f / 5);
-  r = fmaf(s2, r, 1.f / 3);
-  return fmaxf(v, 0.f) + 2.f * fmaf(s * s2, r, s);
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+// 1 / v of a v in [1, 2^126]
+__device__ __forceinline__ float rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
 }
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + ex2(-kLog2e * v)); }
+__device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
+// softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) <= 1; log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, with a polynomial in s^2
+// for artanh(s) / s (interpolation at Chebyshev's points; within 2e-8).
+__device__ __forceinline__ float2 softplus(float2 v, float2& e) {
+  e = ex2(mul2(make_float2(fabsf(v.x), fabsf(v.y)), both(-kLog2e)));
+  const float2 s = mul2(e, rcp(add2(e, both(2.f)))), s2 = mul2(s, s);
+  float2 r = fma2(s2, both(0.13433775f), both(0.14116978f));
+  r = fma2(s2, r, both(0.20003835f));
+  r = fma2(s2, r, both(0.3333332f));
+  r = fma2(mul2(s, s2), r, s);
+  return fma2(r, both(2.f), make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+__device__ __forceinline__ float softplus(float v, float& e) {
+  float2 e2;
+  const float r = softplus(both(v), e2).x;
+  e = e2.x;
+  return r;
+}
+// sigmoid(v); exp(-v) is held below 2^126, where the reciprocal ends
+__device__ __forceinline__ float2 sigmoid(float2 v) {
+  const float2 u = mul2(v, both(-kLog2e));
+  return rcp(add2(ex2(make_float2(fminf(u.x, 126.f), fminf(u.y, 126.f))), both(1.f)));
+}
+__device__ __forceinline__ float sigmoid(float v) { return sigmoid(both(v)).x; }
 
 // 8 neighbouring channels of a row; those behind the last are zeros.
 template <typename T>
@@ -101,6 +120,10 @@ __device__ __forceinline__ void load8(Pack<T, 8>& k, const T* row, int ch, int D
     }
   }
   k.set(f);
+}
+__device__ __forceinline__ void pairs8(const float (&f)[8], float2 (&q)[4]) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) q[v] = make_float2(f[2 * v], f[2 * v + 1]);
 }
 template <typename T>
 __device__ __forceinline__ void store8(const float (&f)[8], T* row, int ch, int D, bool wide) {
@@ -127,6 +150,11 @@ __device__ __forceinline__ void decay_rates(const Args& a, int p, int ch, int n0
     if (ch < a.d.D && n0 + k < a.d.N)
       A2[k] = -expf(static_cast<const float*>(a.d.a_log.data)[p * a.d.a_log.stride + ch * a.d.a_log.ld + n0 + k]) * kLog2e;
   }
+}
+__device__ __forceinline__ void load_vector8(const lsgd_rows& v, int p, int ch, int D, float2 (&f)[4]) {
+  const float* src = static_cast<const float*>(v.data) + p * v.stride + ch;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) f[k] = make_float2(v.data && ch + 2 * k < D ? src[2 * k] : 0.f, v.data && ch + 2 * k + 1 < D ? src[2 * k + 1] : 0.f);
 }
 __device__ __forceinline__ float vector_at(const lsgd_rows& v, int p, int ch, bool in) {
   return in && v.data ? static_cast<const float*>(v.data)[p * v.stride + ch] : 0.f;
@@ -156,6 +184,7 @@ __device__ __forceinline__ void store_states(float* base, int64_t row, int n0, i
 
 struct Range {
   int t0, t1, base;          // rows of the chain; base: t0 rounded down to a group
+  int lo = 0, hi = 0;        // equal parts: the sequence that was asked for last
   __device__ __forceinline__ Range(const Args& a, int p, int c) {
     if (a.split) {
       t0 = min(a.q.T, c * a.per);
@@ -167,11 +196,18 @@ struct Range {
     }
     base = t0 & ~(kGroup - 1);
   }
-  // Whether rows [base, base + rows) are the chain's and one sequence's, which neither begins nor ends among them.
-  __device__ __forceinline__ bool plain(const Args& a, int p, int base_, int rows) const {
-    if (base_ < t0 || base_ + rows > t1) return false;
-    const int code = a.q.code(p, base_ - 1);
-    return code >= 0 && code == a.q.code(p, base_ + rows);
+  // Whether rows [at, at + rows) are the chain's and one sequence's, which neither begins nor ends among them.
+  __device__ __forceinline__ bool plain(const Args& a, int p, int at, int rows) {
+    if (at < t0 || at + rows > t1) return false;
+    if (a.q.starts) {
+      const int code = a.q.code(p, at - 1);
+      return code >= 0 && code == a.q.code(p, at + rows);
+    }
+    if (at < lo || at >= hi) {
+      lo = at / a.q.len * a.q.len;
+      hi = lo + a.q.len;
+    }
+    return at > lo && at + rows < hi;
   }
 };
 __device__ __forceinline__ bool row_lives(const Args& a, int p, const Range& r, int t) {
@@ -214,11 +250,11 @@ __device__ __forceinline__ int row_of(int lane) { return 2 * (lane & 1) + ((lane
 template <int L, typename Ti>
 __device__ __forceinline__ void keep_sums(float (&y)[4], float* array, int ch, int t, int lane) {
   sum_states<L>(y, lane);
+  float* at = array + Ti::at(ch, t);               // the four rows lie together
   if (L == 2) {
-    array[Ti::at(ch, t + 2 * (lane & 1))] = y[0];
-    array[Ti::at(ch, t + 2 * (lane & 1) + 1)] = y[1];
+    *reinterpret_cast<float2*>(at + 2 * (lane & 1)) = make_float2(y[0], y[1]);
   } else if (lane % L < 4) {
-    array[Ti::at(ch, t + row_of(lane))] = y[0];
+    at[row_of(lane)] = y[0];
   }
 }
 
@@ -226,14 +262,25 @@ __device__ __forceinline__ void keep_sums(float (&y)[4], float* array, int ch, i
 template <typename T, int L, typename Ti>
 struct StageBC {
   Pack<T, 4> k[Ti::kQuads];
-  __device__ __forceinline__ void fetch(const Args& a, int p, const Range& r, int base, bool plain, bool b_too) {
+  const T* from[Ti::kQuads];                       // at row 0; NULL: no such states
+  int64_t ld[Ti::kQuads];
+  __device__ __forceinline__ void init(const Args& a, int p, bool b_too) {
 #pragma unroll
     for (int j = 0; j < Ti::kQuads; ++j) {
-      const int i = threadIdx.x + j * kThreads, which = i / (Ti::kRows * L), row = base + i / L % Ti::kRows, n = i % L * kQuad;
+      const int i = threadIdx.x + j * kThreads, which = i / (Ti::kRows * L), n = i % L * kQuad;
+      from[j] = which > 1 || n >= a.d.N || (which == 0 && !b_too) ? nullptr
+                : static_cast<const T*>(which ? a.d.c.data : a.d.b.data) + p * (which ? a.d.c.stride : a.d.b.stride) + n;
+      ld[j] = which ? a.d.c.ld : a.d.b.ld;
+    }
+  }
+  __device__ __forceinline__ void fetch(const Args& a, int p, const Range& r, int base, bool plain) {
+#pragma unroll
+    for (int j = 0; j < Ti::kQuads; ++j) {
+      const int i = threadIdx.x + j * kThreads, row = base + i / L % Ti::kRows, n = i % L * kQuad;
       const float zero[4] = {};
       k[j].set(zero);
-      if (which > 1 || n >= a.d.N || (which == 0 && !b_too) || !(plain || row_lives(a, p, r, row))) continue;
-      const T* src = view<T>(which ? a.d.c : a.d.b).row(p, row) + n;
+      if (!from[j] || !(plain || row_lives(a, p, r, row))) continue;
+      const T* src = from[j] + row * ld[j];
       if (a.wide_bc) {
         k[j].load(src);
       } else {
@@ -273,14 +320,15 @@ __device__ __forceinline__ float part_of(const float4& v, int i) { return i == 0
 // kEnds: only what the chain adds to the state behind it, and its summed time steps.
 template <typename T, int L, bool kEnds>
 __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_constant__ Args a) {
-  using Ti = Tile<L, 1>;
+  using Ti = Tile<L>;
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ __align__(16) float s_delta[Ti::kArray], s_du[Ti::kArray];      // delta, then the sum over the states; delta x
+  // (arrays of their own: a store of sums does not hold back the next rows' loads)
+  __shared__ __align__(16) float s_delta[Ti::kArray], s_du[Ti::kArray], s_y[kEnds ? 1 : Ti::kArray];   // delta, delta x; C . h
   __shared__ __align__(16) float s_bc[2 * Ti::kRows * Ti::kN];
   __shared__ int s_begin[Ti::kRows], s_end[Ti::kRows];
   const int p = blockIdx.z, c = blockIdx.y, lane = threadIdx.x & 31;
-  const Range r(a, p, c);
+  Range r(a, p, c);
   const lsgd_scan_desc& d = a.d;
   const int local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
   const bool mine = ch < d.D && n0 < d.N;
@@ -303,36 +351,47 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
   const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
   const bool wide = a.wide;
   const Rows<T> x = view<T>(d.x), dt = view<T>(d.dt), z = view<T>(d.z), out = view<T>(d.out);
-  float bias[8], skip[8];
-#pragma unroll
-  for (int v = 0; v < 8; ++v) {
-    bias[v] = vector_at(d.dt_bias, p, pch + v, has_piece && pch + v < d.D);
-    skip[v] = vector_at(d.skip, p, pch + v, !kEnds && has_piece && pch + v < d.D);
-  }
+  float2 bias[4], skip[4];
+  load_vector8(d.dt_bias, p, pch, has_piece ? d.D : 0, bias);
+  load_vector8(d.skip, p, pch, !kEnds && has_piece ? d.D : 0, skip);
+  const int own = Ti::at(piece, prow);                             // its first channel's place in an array
   Pack<T, 8> rx, rdt, rz;
   StageBC<T, L, Ti> bc;
+  bc.init(a, p, true);
+  const bool gated = !kEnds && d.z.data != nullptr, with_state = d.state != nullptr;
   bool live = false, plain = false;
+  const T *px = x.row(p, r.base + prow), *pdt = dt.row(p, r.base + prow), *pz = gated ? z.row(p, r.base + prow) : px;
+  T* pout = out.row(p, r.base + prow);
+  const int64_t step_x = Ti::kRows * d.x.ld, step_dt = Ti::kRows * d.dt.ld, step_z = gated ? Ti::kRows * d.z.ld : 0, step_out = Ti::kRows * d.out.ld;
   auto fetch = [&](int base) {
-    const int t = base + prow;
     plain = r.plain(a, p, base, Ti::kRows);
-    live = has_piece && (plain || row_lives(a, p, r, t));
+    live = has_piece && (plain || row_lives(a, p, r, base + prow));
     if (live) {
-      load8<T>(rx, x.row(p, t), pch, d.D, wide);
-      load8<T>(rdt, dt.row(p, t), pch, d.D, wide);
-      if (!kEnds && d.z.data) load8<T>(rz, z.row(p, t), pch, d.D, wide);
+      load8<T>(rx, px, pch, d.D, wide);
+      load8<T>(rdt, pdt, pch, d.D, wide);
+      if (gated) load8<T>(rz, pz, pch, d.D, wide);
     }
-    bc.fetch(a, p, r, base, plain, true);
+    px += step_x, pdt += step_dt, pz += step_z;
+    bc.fetch(a, p, r, base, plain);
   };
   if (r.base < r.t1) fetch(r.base);
-  const int64_t groups = (a.q.T + kGroup - 1) / kGroup;
+  // the states in front of every 8th row
+  const int64_t saved_step = (int64_t)d.D * d.N;
+  float* saved = !kEnds && d.saved && mine ? d.saved + ((int64_t)p * ((a.q.T + kGroup - 1) / kGroup) + r.base / kGroup) * saved_step + (int64_t)ch * d.N : nullptr;
+  const int turn = 4 * (local >> 3);
+  const float *delta_of = s_delta + local * Ti::kPitch, *du_of = s_du + local * Ti::kPitch;
   // four rows of the recurrence
   auto rows4 = [&](int base, int t4, auto special) {
-    if (!kEnds && d.saved && t4 % kGroup == 0 && mine && (!special || (base + t4 >= r.t0 && base + t4 < r.t1))) {
-      const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
-      store_states(d.saved, ((int64_t)p * groups + (base + t4) / kGroup) * d.D + ch, n0, d.N, f);
+    if (!kEnds && saved && t4 % kGroup == 0) {
+      if (!special || (base + t4 >= r.t0 && base + t4 < r.t1)) {
+        const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
+        store_states(saved, 0, n0, d.N, f);
+      }
+      saved += saved_step;
     }
-    const float4 delta4 = *reinterpret_cast<const float4*>(s_delta + Ti::at(local, t4));
-    const float4 du4 = *reinterpret_cast<const float4*>(s_du + Ti::at(local, t4));
+    const int place = (t4 + turn) & (Ti::kRows - 1);
+    const float4 delta4 = *reinterpret_cast<const float4*>(delta_of + place);
+    const float4 du4 = *reinterpret_cast<const float4*>(du_of + place);
     float y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -342,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
         if (s >= 0) {
           fresh = true;
           float f[kQuad] = {};
-          if (d.state && mine) {
+          if (with_state && mine) {
             const int64_t row = ((int64_t)p * a.q.S + s) * d.D + ch;
             load_states(from, row, n0, d.N, f);
             if (kEnds) store_states(a.old_state, row, n0, d.N, f);
@@ -361,29 +420,33 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
         pairs(*reinterpret_cast<const float4*>(s_bc + (Ti::kRows + t) * Ti::kN + n0), C);
         const float2 s = fma2(C[0], h[0], mul2(C[1], h[1]));
         y[i] = s.x + s.y;
-        if (special && d.state && mine && s_end[t] >= 0) {
+        if (special && with_state && mine && s_end[t] >= 0) {
           const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
           store_states(d.state, ((int64_t)p * a.q.S + s_end[t]) * d.D + ch, n0, d.N, f);
         }
       }
     }
-    if (!kEnds) keep_sums<L, Ti>(y, s_delta, local, t4, lane);     // every lane of the channel has read these rows
+    if (!kEnds) keep_sums<L, Ti>(y, s_y, local, t4, lane);
   };
   for (int base = r.base; base < r.t1; base += Ti::kRows) {
     // stage
-    if (threadIdx.x < Ti::kPieces) {
-      float fx[8] = {}, fd[8] = {};
-      if (live) {
-        rx.get(fx);
-        rdt.get(fd);
-      }
+    if (live) {
+      float fx[8], fd[8];
+      float2 x2[4], dt2[4];
+      rx.get(fx);
+      rdt.get(fd);
+      pairs8(fx, x2);
+      pairs8(fd, dt2);
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        float e;
-        const float delta = live ? softplus(fd[v] + bias[v], e) : 0.f;
-        s_delta[Ti::at(piece + v, prow)] = delta;
-        s_du[Ti::at(piece + v, prow)] = delta * fx[v];
+      for (int v = 0; v < 4; ++v) {
+        float2 e;
+        const float2 delta = softplus(add2(dt2[v], bias[v]), e), du = mul2(delta, x2[v]);
+        s_delta[own + 2 * v * Ti::kPitch] = delta.x, s_delta[own + (2 * v + 1) * Ti::kPitch] = delta.y;
+        s_du[own + 2 * v * Ti::kPitch] = du.x, s_du[own + (2 * v + 1) * Ti::kPitch] = du.y;
       }
+    } else if (threadIdx.x < Ti::kPieces) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s_delta[own + v * Ti::kPitch] = s_du[own + v * Ti::kPitch] = 0.f;
     }
     bc.store(s_bc);
     const bool is_plain = plain, was_live = live;
@@ -399,17 +462,26 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
       for (int t4 = 0; t4 < Ti::kRows; t4 += 4) rows4(base, t4, std::true_type());
     }
     __syncthreads();
+    pout += step_out;
     if (kEnds || !was_live) continue;
-    // finish: the thread reads and later overwrites its own piece only
-    float fx[8], fz[8], o[8];
+    // finish (s_y is written again behind the next barrier)
+    float fx[8], o[8];
+    float2 x2[4], y2[4];
     kx.get(fx);
-    if (d.z.data) kz.get(fz);
+    pairs8(fx, x2);
 #pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      o[v] = fmaf(skip[v], fx[v], s_delta[Ti::at(piece + v, prow)]);
-      if (d.z.data) o[v] *= fz[v] * sigmoid(fz[v]);
+    for (int v = 0; v < 4; ++v)
+      y2[v] = fma2(skip[v], x2[v], make_float2(s_y[own + 2 * v * Ti::kPitch], s_y[own + (2 * v + 1) * Ti::kPitch]));
+    if (gated) {
+      float2 z2[4];
+      kz.get(fx);
+      pairs8(fx, z2);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y2[v] = mul2(y2[v], mul2(z2[v], sigmoid(z2[v])));
     }
-    store8<T>(o, out.row(p, base + prow), pch, d.D, wide);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) o[2 * v] = y2[v].x, o[2 * v + 1] = y2[v].y;
+    store8<T>(o, pout - step_out, pch, d.D, wide);
   }
   if (kEnds && mine) {
     const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
@@ -470,13 +542,13 @@ __global__ void __launch_bounds__(kThreads) single_kernel(const __grid_constant_
 // Split chains: what the chain's rows add to the adjoint in front of it, and its summed time steps.
 template <typename T, int L>
 __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_constant__ Args a) {
-  using Ti = Tile<L, 1>;
+  using Ti = Tile<L>;
   pdl_wait();
   pdl_launch_dependents();
   __shared__ __align__(16) float s_delta[Ti::kArray], s_d[Ti::kArray], s_bc[2 * Ti::kRows * Ti::kN];
   __shared__ int s_begin[Ti::kRows], s_end[Ti::kRows];
   const int p = blockIdx.z, c = blockIdx.y;
-  const Range r(a, p, c);
+  Range r(a, p, c);
   const lsgd_scan_desc& d = a.d;
   const int local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
   const bool mine = ch < d.D && n0 < d.N;
@@ -494,11 +566,13 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
   const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
   const bool wide = a.wide;
   const Rows<T> dt = view<T>(d.dt), z = view<T>(d.z), up = view<T>(d.d_out);
-  float bias[8];
-#pragma unroll
-  for (int v = 0; v < 8; ++v) bias[v] = vector_at(d.dt_bias, p, pch + v, has_piece && pch + v < d.D);
+  float2 bias[4];
+  load_vector8(d.dt_bias, p, pch, has_piece ? d.D : 0, bias);
+  const int own = Ti::at(piece, prow);
+  const bool gated = d.z.data != nullptr;
   Pack<T, 8> rup, rdt, rz;
   StageBC<T, L, Ti> bc;
+  bc.init(a, p, false);
   bool live = false, plain = false;
   auto fetch = [&](int base) {
     const int t = base + prow;
@@ -509,25 +583,36 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
       load8<T>(rdt, dt.row(p, t), pch, d.D, wide);
       if (d.z.data) load8<T>(rz, z.row(p, t), pch, d.D, wide);
     }
-    bc.fetch(a, p, r, base, plain, false);
+    bc.fetch(a, p, r, base, plain);
   };
   const int n_tiles = r.base < r.t1 ? (r.t1 - r.base + Ti::kRows - 1) / Ti::kRows : 0;
   if (n_tiles > 0) fetch(r.base + (n_tiles - 1) * Ti::kRows);
   for (int it = n_tiles - 1; it >= 0; --it) {
     const int base = r.base + it * Ti::kRows;
-    if (threadIdx.x < Ti::kPieces) {
-      float fu[8] = {}, fd[8] = {}, fz[8] = {};
-      if (live) {
-        rup.get(fu);
-        rdt.get(fd);
-        if (d.z.data) rz.get(fz);
+    if (live) {
+      float f[8];
+      float2 up2[4], dt2[4];
+      rup.get(f);
+      pairs8(f, up2);
+      rdt.get(f);
+      pairs8(f, dt2);
+      if (gated) {
+        float2 z2[4];
+        rz.get(f);
+        pairs8(f, z2);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) up2[v] = mul2(up2[v], mul2(z2[v], sigmoid(z2[v])));
       }
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        float e;
-        s_delta[Ti::at(piece + v, prow)] = live ? softplus(fd[v] + bias[v], e) : 0.f;
-        s_d[Ti::at(piece + v, prow)] = d.z.data ? fu[v] * (fz[v] * sigmoid(fz[v])) : fu[v];
+      for (int v = 0; v < 4; ++v) {
+        float2 e;
+        const float2 delta = softplus(add2(dt2[v], bias[v]), e);
+        s_delta[own + 2 * v * Ti::kPitch] = delta.x, s_delta[own + (2 * v + 1) * Ti::kPitch] = delta.y;
+        s_d[own + 2 * v * Ti::kPitch] = up2[v].x, s_d[own + (2 * v + 1) * Ti::kPitch] = up2[v].y;
       }
+    } else if (threadIdx.x < Ti::kPieces) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s_delta[own + v * Ti::kPitch] = s_d[own + v * Ti::kPitch] = 0.f;
     }
     bc.store(s_bc);
     const bool special = !plain;
@@ -588,182 +673,200 @@ struct ChannelSum {
   }
 };
 
-// A thread takes two channels, a warp's lanes apart, so that B and C are read and dB and dC exchanged for both at once.
-template <int L>
-struct BackSmem {
-  using Ti = Tile<L, 2>;
-  static constexpr int kOwn = 8 * kThreads;                        // values of a thread's own piece, [value][thread]
-  static constexpr int kPart = kThreads / 32 * kGroup * 8 * L;     // warps x rows x (4 dB, 4 dC) x L
-  static constexpr size_t bytes = sizeof(float) * (6 * Ti::kArray + 3 * kOwn + 2 * Ti::kRows * Ti::kN + 2 * kPart) + 2 * sizeof(int) * Ti::kRows;
-};
+__device__ __forceinline__ void copy_async(void* dst, const void* src, int bytes) {       // 8 or 16
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
+  if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(src) : "memory");
+  else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
+}
+
+// Shared memory of a block, the dynamic part: what a thread keeps for itself.
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Args a) {
-  using Ti = Tile<L, 2>;
-  using Sm = BackSmem<L>;
+struct BackSmem {
+  static constexpr int kBufs = L == 16 ? 1 : 2;
+  static constexpr int kPart = kThreads / 32 * kGroup * 8 * L;     // warps x rows x (4 dB, 4 dC) x L
+  static constexpr int kOwn = 8 * kThreads;                        // values of a thread's piece, [value][thread]
+  static constexpr int kRaw = kThreads;                            // pieces of 8 values as they came, [thread]
+  static constexpr size_t bytes = sizeof(float) * 2 * kOwn + sizeof(Pack<T, 8>) * 5 * kRaw + sizeof(Pack<T, 4>) * Tile<L>::kQuads * kThreads;
+};
+// Registers: the four rows in hand (states, decays, B, C and time steps, which both directions use), so that four blocks fit an SM;
+// what is fetched for the next tile therefore goes to shared memory.
+template <typename T, int L>
+__global__ void __launch_bounds__(kThreads, 4) backward_kernel(const __grid_constant__ Args a) {
+  using Ti = Tile<L>;
+  using Sm = BackSmem<T, L>;
   pdl_wait();
   pdl_launch_dependents();
-  extern __shared__ __align__(16) float smem[];
-  float* s_delta = smem;                                           // what the recurrence reads
-  float* s_du = s_delta + Ti::kArray;
-  float* s_d = s_du + Ti::kArray;
-  float* s_qa = s_d + Ti::kArray;                                  // its sums over the states: q A log2(e), g B, C h
-  float* s_gb = s_qa + Ti::kArray;
-  float* s_y = s_gb + Ti::kArray;
-  float* s_bc = s_y + Ti::kArray;
-  float* s_part = s_bc + 2 * Ti::kRows * Ti::kN;
-  float* s_x = s_part + 2 * Sm::kPart + threadIdx.x;               // the thread's own: x, the slopes of softplus and of the gate
-  float* s_slope = s_x + Sm::kOwn;
-  float* s_gate = s_slope + Sm::kOwn;
-  int* s_begin = reinterpret_cast<int*>(s_part + 2 * Sm::kPart + 3 * Sm::kOwn);
-  int* s_end = s_begin + Ti::kRows;
+  // what the recurrence reads (delta, delta x, d), and its sums over the states (g B, C h; q A log2(e) takes delta x's place)
+  __shared__ __align__(16) float s_delta[Ti::kArray], s_du[Ti::kArray], s_d[Ti::kArray], s_gb[Ti::kArray], s_y[Ti::kArray];
+  __shared__ __align__(16) float s_bc[2 * Ti::kRows * Ti::kN], s_part[Sm::kBufs * Sm::kPart];
+  __shared__ int s_begin[Ti::kRows], s_end[Ti::kRows];
+  extern __shared__ __align__(16) float s_own[];
+  float *s_slope = s_own + threadIdx.x, *s_gate = s_slope + Sm::kOwn;
+  Pack<T, 8>* raw = reinterpret_cast<Pack<T, 8>*>(s_own + 2 * Sm::kOwn) + threadIdx.x;       // dt, d_out, z, x, the other tile's x
+  Pack<T, 4>* raw_bc = reinterpret_cast<Pack<T, 4>*>(reinterpret_cast<Pack<T, 8>*>(s_own + 2 * Sm::kOwn) + 5 * Sm::kRaw) + threadIdx.x;
   const int p = blockIdx.z, c = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Range r(a, p, c);
+  Range r(a, p, c);
   const lsgd_scan_desc& d = a.d;
-  constexpr int kWarpCh = 32 / L;                                  // a thread's channels: this far apart
-  const int local = warp * 2 * kWarpCh + lane / L, ch0 = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
-  const bool states = n0 < d.N;
-  const int64_t chain_row = ((int64_t)p * a.chains + c) * d.D;
-  float2 A2[2][2], carry[2][2], dA[2][2] = {};                     // carry: a_(t+1) g_(t+1)
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int ch = ch0 + j * kWarpCh;
+  const int local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
+  const bool mine = ch < d.D && n0 < d.N;
+  float2 A2[2], carry[2], dA[2] = {};                              // carry: a_(t+1) g_(t+1)
+  {
     float f[kQuad], g[kQuad] = {};
     decay_rates(a, p, ch, n0, f);
-    if (a.split && states && ch < d.D) load_states(a.ends, chain_row + ch, n0, d.N, g);
-    A2[j][0] = make_float2(f[0], f[1]), A2[j][1] = make_float2(f[2], f[3]);
-    carry[j][0] = make_float2(g[0], g[1]), carry[j][1] = make_float2(g[2], g[3]);
+    if (a.split && mine) load_states(a.ends, ((int64_t)p * a.chains + c) * d.D + ch, n0, d.N, g);
+    A2[0] = make_float2(f[0], f[1]), A2[1] = make_float2(f[2], f[3]);
+    carry[0] = make_float2(g[0], g[1]), carry[1] = make_float2(g[2], g[3]);
   }
   const int prow = threadIdx.x / (Ti::kCh / 8), piece = (threadIdx.x % (Ti::kCh / 8)) * 8;
-  const int pch = blockIdx.x * Ti::kCh + piece;
+  const int pch = blockIdx.x * Ti::kCh + piece, own = Ti::at(piece, prow);
   const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
-  const bool wide = a.wide;
-  const Rows<T> x = view<T>(d.x), dt = view<T>(d.dt), z = view<T>(d.z), up = view<T>(d.d_out);
-  float d_skip[8] = {}, d_bias[8] = {};
-  Pack<T, 8> rx, rdt, rz, rup;
-  constexpr bool kAhead = Ti::kQuads <= 2;
-  StageBC<T, L, Ti> bc;
-  bool live = false, plain = false;
-  auto fetch = [&](int base) {
-    const int t = base + prow;
-    plain = r.plain(a, p, base, Ti::kRows);
-    live = has_piece && (plain || row_lives(a, p, r, t));
-    if (live) {
-      load8<T>(rx, x.row(p, t), pch, d.D, wide);
-      load8<T>(rdt, dt.row(p, t), pch, d.D, wide);
-      load8<T>(rup, up.row(p, t), pch, d.D, wide);
-      if (d.z.data) load8<T>(rz, z.row(p, t), pch, d.D, wide);
-    }
-    if (kAhead) bc.fetch(a, p, r, base, plain, true);
-  };
-  const int64_t groups = (a.q.T + kGroup - 1) / kGroup;
+  const bool gated = d.z.data != nullptr;
   const int n_tiles = r.base < r.t1 ? (r.t1 - r.base + Ti::kRows - 1) / Ti::kRows : 0;
-  if (n_tiles > 0) fetch(r.base + (n_tiles - 1) * Ti::kRows);
+  int base = r.base + (n_tiles - 1) * Ti::kRows;
+  bool live = false, plain = false;
+  auto fetch8 = [&](Pack<T, 8>* to, const lsgd_rows& m, int t) {
+    const T* src = view<T>(m).row(p, t);
+    if (a.wide) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(Pack<T, 8>); k += 16)
+        copy_async(reinterpret_cast<char*>(to) + k, reinterpret_cast<const char*>(src + pch) + k, 16);
+    } else {
+      Pack<T, 8> k;
+      load8<T>(k, src, pch, d.D, false);
+      *to = k;
+    }
+  };
+  auto fetch = [&](int at, int which) {
+    plain = r.plain(a, p, at, Ti::kRows);
+    live = has_piece && (plain || row_lives(a, p, r, at + prow));
+    if (live) {
+      fetch8(raw, d.dt, at + prow);
+      fetch8(raw + Sm::kRaw, d.d_out, at + prow);
+      if (gated) fetch8(raw + 2 * Sm::kRaw, d.z, at + prow);
+      fetch8(raw + (3 + which) * Sm::kRaw, d.x, at + prow);
+    }
+#pragma unroll
+    for (int j = 0; j < Ti::kQuads; ++j) {
+      const int i = threadIdx.x + j * kThreads, w = i / (Ti::kRows * L), row = at + i / L % Ti::kRows, n = i % L * kQuad;
+      if (w > 1) continue;
+      Pack<T, 4>* to = raw_bc + j * kThreads;
+      if (n < d.N && (plain || row_lives(a, p, r, row))) {
+        const T* src = view<T>(w ? d.c : d.b).row(p, row) + n;
+        if (a.wide_bc) {
+          copy_async(to, src, (int)sizeof(Pack<T, 4>));
+          continue;
+        }
+        float f[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          Pack<T, 1> one;
+          f[v] = 0.f;
+          if (n + v < d.N) {
+            one.load(src + v);
+            one.get(f + v);
+          }
+        }
+        to->set(f);
+      } else {
+        const float zero[4] = {};
+        to->set(zero);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int parity = 0;
+  if (n_tiles > 0) fetch(base, parity);
+  const int place0 = local * Ti::kPitch, turn = 4 * (local >> 3);
+  // the saved state in front of a group, fetched a group ahead
+  const float* saved = d.saved + ((int64_t)p * ((a.q.T + kGroup - 1) / kGroup) * d.D + ch) * d.N;
+  float next[kQuad] = {};
+  auto fetch_state = [&](int row0) {
+    if (mine && row0 >= r.t0 && row0 < r.t1) load_states(saved, (int64_t)(row0 / kGroup) * d.D, n0, d.N, next);
+    else next[0] = next[1] = next[2] = next[3] = 0.f;
+  };
+  if (n_tiles > 0) fetch_state(base + Ti::kRows - kGroup);
+  float* part_bc = a.part_bc + ((int64_t)p * a.tiles + blockIdx.x) * a.q.T * 2 * d.N;
+  float column = 0.f;                                              // of d skip or d dt_bias
   int buf = 0;
-  // a group of 8 rows from row0 = base + g8
-  auto group = [&](int base, int g8, auto special) {
-    const int row0 = base + g8;
-    float2 hs[kGroup][2][2], as[kGroup][2][2], first[2][2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float f[kQuad] = {};
-      const int ch = ch0 + j * kWarpCh;
-      if (states && ch < d.D && (!special || row0 >= r.t0)) load_states(d.saved, ((int64_t)p * groups + row0 / kGroup) * d.D + ch, n0, d.N, f);
-      first[j][0] = make_float2(f[0], f[1]), first[j][1] = make_float2(f[2], f[3]);
-    }
-    float2 h[2][2] = {{first[0][0], first[0][1]}, {first[1][0], first[1][1]}};
-#pragma unroll
-    for (int half = 0; half < kGroup; half += 4) {
-      float y[2][4];
-      float4 delta4[2], du4[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        delta4[j] = *reinterpret_cast<const float4*>(s_delta + Ti::at(local + j * kWarpCh, g8 + half));
-        du4[j] = *reinterpret_cast<const float4*>(s_du + Ti::at(local + j * kWarpCh, g8 + half));
-      }
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const int i = half + i4, t = g8 + i;
-        if (special && s_begin[t] >= 0) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) h[j][0] = h[j][1] = make_float2(0.f, 0.f);
-        }
-        float2 B[2], C[2];
-        pairs(*reinterpret_cast<const float4*>(s_bc + t * Ti::kN + n0), B);
-        pairs(*reinterpret_cast<const float4*>(s_bc + (Ti::kRows + t) * Ti::kN + n0), C);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 delta = both(part_of(delta4[j], i4)), du = both(part_of(du4[j], i4));
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            as[i][j][k] = ex2(mul2(delta, A2[j][k]));
-            h[j][k] = fma2(as[i][j][k], h[j][k], mul2(du, B[k]));
-            hs[i][j][k] = h[j][k];
-          }
-          const float2 s = fma2(C[0], h[j][0], mul2(C[1], h[j][1]));
-          y[j][i4] = s.x + s.y;
-        }
-      }
-      if (d.z.data) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) keep_sums<L, Ti>(y[j], s_y, local + j * kWarpCh, g8 + half, lane);
-      }
-    }
+  // a group of 8 rows from row0 = base + g8: the later four first, whose states are found through the earlier ones'
+  auto group = [&](int row0, int g8, auto special) {
+    const float2 first[2] = {make_float2(next[0], next[1]), make_float2(next[2], next[3])};
+    fetch_state(row0 - kGroup);
     float* part = s_part + buf * Sm::kPart + warp * kGroup * 8 * L;
-    float2 sum_a[2][2] = {};                                       // of the group's rows
+    float2 h[2] = {first[0], first[1]};
+    {
+      const int place = place0 + ((g8 + turn) & (Ti::kRows - 1));
+      const float4 delta4 = *reinterpret_cast<const float4*>(s_delta + place), du4 = *reinterpret_cast<const float4*>(s_du + place);
 #pragma unroll
-    for (int half = kGroup - 4; half >= 0; half -= 4) {
-      float gb[2][4], qa[2][4];
-      float4 delta4[2], du4[2], d4[2];
+      for (int i = 0; i < 4; ++i) {
+        if (special && s_begin[g8 + i] >= 0) h[0] = h[1] = make_float2(0.f, 0.f);
+        float2 B[2];
+        pairs(*reinterpret_cast<const float4*>(s_bc + (g8 + i) * Ti::kN + n0), B);
+        const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        delta4[j] = *reinterpret_cast<const float4*>(s_delta + Ti::at(local + j * kWarpCh, g8 + half));
-        du4[j] = *reinterpret_cast<const float4*>(s_du + Ti::at(local + j * kWarpCh, g8 + half));
-        d4[j] = *reinterpret_cast<const float4*>(s_d + Ti::at(local + j * kWarpCh, g8 + half));
+        for (int k = 0; k < 2; ++k) h[k] = fma2(ex2(mul2(delta, A2[k])), h[k], mul2(du, B[k]));
       }
+    }
+#pragma unroll 1
+    for (int half = 4; half >= 0; half -= 4) {
+      if (half == 0) h[0] = first[0], h[1] = first[1];
+      const float2 prior[2] = {h[0], h[1]};                        // the state in front of the four rows
+      float2 hs[4][2], as[4][2], B[4][2], C[4][2];
+      float y[4], gb[4], qa[4];
+      const int place = place0 + ((g8 + half + turn) & (Ti::kRows - 1));
+      const float4 delta4 = *reinterpret_cast<const float4*>(s_delta + place), du4 = *reinterpret_cast<const float4*>(s_du + place);
+      const float4 d4 = *reinterpret_cast<const float4*>(s_d + place);
+      const float *b_of = s_bc + (g8 + half) * Ti::kN + n0, *c_of = b_of + Ti::kRows * Ti::kN;
 #pragma unroll
-      for (int i4 = 3; i4 >= 0; --i4) {
-        const int i = half + i4, t = g8 + i;
-        const bool begins = special && s_begin[t] >= 0;
-        float2 B[2], C[2], db[2], dc[2];
-        pairs(*reinterpret_cast<const float4*>(s_bc + t * Ti::kN + n0), B);
-        pairs(*reinterpret_cast<const float4*>(s_bc + (Ti::kRows + t) * Ti::kN + n0), C);
+      for (int i = 0; i < 4; ++i) {
+        if (special && s_begin[g8 + half + i] >= 0) h[0] = h[1] = make_float2(0.f, 0.f);
+        pairs(*reinterpret_cast<const float4*>(b_of + i * Ti::kN), B[i]);
+        pairs(*reinterpret_cast<const float4*>(c_of + i * Ti::kN), C[i]);
+        const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 delta = both(part_of(delta4[j], i4)), du = both(part_of(du4[j], i4)), dy = both(part_of(d4[j], i4));
-          float2 sb = make_float2(0.f, 0.f), sq = sb;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float2 g = fma2(C[k], dy, carry[j][k]);
-            db[k] = j == 0 ? mul2(g, du) : fma2(g, du, db[k]);
-            dc[k] = j == 0 ? mul2(dy, hs[i][j][k]) : fma2(dy, hs[i][j][k], dc[k]);
-            sb = k == 0 ? mul2(g, B[k]) : fma2(g, B[k], sb);
-            carry[j][k] = mul2(as[i][j][k], g);
-            float2 q = mul2(carry[j][k], i > 0 ? hs[i > 0 ? i - 1 : 0][j][k] : first[j][k]);
-            if (begins) carry[j][k] = q = make_float2(0.f, 0.f);
-            sum_a[j][k] = fma2(q, delta, sum_a[j][k]);
-            sq = k == 0 ? mul2(q, A2[j][k]) : fma2(q, A2[j][k], sq);
-          }
-          gb[j][i4] = sb.x + sb.y;
-          qa[j][i4] = sq.x + sq.y;
+        for (int k = 0; k < 2; ++k) {
+          as[i][k] = ex2(mul2(delta, A2[k]));
+          h[k] = fma2(as[i][k], h[k], mul2(du, B[i][k]));
+          hs[i][k] = h[k];
         }
+        if (gated) {
+          const float2 s = fma2(C[i][0], h[0], mul2(C[i][1], h[1]));
+          y[i] = s.x + s.y;
+        }
+      }
+      float2 sum_a[2] = {};                                        // of the four rows
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        float2 db[2], dc[2], sb, sq;
+        const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i)), dy = both(part_of(d4, i));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float2 g = fma2(C[i][k], dy, carry[k]);
+          db[k] = mul2(g, du);
+          dc[k] = mul2(dy, hs[i][k]);
+          sb = k == 0 ? mul2(g, B[i][k]) : fma2(g, B[i][k], sb);
+          carry[k] = mul2(as[i][k], g);
+          float2 q = mul2(carry[k], i > 0 ? hs[i > 0 ? i - 1 : 0][k] : prior[k]);
+          if (special && s_begin[g8 + half + i] >= 0) carry[k] = q = make_float2(0.f, 0.f);
+          sum_a[k] = fma2(q, delta, sum_a[k]);
+          sq = k == 0 ? mul2(q, A2[k]) : fma2(q, A2[k], sq);
+        }
+        gb[i] = sb.x + sb.y;
+        qa[i] = sq.x + sq.y;
         float v[8] = {db[0].x, db[0].y, db[1].x, db[1].y, dc[0].x, dc[0].y, dc[1].x, dc[1].y};
         ChannelSum<L>::run(v, lane);
-        const int f = ChannelSum<L>::first(lane);
         if (8 * L > 16 || !(lane & (8 * L))) {
+          const int f = ChannelSum<L>::first(lane);
 #pragma unroll
-          for (int q = 0; q < ChannelSum<L>::kCount; ++q) part[(i * 8 + f + q) * L + lane % L] = v[q];
+          for (int q = 0; q < ChannelSum<L>::kCount; ++q) part[((half + i) * 8 + f + q) * L + lane % L] = v[q];
         }
       }
+      if (gated) keep_sums<L, Ti>(y, s_y, local, g8 + half, lane);
+      keep_sums<L, Ti>(gb, s_gb, local, g8 + half, lane);
+      keep_sums<L, Ti>(qa, s_du, local, g8 + half, lane);          // whose four rows every lane of the channel has read
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        keep_sums<L, Ti>(gb[j], s_gb, local + j * kWarpCh, g8 + half, lane);
-        keep_sums<L, Ti>(qa[j], s_qa, local + j * kWarpCh, g8 + half, lane);
-      }
+      for (int k = 0; k < 2; ++k) dA[k] = add2(dA[k], sum_a[k]);
     }
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) dA[j][k] = make_float2(dA[j][k].x + sum_a[j][k].x, dA[j][k].y + sum_a[j][k].y);
     __syncthreads();
     // the block's sums over its channels, the warps' in order
 #pragma unroll
@@ -772,103 +875,129 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
       float s = 0.f;
 #pragma unroll
       for (int w = 0; w < kThreads / 32; ++w) s += s_part[buf * Sm::kPart + w * kGroup * 8 * L + i];
-      if (n < d.N && (!special || (row >= r.t0 && row < r.t1)))
-        a.part_bc[((((int64_t)p * a.tiles + blockIdx.x) * a.q.T + row) * 2 + which / 4) * d.N + n] = s;
+      if (n < d.N && (!special || (row >= r.t0 && row < r.t1))) part_bc[(int64_t)row * 2 * d.N + which / 4 * d.N + n] = s;
     }
-    buf ^= 1;
+    if (Sm::kBufs == 1) __syncthreads();
+    else buf ^= 1;
   };
-  for (int it = n_tiles - 1; it >= 0; --it) {
-    const int base = r.base + it * Ti::kRows;
-    if (threadIdx.x < Ti::kPieces) {
-      float fx[8] = {}, fd[8] = {}, fu[8] = {}, fz[8] = {};
-      if (live) {
-        rx.get(fx);
-        rdt.get(fd);
-        rup.get(fu);
-        if (d.z.data) rz.get(fz);
+  for (int it = n_tiles - 1; it >= 0; --it, base -= Ti::kRows, parity ^= 1) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");           // a thread reads only what it has copied
+    if (live) {
+      float f[8];
+      float2 x2[4], up2[4], dt2[4], bias[4];
+      raw[(3 + parity) * Sm::kRaw].get(f);
+      pairs8(f, x2);
+      raw[Sm::kRaw].get(f);
+      pairs8(f, up2);
+      raw[0].get(f);
+      pairs8(f, dt2);
+      load_vector8(d.dt_bias, p, pch, d.D, bias);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float2 e;
+        const float2 pre = add2(dt2[v], bias[v]), delta = softplus(pre, e), du = mul2(delta, x2[v]);
+        const float2 slope = mul2(make_float2(pre.x >= 0.f ? 1.f : e.x, pre.y >= 0.f ? 1.f : e.y), rcp(add2(e, both(1.f))));
+        s_delta[own + 2 * v * Ti::kPitch] = delta.x, s_delta[own + (2 * v + 1) * Ti::kPitch] = delta.y;
+        s_du[own + 2 * v * Ti::kPitch] = du.x, s_du[own + (2 * v + 1) * Ti::kPitch] = du.y;
+        s_slope[2 * v * kThreads] = slope.x, s_slope[(2 * v + 1) * kThreads] = slope.y;
+      }
+      if (gated) {
+        float2 z2[4];
+        raw[2 * Sm::kRaw].get(f);
+        pairs8(f, z2);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float2 sg = sigmoid(z2[v]), sl = mul2(z2[v], sg);
+          const float2 gate = mul2(up2[v], fma2(sl, make_float2(1.f - sg.x, 1.f - sg.y), sg));
+          s_gate[2 * v * kThreads] = gate.x, s_gate[(2 * v + 1) * kThreads] = gate.y;
+          up2[v] = mul2(up2[v], sl);
+        }
       }
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        float e;
-        const float pre = fd[v] + vector_at(d.dt_bias, p, pch + v, has_piece && pch + v < d.D), delta = live ? softplus(pre, e) : 0.f;
-        const int o = Ti::at(piece + v, prow);
-        s_delta[o] = delta;
-        s_du[o] = delta * fx[v];
-        s_x[v * kThreads] = fx[v];
-        s_slope[v * kThreads] = live ? __fdividef(pre >= 0.f ? 1.f : e, 1.f + e) : 0.f;
-        if (d.z.data) {
-          const float sg = sigmoid(fz[v]), sl = fz[v] * sg;
-          s_gate[v * kThreads] = fu[v] * fmaf(sl, 1.f - sg, sg);
-          fu[v] *= sl;
-        }
-        s_d[o] = fu[v];
-      }
+      for (int v = 0; v < 4; ++v) s_d[own + 2 * v * Ti::kPitch] = up2[v].x, s_d[own + (2 * v + 1) * Ti::kPitch] = up2[v].y;
+    } else if (threadIdx.x < Ti::kPieces) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s_delta[own + v * Ti::kPitch] = s_du[own + v * Ti::kPitch] = s_d[own + v * Ti::kPitch] = 0.f;
     }
-    if (!kAhead) bc.fetch(a, p, r, base, plain, true);
-    bc.store(s_bc);
+#pragma unroll
+    for (int j = 0; j < Ti::kQuads; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      if (i >= 2 * Ti::kRows * L) continue;
+      float f[4];
+      raw_bc[j * kThreads].get(f);
+      *reinterpret_cast<float4*>(s_bc + i * kQuad) = make_float4(f[0], f[1], f[2], f[3]);
+    }
     const bool is_plain = plain, was_live = live;
     if (!is_plain) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end);
     __syncthreads();
-    if (it > 0) fetch(base - Ti::kRows);
+    if (it > 0) fetch(base - Ti::kRows, parity ^ 1);
     if (is_plain) {
 #pragma unroll 1
-      for (int g8 = Ti::kRows - kGroup; g8 >= 0; g8 -= kGroup) group(base, g8, std::false_type());
+      for (int g8 = Ti::kRows - kGroup; g8 >= 0; g8 -= kGroup) group(base + g8, g8, std::false_type());
     } else {
 #pragma unroll 1
-      for (int g8 = Ti::kRows - kGroup; g8 >= 0; g8 -= kGroup)
-        if (base + g8 < r.t1 && base + g8 + kGroup > r.t0) group(base, g8, std::true_type());      // the same for the whole block
+      for (int g8 = Ti::kRows - kGroup; g8 >= 0; g8 -= kGroup) {
+        if (base + g8 < r.t1 && base + g8 + kGroup > r.t0) group(base + g8, g8, std::true_type());      // the same for the whole block
+        else fetch_state(base + g8 - kGroup);
+      }
     }
     // the last group's barrier has passed: every warp's sums are there
     if (was_live) {
-      float o_x[8], o_dt[8], o_z[8];
-#pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        const int o = Ti::at(piece + v, prow);
-        const float fx = s_x[v * kThreads], gB = s_gb[o], g = s_d[o];
-        const float skip = vector_at(d.skip, p, pch + v, pch + v < d.D);
-        o_x[v] = fmaf(s_delta[o], gB, skip * g);
-        o_dt[v] = fmaf(fx, gB, s_qa[o] * kLn2) * s_slope[v * kThreads];
-        if (d.z.data) o_z[v] = s_gate[v * kThreads] * fmaf(skip, fx, s_y[o]);
-        d_skip[v] = fmaf(g, fx, d_skip[v]);
-        d_bias[v] += o_dt[v];
-      }
+      float f[8];
+      float2 x2[4], skip[4];
+      raw[(3 + parity) * Sm::kRaw].get(f);
+      pairs8(f, x2);
+      load_vector8(d.skip, p, pch, d.D, skip);
+      auto pair_of = [&](const float* array, int v) { return make_float2(array[own + 2 * v * Ti::kPitch], array[own + (2 * v + 1) * Ti::kPitch]); };
+      auto mine_of = [&](const float* array, int v) { return make_float2(array[2 * v * kThreads], array[(2 * v + 1) * kThreads]); };
       const int t = base + prow;
-      store8<T>(o_x, view<T>(d.dx).row(p, t), pch, d.D, wide);
-      store8<T>(o_dt, view<T>(d.d_dt).row(p, t), pch, d.D, wide);
-      if (d.z.data) store8<T>(o_z, view<T>(d.dz).row(p, t), pch, d.D, wide);
+      if (gated) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float2 o = mul2(mine_of(s_gate, v), fma2(skip[v], x2[v], pair_of(s_y, v)));
+          f[2 * v] = o.x, f[2 * v + 1] = o.y;
+        }
+        store8<T>(f, view<T>(d.dz).row(p, t), pch, d.D, a.wide);
+      }
+      float2 gB[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        gB[v] = pair_of(s_gb, v);
+        const float2 g = pair_of(s_d, v), o = fma2(pair_of(s_delta, v), gB[v], mul2(skip[v], g)), gx = mul2(g, x2[v]);
+        f[2 * v] = o.x, f[2 * v + 1] = o.y;
+        s_y[own + 2 * v * Ti::kPitch] = gx.x, s_y[own + (2 * v + 1) * Ti::kPitch] = gx.y;
+      }
+      store8<T>(f, view<T>(d.dx).row(p, t), pch, d.D, a.wide);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float2 o = mul2(fma2(x2[v], gB[v], mul2(pair_of(s_du, v), both(kLn2))), mine_of(s_slope, v));
+        f[2 * v] = o.x, f[2 * v + 1] = o.y;
+        s_gb[own + 2 * v * Ti::kPitch] = o.x, s_gb[own + (2 * v + 1) * Ti::kPitch] = o.y;
+      }
+      store8<T>(f, view<T>(d.d_dt).row(p, t), pch, d.D, a.wide);
+    } else if (threadIdx.x < Ti::kPieces) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s_gb[own + v * Ti::kPitch] = s_y[own + v * Ti::kPitch] = 0.f;
     }
     __syncthreads();
-  }
+    // d skip and d dt_bias: a channel's rows of the tile in order (these arrays are written again behind the next barrier)
+    if (threadIdx.x < 2 * Ti::kCh) {
+      const float* src = (threadIdx.x < Ti::kCh ? s_y : s_gb) + threadIdx.x % Ti::kCh * Ti::kPitch;
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int ch = ch0 + j * kWarpCh;
-    if (!states || ch >= d.D) continue;
-    float f[kQuad];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      f[2 * k] = dA[j][k].x * (A2[j][k].x * kLn2);
-      f[2 * k + 1] = dA[j][k].y * (A2[j][k].y * kLn2);
-    }
-    store_states(a.part_a, chain_row + ch, n0, d.N, f);
-  }
-  // the rows' sums of d skip and d dt_bias, in order
-  if (threadIdx.x < Ti::kPieces) {
-#pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      s_gb[Ti::at(piece + v, prow)] = d_skip[v];
-      s_y[Ti::at(piece + v, prow)] = d_bias[v];
+      for (int k = 0; k < Ti::kRows; k += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(src + k);
+        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+      }
+      column += (s.x + s.y) + (s.z + s.w);
     }
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 2 * Ti::kCh; i += kThreads) {
-    const int which = i / Ti::kCh, ch = i % Ti::kCh;
-    const float* src = which ? s_y : s_gb;
-    float s = 0.f;
-#pragma unroll 8
-    for (int row = 0; row < Ti::kRows; ++row) s += src[Ti::at(ch, row)];
-    const int col = blockIdx.x * Ti::kCh + ch;
-    if (col < d.D) a.part_v[(((int64_t)p * a.chains + c) * 2 + which) * d.D + col] = s;
+  if (mine) {
+    const float f[kQuad] = {dA[0].x * (A2[0].x * kLn2), dA[0].y * (A2[0].y * kLn2), dA[1].x * (A2[1].x * kLn2), dA[1].y * (A2[1].y * kLn2)};
+    store_states(a.part_a, ((int64_t)p * a.chains + c) * d.D + ch, n0, d.N, f);
   }
+  const int which = threadIdx.x / Ti::kCh, col = blockIdx.x * Ti::kCh + threadIdx.x % Ti::kCh;
+  if (which < 2 && col < d.D) a.part_v[(((int64_t)p * a.chains + c) * 2 + which) * d.D + col] = column;
 }
 
 // db and dc: the channel blocks' sums in order.
@@ -893,7 +1022,7 @@ __global__ void __launch_bounds__(256) join_bc_kernel(const __grid_constant__ Ar
 struct Launch {
   int L;
   bool single;
-  dim3 grid, back;           // blocks of one and of two channels a thread
+  dim3 grid;
 };
 cudaError_t launch_forward_f32(const Args& a, const Launch& l, cudaStream_t s);
 cudaError_t launch_forward_bf16(const Args& a, const Launch& l, cudaStream_t s);
@@ -914,7 +1043,7 @@ cudaError_t forward_of(const Args& a, const Launch& l, cudaStream_t s) {
 }
 template <typename T, int L>
 cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
-  constexpr size_t smem = BackSmem<L>::bytes;
+  constexpr size_t smem = BackSmem<T, L>::bytes;
   static OncePerDevice attr;
   if (!attr.here()) {
     const cudaError_t e = cudaFuncSetAttribute(backward_kernel<T, L>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -926,7 +1055,7 @@ cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
     e = launch_pdl(adjoint_kernel<T, L>, l.grid, dim3(kThreads), 0, s, a);
     if (e == cudaSuccess) e = launch_chain_join(a, true, s);
   }
-  if (e == cudaSuccess) e = launch_pdl(backward_kernel<T, L>, l.back, dim3(kThreads), smem, s, a);
+  if (e == cudaSuccess) e = launch_pdl(backward_kernel<T, L>, l.grid, dim3(kThreads), smem, s, a);
   if (e != cudaSuccess) return e;
   const int64_t values = (int64_t)a.q.T * 2 * a.d.N;
   return launch_pdl(join_bc_kernel<T>, dim3((unsigned)((values + 255) / 256), a.d.P), dim3(256), 0, s, a);
