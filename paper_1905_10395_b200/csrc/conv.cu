@@ -36,54 +36,100 @@ struct ConvArgs {
   uint32_t blocks_t;
 };
 
+__device__ __forceinline__ float exp2f_fast(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
 template <typename T>
 __device__ __forceinline__ Rows<T> view(const lsgd_rows& r) {
   return Rows<T>{static_cast<T*>(r.data), r.ld, r.stride};
 }
 
-// pre and its factor: out = pre * s, d out / d pre = s + pre s (1 - s)
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// VEC (4 or 1) neighbouring values as pairs, two to an instruction (of a single value the second is idle).
+template <int VEC>
+struct Vals {
+  static constexpr int kPairs = (VEC + 1) / 2;
+  float2 v[kPairs];
+};
+template <typename T, int VEC>
+__device__ __forceinline__ Vals<VEC> values(const Pack<T, VEC>& k) {
+  float f[VEC + 1];
+  k.get(f);
+  if (VEC == 1) f[1] = 0.f;
+  Vals<VEC> r;
+#pragma unroll
+  for (int i = 0; i < Vals<VEC>::kPairs; ++i) r.v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void put(const Vals<VEC>& r, T* to) {
+  float f[VEC + 1];
+#pragma unroll
+  for (int i = 0; i < Vals<VEC>::kPairs; ++i) f[2 * i] = r.v[i].x, f[2 * i + 1] = r.v[i].y;
+  Pack<T, VEC> k;
+  k.set(f);
+  k.store(to);
+}
+// sigmoid(v) = 1 / (1 + exp(-v)); exp(-v) is held below 2^126, where the fast quotient ends
+__device__ __forceinline__ float2 sigmoid(float2 v) {
+  return make_float2(__fdividef(1.f, 1.f + exp2f_fast(fminf(v.x * -1.4426950408889634f, 126.f))),
+                     __fdividef(1.f, 1.f + exp2f_fast(fminf(v.y * -1.4426950408889634f, 126.f))));
+}
 
 // A thread's weights: tap j multiplies the input W - 1 - j rows back.  (The number of taps is a template parameter: a weight of zero
 // would not keep an infinite input out.)
 template <int VEC, int W>
 struct Taps {
-  float w[W][VEC], bias[VEC];
+  Vals<VEC> w[W], bias;
   __device__ __forceinline__ void load(const lsgd_conv_desc& d, int p, int ch) {
+    const float* wp = static_cast<const float*>(d.w.data) + p * d.w.stride + ch * d.w.ld;
+    const float* bp = static_cast<const float*>(d.bias.data) + p * d.bias.stride + ch;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const bool in = ch + v < d.D;
+    for (int i = 0; i < Vals<VEC>::kPairs; ++i) {
+      const bool x = ch + 2 * i < d.D, y = VEC > 1 && ch + 2 * i + 1 < d.D;
 #pragma unroll
-      for (int j = 0; j < W; ++j) w[j][v] = in ? static_cast<const float*>(d.w.data)[p * d.w.stride + (ch + v) * d.w.ld + j] : 0.f;
-      bias[v] = in && d.bias.data ? static_cast<const float*>(d.bias.data)[p * d.bias.stride + ch + v] : 0.f;
+      for (int j = 0; j < W; ++j) w[j].v[i] = make_float2(x ? wp[2 * i * d.w.ld + j] : 0.f, y ? wp[(2 * i + 1) * d.w.ld + j] : 0.f);
+      bias.v[i] = make_float2(x && d.bias.data ? bp[2 * i] : 0.f, y && d.bias.data ? bp[2 * i + 1] : 0.f);
     }
   }
+  // win[0 .. W - 2]: the inputs in front of a row, oldest first; last: the row's own
+  __device__ __forceinline__ Vals<VEC> apply(const Vals<VEC> (&win)[W], const Vals<VEC>& last) const {
+    Vals<VEC> s = bias;
+#pragma unroll
+    for (int i = 0; i < Vals<VEC>::kPairs; ++i) {
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) s.v[i] = fma2(w[j].v[i], win[j].v[i], s.v[i]);
+      s.v[i] = fma2(w[W - 1].v[i], last.v[i], s.v[i]);
+    }
+    return s;
+  }
 };
-
-template <typename T, int VEC>
-__device__ __forceinline__ void fetch(const T* row, int ch, float (&f)[VEC]) {
-  Pack<T, VEC> k;
-  k.load(row + ch);
-  k.get(f);
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> activate(Vals<VEC> s, bool silu) {
+  if (silu) {
+#pragma unroll
+    for (int i = 0; i < Vals<VEC>::kPairs; ++i) s.v[i] = mul2(s.v[i], sigmoid(s.v[i]));
+  }
+  return s;
 }
 
-// The W - 1 inputs in front of row t (oldest first) of its own sequence, from the rows or the state; zeros where there is none.
-// Returns how many rows of the sequence lie in front of t, at most W - 1.
+// The W - 1 inputs in front of row t (oldest first) of its own sequence, whose rows begin at lo, from the rows or the state; zeros
+// where there is none.
 template <typename T, int VEC, int W>
-__device__ __forceinline__ int window(const ConvArgs& a, int p, int t, int ch, int code, float (&win)[W][VEC]) {
+__device__ __forceinline__ void window(const ConvArgs& a, int p, int t, int ch, const SeqView::Span& q, Vals<VEC> (&win)[W]) {
   const Rows<T> x = view<T>(a.d.x);
-  int pos = 0;
-  while (pos < W - 1 && a.q.code(p, t - 1 - pos) == code) ++pos;
   const T* state = static_cast<const T*>(a.d.state);
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) {
-    const int back = W - 1 - j;                  // rows in front of t
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) win[j][v] = 0.f;
-    if (back <= pos) fetch<T, VEC>(x.row(p, t - back), ch, win[j]);
-    else if (state) fetch<T, VEC>(state + (((int64_t)p * a.q.S + code) * (W - 1) + j + pos) * a.d.D, ch, win[j]);
+    const int row = t - (W - 1) + j;
+    Pack<T, VEC> k;
+    const float zero[VEC] = {};
+    if (row >= q.lo) k.load(x.row(p, row) + ch);
+    else if (state) k.load(state + (((int64_t)p * a.q.S + q.code) * (W - 1) + (row - q.lo + W - 1)) * a.d.D + ch);
+    else k.set(zero);
+    win[j] = values<T, VEC>(k);
   }
-  return pos;
 }
 
 template <typename T, int VEC, int W>
@@ -91,48 +137,42 @@ __global__ void __launch_bounds__(kLanes * kRuns) conv_forward_kernel(const __gr
   pdl_wait();
   pdl_launch_dependents();
   const int ch = (blockIdx.x * kLanes + threadIdx.x) * VEC, p = blockIdx.z;
-  const int t0 = (blockIdx.y * kRuns + threadIdx.y) * a.run, t1 = min(a.q.T, t0 + a.run);
-  if (ch >= a.d.D || t0 >= t1) return;
-  const Rows<T> x = view<T>(a.d.x), out = view<T>(a.d.out);
+  int t = (blockIdx.y * kRuns + threadIdx.y) * a.run;
+  const int t1 = min(a.q.T, t + a.run);
+  if (ch >= a.d.D || t >= t1) return;
+  const bool silu = a.d.act == LSGD_CONV_SILU;
+  const int64_t ldx = a.d.x.ld, ldo = a.d.out.ld;
   Taps<VEC, W> taps;
   taps.load(a.d, p, ch);
-  float win[W][VEC];                             // the last W - 1 inputs and row t's
-  int before = -2;                               // no row's code
-  for (int t = t0; t < t1; t += kAhead) {
-    Pack<T, VEC> in[kAhead];
-    int code[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      code[i] = t + i < t1 ? a.q.code(p, t + i) : -1;
-      if (code[i] >= 0) in[i].load(x.row(p, t + i) + ch);
+  while (t < t1) {
+    const SeqView::Span q = a.q.span(p, t);
+    const int end = min(t1, q.hi);
+    if (q.code < 0) {
+      t = end;
+      continue;
     }
+    Vals<VEC> win[W];
+    window<T, VEC, W>(a, p, t, ch, q, win);
+    const T* px = view<T>(a.d.x).row(p, t) + ch;
+    T* po = view<T>(a.d.out).row(p, t) + ch;
+    for (; t < end; t += kAhead) {
+      Pack<T, VEC> in[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (code[i] < 0) {
-        before = -2;
-        continue;
+      for (int i = 0; i < kAhead; ++i)
+        if (t + i < end) in[i].load(px + i * ldx);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (t + i >= end) break;
+        const Vals<VEC> last = values<T, VEC>(in[i]);
+        put<T, VEC>(activate(taps.apply(win, last), silu), po + i * ldo);
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
+        if (W > 1) win[W > 1 ? W - 2 : 0] = last;
       }
-      if (code[i] != before) {
-        window<T, VEC, W>(a, p, t + i, ch, code[i], win);
-        before = code[i];
-      }
-      in[i].get(win[W - 1]);
-      float o[VEC];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        float s = taps.bias[v];
-#pragma unroll
-        for (int j = 0; j < W; ++j) s = fmaf(taps.w[j][v], win[j][v], s);
-        o[v] = a.d.act == LSGD_CONV_SILU ? s * sigmoid(s) : s;
-      }
-      Pack<T, VEC> k;
-      k.set(o);
-      k.store(out.row(p, t + i) + ch);
-#pragma unroll
-      for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) win[j][v] = win[j + 1][v];
+      px += kAhead * ldx;
+      po += kAhead * ldo;
     }
+    t = end;
   }
 }
 
@@ -164,22 +204,10 @@ __global__ void __launch_bounds__(kLanes * kRuns) conv_state_kernel(const __grid
     if (SINGLE) {
       Taps<VEC, W> taps;
       taps.load(a.d, p, ch);
-      float o[VEC];
+      Vals<VEC> win[W];
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) o[v] = taps.bias[v];
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        float f[VEC];
-        kept[k].get(f);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) o[v] = fmaf(taps.w[k][v], f[v], o[v]);
-      }
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (a.d.act == LSGD_CONV_SILU) o[v] *= sigmoid(o[v]);
-      Pack<T, VEC> k;
-      k.set(o);
-      k.store(view<T>(a.d.out).row(p, lo) + ch);
+      for (int k = 0; k < W; ++k) win[k] = values<T, VEC>(kept[k]);
+      put<T, VEC>(activate(taps.apply(win, win[W - 1]), a.d.act == LSGD_CONV_SILU), view<T>(a.d.out).row(p, lo) + ch);
     }
     if (!state) continue;
 #pragma unroll
@@ -191,86 +219,83 @@ template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(kLanes * kRuns) conv_backward_kernel(const __grid_constant__ ConvArgs a) {
   pdl_wait();
   pdl_launch_dependents();
+  constexpr int kPairs = Vals<VEC>::kPairs, kTake = 4;
   const int ch = (blockIdx.x * kLanes + threadIdx.x) * VEC, p = blockIdx.z;
-  const int t0 = (blockIdx.y * kRuns + threadIdx.y) * a.run, t1 = min(a.q.T, t0 + a.run);
-  const Rows<T> x = view<T>(a.d.x), d_out = view<T>(a.d.d_out), dx = view<T>(a.d.dx);
-  Taps<VEC, W> taps;
-  float dw[W][VEC] = {}, db[VEC] = {};
-  if (ch < a.d.D && t0 < t1) {
+  int t = (blockIdx.y * kRuns + threadIdx.y) * a.run;
+  const int t1 = min(a.q.T, t + a.run);
+  const bool silu = a.d.act == LSGD_CONV_SILU;
+  Vals<VEC> dw[W] = {}, db = {};
+  if (ch < a.d.D && t < t1) {
+    const int64_t ldx = a.d.x.ld, ldu = a.d.d_out.ld, ldd = a.d.dx.ld;
+    Taps<VEC, W> taps;
     taps.load(a.d, p, ch);
-    float win[W][VEC];
-    float wait[W][VEC];                          // dx of rows t - W + 1 .. t as far as it is known
-    int before = -2, pos = 0;                    // code of row t - 1; rows of its sequence in front of t, at most W - 1
-    const int last = min(a.q.T, t1 + W - 1);
-    for (int t = t0; t < last; t += 4) {
-      Pack<T, VEC> in[4], up[4];
-      int code[4];
+    while (t < t1) {
+      const SeqView::Span q = a.q.span(p, t);
+      const int own = min(t1, q.hi), end = min(q.hi, t1 + W - 1);       // rows of this run; rows that reach into it
+      if (q.code < 0) {
+        t = own;
+        continue;
+      }
+      Vals<VEC> win[W], wait[W] = {};              // wait[j]: dx of row t - (W - 1) + j as far as it is known
+      window<T, VEC, W>(a, p, t, ch, q, win);
+      const int first = t;                         // dx of the rows in front belongs to another thread
+      const T* px = view<T>(a.d.x).row(p, t) + ch;
+      const T* pu = view<T>(a.d.d_out).row(p, t) + ch;
+      T* pd = view<T>(a.d.dx).row(p, t) + ch;
+      for (; t < end; t += kTake) {
+        Pack<T, VEC> in[kTake], up[kTake];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        code[i] = t + i < last ? a.q.code(p, t + i) : -1;
-        if (code[i] >= 0) {
-          in[i].load(x.row(p, t + i) + ch);
-          up[i].load(d_out.row(p, t + i) + ch);
+        for (int i = 0; i < kTake; ++i)
+          if (t + i < end) {
+            in[i].load(px + i * ldx);
+            up[i].load(pu + i * ldu);
+          }
+#pragma unroll
+        for (int i = 0; i < kTake; ++i) {
+          if (t + i >= end) break;
+          const Vals<VEC> last = values<T, VEC>(in[i]);
+          Vals<VEC> g = values<T, VEC>(up[i]);
+          if (silu) {
+            const Vals<VEC> s = taps.apply(win, last);
+#pragma unroll
+            for (int v = 0; v < kPairs; ++v) {
+              const float2 sg = sigmoid(s.v[v]), sl = mul2(s.v[v], sg);
+              g.v[v] = mul2(g.v[v], fma2(sl, make_float2(1.f - sg.x, 1.f - sg.y), sg));
+            }
+          }
+          const bool mine = t + i < own;
+#pragma unroll
+          for (int v = 0; v < kPairs; ++v) {
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) wait[j].v[v] = fma2(taps.w[j].v[v], g.v[v], wait[j].v[v]);
+            wait[W - 1].v[v] = mul2(taps.w[W - 1].v[v], g.v[v]);
+            if (mine) {
+              db.v[v] = make_float2(db.v[v].x + g.v[v].x, db.v[v].y + g.v[v].y);
+#pragma unroll
+              for (int j = 0; j < W - 1; ++j) dw[j].v[v] = fma2(win[j].v[v], g.v[v], dw[j].v[v]);
+              dw[W - 1].v[v] = fma2(last.v[v], g.v[v], dw[W - 1].v[v]);
+            }
+          }
+          if (t + i - (W - 1) >= first) put<T, VEC>(wait[0], pd + (i - (W - 1)) * ldd);      // complete W - 1 rows on
+#pragma unroll
+          for (int j = 0; j + 1 < W; ++j) wait[j] = wait[j + 1];
+#pragma unroll
+          for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
+          if (W > 1) win[W > 1 ? W - 2 : 0] = last;
+        }
+        px += kTake * ldx;
+        pu += kTake * ldu;
+        pd += kTake * ldd;
+      }
+      // the rows that wait are complete where their sequence ends
+      if (end == q.hi) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+          const int row = end - (W - 1) + j;
+          if (row >= first && row < own) put<T, VEC>(wait[j], view<T>(a.d.dx).row(p, row) + ch);
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = t + i;
-        if (r >= t1 && (code[i] < 0 || code[i] != before)) {       // nothing behind the run reaches into it any more
-          t = last;
-          break;
-        }
-        if (code[i] < 0) {
-          before = -2;
-          continue;
-        }
-        if (code[i] != before) {
-          // the run's first row may lie inside a sequence; dx of the rows in front of the run belongs to another thread
-          pos = window<T, VEC, W>(a, p, r, ch, code[i], win);
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) wait[j][v] = 0.f;
-          before = code[i];
-        }
-        in[i].get(win[W - 1]);
-        float g[VEC];
-        up[i].get(g);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          wait[W - 1][v] = 0.f;
-          if (a.d.act == LSGD_CONV_SILU) {
-            float s = taps.bias[v];
-#pragma unroll
-            for (int j = 0; j < W; ++j) s = fmaf(taps.w[j][v], win[j][v], s);
-            const float sg = sigmoid(s);
-            g[v] *= fmaf(s * sg, 1.f - sg, sg);
-          }
-#pragma unroll
-          for (int j = 0; j < W; ++j) wait[j][v] = fmaf(taps.w[j][v], g[v], wait[j][v]);
-          if (r < t1) {
-            db[v] += g[v];
-#pragma unroll
-            for (int j = 0; j < W; ++j) dw[j][v] = fmaf(win[j][v], g[v], dw[j][v]);
-          }
-        }
-        // a row's dx is complete W - 1 rows on, or where its sequence ends
-        const bool ends = a.q.code(p, r + 1) != code[i];
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const int row = r - (W - 1) + j;
-          if ((j == 0 || ends) && row >= t0 && row < t1 && row >= r - pos) {
-            Pack<T, VEC> k;
-            k.set(wait[j]);
-            k.store(dx.row(p, row) + ch);
-          }
-        }
-        pos = min(pos + 1, W - 1);
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) win[j][v] = win[j + 1][v], wait[j][v] = wait[j + 1][v];
-      }
+      t = own;
     }
   }
   // the block's sums: the runs' in order
@@ -278,8 +303,9 @@ __global__ void __launch_bounds__(kLanes * kRuns) conv_backward_kernel(const __g
 #pragma unroll
   for (int j = 0; j <= W; ++j) {
     __syncthreads();
+    const Vals<VEC>& mine = j < W ? dw[j < W ? j : 0] : db;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sums[threadIdx.y][threadIdx.x * VEC + v] = j < W ? dw[j < W ? j : 0][v] : db[v];
+    for (int v = 0; v < VEC; ++v) sums[threadIdx.y][threadIdx.x * VEC + v] = v % 2 ? mine.v[v / 2].y : mine.v[v / 2].x;
     __syncthreads();
     for (int i = threadIdx.y * kLanes + threadIdx.x; i < kLanes * VEC; i += kLanes * kRuns) {
       const int c = blockIdx.x * kLanes * VEC + i;
@@ -292,36 +318,36 @@ __global__ void __launch_bounds__(kLanes * kRuns) conv_backward_kernel(const __g
   }
 }
 
-// Adds the blocks' sums in order: a warp takes 32 neighbouring sums of a worker (of all workers where they share the vector).
-__global__ void __launch_bounds__(1024) conv_join_kernel(const __grid_constant__ ConvArgs a) {
+// Adds the blocks' sums in order: columns of a worker (of all workers where they share the vector), a thread a column where there are
+// few sums of each (SPLIT 1), else 8 warps 32 columns.
+template <int SPLIT>
+__global__ void __launch_bounds__(256) conv_join_kernel(const __grid_constant__ ConvArgs a) {
   pdl_wait();
   const int per = a.d.W + 1, n = a.d.D * per;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
-  __shared__ float s[32][33];
+  const int part = SPLIT == 1 ? 0 : threadIdx.x >> 5;
+  const int i = SPLIT == 1 ? blockIdx.x * 256 + threadIdx.x : blockIdx.x * 32 + (threadIdx.x & 31);
+  __shared__ float s[SPLIT][33];
   const int k = i % per, c = i / per;
   const lsgd_rows& o = k < a.d.W ? a.d.dw : a.d.d_bias;
-  const bool share_w = a.d.P > 1 && a.d.dw.stride == 0, share_b = a.d.P > 1 && a.d.d_bias.stride == 0;
-  const int workers = share_w || share_b ? a.d.P : 1;
-  // where only one of the two is shared, a sum is one worker's or all workers' by its own kind
-  const bool shared = k < a.d.W ? share_w : share_b;
-  const uint32_t rows = a.blocks_t, share = (rows + 31) / 32, r0 = min(rows, warp * share), r1 = min(rows, r0 + share);
+  const bool shared = a.d.P > 1 && o.stride == 0, idle = i >= n || !o.data || (shared && blockIdx.y > 0);
+  const uint32_t rows = a.blocks_t, share = (rows + SPLIT - 1) / SPLIT, r0 = min(rows, part * share), r1 = min(rows, r0 + share);
   float total = 0.f;
-  for (int w = 0; w < workers; ++w) {
-    const int p = workers > 1 && shared ? w : blockIdx.z;
-    float v = 0.f;
-    if (i < n && (shared ? blockIdx.z == 0 : w == 0)) {
+  if (!idle) {
+    for (int p = shared ? 0 : blockIdx.y, last = shared ? a.d.P - 1 : p; p <= last; ++p) {
       const float* src = a.part + (int64_t)p * rows * n + i;
-#pragma unroll 4
-      for (uint32_t r = r0; r < r1; ++r) v += src[(int64_t)r * n];
+#pragma unroll 8
+      for (uint32_t r = r0; r < r1; ++r) total += src[(int64_t)r * n];
     }
-    __syncthreads();
-    s[warp][lane] = v;
-    __syncthreads();
-    if (warp == 0)
-      for (int q = 0; q < 32; ++q) total += s[q][lane];
   }
-  if (warp != 0 || i >= n || !o.data || (shared && blockIdx.z > 0)) return;
-  float* dst = static_cast<float*>(o.data) + (shared ? 0 : blockIdx.z * o.stride) + (k < a.d.W ? c * o.ld + k : c);
+  if (SPLIT > 1) {
+    s[part][threadIdx.x & 31] = total;
+    __syncthreads();
+    if (part > 0) return;
+    total = 0.f;
+    for (int q = 0; q < SPLIT; ++q) total += s[q][threadIdx.x & 31];
+  }
+  if (idle) return;
+  float* dst = static_cast<float*>(o.data) + (shared ? 0 : blockIdx.y * o.stride) + (k < a.d.W ? c * o.ld + k : c);
   *dst = a.d.accumulate ? *dst + total : total;
 }
 
@@ -431,8 +457,11 @@ lsgd_status run_conv(const lsgd_conv_desc* d, bool backward, cudaStream_t s) {
       e = d->act_dtype == LSGD_BF16 ? (c.vec == 4 ? launch_conv<__nv_bfloat16, 4>(a, c, backward, s) : launch_conv<__nv_bfloat16, 1>(a, c, backward, s))
                                     : (c.vec == 4 ? launch_conv<float, 4>(a, c, backward, s) : launch_conv<float, 1>(a, c, backward, s));
   }
-  if (e == cudaSuccess && backward)
-    e = launch_pdl(conv_join_kernel, dim3((d->D * (d->W + 1) + 31) / 32, 1, d->P), dim3(1024), 0, s, a);
+  if (e == cudaSuccess && backward) {
+    const unsigned n = (unsigned)d->D * (d->W + 1);
+    e = c.blocks_t <= 32 ? launch_pdl(conv_join_kernel<1>, dim3((n + 255) / 256, d->P), dim3(256), 0, s, a)
+                         : launch_pdl(conv_join_kernel<8>, dim3((n + 31) / 32, d->P), dim3(256), 0, s, a);
+  }
   return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
 }
 

@@ -139,9 +139,17 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
   const int ch = kThreads / m.l.L, rows = 32;              // channels of a block; a chain's rows are a multiple of any tile's
   m.tiles = (uint32_t)((D + ch - 1) / ch);
   const int ab = elem_bytes(d->act_dtype);
-  auto fits = [&](const lsgd_rows& r) { return row_vec(r, P, T, D, ab) == 8; };
-  m.wide = fits(d->x) && fits(d->dt) && fits(d->z) &&
-           (backward ? fits(d->d_out) && fits(d->dx) && fits(d->d_dt) && fits(d->dz) : fits(d->out));
+  m.wide = 8;
+  auto fits = [&](const lsgd_rows& r) {
+    while (m.wide > 1 && r.data && !(D % m.wide == 0 && reinterpret_cast<uintptr_t>(r.data) % (m.wide * ab) == 0 &&
+                                     (T <= 1 || r.ld % m.wide == 0) && (P <= 1 || r.stride % m.wide == 0)))
+      m.wide /= 2;
+  };
+  for (const lsgd_rows* r : {&d->x, &d->dt, &d->z}) fits(*r);
+  if (backward)
+    for (const lsgd_rows* r : {&d->d_out, &d->dx, &d->d_dt, &d->dz}) fits(*r);
+  else
+    fits(d->out);
   const bool equal = !d->seq.starts;
   m.l.single = !backward && equal && S == T && !d->saved;
   // Chains: whole sequences where that gives every SM a block; else equal runs of rows, four blocks an SM.
@@ -152,13 +160,13 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
     chains = 1;
     m.per = (int32_t)S;
   } else if (equal && columns * S >= sms) {
-    int64_t want = (4 * sms + columns - 1) / columns;
+    int64_t want = 4 * sms / columns;
     if (want > S) want = S;
     m.per = (int32_t)((S + want - 1) / want);
     chains = (S + m.per - 1) / m.per;
   } else {
     m.split = 1;
-    const int64_t want = (4 * sms + columns - 1) / columns;
+    const int64_t want = 4 * sms / columns;        // all of them resident at once: one block more would be a second round
     int64_t per = (T + want - 1) / want;
     per = (per + rows - 1) / rows * rows;
     if (per < 2 * rows) per = 2 * rows;

@@ -49,7 +49,7 @@ struct Args {
   lsgd_scan_desc d;
   SeqView q;
   int32_t chains, per;       // chains of a worker; sequences of a chain, or (split) rows
-  int32_t split, wide;       // wide: every row can be moved 8 values at a time
+  int32_t split, wide;       // wide: values that every row can be moved at a time (8, 4, 2 or 1)
   int32_t wide_bc;           // rows of b and c can be moved 4 values at a time
   uint32_t tiles;            // blocks of channels
   float* ends;               // split: [P][chains][D][N], what a chain adds, then the state (adjoint) it starts from
@@ -102,46 +102,53 @@ __device__ __forceinline__ float2 sigmoid(float2 v) {
 }
 __device__ __forceinline__ float sigmoid(float v) { return sigmoid(both(v)).x; }
 
-// 8 neighbouring channels of a row; those behind the last are zeros.
+// 8 neighbouring channels of a row, `width` (8, 4, 2 or 1) at a time; those behind the last are zeros.
+template <typename T, int W>
+__device__ __forceinline__ void load_by(float (&f)[8], const T* row, int ch, int D) {
+#pragma unroll
+  for (int v = 0; v < 8; v += W) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) f[v + k] = 0.f;
+    if (ch + v < D) {
+      Pack<T, W> k;
+      k.load(row + ch + v);
+      k.get(f + v);
+    }
+  }
+}
 template <typename T>
-__device__ __forceinline__ void load8(Pack<T, 8>& k, const T* row, int ch, int D, bool wide) {
-  if (wide) {
+__device__ __forceinline__ void load8(Pack<T, 8>& k, const T* row, int ch, int D, int width) {
+  if (width == 8) {
     k.load(row + ch);
     return;
   }
   float f[8];
-#pragma unroll
-  for (int v = 0; v < 8; ++v) {
-    Pack<T, 1> one;
-    f[v] = 0.f;
-    if (ch + v < D) {
-      one.load(row + ch + v);
-      one.get(f + v);
-    }
-  }
+  if (width == 4) load_by<T, 4>(f, row, ch, D);
+  else if (width == 2) load_by<T, 2>(f, row, ch, D);
+  else load_by<T, 1>(f, row, ch, D);
   k.set(f);
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_by(const float (&f)[8], T* row, int ch, int D) {
+#pragma unroll
+  for (int v = 0; v < 8; v += W)
+    if (ch + v < D) {
+      Pack<T, W> k;
+      k.set(f + v);
+      k.store(row + ch + v);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(const float (&f)[8], T* row, int ch, int D, int width) {
+  if (width == 8) store_by<T, 8>(f, row, ch, ch + 8);
+  else if (width == 4) store_by<T, 4>(f, row, ch, D);
+  else if (width == 2) store_by<T, 2>(f, row, ch, D);
+  else store_by<T, 1>(f, row, ch, D);
 }
 __device__ __forceinline__ void pairs8(const float (&f)[8], float2 (&q)[4]) {
 #pragma unroll
   for (int v = 0; v < 4; ++v) q[v] = make_float2(f[2 * v], f[2 * v + 1]);
 }
-template <typename T>
-__device__ __forceinline__ void store8(const float (&f)[8], T* row, int ch, int D, bool wide) {
-  if (wide) {
-    Pack<T, 8> k;
-    k.set(f);
-    k.store(row + ch);
-    return;
-  }
-#pragma unroll
-  for (int v = 0; v < 8; ++v)
-    if (ch + v < D) {
-      Pack<T, 1> one;
-      one.set(f + v);
-      one.store(row + ch + v);
-    }
-}
-
 // A log2(e) of 4 states of a channel; 0 for those that do not exist (they stay zero, for B is zero there)
 __device__ __forceinline__ void decay_rates(const Args& a, int p, int ch, int n0, float (&A2)[kQuad]) {
 #pragma unroll
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
   const int prow = threadIdx.x / (Ti::kCh / 8), piece = (threadIdx.x % (Ti::kCh / 8)) * 8;
   const int pch = blockIdx.x * Ti::kCh + piece;
   const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
-  const bool wide = a.wide;
+  const int wide = a.wide;
   const Rows<T> x = view<T>(d.x), dt = view<T>(d.dt), z = view<T>(d.z), out = view<T>(d.out);
   float2 bias[4], skip[4];
   load_vector8(d.dt_bias, p, pch, has_piece ? d.D : 0, bias);
@@ -564,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
   const int prow = threadIdx.x / (Ti::kCh / 8), piece = (threadIdx.x % (Ti::kCh / 8)) * 8;
   const int pch = blockIdx.x * Ti::kCh + piece;
   const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
-  const bool wide = a.wide;
+  const int wide = a.wide;
   const Rows<T> dt = view<T>(d.dt), z = view<T>(d.z), up = view<T>(d.d_out);
   float2 bias[4];
   load_vector8(d.dt_bias, p, pch, has_piece ? d.D : 0, bias);
@@ -726,13 +733,13 @@ __global__ void __launch_bounds__(kThreads, 4) backward_kernel(const __grid_cons
   bool live = false, plain = false;
   auto fetch8 = [&](Pack<T, 8>* to, const lsgd_rows& m, int t) {
     const T* src = view<T>(m).row(p, t);
-    if (a.wide) {
+    if (a.wide == 8) {
 #pragma unroll
       for (int k = 0; k < (int)sizeof(Pack<T, 8>); k += 16)
         copy_async(reinterpret_cast<char*>(to) + k, reinterpret_cast<const char*>(src + pch) + k, 16);
     } else {
       Pack<T, 8> k;
-      load8<T>(k, src, pch, d.D, false);
+      load8<T>(k, src, pch, d.D, a.wide);
       *to = k;
     }
   };

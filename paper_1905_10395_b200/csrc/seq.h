@@ -24,6 +24,29 @@ struct SeqView {
     const int v = starts[p * stride + s];
     return v < 0 ? 0 : v > T ? T : v;
   }
+  // The rows around row t that are of one sequence, or of none (code -1).
+  struct Span {
+    int code, lo, hi;
+  };
+  __device__ __forceinline__ Span span(int p, int t) const {
+    Span s;
+    if (!starts) {
+      s.code = t / len;
+      s.lo = s.code * len;
+      s.hi = s.lo + len;
+    } else {
+      s.code = codes[(int64_t)p * T + t];
+      if (s.code >= 0) {
+        s.lo = edge(p, s.code);
+        s.hi = max(edge(p, s.code + 1), t + 1);
+      } else {
+        const int first = edge(p, 0);
+        s.lo = t < first ? 0 : t;
+        s.hi = t < first ? first : T;
+      }
+    }
+    return s;
+  }
 };
 
 inline lsgd_status check_sequences(const lsgd_sequences& q, int64_t P, int64_t T) {
