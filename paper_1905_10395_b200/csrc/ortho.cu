@@ -10,7 +10,10 @@
 //
 // Operands are fp16 times 2^10, sums fp32.  Entries of X and G are below 2 (singular values stay below 1.3 with the usual
 // coefficients) and those that matter are not below 2^-13 of their matrix's largest, so fp16's range holds them and its 11 bits
-// lose an eighth of what bf16's 8 would.
+// lose an eighth of what bf16's 8 would.  The first X's rounding is amplified by every later step where singular values are small:
+// for matrices of at most kTwofoldRows rows it is kept as two such numbers, of which the first step's last product takes both.  The
+// whole chain is then off by at most 1.6e-3 of the result's norm instead of 2e-3 (300 x 300; 16 x 16: 1.4e-3 instead of 3.7e-3),
+// rounding to bf16 by 1.7e-3.  Larger matrices are off by less (1024 x 1024: 1.6e-3 to 1.8e-3), and would take 6 to 11 % longer.
 //
 // product_kernel is a persistent kernel of one CTA an SM on 128 x 128 tiles, or of pairs of CTAs on 256 x 256, with the roles of the
 // batched product of gemm_tc.cu: one thread fetches operands by tiled bulk copies into a ring, one issues tcgen05.mma into one of two
@@ -32,6 +35,7 @@ constexpr float kScale = 1024.f;                 // of X, G and Q as stored
 constexpr int BM = 128, BN = 128, BK = 64, kStages = 5;
 constexpr int kBoxBytes = 64 * 64 * 2, kStageBytes = (BM + BN) * BK * 2, kTileBytes = BM * BN * 2;
 constexpr int kSmemBytes = kStages * kStageBytes + 2 * kTileBytes + 1024;
+constexpr int kTwofoldRows = 768;
 constexpr int kEpiWarps = 8, kThreads = 96 + 32 * kEpiWarps;    // operands, products, the added tile; the epilogue
 
 // ------------------------------------------------------------------------------------------------ momentum and norm
@@ -39,7 +43,7 @@ struct Prep {
   lsgd_ortho_desc d;
   double* part;              // [P][blocks] sums of squares
   uint32_t blocks;
-  __half* x;                 // [P][r][ld]
+  __half *x, *lo;            // [P][r][ld]: X and what it was rounded by
   int32_t r, n, tall;        // rows and columns of X; tall: X is the matrix transposed
   int64_t ld, stride;
 };
@@ -93,12 +97,16 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prep 
   }
 }
 
-// 1 / (|U| + eps); 0 for a zero matrix, NaN where a value is not finite.
+// 1 / (|U| + eps) from the sum of squares; 0 for a zero matrix, NaN where a value is not finite.
+__device__ __forceinline__ float inverse_of(double sum, float eps) {
+  const double t = sqrt(sum) + (double)eps;
+  return t > 0.0 && t < 1e300 ? (float)fmin(1.0 / t, 1e35) : t == 0.0 ? 0.f : __int_as_float(0x7FC00000);
+}
 __device__ __forceinline__ float inverse_norm(const Prep& a, int p) {
   __shared__ float s;
   if (threadIdx.x < 32) {
-    const double t = sqrt(warp_sum_fixed(a.part + (int64_t)p * a.blocks, a.blocks)) + (double)a.d.eps;
-    if (threadIdx.x == 0) s = t > 0.0 && t < 1e300 ? (float)fmin(1.0 / t, 3e38) : t == 0.0 ? 0.f : __int_as_float(0x7FC00000);
+    const float t = inverse_of(warp_sum_fixed(a.part + (int64_t)p * a.blocks, a.blocks), a.d.eps);
+    if (threadIdx.x == 0) s = t;
   }
   __syncthreads();
   return s;
@@ -128,20 +136,21 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
     }
     return;
   }
-  __half* x = a.x + p * a.stride;
   for (int i = threadIdx.x; i < 64 * 8; i += 256) {
     const int row = i / 8, col = i % 8 * 8;                                  // of X within its tile
     const int xr = (a.tall ? c0 : r0) + row, xc = (a.tall ? r0 : c0) + col;
     if (xr >= a.r || xc >= a.ld) continue;
-    uint4 w;
-    __half2* h = reinterpret_cast<__half2*>(&w);
+    uint4 hi, lo;
+    __half2 *h = reinterpret_cast<__half2*>(&hi), *l = reinterpret_cast<__half2*>(&lo);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const float f0 = a.tall ? tile[col + 2 * v][row] : tile[row][col + 2 * v];
-      const float f1 = a.tall ? tile[col + 2 * v + 1][row] : tile[row][col + 2 * v + 1];
-      h[v] = __floats2half2_rn(f0 * kScale, f1 * kScale);
+      const float f0 = kScale * (a.tall ? tile[col + 2 * v][row] : tile[row][col + 2 * v]);
+      const float f1 = kScale * (a.tall ? tile[col + 2 * v + 1][row] : tile[row][col + 2 * v + 1]);
+      h[v] = __floats2half2_rn(f0, f1);
+      l[v] = __floats2half2_rn(f0 - __low2float(h[v]), f1 - __high2float(h[v]));
     }
-    *reinterpret_cast<uint4*>(x + xr * a.ld + xc) = w;
+    *reinterpret_cast<uint4*>(a.x + p * a.stride + xr * a.ld + xc) = hi;
+    if (a.lo) *reinterpret_cast<uint4*>(a.lo + p * a.stride + xr * a.ld + xc) = lo;
   }
 }
 
@@ -151,6 +160,7 @@ struct Product {
   int b_mn;                  // B is stored [K][N] (else [N][K])
   int symmetric;             // square: tiles on and above the diagonal, stored twice
   int add;                   // C = alpha acc + beta D + diag I
+  int twofold;               // C = A B + A D, D of B's layout (instead of an added tile)
   float alpha, beta, diag;
   __nv_bfloat16* out;        // last product: bf16 rows instead of C, times scale
   int64_t out_ld, out_stride;
@@ -204,7 +214,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)cluster_rank() : 0;
   const int mt = (p.M + kTile - 1) / kTile, nt = (p.N + kTile - 1) / kTile, per = p.symmetric ? nt * (nt + 1) / 2 : mt * nt;
-  const int n_tiles = per * p.batch, nk = (p.K + BK - 1) / BK;
+  const int n_tiles = per * p.batch, nk1 = (p.K + BK - 1) / BK, nk = p.twofold ? 2 * nk1 : nk1;
   const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, stride = PAIR ? gridDim.x >> 1 : gridDim.x;
   uint32_t* status = &g_status;
   if (threadIdx.x == 0) {
@@ -256,7 +266,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (!ok) break;
         uint8_t* sa = smem + s * kStageBytes;
         uint8_t* sb = sa + BM * BK * 2;
-        const int k0 = kt * BK;
+        const int k0 = (kt < nk1 ? kt : kt - nk1) * BK;
+        const CUtensorMap* from_b = kt < nk1 ? &map_b : &map_d;
         if (rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * kStageBytes);
         const uint32_t bar = PAIR ? map_to_rank(smem_u32(&full_bar[s]), 0) : 0;
 #pragma unroll
@@ -264,10 +275,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           const int bx = p.b_mn ? n0 + 64 * j : k0, by = p.b_mn ? k0 : n0 + 64 * j;
           if (PAIR) {
             tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, k0, m0 + 64 * j, q.z);
-            tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, bx, by, q.z);
+            tma_load_3d_pair(sb + j * kBoxBytes, from_b, bar, bx, by, q.z);
           } else {
             tma_load_3d(sa + j * kBoxBytes, &map_a, &full_bar[s], k0, m0 + 64 * j, q.z);
-            tma_load_3d(sb + j * kBoxBytes, &map_b, &full_bar[s], bx, by, q.z);
+            tma_load_3d(sb + j * kBoxBytes, from_b, &full_bar[s], bx, by, q.z);
           }
         }
       }
@@ -471,6 +482,209 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   }
 }
 
+// ------------------------------------------------------------------------------------------------ small matrices
+// X of at most 128 x 256 (and G, Q): one block a matrix does everything in one launch.  Operands stay in shared memory as the tensor
+// cores read them: 64 columns a box, 128 rows of 128 bytes, 128-byte swizzle.  The same box serves as rows of a K-major operand (G = X
+// X^T) and as the K index of an MN-major one (Q X).  A product is issued by one thread, everybody waits for it and takes part
+// in the epilogue; what bounds it is that chain of latencies, about 1 us a product.
+constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallParts = kSmallThreads / 128;
+constexpr int kSmallBox = kSmallRows * 128;
+
+__device__ __forceinline__ int small_at(int row, int col) { return (col >> 6) * kSmallBox + (int)swz(row, (col & 63) >> 3) + (col & 7) * 2; }
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_constant__ Prep a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sx = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int boxes = (a.n + 63) / 64;
+  uint8_t *slo = sx + boxes * kSmallBox, *sg = slo + boxes * kSmallBox, *sq = sg + 2 * kSmallBox;
+  __shared__ uint64_t bar;
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_s;
+  __shared__ double warp_sums[kSmallThreads / 32];
+  const int p = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr uint32_t kTmemCols = 512;            // 128 of G and Q, 256 of X
+  if (threadIdx.x == 0) {
+    abort_s = 0;
+    mbar_init(&bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  for (int i = threadIdx.x; i < (2 * boxes + 4) * kSmallBox / 16; i += kSmallThreads) reinterpret_cast<uint4*>(sx)[i] = make_uint4(0, 0, 0, 0);
+  pdl_wait();
+  pdl_launch_dependents();
+  // momentum and norm; the update stays in registers
+  constexpr int kMost = kSmallRows * kSmallCols / VEC / kSmallThreads;
+  const int per = a.d.n / VEC, pieces = a.d.m * per;
+  float u[kMost][VEC];
+  double sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = threadIdx.x + k * kSmallThreads;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) u[k][v] = 0.f;
+    if (i < pieces) update_of<T, VEC>(a, p, i / per, i % per * VEC, true, u[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kMost; ++k)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sum = fma((double)u[k][v], (double)u[k][v], sum);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (lane == 0) warp_sums[warp] = sum;
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_s;
+  double total = 0.0;
+  for (int w = 0; w < kSmallThreads / 32; ++w) total += warp_sums[w];
+  const float inv = inverse_of(total, a.d.eps) * kScale;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = threadIdx.x + k * kSmallThreads;
+    if (i >= pieces) break;
+    const int row = i / per, col = i % per * VEC;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float f = u[k][v] * inv;
+      const int at = a.tall ? small_at(col + v, row) : small_at(row, col + v);
+      const __half h = __float2half_rn(f);
+      *reinterpret_cast<__half*>(sx + at) = h;
+      *reinterpret_cast<__half*>(slo + at) = __float2half_rn(f - __half2float(h));
+    }
+  }
+  // the products' shapes, padded with the zeros above to what an instruction takes
+  const int rows16 = (a.r + 15) / 16, cols16 = (a.n + 15) / 16;
+  const uint32_t idesc = (1u << 4) | ((uint32_t)(rows16 * 2) << 17) | ((uint32_t)(kSmallRows >> 4) << 24);
+  const uint32_t idesc_x = (1u << 4) | (1u << 16) | ((uint32_t)(cols16 * 2) << 17) | ((uint32_t)(kSmallRows >> 4) << 24);
+  const uint32_t ax = smem_u32(sx), alo = smem_u32(slo), ag = smem_u32(sg), aq = smem_u32(sq);
+  const int q4 = warp & 3, part = warp >> 2, row = q4 * 32 + lane;
+  const uint32_t tg = tmem, tx = tmem + 128, quarter = (uint32_t)(q4 * 32) << 16;
+  uint32_t phase = 0;
+  // shared memory and tensor memory as everybody has left them -> one thread's products -> everybody
+  auto product = [&](auto issue) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      issue();
+      mma_commit(&bar);
+    }
+    const bool ok = mbar_wait(&bar, phase, &abort_s, &g_status);
+    phase ^= 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    return ok;
+  };
+  bool ok = true;
+  for (int step = 0; step < a.d.steps; ++step) {
+    ok = product([&] {
+      for (int k = 0; k < cols16; ++k) {
+        const uint64_t d = smem_desc(ax + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
+        mma_bf16(tg, d, d, idesc, k > 0);
+      }
+    });
+    if (__syncthreads_or(!ok)) break;
+    for (int c = part * 32; c < rows16 * 16; c += 32 * kSmallParts) {
+      uint32_t r[32];
+      tmem_ld32(tg + quarter + c, r);
+      asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint4 w;
+        w.x = half_pair(__uint_as_float(r[8 * u]) * (1 / kScale), __uint_as_float(r[8 * u + 1]) * (1 / kScale));
+        w.y = half_pair(__uint_as_float(r[8 * u + 2]) * (1 / kScale), __uint_as_float(r[8 * u + 3]) * (1 / kScale));
+        w.z = half_pair(__uint_as_float(r[8 * u + 4]) * (1 / kScale), __uint_as_float(r[8 * u + 5]) * (1 / kScale));
+        w.w = half_pair(__uint_as_float(r[8 * u + 6]) * (1 / kScale), __uint_as_float(r[8 * u + 7]) * (1 / kScale));
+        if (c + 8 * u < rows16 * 16) *reinterpret_cast<uint4*>(sg + small_at(row, c + 8 * u)) = w;
+      }
+    }
+    ok = product([&] {
+      for (int k = 0; k < rows16; ++k) {
+        const uint64_t d = smem_desc(ag + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
+        mma_bf16(tg, d, d, idesc, k > 0);
+      }
+    });
+    if (__syncthreads_or(!ok)) break;
+    for (int c = part * 32; c < rows16 * 16; c += 32 * kSmallParts) {
+      uint32_t r[32];
+      tmem_ld32(tg + quarter + c, r);
+      asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (c + 8 * u >= rows16 * 16) continue;
+        const uint4 g = *reinterpret_cast<const uint4*>(sg + small_at(row, c + 8 * u));
+        const __half2* h = reinterpret_cast<const __half2*>(&g);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = __half22float2(h[j]);
+          v[2 * j] = fmaf(a.d.b, f.x, a.d.c * (1 / kScale) * __uint_as_float(r[8 * u + 2 * j]));
+          v[2 * j + 1] = fmaf(a.d.b, f.y, a.d.c * (1 / kScale) * __uint_as_float(r[8 * u + 2 * j + 1]));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + 8 * u + j == row && row < a.r) v[j] += a.d.a * kScale;
+        *reinterpret_cast<uint4*>(sq + small_at(row, c + 8 * u)) =
+            make_uint4(half_pair(v[0], v[1]), half_pair(v[2], v[3]), half_pair(v[4], v[5]), half_pair(v[6], v[7]));
+      }
+    }
+    ok = product([&] {
+      for (int twice = 0; twice < (step == 0 ? 2 : 1); ++twice)
+        for (int k = 0; k < rows16; ++k) {
+          const uint64_t da = smem_desc(aq + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
+          mma_bf16(tx, da, smem_desc((twice ? alo : ax) + k * 2048, kSmallBox, 1024), idesc_x, (k | twice) > 0);
+        }
+    });
+    if (__syncthreads_or(!ok)) break;
+    const bool last = step + 1 == a.d.steps;
+    const float down = last ? a.d.scale / kScale / kScale : 1 / kScale;
+    for (int c = part * 32; c < cols16 * 16; c += 32 * kSmallParts) {
+      uint32_t r[32];
+      tmem_ld32(tx + quarter + c, r);
+      asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+      if (last) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.d.out.data) + p * a.d.out.stride;
+        if (row < a.r) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (c + j < a.n) o[a.tall ? (c + j) * a.d.out.ld + row : row * a.d.out.ld + c + j] = __float2bfloat16_rn(__uint_as_float(r[j]) * down);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint4 w;
+        w.x = half_pair(__uint_as_float(r[8 * u]) * down, __uint_as_float(r[8 * u + 1]) * down);
+        w.y = half_pair(__uint_as_float(r[8 * u + 2]) * down, __uint_as_float(r[8 * u + 3]) * down);
+        w.z = half_pair(__uint_as_float(r[8 * u + 4]) * down, __uint_as_float(r[8 * u + 5]) * down);
+        w.w = half_pair(__uint_as_float(r[8 * u + 6]) * down, __uint_as_float(r[8 * u + 7]) * down);
+        if (c + 8 * u < cols16 * 16) *reinterpret_cast<uint4*>(sx + small_at(row, c + 8 * u)) = w;
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 0) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+template <typename T, int VEC>
+cudaError_t launch_small(const Prep& a, cudaStream_t s) {
+  static OncePerDevice attr;
+  const auto bytes = [](int n) { return (2 * ((n + 63) / 64) + 4) * kSmallBox + 1024; };
+  if (!attr.here()) {
+    const cudaError_t e = cudaFuncSetAttribute(small_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(kSmallCols));
+    if (e != cudaSuccess) return e;
+    attr.here() = true;
+  }
+  return launch_pdl(small_kernel<T, VEC>, dim3(a.d.P), dim3(kSmallThreads), (size_t)bytes(a.n), s, a);
+}
+
 // ------------------------------------------------------------------------------------------------ host
 lsgd_status check_ortho(const lsgd_ortho_desc* d) {
   if (!d || d->struct_size != sizeof(lsgd_ortho_desc)) return LSGD_ERR_INVALID_ARG;
@@ -492,7 +706,9 @@ struct Plan {
   int r, n;                  // rows and columns of X
   int64_t ldx, ldg;
   uint32_t blocks;
-  uint64_t part, x0, x1, g, q, total;
+  bool small;                // one block a matrix
+  bool twofold;              // the first X as two fp16 numbers
+  uint64_t part, x0, x1, lo, g, q, total;
 };
 Plan plan_of(const lsgd_ortho_desc* d) {
   Plan m{};
@@ -508,11 +724,15 @@ Plan plan_of(const lsgd_ortho_desc* d) {
     at += (bytes + 255) & ~uint64_t(255);
     return here;
   };
+  m.small = m.r <= kSmallRows && m.n <= kSmallCols && d->steps > 0;
+  if (m.small) return m;
+  m.twofold = m.r <= kTwofoldRows;
   m.part = take(sizeof(double) * (uint64_t)d->P * m.blocks);
   if (d->steps > 0) {
     const uint64_t x = 2 * (uint64_t)d->P * m.r * m.ldx, g = 2 * (uint64_t)d->P * m.r * m.ldg;
     m.x0 = take(x);
     if (d->steps > 1) m.x1 = take(x);
+    if (m.twofold) m.lo = take(x);
     m.g = take(g);
     m.q = take(g);
   }
@@ -580,6 +800,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   a.part = reinterpret_cast<double*>(scratch + m.part);
   a.blocks = m.blocks;
   a.x = reinterpret_cast<__half*>(scratch + m.x0);
+  a.lo = m.twofold ? reinterpret_cast<__half*>(scratch + m.lo) : nullptr;
   a.r = m.r;
   a.n = m.n;
   a.tall = d->m > d->n;
@@ -590,7 +811,12 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     return !r.data || (d->n % 4 == 0 && reinterpret_cast<uintptr_t>(r.data) % (4 * bytes) == 0 && (d->m <= 1 || r.ld % 4 == 0) && (d->P <= 1 || r.stride % 4 == 0));
   };
   const int vec = fits(d->grad, gb) && fits(d->momentum, 4) ? 4 : 1;
-  cudaError_t e = d->grad_dtype == LSGD_BF16 ? launch_prep<__nv_bfloat16>(a, vec, s) : launch_prep<float>(a, vec, s);
+  cudaError_t e = cudaSuccess;
+  if (m.small)
+    e = d->grad_dtype == LSGD_BF16 ? (vec == 4 ? launch_small<__nv_bfloat16, 4>(a, s) : launch_small<__nv_bfloat16, 1>(a, s))
+                                   : (vec == 4 ? launch_small<float, 4>(a, s) : launch_small<float, 1>(a, s));
+  if (m.small) return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
+  e = d->grad_dtype == LSGD_BF16 ? launch_prep<__nv_bfloat16>(a, vec, s) : launch_prep<float>(a, vec, s);
   if (e != cudaSuccess) return LSGD_ERR_CUDA;
   void* x[2] = {scratch + m.x0, scratch + m.x1};
   void *g = scratch + m.g, *q = scratch + m.q;
@@ -599,8 +825,8 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     const void* from = x[step & 1];
     void* to = x[(step & 1) ^ 1];
     const bool last = step + 1 == d->steps;
-    CUtensorMap x_op, g_op, q_op, g_tile, q_tile, to_tile;
-    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
+    CUtensorMap x_op, lo_op, g_op, q_op, g_tile, q_tile, to_tile;
+    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&lo_op, m.twofold ? scratch + m.lo : from, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
         !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) ||
         !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P) ||
         !tile_map(&to_tile, last ? from : to, m.n, m.r, m.ldx, d->P))
@@ -622,6 +848,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.symmetric = 0;
     p.b_mn = 1;
     p.add = 0;
+    p.twofold = step == 0 && m.twofold;
     p.alpha = down;
     if (last) {
       p.out = static_cast<__nv_bfloat16*>(d->out.data);
@@ -631,7 +858,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
       p.out_wide = row_vec(d->out, d->P, d->m, d->n, 2) == 8;
       p.scale = d->scale * down;
     }
-    if (launch_product(q_op, x_op, to_tile, to_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(q_op, x_op, to_tile, lo_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
   }
   return LSGD_OK;
 }
