@@ -45,29 +45,38 @@ struct Prep {
   uint32_t blocks;
   __half *x, *lo;            // [P][r][ld]: X and what it was rounded by
   int32_t r, n, tall;        // rows and columns of X; tall: X is the matrix transposed
+  int32_t out_wide;          // out's rows can be written 8 values at a time
   int64_t ld, stride;
 };
 
+// A piece of the update: its gradient and momentum, and what becomes of them.
 template <typename T, int VEC>
-__device__ __forceinline__ void update_of(const Prep& a, int p, int row, int col, bool write, float (&u)[VEC]) {
+struct Piece {
   Pack<T, VEC> g;
-  g.load(Rows<T>{static_cast<T*>(a.d.grad.data), a.d.grad.ld, a.d.grad.stride}.row(p, row) + col);
-  g.get(u);
-  if (!a.d.momentum.data) return;
-  float* at = Rows<float>{static_cast<float*>(a.d.momentum.data), a.d.momentum.ld, a.d.momentum.stride}.row(p, row) + col;
-  Pack<float, VEC> k;
-  float m[VEC];
-  k.load(at);
-  k.get(m);
-  if (write) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) m[v] = fmaf(a.d.mu, m[v], u[v]);
-    k.set(m);
-    k.store(at);
+  Pack<float, VEC> m;
+  __device__ __forceinline__ void load(const Prep& a, int p, int row, int col) {
+    g.load(Rows<T>{static_cast<T*>(a.d.grad.data), a.d.grad.ld, a.d.grad.stride}.row(p, row) + col);
+    if (a.d.momentum.data) m.load(momentum(a, p, row, col));
   }
+  // u: the update; `step`: the momentum moves first, and is written
+  __device__ __forceinline__ void update(const Prep& a, int p, int row, int col, bool step, float (&u)[VEC]) {
+    g.get(u);
+    if (!a.d.momentum.data) return;
+    float v[VEC];
+    m.get(v);
+    if (step) {
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) u[v] = a.d.nesterov ? fmaf(a.d.mu, m[v], u[v]) : m[v];
-}
+      for (int k = 0; k < VEC; ++k) v[k] = fmaf(a.d.mu, v[k], u[k]);
+      m.set(v);
+      m.store(momentum(a, p, row, col));
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) u[k] = a.d.nesterov ? fmaf(a.d.mu, v[k], u[k]) : v[k];
+  }
+  static __device__ __forceinline__ float* momentum(const Prep& a, int p, int row, int col) {
+    return Rows<float>{static_cast<float*>(a.d.momentum.data), a.d.momentum.ld, a.d.momentum.stride}.row(p, row) + col;
+  }
+};
 
 // The momentum's step, and every block's sum of squares of the update: in 64 bits, since squares of small gradients leave fp32's range.
 template <typename T, int VEC>
@@ -78,12 +87,24 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prep 
   const uint32_t per = (a.d.n + VEC - 1) / VEC;
   const int64_t pieces = (int64_t)a.d.m * per;
   double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
-    const int row = (int)((uint32_t)i / per), col = (int)((uint32_t)i % per) * VEC;
-    float u[VEC];
-    update_of<T, VEC>(a, p, row, col, true, u);
+  constexpr int kTake = 4;           // pieces fetched before the first is used
+  const int64_t apart = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += kTake * apart) {
+    Piece<T, VEC> piece[kTake];
+    int row[kTake], col[kTake];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) s = fma((double)u[v], (double)u[v], s);
+    for (int k = 0; k < kTake; ++k) {
+      row[k] = (int)((uint32_t)(i + k * apart) / per), col[k] = (int)((uint32_t)(i + k * apart) % per) * VEC;
+      if (i + k * apart < pieces) piece[k].load(a, p, row[k], col[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kTake; ++k) {
+      if (i + k * apart >= pieces) break;
+      float u[VEC];
+      piece[k].update(a, p, row[k], col[k], true, u);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) s = fma((double)u[v], (double)u[v], s);
+    }
   }
   __shared__ double warps[8];
 #pragma unroll
@@ -120,12 +141,23 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
   const int p = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;       // of the matrix as given
   const float inv = inverse_norm(a, p);
   __shared__ float tile[64][65];
-  for (int i = threadIdx.x; i < 64 * (64 / VEC); i += 256) {
-    const int row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
-    float u[VEC] = {};
-    if (r0 + row < a.d.m && c0 + col < a.d.n) update_of<T, VEC>(a, p, r0 + row, c0 + col, false, u);
+  constexpr int kPieces = 64 * (64 / VEC) / 256, kTake = kPieces < 8 ? kPieces : 8;
+#pragma unroll 1
+  for (int k0 = 0; k0 < kPieces; k0 += kTake) {
+    Piece<T, VEC> piece[kTake];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) tile[row][col + v] = u[v] * inv;
+    for (int k = 0; k < kTake; ++k) {
+      const int i = threadIdx.x + (k0 + k) * 256, row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
+      if (r0 + row < a.d.m && c0 + col < a.d.n) piece[k].load(a, p, r0 + row, c0 + col);
+    }
+#pragma unroll
+    for (int k = 0; k < kTake; ++k) {
+      const int i = threadIdx.x + (k0 + k) * 256, row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
+      float u[VEC] = {};
+      if (r0 + row < a.d.m && c0 + col < a.d.n) piece[k].update(a, p, r0 + row, c0 + col, false, u);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) tile[row][col + v] = u[v] * inv;
+    }
   }
   __syncthreads();
   if (a.d.steps == 0) {
@@ -490,6 +522,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallParts = kSmallThreads / 128;
 constexpr int kSmallBox = kSmallRows * 128;
 
+__device__ __forceinline__ uint32_t two(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
 __device__ __forceinline__ int small_at(int row, int col) { return (col >> 6) * kSmallBox + (int)swz(row, (col & 63) >> 3) + (col & 7) * 2; }
 
 template <typename T, int VEC>
@@ -521,12 +554,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   const int per = a.d.n / VEC, pieces = a.d.m * per;
   float u[kMost][VEC];
   double sum = 0.0;
+  constexpr int kTake = 8;                       // pieces fetched before the first is used
 #pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-    const int i = threadIdx.x + k * kSmallThreads;
+  for (int k0 = 0; k0 < kMost; k0 += kTake) {
+    Piece<T, VEC> piece[kTake];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) u[k][v] = 0.f;
-    if (i < pieces) update_of<T, VEC>(a, p, i / per, i % per * VEC, true, u[k]);
+    for (int k = 0; k < kTake; ++k) {
+      const int i = threadIdx.x + (k0 + k) * kSmallThreads;
+      if (i < pieces) piece[k].load(a, p, i / per, i % per * VEC);
+    }
+#pragma unroll
+    for (int k = 0; k < kTake; ++k) {
+      const int i = threadIdx.x + (k0 + k) * kSmallThreads;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) u[k0 + k][v] = 0.f;
+      if (i < pieces) piece[k].update(a, p, i / per, i % per * VEC, true, u[k0 + k]);
+    }
   }
 #pragma unroll
   for (int k = 0; k < kMost; ++k)
@@ -547,13 +590,23 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
     const int i = threadIdx.x + k * kSmallThreads;
     if (i >= pieces) break;
     const int row = i / per, col = i % per * VEC;
+    __half hi[VEC], lo[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       const float f = u[k][v] * inv;
-      const int at = a.tall ? small_at(col + v, row) : small_at(row, col + v);
-      const __half h = __float2half_rn(f);
-      *reinterpret_cast<__half*>(sx + at) = h;
-      *reinterpret_cast<__half*>(slo + at) = __float2half_rn(f - __half2float(h));
+      hi[v] = __float2half_rn(f);
+      lo[v] = __float2half_rn(f - __half2float(hi[v]));
+    }
+    if (VEC == 4 && !a.tall) {
+      *reinterpret_cast<uint2*>(sx + small_at(row, col)) = make_uint2(two(hi[0], hi[VEC > 1]), two(hi[VEC / 2], hi[VEC - 1]));
+      *reinterpret_cast<uint2*>(slo + small_at(row, col)) = make_uint2(two(lo[0], lo[VEC > 1]), two(lo[VEC / 2], lo[VEC - 1]));
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const int at = a.tall ? small_at(col + v, row) : small_at(row, col + v);
+        *reinterpret_cast<__half*>(sx + at) = hi[v];
+        *reinterpret_cast<__half*>(slo + at) = lo[v];
+      }
     }
   }
   // the products' shapes, padded with the zeros above to what an instruction takes
@@ -648,7 +701,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
       if (last) {
         __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.d.out.data) + p * a.d.out.stride;
-        if (row < a.r) {
+        if (row < a.r && !a.tall && a.out_wide) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (c + 8 * u < a.n) {
+              float f[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(r[8 * u + j]) * down;
+              Pack<__nv_bfloat16, 8> k;
+              k.set(f);
+              k.store(o + row * a.d.out.ld + c + 8 * u);
+            }
+        } else if (row < a.r) {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
             if (c + j < a.n) o[a.tall ? (c + j) * a.d.out.ld + row : row * a.d.out.ld + c + j] = __float2bfloat16_rn(__uint_as_float(r[j]) * down);
@@ -804,6 +868,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   a.r = m.r;
   a.n = m.n;
   a.tall = d->m > d->n;
+  a.out_wide = row_vec(d->out, d->P, d->m, d->n, 2) == 8;
   a.ld = m.ldx;
   a.stride = m.ldx * m.r;
   const int gb = elem_bytes(d->grad_dtype);
@@ -855,7 +920,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
       p.out_ld = d->out.ld;
       p.out_stride = d->out.stride;
       p.out_transposed = a.tall;
-      p.out_wide = row_vec(d->out, d->P, d->m, d->n, 2) == 8;
+      p.out_wide = a.out_wide;
       p.scale = d->scale * down;
     }
     if (launch_product(q_op, x_op, to_tile, lo_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
