@@ -373,13 +373,15 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
   LSGD_ROWS(d->w, D, d->W, 4, false, false);
   LSGD_ROWS(d->bias, 1, D, 4, false, false);
   if (!backward) {
-    if (rows && (!d->out.data || d->out.data == d->x.data)) return LSGD_ERR_INVALID_ARG;
+    if (rows && !d->out.data) return LSGD_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(d->state) % ab) return LSGD_ERR_ALIGNMENT;
     LSGD_ROWS(d->out, T, D, ab, true, false);
-    return LSGD_OK;
+    const Extent ins[] = {extent(d->x, P, T, D, ab)};
+    const Extent outs[] = {extent(d->out, P, T, D, ab), extent({d->state, D, (int64_t)d->seq.S * (d->W - 1) * D}, P, (int64_t)d->seq.S * (d->W - 1), D, ab)};
+    return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
   }
   if (d->state) return LSGD_ERR_INVALID_ARG;
-  if (rows && (!d->d_out.data || !d->dx.data || d->dx.data == d->x.data || d->dx.data == d->d_out.data)) return LSGD_ERR_INVALID_ARG;
+  if (rows && (!d->d_out.data || !d->dx.data)) return LSGD_ERR_INVALID_ARG;
   if (!d->dw.data || (d->bias.data != nullptr) != (d->d_bias.data != nullptr)) return LSGD_ERR_INVALID_ARG;
   LSGD_ROWS(d->d_out, T, D, ab, false, false);
   LSGD_ROWS(d->dx, T, D, ab, true, false);
@@ -387,7 +389,9 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
   LSGD_ROWS(d->dw, D, d->W, 4, true, true);
   LSGD_ROWS(d->d_bias, 1, D, 4, true, true);
 #undef LSGD_ROWS
-  return LSGD_OK;
+  const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->d_out, P, T, D, ab), extent(d->w, P, D, d->W, 4), extent(d->bias, P, 1, D, 4)};
+  const Extent outs[] = {extent(d->dx, P, T, D, ab), extent(d->dw, P, D, d->W, 4), extent(d->d_bias, P, 1, D, 4)};
+  return all_apart(outs, 3, ins, 4) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
 // Four values a thread where every row allows it, else one.

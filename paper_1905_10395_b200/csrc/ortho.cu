@@ -758,12 +758,14 @@ lsgd_status check_ortho(const lsgd_ortho_desc* d) {
   if (d->grad_dtype < LSGD_F32 || d->grad_dtype > LSGD_BF16) return LSGD_ERR_INVALID_ARG;
   if (!(fabsf(d->a) <= 16.f) || !(fabsf(d->b) <= 16.f) || !(fabsf(d->c) <= 16.f)) return LSGD_ERR_INVALID_ARG;
   if (!(d->mu >= 0.f && d->mu < 1.f) || !(d->eps >= 0.f && d->eps < 1e30f) || !(d->scale - d->scale == 0.f)) return LSGD_ERR_INVALID_ARG;
-  if (!d->grad.data || !d->out.data || d->out.data == d->grad.data || d->momentum.data == d->grad.data || d->out.data == d->momentum.data)
-    return LSGD_ERR_INVALID_ARG;
+  if (!d->grad.data || !d->out.data) return LSGD_ERR_INVALID_ARG;
   lsgd_status st;
   if ((st = check_rows(d->grad, d->P, d->m, d->n, elem_bytes(d->grad_dtype), false)) != LSGD_OK) return st;
   if (d->momentum.data && (st = check_rows(d->momentum, d->P, d->m, d->n, 4, true)) != LSGD_OK) return st;
-  return check_rows(d->out, d->P, d->m, d->n, 2, true);
+  if ((st = check_rows(d->out, d->P, d->m, d->n, 2, true)) != LSGD_OK) return st;
+  const Extent ins[] = {extent(d->grad, d->P, d->m, d->n, elem_bytes(d->grad_dtype))};
+  const Extent outs[] = {extent(d->out, d->P, d->m, d->n, 2), extent(d->momentum, d->P, d->m, d->n, 4)};
+  return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
 struct Plan {

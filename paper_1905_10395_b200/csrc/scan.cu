@@ -90,24 +90,19 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   LSGD_ROWS(d->dt_bias, 1, D, 4, false, false);
   if ((reinterpret_cast<uintptr_t>(d->state) | reinterpret_cast<uintptr_t>(d->saved)) % 16) return LSGD_ERR_ALIGNMENT;
   if (!backward) {
-    const void* o = d->out.data;
-    if (rows && (!o || o == d->x.data || o == d->dt.data || o == d->z.data || o == d->b.data || o == d->c.data)) return LSGD_ERR_INVALID_ARG;
+    if (rows && !d->out.data) return LSGD_ERR_INVALID_ARG;
     LSGD_ROWS(d->out, T, D, ab, true, false);
-    return LSGD_OK;
+    const int64_t states = D * N, kept = (int64_t)d->seq.S, groups = (T + kGroup - 1) / kGroup;
+    const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->dt, P, T, D, ab), extent(d->z, P, T, D, ab), extent(d->b, P, T, N, ab), extent(d->c, P, T, N, ab)};
+    const Extent outs[] = {extent(d->out, P, T, D, ab), extent({d->state, states, kept * states}, P, kept, states, 4),
+                           extent({d->saved, states, groups * states}, P, groups, states, 4)};
+    return all_apart(outs, 3, ins, 5) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
   }
   if (d->state || (rows && (!d->saved || !d->d_out.data || !d->dx.data || !d->d_dt.data || !d->db.data || !d->dc.data))) return LSGD_ERR_INVALID_ARG;
   if (!d->d_a_log.data) return LSGD_ERR_INVALID_ARG;
   if ((rows && (d->z.data != nullptr) != (d->dz.data != nullptr)) || (d->skip.data != nullptr) != (d->d_skip.data != nullptr) ||
       (d->dt_bias.data != nullptr) != (d->d_dt_bias.data != nullptr))
     return LSGD_ERR_INVALID_ARG;
-  const void* ins[] = {d->x.data, d->dt.data, d->z.data, d->b.data, d->c.data, d->d_out.data};
-  const void* outs[] = {d->dx.data, d->d_dt.data, d->dz.data, d->db.data, d->dc.data};
-  for (int i = 0; i < 5; ++i) {
-    for (const void* in : ins)
-      if (outs[i] && outs[i] == in) return LSGD_ERR_INVALID_ARG;
-    for (int j = 0; j < i; ++j)
-      if (outs[i] && outs[i] == outs[j]) return LSGD_ERR_INVALID_ARG;
-  }
   LSGD_ROWS(d->d_out, T, D, ab, false, false);
   LSGD_ROWS(d->dx, T, D, ab, true, false);
   LSGD_ROWS(d->d_dt, T, D, ab, true, false);
@@ -118,7 +113,12 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   LSGD_ROWS(d->d_skip, 1, D, 4, true, true);
   LSGD_ROWS(d->d_dt_bias, 1, D, 4, true, true);
 #undef LSGD_ROWS
-  return LSGD_OK;
+  const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->dt, P, T, D, ab),   extent(d->z, P, T, D, ab),     extent(d->b, P, T, N, ab),
+                        extent(d->c, P, T, N, ab), extent(d->d_out, P, T, D, ab), extent(d->a_log, P, D, N, 4), extent(d->skip, P, 1, D, 4),
+                        extent(d->dt_bias, P, 1, D, 4)};
+  const Extent outs[] = {extent(d->dx, P, T, D, ab),     extent(d->d_dt, P, T, D, ab),  extent(d->dz, P, T, D, ab),    extent(d->db, P, T, N, ab),
+                         extent(d->dc, P, T, N, ab),     extent(d->d_a_log, P, D, N, 4), extent(d->d_skip, P, 1, D, 4), extent(d->d_dt_bias, P, 1, D, 4)};
+  return all_apart(outs, 8, ins, 9) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
 bool row_vec4(const lsgd_rows& r, int64_t P, int64_t T, int bytes) {

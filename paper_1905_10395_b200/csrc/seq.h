@@ -60,6 +60,47 @@ inline lsgd_status check_sequences(const lsgd_sequences& q, int64_t P, int64_t T
 inline SeqView seq_view(const lsgd_sequences& q, int64_t T, const int32_t* codes) {
   return SeqView{q.starts, q.stride, codes, q.S, (int32_t)T, q.starts ? 0 : (int32_t)(T / q.S)};
 }
+// A matrix of rows in memory, for the check that outputs overlap no input.
+struct Extent {
+  uintptr_t at, end;         // first byte, one behind the last
+  uint64_t ld, stride, width, block;     // in bytes; block: one worker's rows, from the first to the last
+};
+inline Extent extent(const lsgd_rows& r, int64_t P, int64_t T, int64_t D, int bytes) {
+  Extent e{};
+  if (!r.data || P < 1 || T < 1 || D < 1) return e;
+  e.at = reinterpret_cast<uintptr_t>(r.data);
+  e.ld = T > 1 ? (uint64_t)r.ld * bytes : 0;
+  e.stride = P > 1 ? (uint64_t)r.stride * bytes : 0;
+  e.width = (uint64_t)D * bytes;
+  e.block = (uint64_t)(T - 1) * e.ld + e.width;
+  e.end = e.at + (uint64_t)(P - 1) * e.stride + e.block;
+  return e;
+}
+// Whether pieces of `wa` and `wb` bytes, each set a multiple of `unit` apart, never meet.
+inline bool interleaved(uintptr_t a, uint64_t wa, uintptr_t b, uint64_t wb, uint64_t unit) {
+  if (unit == 0) return false;
+  const uint64_t from = (a % unit + unit - b % unit) % unit;      // where a's pieces begin, from b's
+  return from >= wb && from + wa <= unit;
+}
+// Whether two matrices certainly have no byte in common: apart as a whole, workers' blocks between one another (tensors of one
+// parameter row), or columns of one buffer's rows.
+inline bool apart(const Extent& a, const Extent& b) {
+  if (a.at == a.end || b.at == b.end || a.end <= b.at || b.end <= a.at) return true;
+  if (a.stride == b.stride && interleaved(a.at, a.block, b.at, b.block, a.stride)) return true;
+  if (a.ld != b.ld || a.stride != b.stride) return false;
+  // both matrices' rows begin at multiples of one number, each from its own place
+  const uint64_t unit = a.stride == 0 ? a.ld : a.ld == 0 || a.ld % a.stride == 0 ? a.stride : a.stride % a.ld == 0 ? a.ld : 0;
+  return interleaved(a.at, a.width, b.at, b.width, unit);
+}
+inline bool all_apart(const Extent* outs, int n_outs, const Extent* ins, int n_ins) {
+  for (int i = 0; i < n_outs; ++i) {
+    for (int j = 0; j < n_ins; ++j)
+      if (!apart(outs[i], ins[j])) return false;
+    for (int j = 0; j < i; ++j)
+      if (!apart(outs[i], outs[j])) return false;
+  }
+  return true;
+}
 inline uint64_t align256(uint64_t n) { return (n + 255) & ~uint64_t(255); }
 inline uint64_t codes_bytes(const lsgd_sequences& q, int64_t P, int64_t T) {
   return q.starts ? align256(sizeof(int32_t) * (uint64_t)(P * T)) : 0;

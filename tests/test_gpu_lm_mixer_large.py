@@ -1,0 +1,100 @@
+"""Rows whose offsets pass 32 bits: every operand is some columns of one buffer of 4096 rows of 600 000 values, and the results are those of
+the same rows packed, bit for bit."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+T, LD, D, N = 4096, 600_000, 64, 16
+
+
+@pytest.fixture(scope="module")
+def buffer():
+    if torch.cuda.get_device_properties(0).total_memory < 40e9:
+        pytest.skip("needs 10 GB")
+    buf = torch.zeros((1, T, LD), dtype=torch.bfloat16, device="cuda")
+    yield buf
+    del buf
+    torch.cuda.empty_cache()
+
+
+def _columns(buffer, sizes, gen):
+    """Views of the buffer's columns, filled, and packed copies of them."""
+    far, near, at = {}, {}, LD - 4096
+    for k, n in sizes.items():
+        far[k] = buffer[:, :, at:at + n]
+        far[k].copy_(torch.randn((1, T, n), generator=gen))
+        near[k] = far[k].clone(memory_format=torch.contiguous_format)
+        at += n
+    return far, near
+
+
+def test_convolution(buffer):
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator().manual_seed(0)
+    w, got = torch.randn((1, D, 4), generator=gen).cuda(), []
+    for t in _columns(buffer, dict(x=D, out=D, d_out=D, dx=D), gen):
+        dw = torch.empty_like(w)
+        op = lm.CausalConv(t["x"], w, out=t["out"], d_out=t["d_out"], dx=t["dx"], dw=dw, sequences=2)
+        op.forward()
+        op.backward()
+        got.append((t["out"].clone(), t["dx"].clone(), dw))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_scan(buffer):
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator().manual_seed(1)
+    a_log, skip, got = torch.randn((1, D, N), generator=gen).cuda(), torch.randn((1, D), generator=gen).cuda(), []
+    wide = {k: D for k in ("x", "dt", "z", "out", "d_out", "d_x", "d_dt", "d_z")}
+    for t in _columns(buffer, wide | {k: N for k in ("b", "c", "d_b", "d_c")}, gen):
+        da, ds = torch.empty_like(a_log), torch.empty_like(skip)
+        op = lm.SelectiveScan(t.pop("x"), t.pop("dt"), a_log, t.pop("b"), t.pop("c"), skip=skip, d_a_log=da, d_skip=ds, sequences=2, **t)
+        op.forward()
+        op.backward()
+        got.append((da, ds, *(t[k].clone() for k in ("out", "d_x", "d_dt", "d_z", "d_b", "d_c"))))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_single_tokens(buffer):
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator().manual_seed(2)
+    a_log, w, got = torch.randn((1, D, N), generator=gen).cuda(), torch.randn((1, D, 4), generator=gen).cuda(), []
+    for t in _columns(buffer, dict(x=D, dt=D, out=D, b=N, c=N, conv=D), gen):
+        state, inputs = torch.ones((1, T, D, N), device="cuda"), torch.ones((1, T, 3, D), dtype=torch.bfloat16, device="cuda")
+        lm.SelectiveScan(t["x"], t["dt"], a_log, t["b"], t["c"], out=t["out"], state=state, sequences=T).forward()
+        lm.CausalConv(t["x"], w, out=t["conv"], state=inputs, sequences=T).forward()
+        got.append((t["out"].clone(), t["conv"].clone(), state, inputs))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("n", [40, 200])
+def test_orthogonalisation(buffer, n):
+    from paper_1905_10395_b200 import lm
+    gen, got = torch.Generator().manual_seed(3), []
+    for t in _columns(buffer, dict(grad=n, out=n), gen):
+        lm.Orthogonalize(t["grad"], t["out"]).forward()
+        got.append(t["out"].clone())
+    torch.cuda.synchronize()
+    assert torch.isfinite(got[0]).all() and torch.equal(*got)
+
+
+def test_states_beyond_32_bits():
+    """Kept and saved states of more than 2^32 bytes: the last sequence's are those of the sequence alone."""
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator().manual_seed(4)
+    S, D2, N2 = 600, 60_000, 64
+    a_log = torch.randn((1, D2, N2), generator=gen).cuda()
+    x, dt = torch.randn((1, S, D2), generator=gen).cuda(), torch.randn((1, S, D2), generator=gen).cuda()
+    b, c = torch.randn((1, S, N2), generator=gen).cuda(), torch.randn((1, S, N2), generator=gen).cuda()
+    state, out = torch.full((1, S, D2, N2), 0.5, device="cuda"), torch.empty_like(x)
+    lm.SelectiveScan(x, dt, a_log, b, c, out=out, state=state, sequences=S).forward()
+    for i in (0, 290, S - 1):
+        one, own = torch.full((1, 1, D2, N2), 0.5, device="cuda"), torch.empty_like(x[:, :1])
+        cut = [v[:, i:i + 1] for v in (x, dt, b, c)]
+        lm.SelectiveScan(cut[0], cut[1], a_log, cut[2], cut[3], out=own, state=one).forward()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, i:i + 1], own) and torch.equal(state[:, i:i + 1], one)
