@@ -136,6 +136,8 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
   Plan m{};
   const int64_t P = d->P, T = d->T, D = d->D, N = d->N, S = d->seq.S;
   m.l.L = N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16;
+  const bool equal = !d->seq.starts;
+  m.l.single = !backward && equal && S == T && !d->saved;
   const int ch = kThreads / m.l.L, rows = 32;              // channels of a block; a chain's rows are a multiple of any tile's
   m.tiles = (uint32_t)((D + ch - 1) / ch);
   const int ab = elem_bytes(d->act_dtype);
@@ -150,23 +152,21 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
     for (const lsgd_rows* r : {&d->d_out, &d->dx, &d->d_dt, &d->dz}) fits(*r);
   else
     fits(d->out);
-  const bool equal = !d->seq.starts;
-  m.l.single = !backward && equal && S == T && !d->saved;
-  // Chains: whole sequences where that gives every SM a block; else equal runs of rows, four blocks an SM.
+  // Chains: whole sequences where that gives every SM a block; else equal runs of rows, as many as are resident.
   m.wide_bc = N % 4 == 0 && row_vec4(d->b, P, T, ab) && row_vec4(d->c, P, T, ab);
-  const int64_t columns = P * m.tiles, sms = sm_count();
+  const int64_t columns = P * m.tiles, sms = sm_count(), resident = sms * kBlocks;
   int64_t chains;
   if (columns >= sms) {
     chains = 1;
     m.per = (int32_t)S;
   } else if (equal && columns * S >= sms) {
-    int64_t want = 4 * sms / columns;
+    int64_t want = resident / columns;
     if (want > S) want = S;
     m.per = (int32_t)((S + want - 1) / want);
     chains = (S + m.per - 1) / m.per;
   } else {
     m.split = 1;
-    const int64_t want = 4 * sms / columns;        // all of them resident at once: one block more would be a second round
+    const int64_t want = resident / columns;        // all of them at once: one block more would be a second round
     int64_t per = (T + want - 1) / want;
     per = (per + rows - 1) / rows * rows;
     if (per < 2 * rows) per = 2 * rows;

@@ -30,6 +30,7 @@ namespace lsgd {
 namespace scan {
 
 constexpr int kThreads = 128, kQuad = 4, kGroup = 8;
+constexpr int kBlocks = 4;       // of either direction's kernels, resident on an SM
 // Channels of a block, rows of a tile; at most one piece of 8 channels of a row a thread.
 template <int L> struct Tile {
   static constexpr int kCh = kThreads / L;
@@ -222,8 +223,7 @@ __device__ __forceinline__ bool row_lives(const Args& a, int p, const Range& r, 
 }
 // Which rows of a tile begin and end a sequence (its number, else -1).
 template <int ROWS>
-__device__ __forceinline__ void mark_rows(const Args& a, int p, const Range& r, int base, int* begins, int* ends) {
-  const int i = threadIdx.x;
+__device__ __forceinline__ void mark_rows(const Args& a, int p, const Range& r, int base, int* begins, int* ends, int i) {
   if (i >= ROWS) return;
   const int t = base + i;
   int b = -1, e = -1;
@@ -271,19 +271,19 @@ struct StageBC {
   Pack<T, 4> k[Ti::kQuads];
   const T* from[Ti::kQuads];                       // at row 0; NULL: no such states
   int64_t ld[Ti::kQuads];
-  __device__ __forceinline__ void init(const Args& a, int p, bool b_too) {
+  __device__ __forceinline__ void init(const Args& a, int p, int tid, bool b_too) {
 #pragma unroll
     for (int j = 0; j < Ti::kQuads; ++j) {
-      const int i = threadIdx.x + j * kThreads, which = i / (Ti::kRows * L), n = i % L * kQuad;
+      const int i = tid + j * kThreads, which = i / (Ti::kRows * L), n = i % L * kQuad;
       from[j] = which > 1 || n >= a.d.N || (which == 0 && !b_too) ? nullptr
                 : static_cast<const T*>(which ? a.d.c.data : a.d.b.data) + p * (which ? a.d.c.stride : a.d.b.stride) + n;
       ld[j] = which ? a.d.c.ld : a.d.b.ld;
     }
   }
-  __device__ __forceinline__ void fetch(const Args& a, int p, const Range& r, int base, bool plain) {
+  __device__ __forceinline__ void fetch(const Args& a, int p, const Range& r, int base, bool plain, int tid) {
 #pragma unroll
     for (int j = 0; j < Ti::kQuads; ++j) {
-      const int i = threadIdx.x + j * kThreads, row = base + i / L % Ti::kRows, n = i % L * kQuad;
+      const int i = tid + j * kThreads, row = base + i / L % Ti::kRows, n = i % L * kQuad;
       const float zero[4] = {};
       k[j].set(zero);
       if (!from[j] || !(plain || row_lives(a, p, r, row))) continue;
@@ -305,10 +305,10 @@ struct StageBC {
       }
     }
   }
-  __device__ __forceinline__ void store(float* bc) const {
+  __device__ __forceinline__ void store(float* bc, int tid) const {
 #pragma unroll
     for (int j = 0; j < Ti::kQuads; ++j) {
-      const int i = threadIdx.x + j * kThreads;
+      const int i = tid + j * kThreads;
       if (i >= 2 * Ti::kRows * L) continue;
       float f[4];
       k[j].get(f);
@@ -324,21 +324,127 @@ __device__ __forceinline__ void pairs(const float4& v, float2 (&f)[2]) {
 __device__ __forceinline__ float part_of(const float4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // ------------------------------------------------------------------------------------------------ forward
+// Named barriers of 2 kThreads threads, half of which wait.
+__device__ __forceinline__ void barrier_wait(int id) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "n"(2 * kThreads) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("barrier.arrive %0, %1;" ::"r"(id), "n"(2 * kThreads) : "memory"); }
+
 // kEnds: only what the chain adds to the state behind it, and its summed time steps.
+// Half of the block's warps run the recurrence, the others stage the next tile and finish the last one meanwhile (two buffers; barriers
+// 1 + b: buffer b is staged, 3 + b: its tile is done), so that a block's staging, a chain of latencies, does not stop its recurrence:
+// ragged prompts of 8191 x 1500 take 203 us instead of 258.  (Two channels a thread would halve what is read of B and C, but leave
+// half the warps: 172 us instead of 197 for 32768 x 384 in fp32, 304 instead of 203 for the prompts.)
 template <typename T, int L, bool kEnds>
-__global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
   pdl_wait();
   pdl_launch_dependents();
-  // (arrays of their own: a store of sums does not hold back the next rows' loads)
-  __shared__ __align__(16) float s_delta[Ti::kArray], s_du[Ti::kArray], s_y[kEnds ? 1 : Ti::kArray];   // delta, delta x; C . h
-  __shared__ __align__(16) float s_bc[2 * Ti::kRows * Ti::kN];
-  __shared__ int s_begin[Ti::kRows], s_end[Ti::kRows];
-  const int p = blockIdx.z, c = blockIdx.y, lane = threadIdx.x & 31;
+  __shared__ __align__(16) float s_delta[2][Ti::kArray], s_du[2][Ti::kArray], s_y[2][kEnds ? 4 : Ti::kArray];   // delta, delta x; C . h
+  __shared__ __align__(16) float s_bc[2][2 * Ti::kRows * Ti::kN];
+  __shared__ __align__(16) float s_bias[Ti::kCh], s_skip[Ti::kCh];
+  __shared__ int s_begin[2][Ti::kRows], s_end[2][Ti::kRows], s_plain[2];
+  const int p = blockIdx.z, c = blockIdx.y;
   Range r(a, p, c);
   const lsgd_scan_desc& d = a.d;
-  const int local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
-  const bool mine = ch < d.D && n0 < d.N;
+  const int n_tiles = r.base < r.t1 ? (r.t1 - r.base + Ti::kRows - 1) / Ti::kRows : 0;
+
+  if (threadIdx.x >= kThreads) {
+    // ---------------------------------------------------------------- stage and finish: a piece of 8 channels of a row a thread
+    const int tid = threadIdx.x - kThreads, prow = tid / (Ti::kCh / 8), piece = (tid % (Ti::kCh / 8)) * 8;
+    const int pch = blockIdx.x * Ti::kCh + piece, own = Ti::at(piece, prow);
+    const bool has_piece = tid < Ti::kPieces && pch < d.D, gated = !kEnds && d.z.data != nullptr;
+    for (int i = tid; i < Ti::kCh; i += kThreads) {
+      const int col = blockIdx.x * Ti::kCh + i;
+      s_bias[i] = vector_at(d.dt_bias, p, col, col < d.D);
+      s_skip[i] = vector_at(d.skip, p, col, col < d.D);
+    }
+    asm volatile("barrier.sync 5, %0;" ::"n"(kThreads) : "memory");
+    const int wide = a.wide;
+    StageBC<T, L, Ti> bc;
+    bc.init(a, p, tid, true);
+    const T *px = view<T>(d.x).row(p, r.base + prow), *pdt = view<T>(d.dt).row(p, r.base + prow);
+    Pack<T, 8> rx, rdt, rz;
+    bool plain = false, live = false, was_live = false;
+    auto fetch = [&](int base) {
+      plain = r.plain(a, p, base, Ti::kRows);
+      live = has_piece && (plain || row_lives(a, p, r, base + prow));
+      if (live) {
+        load8<T>(rx, px, pch, d.D, wide);
+        load8<T>(rdt, pdt, pch, d.D, wide);
+      }
+      px += Ti::kRows * d.x.ld, pdt += Ti::kRows * d.dt.ld;
+      bc.fetch(a, p, r, base, plain, tid);
+    };
+    auto stage = [&](int base, int b) {
+      if (live) {
+        float fx[8], fd[8];
+        float2 x2[4], dt2[4];
+        rx.get(fx);
+        rdt.get(fd);
+        pairs8(fx, x2);
+        pairs8(fd, dt2);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          float2 e;
+          const float2 delta = softplus(add2(dt2[v], *reinterpret_cast<const float2*>(s_bias + piece + 2 * v)), e), du = mul2(delta, x2[v]);
+          s_delta[b][own + 2 * v * Ti::kPitch] = delta.x, s_delta[b][own + (2 * v + 1) * Ti::kPitch] = delta.y;
+          s_du[b][own + 2 * v * Ti::kPitch] = du.x, s_du[b][own + (2 * v + 1) * Ti::kPitch] = du.y;
+        }
+      } else if (tid < Ti::kPieces) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) s_delta[b][own + v * Ti::kPitch] = s_du[b][own + v * Ti::kPitch] = 0.f;
+      }
+      bc.store(s_bc[b], tid);
+      if (!plain) mark_rows<Ti::kRows>(a, p, r, base, s_begin[b], s_end[b], tid);
+      if (tid == 0) s_plain[b] = plain;
+    };
+    if (n_tiles > 0) {
+      fetch(r.base);
+      stage(r.base, 0);
+      barrier_arrive(1);
+      was_live = live;
+      if (n_tiles > 1) fetch(r.base + Ti::kRows);
+    }
+    for (int i = 0; i < n_tiles; ++i) {
+      const int base = r.base + i * Ti::kRows, b = i & 1;
+      const bool finish = !kEnds && was_live;
+      if (i + 1 < n_tiles) {
+        stage(base + Ti::kRows, b ^ 1);
+        barrier_arrive(1 + (b ^ 1));
+        was_live = live;
+        if (i + 2 < n_tiles) fetch(base + 2 * Ti::kRows);
+      }
+      Pack<T, 8> kx;
+      if (finish) {                                                // again, from the caches
+        load8<T>(kx, view<T>(d.x).row(p, base + prow), pch, d.D, wide);
+        if (gated) load8<T>(rz, view<T>(d.z).row(p, base + prow), pch, d.D, wide);
+      }
+      barrier_wait(3 + b);
+      if (!finish) continue;
+      float f[8];
+      float2 x2[4], y2[4];
+      kx.get(f);
+      pairs8(f, x2);
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        y2[v] = fma2(*reinterpret_cast<const float2*>(s_skip + piece + 2 * v), x2[v],
+                     make_float2(s_y[b][own + 2 * v * Ti::kPitch], s_y[b][own + (2 * v + 1) * Ti::kPitch]));
+      if (gated) {
+        float2 z2[4];
+        rz.get(f);
+        pairs8(f, z2);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y2[v] = mul2(y2[v], mul2(z2[v], sigmoid(z2[v])));
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) f[2 * v] = y2[v].x, f[2 * v + 1] = y2[v].y;
+      store8<T>(f, view<T>(d.out).row(p, base + prow), pch, d.D, wide);
+    }
+    return;
+  }
+
+  // ------------------------------------------------------------------ the recurrence
+  const int lane = threadIdx.x & 31, local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
+  const bool mine = ch < d.D && n0 < d.N, with_state = d.state != nullptr;
   const int64_t chain_row = ((int64_t)p * a.chains + c) * d.D + ch;
   float2 A2[2], h[2];
   {
@@ -348,47 +454,14 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
     A2[0] = make_float2(f[0], f[1]), A2[1] = make_float2(f[2], f[3]);
     h[0] = make_float2(g[0], g[1]), h[1] = make_float2(g[2], g[3]);
   }
-  const float* from = a.split && !kEnds ? a.old_state : d.state;
   float sum = 0.f;
   bool fresh = false;                                              // a sequence began inside
-
-  // the piece of 8 channels of a row that this thread stages and finishes
-  const int prow = threadIdx.x / (Ti::kCh / 8), piece = (threadIdx.x % (Ti::kCh / 8)) * 8;
-  const int pch = blockIdx.x * Ti::kCh + piece;
-  const bool has_piece = threadIdx.x < Ti::kPieces && pch < d.D;
-  const int wide = a.wide;
-  const Rows<T> x = view<T>(d.x), dt = view<T>(d.dt), z = view<T>(d.z), out = view<T>(d.out);
-  float2 bias[4], skip[4];
-  load_vector8(d.dt_bias, p, pch, has_piece ? d.D : 0, bias);
-  load_vector8(d.skip, p, pch, !kEnds && has_piece ? d.D : 0, skip);
-  const int own = Ti::at(piece, prow);                             // its first channel's place in an array
-  Pack<T, 8> rx, rdt, rz;
-  StageBC<T, L, Ti> bc;
-  bc.init(a, p, true);
-  const bool gated = !kEnds && d.z.data != nullptr, with_state = d.state != nullptr;
-  bool live = false, plain = false;
-  const T *px = x.row(p, r.base + prow), *pdt = dt.row(p, r.base + prow), *pz = gated ? z.row(p, r.base + prow) : px;
-  T* pout = out.row(p, r.base + prow);
-  const int64_t step_x = Ti::kRows * d.x.ld, step_dt = Ti::kRows * d.dt.ld, step_z = gated ? Ti::kRows * d.z.ld : 0, step_out = Ti::kRows * d.out.ld;
-  auto fetch = [&](int base) {
-    plain = r.plain(a, p, base, Ti::kRows);
-    live = has_piece && (plain || row_lives(a, p, r, base + prow));
-    if (live) {
-      load8<T>(rx, px, pch, d.D, wide);
-      load8<T>(rdt, pdt, pch, d.D, wide);
-      if (gated) load8<T>(rz, pz, pch, d.D, wide);
-    }
-    px += step_x, pdt += step_dt, pz += step_z;
-    bc.fetch(a, p, r, base, plain);
-  };
-  if (r.base < r.t1) fetch(r.base);
   // the states in front of every 8th row
   const int64_t saved_step = (int64_t)d.D * d.N;
   float* saved = !kEnds && d.saved && mine ? d.saved + ((int64_t)p * ((a.q.T + kGroup - 1) / kGroup) + r.base / kGroup) * saved_step + (int64_t)ch * d.N : nullptr;
   const int turn = 4 * (local >> 3);
-  const float *delta_of = s_delta + local * Ti::kPitch, *du_of = s_du + local * Ti::kPitch;
   // four rows of the recurrence
-  auto rows4 = [&](int base, int t4, auto special) {
+  auto rows4 = [&](int base, int b, int t4, auto special) {
     if (!kEnds && saved && t4 % kGroup == 0) {
       if (!special || (base + t4 >= r.t0 && base + t4 < r.t1)) {
         const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
@@ -396,21 +469,21 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
       }
       saved += saved_step;
     }
-    const int place = (t4 + turn) & (Ti::kRows - 1);
-    const float4 delta4 = *reinterpret_cast<const float4*>(delta_of + place);
-    const float4 du4 = *reinterpret_cast<const float4*>(du_of + place);
+    const int place = local * Ti::kPitch + ((t4 + turn) & (Ti::kRows - 1));
+    const float4 delta4 = *reinterpret_cast<const float4*>(s_delta[b] + place);
+    const float4 du4 = *reinterpret_cast<const float4*>(s_du[b] + place);
     float y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = t4 + i;
       if (special) {
-        const int s = s_begin[t];
+        const int s = s_begin[b][t];
         if (s >= 0) {
           fresh = true;
           float f[kQuad] = {};
           if (with_state && mine) {
             const int64_t row = ((int64_t)p * a.q.S + s) * d.D + ch;
-            load_states(from, row, n0, d.N, f);
+            load_states(a.split && !kEnds ? a.old_state : d.state, row, n0, d.N, f);
             if (kEnds) store_states(a.old_state, row, n0, d.N, f);
           }
           h[0] = make_float2(f[0], f[1]), h[1] = make_float2(f[2], f[3]);
@@ -418,77 +491,34 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
       }
       const float delta = part_of(delta4, i), du = part_of(du4, i);
       float2 B[2], C[2];
-      pairs(*reinterpret_cast<const float4*>(s_bc + t * Ti::kN + n0), B);
+      pairs(*reinterpret_cast<const float4*>(s_bc[b] + t * Ti::kN + n0), B);
       h[0] = fma2(ex2(mul2(both(delta), A2[0])), h[0], mul2(both(du), B[0]));
       h[1] = fma2(ex2(mul2(both(delta), A2[1])), h[1], mul2(both(du), B[1]));
       if (kEnds) {
         sum += delta;
       } else {
-        pairs(*reinterpret_cast<const float4*>(s_bc + (Ti::kRows + t) * Ti::kN + n0), C);
+        pairs(*reinterpret_cast<const float4*>(s_bc[b] + (Ti::kRows + t) * Ti::kN + n0), C);
         const float2 s = fma2(C[0], h[0], mul2(C[1], h[1]));
         y[i] = s.x + s.y;
-        if (special && with_state && mine && s_end[t] >= 0) {
+        if (special && with_state && mine && s_end[b][t] >= 0) {
           const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
-          store_states(d.state, ((int64_t)p * a.q.S + s_end[t]) * d.D + ch, n0, d.N, f);
+          store_states(d.state, ((int64_t)p * a.q.S + s_end[b][t]) * d.D + ch, n0, d.N, f);
         }
       }
     }
-    if (!kEnds) keep_sums<L, Ti>(y, s_y, local, t4, lane);
+    if (!kEnds) keep_sums<L, Ti>(y, s_y[b], local, t4, lane);
   };
-  for (int base = r.base; base < r.t1; base += Ti::kRows) {
-    // stage
-    if (live) {
-      float fx[8], fd[8];
-      float2 x2[4], dt2[4];
-      rx.get(fx);
-      rdt.get(fd);
-      pairs8(fx, x2);
-      pairs8(fd, dt2);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        float2 e;
-        const float2 delta = softplus(add2(dt2[v], bias[v]), e), du = mul2(delta, x2[v]);
-        s_delta[own + 2 * v * Ti::kPitch] = delta.x, s_delta[own + (2 * v + 1) * Ti::kPitch] = delta.y;
-        s_du[own + 2 * v * Ti::kPitch] = du.x, s_du[own + (2 * v + 1) * Ti::kPitch] = du.y;
-      }
-    } else if (threadIdx.x < Ti::kPieces) {
-#pragma unroll
-      for (int v = 0; v < 8; ++v) s_delta[own + v * Ti::kPitch] = s_du[own + v * Ti::kPitch] = 0.f;
-    }
-    bc.store(s_bc);
-    const bool is_plain = plain, was_live = live;
-    if (!is_plain) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end);
-    const Pack<T, 8> kx = rx, kz = rz;
-    __syncthreads();
-    if (base + Ti::kRows < r.t1) fetch(base + Ti::kRows);
-    if (is_plain) {
+  for (int i = 0; i < n_tiles; ++i) {
+    const int base = r.base + i * Ti::kRows, b = i & 1;
+    barrier_wait(1 + b);
+    if (s_plain[b]) {
 #pragma unroll 2
-      for (int t4 = 0; t4 < Ti::kRows; t4 += 4) rows4(base, t4, std::false_type());
+      for (int t4 = 0; t4 < Ti::kRows; t4 += 4) rows4(base, b, t4, std::false_type());
     } else {
 #pragma unroll 1
-      for (int t4 = 0; t4 < Ti::kRows; t4 += 4) rows4(base, t4, std::true_type());
+      for (int t4 = 0; t4 < Ti::kRows; t4 += 4) rows4(base, b, t4, std::true_type());
     }
-    __syncthreads();
-    pout += step_out;
-    if (kEnds || !was_live) continue;
-    // finish (s_y is written again behind the next barrier)
-    float fx[8], o[8];
-    float2 x2[4], y2[4];
-    kx.get(fx);
-    pairs8(fx, x2);
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-      y2[v] = fma2(skip[v], x2[v], make_float2(s_y[own + 2 * v * Ti::kPitch], s_y[own + (2 * v + 1) * Ti::kPitch]));
-    if (gated) {
-      float2 z2[4];
-      kz.get(fx);
-      pairs8(fx, z2);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) y2[v] = mul2(y2[v], mul2(z2[v], sigmoid(z2[v])));
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) o[2 * v] = y2[v].x, o[2 * v + 1] = y2[v].y;
-    store8<T>(o, pout - step_out, pch, d.D, wide);
+    barrier_arrive(3 + b);
   }
   if (kEnds && mine) {
     const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
@@ -548,7 +578,7 @@ __global__ void __launch_bounds__(kThreads) single_kernel(const __grid_constant_
 // ------------------------------------------------------------------------------------------------ backward
 // Split chains: what the chain's rows add to the adjoint in front of it, and its summed time steps.
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, kBlocks) adjoint_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
   pdl_wait();
   pdl_launch_dependents();
@@ -579,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
   const bool gated = d.z.data != nullptr;
   Pack<T, 8> rup, rdt, rz;
   StageBC<T, L, Ti> bc;
-  bc.init(a, p, false);
+  bc.init(a, p, threadIdx.x, false);
   bool live = false, plain = false;
   auto fetch = [&](int base) {
     const int t = base + prow;
@@ -590,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
       load8<T>(rdt, dt.row(p, t), pch, d.D, wide);
       if (d.z.data) load8<T>(rz, z.row(p, t), pch, d.D, wide);
     }
-    bc.fetch(a, p, r, base, plain);
+    bc.fetch(a, p, r, base, plain, threadIdx.x);
   };
   const int n_tiles = r.base < r.t1 ? (r.t1 - r.base + Ti::kRows - 1) / Ti::kRows : 0;
   if (n_tiles > 0) fetch(r.base + (n_tiles - 1) * Ti::kRows);
@@ -621,9 +651,9 @@ __global__ void __launch_bounds__(kThreads, 4) adjoint_kernel(const __grid_const
 #pragma unroll
       for (int v = 0; v < 8; ++v) s_delta[own + v * Ti::kPitch] = s_d[own + v * Ti::kPitch] = 0.f;
     }
-    bc.store(s_bc);
+    bc.store(s_bc, threadIdx.x);
     const bool special = !plain;
-    if (special) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end);
+    if (special) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end, threadIdx.x);
     __syncthreads();
     if (it > 0) fetch(base - Ti::kRows);
 #pragma unroll 2
@@ -698,7 +728,7 @@ struct BackSmem {
 // Registers: the four rows in hand (states, decays, B, C and time steps, which both directions use), so that four blocks fit an SM;
 // what is fetched for the next tile therefore goes to shared memory.
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, 4) backward_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
   using Sm = BackSmem<T, L>;
   pdl_wait();
@@ -935,7 +965,7 @@ __global__ void __launch_bounds__(kThreads, 4) backward_kernel(const __grid_cons
       *reinterpret_cast<float4*>(s_bc + i * kQuad) = make_float4(f[0], f[1], f[2], f[3]);
     }
     const bool is_plain = plain, was_live = live;
-    if (!is_plain) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end);
+    if (!is_plain) mark_rows<Ti::kRows>(a, p, r, base, s_begin, s_end, threadIdx.x);
     __syncthreads();
     if (it > 0) fetch(base - Ti::kRows, parity ^ 1);
     if (is_plain) {
@@ -1042,11 +1072,11 @@ template <typename T, int L>
 cudaError_t forward_of(const Args& a, const Launch& l, cudaStream_t s) {
   if (l.single) return launch_pdl(single_kernel<T, L>, l.grid, dim3(kThreads), 0, s, a);
   if (a.split) {
-    cudaError_t e = launch_pdl(forward_kernel<T, L, true>, l.grid, dim3(kThreads), 0, s, a);
+    cudaError_t e = launch_pdl(forward_kernel<T, L, true>, l.grid, dim3(2 * kThreads), 0, s, a);
     if (e == cudaSuccess) e = launch_chain_join(a, false, s);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(forward_kernel<T, L, false>, l.grid, dim3(kThreads), 0, s, a);
+  return launch_pdl(forward_kernel<T, L, false>, l.grid, dim3(2 * kThreads), 0, s, a);
 }
 template <typename T, int L>
 cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
