@@ -180,7 +180,11 @@ Plan plan_of(const lsgd_scan_desc* d, bool backward) {
     }
   }
   m.chains = (int32_t)chains;
-  m.l.grid = dim3(m.tiles, (unsigned)(m.l.single ? (S < 65535 ? S : 65535) : chains), (unsigned)P);
+  // single rows: several sequences a block one after another, which share its decays, while 32 blocks an SM are left
+  int64_t singles = 32 * sms / columns < S ? 32 * sms / columns : S;
+  if (singles < (S + 15) / 16) singles = (S + 15) / 16;
+  if (singles > 65535) singles = 65535;
+  m.l.grid = dim3(m.tiles, (unsigned)(m.l.single ? singles : chains), (unsigned)P);
   uint64_t at = codes_bytes(d->seq, P, T);
   auto take = [&](uint64_t floats) {
     const uint64_t here = at;

@@ -152,12 +152,11 @@ __device__ __forceinline__ void pairs8(const float (&f)[8], float2 (&q)[4]) {
 }
 // A log2(e) of 4 states of a channel; 0 for those that do not exist (they stay zero, for B is zero there)
 __device__ __forceinline__ void decay_rates(const Args& a, int p, int ch, int n0, float (&A2)[kQuad]) {
+  const float* src = static_cast<const float*>(a.d.a_log.data) + p * a.d.a_log.stride + ch * a.d.a_log.ld + n0;
 #pragma unroll
-  for (int k = 0; k < kQuad; ++k) {
-    A2[k] = 0.f;
-    if (ch < a.d.D && n0 + k < a.d.N)
-      A2[k] = -expf(static_cast<const float*>(a.d.a_log.data)[p * a.d.a_log.stride + ch * a.d.a_log.ld + n0 + k]) * kLog2e;
-  }
+  for (int k = 0; k < kQuad; ++k) A2[k] = ch < a.d.D && n0 + k < a.d.N ? src[k] : 0.f;
+#pragma unroll
+  for (int k = 0; k < kQuad; ++k) A2[k] = ch < a.d.D && n0 + k < a.d.N ? -expf(A2[k]) * kLog2e : 0.f;
 }
 __device__ __forceinline__ void load_vector8(const lsgd_rows& v, int p, int ch, int D, float2 (&f)[4]) {
   const float* src = static_cast<const float*>(v.data) + p * v.stride + ch;
@@ -527,47 +526,82 @@ __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __
   }
 }
 
-// Sequences of one row each: a thread takes 4 states of a channel of one sequence, read and written once.
+// Sequences of one row each: a thread takes 4 states of a channel of one sequence after another.  Everything that a row needs is under
+// way before the first of it, the decays' logarithms included, is used: what bounds a block is one latency of memory and its
+// own work, so many small blocks overlap (64 x 4096 x 16: 12 us; four rows a thread at a time, in half the warps, 16).
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads) single_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 10) single_kernel(const __grid_constant__ Args a) {
   pdl_wait();
   pdl_launch_dependents();
   const int p = blockIdx.z, lane = threadIdx.x & 31;
   const lsgd_scan_desc& d = a.d;
   const int ch = blockIdx.x * (kThreads / L) + threadIdx.x / L, n0 = (threadIdx.x % L) * kQuad;
   const bool in = ch < d.D, mine = in && n0 < d.N;
-  float A2[kQuad];
-  decay_rates(a, p, ch, n0, A2);
-  const float bias = vector_at(d.dt_bias, p, ch, in), skip = vector_at(d.skip, p, ch, in);
-  auto one = [&](const lsgd_rows& m, int t, int i, bool there) {
+  auto one = [&](const lsgd_rows& m, int t) {
+    Pack<T, 1> k;
     float f = 0.f;
-    if (there) {
-      Pack<T, 1> k;
-      k.load(view<T>(m).row(p, t) + i);
-      k.get(&f);
+    k.set(&f);
+    if (in && m.data) k.load(view<T>(m).row(p, t) + ch);
+    return k;
+  };
+  auto four = [&](const lsgd_rows& m, int t) {
+    const T* src = view<T>(m).row(p, t) + n0;
+    Pack<T, 4> k;
+    float f[kQuad] = {};
+    if (mine && a.wide_bc) {
+      k.load(src);
+      return k;
     }
+#pragma unroll
+    for (int i = 0; i < kQuad; ++i)
+      if (mine && n0 + i < d.N) {
+        Pack<T, 1> v;
+        v.load(src + i);
+        v.get(f + i);
+      }
+    k.set(f);
+    return k;
+  };
+  auto value = [](const Pack<T, 1>& k) {
+    float f;
+    k.get(&f);
     return f;
   };
+  float A2[kQuad];
+  const float* logs = static_cast<const float*>(d.a_log.data) + p * d.a_log.stride + ch * d.a_log.ld + n0;
+#pragma unroll
+  for (int k = 0; k < kQuad; ++k) A2[k] = in && n0 + k < d.N ? logs[k] : 0.f;
+  const float bias = vector_at(d.dt_bias, p, ch, in), skip = vector_at(d.skip, p, ch, in);
+  bool rates = false;
   for (int t = blockIdx.y; t < a.q.S; t += gridDim.y) {
     const int64_t row = ((int64_t)p * a.q.S + t) * d.D + ch;
-    float h[kQuad] = {};
+    float h[kQuad] = {}, B[kQuad], C[kQuad];
     if (d.state && mine) load_states(d.state, row, n0, d.N, h);
-    const float x = one(d.x, t, ch, in), z = one(d.z, t, ch, in && d.z.data);
-    float e;
-    const float delta = softplus(one(d.dt, t, ch, in) + bias, e), du = delta * x;
-    float y = 0.f;
+    const Pack<T, 1> kdt = one(d.dt, t), kx = one(d.x, t), kz = one(d.z, t);
+    const Pack<T, 4> kb = four(d.b, t), kc = four(d.c, t);
+    if (!rates) {
+#pragma unroll
+      for (int k = 0; k < kQuad; ++k) A2[k] = in && n0 + k < d.N ? -expf(A2[k]) * kLog2e : 0.f;
+      rates = true;
+    }
+    float e, y = 0.f;
+    const float x = value(kx), delta = softplus(value(kdt) + bias, e), du = delta * x;
+    kb.get(B);
+    kc.get(C);
 #pragma unroll
     for (int k = 0; k < kQuad; ++k) {
-      const bool there = n0 + k < d.N;
-      h[k] = fmaf(ex2(delta * A2[k]), h[k], du * one(d.b, t, n0 + k, there));
-      y = fmaf(one(d.c, t, n0 + k, there), h[k], y);
+      h[k] = fmaf(ex2(delta * A2[k]), h[k], du * B[k]);
+      y = fmaf(C[k], h[k], y);
     }
     if (d.state && mine) store_states(d.state, row, n0, d.N, h);
 #pragma unroll
     for (int m = 1; m < L; m *= 2) y += __shfl_xor_sync(0xFFFFFFFFu, y, m);
     if (lane % L == 0 && in) {
       float o = fmaf(skip, x, y);
-      if (d.z.data) o *= z * sigmoid(z);
+      if (d.z.data) {
+        const float z = value(kz);
+        o *= z * sigmoid(z);
+      }
       Pack<T, 1> k;
       k.set(&o);
       k.store(view<T>(d.out).row(p, t) + ch);
