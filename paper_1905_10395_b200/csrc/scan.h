@@ -71,6 +71,11 @@ __device__ __forceinline__ float ex2(float v) {
   return r;
 }
 __device__ __forceinline__ float2 ex2(float2 v) { return make_float2(ex2(v.x), ex2(v.y)); }
+// exp(delta A) = 2^(delta A2).  The unit's results are 1e-8 low on average for the small arguments of slowly decaying states (its
+// roundings, measured against 64 bits over [-0.1, 0)), which a thousand rows in front of such a state would all add: the argument is
+// lifted by as much.  The gradient of a_log, of 2048 rows, is then off by 7e-7 of its norm instead of 1.4e-6.
+constexpr float kLift = 1.7e-8f;
+__device__ __forceinline__ float2 decay(float2 delta, float2 A2) { return ex2(fma2(delta, A2, make_float2(kLift, kLift))); }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
 // 1 / v of a v in [1, 2^126]
 __device__ __forceinline__ float rcp(float v) {
@@ -491,8 +496,8 @@ __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __
       const float delta = part_of(delta4, i), du = part_of(du4, i);
       float2 B[2], C[2];
       pairs(*reinterpret_cast<const float4*>(s_bc[b] + t * Ti::kN + n0), B);
-      h[0] = fma2(ex2(mul2(both(delta), A2[0])), h[0], mul2(both(du), B[0]));
-      h[1] = fma2(ex2(mul2(both(delta), A2[1])), h[1], mul2(both(du), B[1]));
+      h[0] = fma2(decay(both(delta), A2[0]), h[0], mul2(both(du), B[0]));
+      h[1] = fma2(decay(both(delta), A2[1]), h[1], mul2(both(du), B[1]));
       if (kEnds) {
         sum += delta;
       } else {
@@ -590,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 10) single_kernel(const __grid_const
     kc.get(C);
 #pragma unroll
     for (int k = 0; k < kQuad; ++k) {
-      h[k] = fmaf(ex2(delta * A2[k]), h[k], du * B[k]);
+      h[k] = fmaf(ex2(fmaf(delta, A2[k], kLift)), h[k], du * B[k]);
       y = fmaf(C[k], h[k], y);
     }
     if (d.state && mine) store_states(d.state, row, n0, d.N, h);
@@ -699,8 +704,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) adjoint_kernel(const __grid
         float2 C[2];
         pairs(*reinterpret_cast<const float4*>(s_bc + (Ti::kRows + t4 + i) * Ti::kN + n0), C);
         const float delta = part_of(delta4, i), g0 = part_of(d4, i);
-        carry[0] = mul2(ex2(mul2(both(delta), A2[0])), fma2(C[0], both(g0), carry[0]));
-        carry[1] = mul2(ex2(mul2(both(delta), A2[1])), fma2(C[1], both(g0), carry[1]));
+        carry[0] = mul2(decay(both(delta), A2[0]), fma2(C[0], both(g0), carry[0]));
+        carry[1] = mul2(decay(both(delta), A2[1]), fma2(C[1], both(g0), carry[1]));
         sum += delta;
         if (special && s_begin[t4 + i] >= 0) {
           fresh = true;
@@ -780,7 +785,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
   const lsgd_scan_desc& d = a.d;
   const int local = threadIdx.x / L, ch = blockIdx.x * Ti::kCh + local, n0 = (threadIdx.x % L) * kQuad;
   const bool mine = ch < d.D && n0 < d.N;
-  float2 A2[2], carry[2], dA[2] = {};                              // carry: a_(t+1) g_(t+1)
+  // carry: a_(t+1) g_(t+1); dA: of a tile's rows, total: of the tiles' (summed by fours, tiles and chains: 2048 terms in a row would
+  // lose three bits)
+  float2 A2[2], carry[2], dA[2] = {}, total[2] = {};
   {
     float f[kQuad], g[kQuad] = {};
     decay_rates(a, p, ch, n0, f);
@@ -875,7 +882,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
         pairs(*reinterpret_cast<const float4*>(s_bc + (g8 + i) * Ti::kN + n0), B);
         const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) h[k] = fma2(ex2(mul2(delta, A2[k])), h[k], mul2(du, B[k]));
+        for (int k = 0; k < 2; ++k) h[k] = fma2(decay(delta, A2[k]), h[k], mul2(du, B[k]));
       }
     }
 #pragma unroll 1
@@ -896,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
         const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          as[i][k] = ex2(mul2(delta, A2[k]));
+          as[i][k] = decay(delta, A2[k]);
           h[k] = fma2(as[i][k], h[k], mul2(du, B[i][k]));
           hs[i][k] = h[k];
         }
@@ -1012,6 +1019,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
         else fetch_state(base + g8 - kGroup);
       }
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) total[k] = add2(total[k], dA[k]), dA[k] = make_float2(0.f, 0.f);
     // the last group's barrier has passed: every warp's sums are there
     if (was_live) {
       float f[8];
@@ -1064,7 +1073,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
     }
   }
   if (mine) {
-    const float f[kQuad] = {dA[0].x * (A2[0].x * kLn2), dA[0].y * (A2[0].y * kLn2), dA[1].x * (A2[1].x * kLn2), dA[1].y * (A2[1].y * kLn2)};
+    const float f[kQuad] = {total[0].x * (A2[0].x * kLn2), total[0].y * (A2[0].y * kLn2), total[1].x * (A2[1].x * kLn2), total[1].y * (A2[1].y * kLn2)};
     store_states(a.part_a, ((int64_t)p * a.chains + c) * d.D + ch, n0, d.N, f);
   }
   const int which = threadIdx.x / Ti::kCh, col = blockIdx.x * Ti::kCh + threadIdx.x % Ti::kCh;
