@@ -8,6 +8,7 @@
 // The gradient walks W - 1 rows further than its run: row t's d = d_out act'(pre) is made from the window of inputs and added to
 // the W sums dx[t - k] that wait in registers; the sums of dw and d_bias stay in registers over the run, are added up by
 // the block and then by a second kernel in a fixed order (67 us for the above; 31 at the rate of a copy).
+#include "activations.h"
 #include "seq.h"
 
 namespace lsgd {
@@ -38,11 +39,6 @@ struct ConvArgs {
   uint32_t blocks_t;
 };
 
-__device__ __forceinline__ float exp2f_fast(float v) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 template <typename T>
 __device__ __forceinline__ Rows<T> view(const lsgd_rows& r) {
   return Rows<T>{static_cast<T*>(r.data), r.ld, r.stride};
@@ -73,12 +69,6 @@ __device__ __forceinline__ void put(const Vals<VEC>& r, T* to) {
   k.set(f);
   k.store(to);
 }
-// sigmoid(v) = 1 / (1 + exp(-v)); exp(-v) is held below 2^126, where the fast quotient ends
-__device__ __forceinline__ float2 sigmoid(float2 v) {
-  return make_float2(__fdividef(1.f, 1.f + exp2f_fast(fminf(v.x * -1.4426950408889634f, 126.f))),
-                     __fdividef(1.f, 1.f + exp2f_fast(fminf(v.y * -1.4426950408889634f, 126.f))));
-}
-
 // A thread's weights: tap j multiplies the input W - 1 - j rows back.  (The number of taps is a template parameter: a weight of zero
 // would not keep an infinite input out.)
 template <int VEC, int W>

@@ -43,6 +43,8 @@ struct Prep {
   lsgd_ortho_desc d;
   double* part;              // [P][blocks] sums of squares
   uint32_t blocks;
+  uint32_t* done;            // counters of the products, cleared: n_done of them
+  uint32_t n_done;
   __half *x, *lo;            // [P][r][ld]: X and what it was rounded by
   int32_t r, n, tall;        // rows and columns of X; tall: X is the matrix transposed
   int32_t out_wide;          // out's rows can be written 8 values at a time
@@ -84,6 +86,8 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prep 
   pdl_wait();
   pdl_launch_dependents();
   const int p = blockIdx.y;
+  if (blockIdx.x == 0 && p == 0)
+    for (uint32_t i = threadIdx.x; i < a.n_done; i += 256) a.done[i] = 0;
   const uint32_t per = (a.d.n + VEC - 1) / VEC;
   const int64_t pieces = (int64_t)a.d.m * per;
   double s = 0.0;
@@ -191,6 +195,9 @@ struct Product {
   int M, N, K, batch;
   int b_mn;                  // B is stored [K][N] (else [N][K])
   int symmetric;             // square: tiles on and above the diagonal, stored twice
+  int split;                 // blocks that share a tile's contraction (1: none do); the last of them to finish adds up
+  float* partial;            // split: [tiles][split][128 columns][128 rows]
+  uint32_t* done;            // split: blocks of a tile that have finished, 0 between products
   int add;                   // C = alpha acc + beta D + diag I
   int twofold;               // C = A B + A D, D of B's layout (instead of an added tile)
   float alpha, beta, diag;
@@ -198,15 +205,30 @@ struct Product {
   int64_t out_ld, out_stride;
   int out_transposed, out_wide;
   float scale;
+
+  __host__ __device__ __forceinline__ int nk1() const { return (K + BK - 1) / BK; }
+  __host__ __device__ __forceinline__ int nk() const { return twofold ? 2 * nk1() : nk1(); }
 };
 
 struct TileAt {
   int z, m0, n0;
+  int part, k0, k1;          // of the contraction's slices, [k0, k1)
+  int number;                // of the tile, without its parts
 };
 // Tile number t: all of a row of tiles, or those from the diagonal on.
 template <int SIZE>
 __device__ __forceinline__ TileAt tile_of(const Product& p, int t, int nt, int per) {
   TileAt q;
+  const int nk = p.nk();
+  q.part = 0, q.k0 = 0, q.k1 = nk;
+  if (p.split > 1) {
+    q.part = t % p.split;
+    t /= p.split;
+    const int share = (nk + p.split - 1) / p.split;
+    q.k0 = q.part * share;
+    q.k1 = min(nk, q.k0 + share);
+  }
+  q.number = t;
   q.z = t / per;
   t -= q.z * per;
   int i = 0;
@@ -242,11 +264,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   uint8_t* mirror = buf + kTileBytes;            // C transposed
   __shared__ uint64_t full_bar[kStages], empty_bar[kStages], acc_full[2], acc_empty[2], in_full, in_free;
   __shared__ uint32_t tmem_base_s;
-  __shared__ int abort_s;
+  __shared__ int abort_s, last_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)cluster_rank() : 0;
   const int mt = (p.M + kTile - 1) / kTile, nt = (p.N + kTile - 1) / kTile, per = p.symmetric ? nt * (nt + 1) / 2 : mt * nt;
-  const int n_tiles = per * p.batch, nk1 = (p.K + BK - 1) / BK, nk = p.twofold ? 2 * nk1 : nk1;
+  const int n_tiles = per * p.batch * p.split, nk1 = p.nk1();
   const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, stride = PAIR ? gridDim.x >> 1 : gridDim.x;
   uint32_t* status = &g_status;
   if (threadIdx.x == 0) {
@@ -292,7 +314,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     for (int t = first; t < n_tiles && ok; t += stride) {
       const TileAt q = tile_of<kTile>(p, t, nt, per);
       const int m0 = q.m0 + rank * 128, n0 = q.n0 + rank * 128;
-      for (int kt = 0; kt < nk; ++kt, ++it) {
+      for (int kt = q.k0; kt < q.k1; ++kt, ++it) {
         const int s = it % kStages;
         ok = mbar_wait(&empty_bar[s], ((it / kStages) & 1) ^ 1, abort_flag, status);
         if (!ok) break;
@@ -333,7 +355,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t tacc = tmem_base + (uint32_t)(b * kTile);
-      for (int kt = 0; kt < nk; ++kt, ++it) {
+      const TileAt q = tile_of<kTile>(p, t, nt, per);
+      for (int kt = q.k0; kt < q.k1; ++kt, ++it) {
         const int s = it % kStages;
         ok = mbar_wait(&full_bar[s], (it / kStages) & 1, abort_flag, status);
         if (!ok) break;
@@ -343,8 +366,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int k = 0; k < BK / 16; ++k) {
           const uint64_t da = smem_desc(sa + k * 32, 16, 1024);
           const uint64_t db = p.b_mn ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024);
-          if (PAIR) mma_bf16_pair(tacc, da, db, idesc, (kt | k) != 0 ? 1u : 0u);
-          else mma_bf16(tacc, da, db, idesc, (kt | k) != 0 ? 1u : 0u);
+          if (PAIR) mma_bf16_pair(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
+          else mma_bf16(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
         }
         if (PAIR) {
           mma_commit_pair(map_to_rank(smem_u32(&empty_bar[s]), 0));
@@ -408,12 +431,48 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           ++use;
         }
         const uint32_t tacc = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * kTile + half * 128);
+        float* partial = nullptr;                                // of the tile, where its contraction is shared
+        if (!PAIR && p.split > 1) {
+          partial = p.partial + (int64_t)q.number * p.split * BM * BN + row;
+#pragma unroll 1
+          for (int c = 2 * part; c < 2 * part + 2; ++c) {
+            if (n0 + c * 32 >= p.N) break;
+            uint32_t r[32];
+            tmem_ld32(tacc + (uint32_t)(c * 32), r);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            float* to = partial + ((int64_t)q.part * BN + c * 32) * BM;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) __stcg(to + j * BM, __uint_as_float(r[j]));
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[b]);
+          __threadfence();
+          epi_barrier();
+          if (leader) last_s = atomicAdd(p.done + q.number, 1u) == (uint32_t)p.split - 1;
+          epi_barrier();
+          if (!last_s) continue;
+          __threadfence();
+          if (leader) p.done[q.number] = 0;
+        }
 #pragma unroll 1
         for (int c = 2 * part; c < 2 * part + 2; ++c) {
           if (!there || n0 + c * 32 >= p.N) break;
           uint32_t r[32];
-          tmem_ld32(tacc + (uint32_t)(c * 32), r);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (partial) {                                         // the parts in order
+            float sum[32] = {};
+#pragma unroll 1
+            for (int k = 0; k < p.split; ++k) {
+              const float* from = partial + ((int64_t)k * BN + c * 32) * BM;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sum[j] += __ldcg(from + j * BM);
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(sum[j]);
+          } else {
+            tmem_ld32(tacc + (uint32_t)(c * 32), r);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          }
           uint8_t* box = buf + (c >> 1) * 2 * kBoxBytes;
           const int u0 = (c & 1) * 4;
           float v[32];
@@ -475,7 +534,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               *reinterpret_cast<__half*>(mbox + swz(c * 32 + j, (row & 63) >> 3) + (row & 7) * 2) = __float2half_rn(v[j]);
           }
         }
-        if (half == kHalves - 1) {                               // the accumulator has been read
+        if (half == kHalves - 1 && !partial) {                   // the accumulator has been read
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
@@ -768,13 +827,27 @@ lsgd_status check_ortho(const lsgd_ortho_desc* d) {
   return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
+// Blocks that share the contraction of G's tiles, where there are few of them and many columns: a block takes a slice of 64 columns
+// in about 0.45 us, and the last one adds a part up in 0.6.
+int split_of(int r, int n, int P) {
+  const int64_t nt = (r + BM - 1) / BM, tiles = nt * (nt + 1) / 2 * P, nk = (n + BK - 1) / BK;
+  if (nk < 24 || 2 * tiles > sm_count()) return 1;
+  int64_t best = 1, cost = 45 * nk;
+  for (int64_t s = 2; s <= 16 && s * tiles <= sm_count(); ++s) {
+    const int64_t c = 45 * ((nk + s - 1) / s) + 60 * s + 100;
+    // (every part has a slice)
+    if (c < cost && (nk + s - 1) / s * (s - 1) < nk) best = s, cost = c;
+  }
+  return (int)best;
+}
 struct Plan {
   int r, n;                  // rows and columns of X
   int64_t ldx, ldg;
-  uint32_t blocks;
+  uint32_t blocks, tiles;    // of the norm; of G
   bool small;                // one block a matrix
   bool twofold;              // the first X as two fp16 numbers
-  uint64_t part, x0, x1, lo, g, q, total;
+  int split;                 // of G's contraction
+  uint64_t part, done, partial, x0, x1, lo, g, q, total;
 };
 Plan plan_of(const lsgd_ortho_desc* d) {
   Plan m{};
@@ -799,6 +872,12 @@ Plan plan_of(const lsgd_ortho_desc* d) {
     m.x0 = take(x);
     if (d->steps > 1) m.x1 = take(x);
     if (m.twofold) m.lo = take(x);
+    m.split = split_of(m.r, m.n, d->P);
+    m.tiles = (uint32_t)(((m.r + BM - 1) / BM) * ((m.r + BM - 1) / BM + 1) / 2 * (int64_t)d->P);
+    if (m.split > 1) {
+      m.done = take(sizeof(uint32_t) * m.tiles);
+      m.partial = take(sizeof(float) * (uint64_t)BM * BN * m.tiles * m.split);
+    }
     m.g = take(g);
     m.q = take(g);
   }
@@ -844,10 +923,10 @@ int64_t tiles_of(const Product& p, int size) {
   return (p.symmetric ? nt * (nt + 1) / 2 : mt * nt) * p.batch;
 }
 cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, cudaStream_t s) {
-  const int64_t one = tiles_of(p, 128), two = tiles_of(p, 256), sms = sm_count();
+  const int64_t one = tiles_of(p, 128) * p.split, two = tiles_of(p, 256), sms = sm_count();
   if (one >= int64_t(1) << 31) return cudaErrorInvalidValue;
   const int64_t t_one = (one + sms - 1) / sms * 14, t_two = (two + sms / 2 - 1) / (sms / 2) * 20;
-  return t_two <= t_one ? launch_product<true>(a, b, c, d, p, two, s) : launch_product<false>(a, b, c, d, p, one, s);
+  return t_two <= t_one && p.split == 1 ? launch_product<true>(a, b, c, d, p, two, s) : launch_product<false>(a, b, c, d, p, one, s);
 }
 
 template <typename T>
@@ -865,6 +944,8 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   a.d = *d;
   a.part = reinterpret_cast<double*>(scratch + m.part);
   a.blocks = m.blocks;
+  a.done = reinterpret_cast<uint32_t*>(scratch + m.done);
+  a.n_done = m.split > 1 ? m.tiles : 0;
   a.x = reinterpret_cast<__half*>(scratch + m.x0);
   a.lo = m.twofold ? reinterpret_cast<__half*>(scratch + m.lo) : nullptr;
   a.r = m.r;
@@ -903,9 +984,13 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.M = p.N = m.r;
     p.K = m.n;
     p.symmetric = 1;
+    p.split = m.split;
+    p.partial = reinterpret_cast<float*>(scratch + m.partial);
+    p.done = a.done;
     p.alpha = down;
     if (launch_product(x_op, x_op, g_tile, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.K = m.r;
+    p.split = 1;
     p.add = 1;
     p.alpha = d->c * down;
     p.beta = d->b;

@@ -24,6 +24,7 @@
 #pragma once
 #include <type_traits>
 
+#include "activations.h"
 #include "seq.h"
 
 namespace lsgd {
@@ -44,7 +45,6 @@ template <int L> struct Tile {
   // channel apart, four rows at a time) meet in a bank.
   static __device__ __forceinline__ int at(int ch, int t) { return ch * kPitch + ((t + 4 * (ch >> 3)) & (kRows - 1)); }
 };
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
   lsgd_scan_desc d;
@@ -65,25 +65,11 @@ template <typename T>
 __device__ __forceinline__ Rows<T> view(const lsgd_rows& r) {
   return Rows<T>{static_cast<T*>(r.data), r.ld, r.stride};
 }
-__device__ __forceinline__ float ex2(float v) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float2 ex2(float2 v) { return make_float2(ex2(v.x), ex2(v.y)); }
 // exp(delta A) = 2^(delta A2).  The unit's results are 1e-8 low on average for the small arguments of slowly decaying states (its
 // roundings, measured against 64 bits over [-0.1, 0)), which a thousand rows in front of such a state would all add: the argument is
 // lifted by as much.  The gradient of a_log, of 2048 rows, is then off by 7e-7 of its norm instead of 1.4e-6.
 constexpr float kLift = 1.7e-8f;
 __device__ __forceinline__ float2 decay(float2 delta, float2 A2) { return ex2(fma2(delta, A2, make_float2(kLift, kLift))); }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
-// 1 / v of a v in [1, 2^126]
-__device__ __forceinline__ float rcp(float v) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
 // softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) <= 1; log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, with a polynomial in s^2
 // for artanh(s) / s (interpolation at Chebyshev's points; within 2e-8).
 __device__ __forceinline__ float2 softplus(float2 v, float2& e) {
@@ -101,13 +87,6 @@ __device__ __forceinline__ float softplus(float v, float& e) {
   e = e2.x;
   return r;
 }
-// sigmoid(v); exp(-v) is held below 2^126, where the reciprocal ends
-__device__ __forceinline__ float2 sigmoid(float2 v) {
-  const float2 u = mul2(v, both(-kLog2e));
-  return rcp(add2(ex2(make_float2(fminf(u.x, 126.f), fminf(u.y, 126.f))), both(1.f)));
-}
-__device__ __forceinline__ float sigmoid(float v) { return sigmoid(both(v)).x; }
-
 // 8 neighbouring channels of a row, `width` (8, 4, 2 or 1) at a time; those behind the last are zeros.
 template <typename T, int W>
 __device__ __forceinline__ void load_by(float (&f)[8], const T* row, int ch, int D) {

@@ -158,3 +158,16 @@ def test_two_operators_on_two_streams():
     torch.cuda.synchronize()
     for g, (_, out) in zip(gs, ops):
         close(out, ref.ortho(g.double().cpu())[0])
+
+
+@pytest.mark.parametrize("P,m,n", [(1, 100, 3000), (1, 3000, 130), (2, 300, 2050), (1, 16, 8192), (3, 129, 1600)])
+def test_shared_contractions(P, m, n):
+    """Few tiles and many columns: several blocks share a tile's contraction, and the last one adds the parts up in order; twice the same
+    bits."""
+    from paper_1905_10395_b200 import lm
+    op, out = run(P, m, n, seed=n)
+    first = out.view.clone()
+    for _ in range(3):
+        op.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(out.view, first)
