@@ -245,6 +245,9 @@ __device__ __forceinline__ TileAt tile_of(const Product& p, int t, int nt, int p
 
 __device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); }
 
+// 16 bytes `unit` of row `row` of a [128][256 bytes] buffer; a warp that writes a unit of 32 rows, or reads a row, meets no bank twice
+__device__ __forceinline__ int out_at(int row, int unit) { return row * 256 + ((unit ^ (row & 15)) << 4); }
+
 __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
   __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&h);
@@ -491,9 +494,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               }
             }
             const int d = m0 + row - n0 - c * 32;                // the diagonal's column in this piece
+            // selects: every lane has its own j, and 32 branches in turn made this the slowest warp (8 x 256 x 256: 118 us for 113)
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (j == d) v[j] += p.diag;
+            for (int j = 0; j < 32; ++j) v[j] = fmaf(j == d ? 1.f : 0.f, p.diag, v[j]);
           }
           if (p.out) {
             const int gr = m0 + row, gc = n0 + c * 32;
@@ -514,11 +517,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     k.set(f);
                     k.store(o + gr * p.out_ld + gc + 8 * u);
                   }
-              } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (gc + j < p.N) o[gr * p.out_ld + gc + j] = __float2bfloat16_rn(v[j] * p.scale);
               }
+            }
+            if (!p.out_transposed && !p.out_wide) {              // through the buffer: 16 columns a row, turned by the row
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                *reinterpret_cast<uint4*>(buf + out_at(row, c * 4 + u)) =
+                    make_uint4(bf16_pair(v[8 * u] * p.scale, v[8 * u + 1] * p.scale), bf16_pair(v[8 * u + 2] * p.scale, v[8 * u + 3] * p.scale),
+                               bf16_pair(v[8 * u + 4] * p.scale, v[8 * u + 5] * p.scale), bf16_pair(v[8 * u + 6] * p.scale, v[8 * u + 7] * p.scale));
             }
             continue;
           }
@@ -542,7 +548,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             else mbar_arrive(&acc_empty[b]);
           }
         }
-        if (!there || p.out) continue;                           // no staging: neither an added tile nor a stored one
+        if (there && p.out && !p.out_transposed && !p.out_wide) {
+          // a warp a row, 32 neighbouring columns at a time (a lane a row, 2 bytes each, took 16 us of a tile)
+          epi_barrier();
+          for (int k = warp - 2; k < BM && m0 + k < p.M; k += kEpiWarps) {
+            __nv_bfloat16* o = p.out + q.z * p.out_stride + (m0 + k) * p.out_ld + n0;
+#pragma unroll
+            for (int col = lane; col < BN; col += 32)
+              if (n0 + col < p.N) o[col] = *reinterpret_cast<const __nv_bfloat16*>(buf + out_at(k, col >> 3) + (col & 7) * 2);
+          }
+          epi_barrier();
+        }
+        if (!there || p.out) continue;                           // neither an added tile nor a stored one
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         epi_barrier();
         if (leader) {
@@ -738,8 +755,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
           v[2 * j + 1] = fmaf(a.d.b, f.y, a.d.c * (1 / kScale) * __uint_as_float(r[8 * u + 2 * j + 1]));
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + 8 * u + j == row && row < a.r) v[j] += a.d.a * kScale;
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(c + 8 * u + j == row && row < a.r ? 1.f : 0.f, a.d.a * kScale, v[j]);
         *reinterpret_cast<uint4*>(sq + small_at(row, c + 8 * u)) =
             make_uint4(half_pair(v[0], v[1]), half_pair(v[2], v[3]), half_pair(v[4], v[5]), half_pair(v[6], v[7]));
       }
@@ -771,10 +787,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
               k.set(f);
               k.store(o + row * a.d.out.ld + c + 8 * u);
             }
-        } else if (row < a.r) {
+        } else if (a.tall) {
+          if (row < a.r) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c + j < a.n) o[a.tall ? (c + j) * a.d.out.ld + row : row * a.d.out.ld + c + j] = __float2bfloat16_rn(__uint_as_float(r[j]) * down);
+            for (int j = 0; j < 32; ++j)
+              if (c + j < a.n) o[(c + j) * a.d.out.ld + row] = __float2bfloat16_rn(__uint_as_float(r[j]) * down);
+          }
+        } else if (!a.out_wide) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            uint4 w;
+            w.x = bf16_pair(__uint_as_float(r[8 * u]) * down, __uint_as_float(r[8 * u + 1]) * down);
+            w.y = bf16_pair(__uint_as_float(r[8 * u + 2]) * down, __uint_as_float(r[8 * u + 3]) * down);
+            w.z = bf16_pair(__uint_as_float(r[8 * u + 4]) * down, __uint_as_float(r[8 * u + 5]) * down);
+            w.w = bf16_pair(__uint_as_float(r[8 * u + 6]) * down, __uint_as_float(r[8 * u + 7]) * down);
+            if (c + 8 * u < cols16 * 16) *reinterpret_cast<uint4*>(sx + small_at(row, c + 8 * u)) = w;
+          }
         }
         continue;
       }
@@ -794,6 +822,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   if (warp == 0) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+  if (ok && !a.tall && !a.out_wide) {            // from X's place, a warp a row
+    for (int k = warp; k < a.r; k += kSmallThreads / 32) {
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.d.out.data) + p * a.d.out.stride + k * a.d.out.ld;
+      for (int col = lane; col < a.n; col += 32) o[col] = *reinterpret_cast<const __nv_bfloat16*>(sx + small_at(k, col));
+    }
   }
 }
 template <typename T, int VEC>
