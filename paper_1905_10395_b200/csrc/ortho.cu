@@ -4,9 +4,8 @@
 //
 // Three batched products a step, with the polynomial in the second one's epilogue (a I belongs to Q, whose diagonal is then what
 // singular values are multiplied by, about 1 in the last steps; stored without it, it would be about -2.5 and its rounding count
-// 2.5 times).  G and Q are symmetric: only tiles on and
-// above the diagonal are computed, each stored twice, the second time transposed, so a step costs 3 r r n + r r r
-// multiply-adds instead of 4 r r n + 2 r r r.
+// 2.5 times).  G and Q are symmetric: only tiles on and above the diagonal are computed, each stored twice, the second time
+// transposed, so a step costs 1.5 r r n + 0.5 r r r multiply-adds instead of 2 r r n + r r r.
 //
 // Operands are fp16 times 2^10, sums fp32.  Entries of X and G are below 2 (singular values stay below 1.3 with the usual
 // coefficients) and those that matter are not below 2^-13 of their matrix's largest, so fp16's range holds them and its 11 bits
@@ -17,8 +16,12 @@
 //
 // product_kernel is a persistent kernel of one CTA an SM on 128 x 128 tiles, or of pairs of CTAs on 256 x 256, with the roles of the
 // batched product of gemm_tc.cu: one thread fetches operands by tiled bulk copies into a ring, one issues tcgen05.mma into one of two
-// accumulators in tensor memory, one fetches the tiles that are added, eight warps run the epilogue.  Every wait is bounded by a clock budget; on expiry the kernel
-// raises a status bit, drains its copies, frees tensor memory and returns.
+// accumulators in tensor memory, one fetches the tiles that are added, eight warps run the epilogue.  Every wait is bounded by a clock
+// budget; on expiry the kernel raises a status bit, drains its copies, frees tensor memory and returns.
+//
+// What bounds it: large batches (2 x 4096 x 4096: 2.5 ms, 1090 TFLOP/s; 32 x 1024 x 1024: 895 us, 770) the operands' way from L2, at
+// 8 TB/s; a few small matrices (8 x 256 x 256: 113 us) the chain of 15 dependent products of 6 to 9 us, of which the contraction itself
+// takes 1.3, its first operands' latency 1.2, the epilogue with its store 1.5 and the change of kernels 1.6.
 #include <cuda_fp16.h>
 
 #include "seq.h"
@@ -245,6 +248,17 @@ __device__ __forceinline__ TileAt tile_of(const Product& p, int t, int nt, int p
 
 __device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); }
 
+// What all of the epilogue's threads say: after a wait that ran out for some of them all leave together, none at a barrier alone.
+__device__ __forceinline__ bool epi_all(bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.red.and.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+      : "=r"(r)
+      : "r"((uint32_t)ok), "n"(32 * kEpiWarps)
+      : "memory");
+  return r;
+}
+
 // 16 bytes `unit` of row `row` of a [128][256 bytes] buffer; a warp that writes a unit of 32 rows, or reads a row, meets no bank twice
 __device__ __forceinline__ int out_at(int row, int unit) { return row * 256 + ((unit ^ (row & 15)) << 4); }
 
@@ -422,17 +436,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const int b = local & 1, m0 = q.m0 + rank * 128;
       const bool twice = p.symmetric && q.m0 != q.n0;
       ok = mbar_wait(&acc_full[b], (local >> 1) & 1, abort_flag, status);
-      if (!ok) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
       for (int half = 0; half < kHalves; ++half) {
         const int n0 = q.n0 + half * 128;
         const bool there = n0 < p.N && m0 < p.M;
-        if (there && p.add) {
-          ok = mbar_wait(&in_full, use & 1, abort_flag, status);
-          if (!ok) break;
-          ++use;
-        }
+        if (there && p.add && ok) ok = mbar_wait(&in_full, use++ & 1, abort_flag, status);
+        ok = epi_all(ok);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t tacc = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * kTile + half * 128);
         float* partial = nullptr;                                // of the tile, where its contraction is shared
         if (!PAIR && p.split > 1) {
@@ -861,8 +872,9 @@ lsgd_status check_ortho(const lsgd_ortho_desc* d) {
   return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
-// Blocks that share the contraction of G's tiles, where there are few of them and many columns: a block takes a slice of 64 columns
-// in about 0.45 us, and the last one adds a part up in 0.6.
+// Blocks that share the contraction of G's tiles, where there are few of them and many columns.  In units of 10 ns a block takes 45
+// for a slice of 64 columns (35 to 45 measured), and the last one adds a part up in 60 (300 x 5000: 327 us unshared, 216 so; 1024 x
+// 4096: 288, 235).
 int split_of(int r, int n, int P) {
   const int64_t nt = (r + BM - 1) / BM, tiles = nt * (nt + 1) / 2 * P, nk = (n + BK - 1) / BK;
   if (nk < 24 || 2 * tiles > sm_count()) return 1;
