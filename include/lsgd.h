@@ -603,7 +603,7 @@ typedef enum {
 typedef struct {
   uint32_t struct_size;      /* = sizeof(lsgd_conv_desc)                                                       */
   int32_t P;                 /* >= 1                                                                          */
-  int64_t T;                 /* >= 0, P * T < 2^31 - 4096                                                     */
+  int64_t T;                 /* >= 0, P * T < 2^31 - 2^20                                                     */
   int32_t D, W;              /* D in [1, 65536], W in [1, 4]                                                  */
   int32_t act_dtype;         /* lsgd_dtype                                                                    */
   int32_t act;               /* lsgd_conv_act                                                                 */
@@ -642,7 +642,7 @@ LSGD_API lsgd_status lsgd_conv_backward(const lsgd_conv_desc* desc, void* stream
 typedef struct {
   uint32_t struct_size;      /* = sizeof(lsgd_scan_desc)                                                       */
   int32_t P;                 /* >= 1                                                                          */
-  int64_t T;                 /* >= 0, P * T < 2^31 - 4096                                                     */
+  int64_t T;                 /* >= 0, P * T < 2^31 - 2^20                                                     */
   int32_t D, N;              /* D in [1, 65536], N in [1, 64]                                                  */
   int32_t act_dtype;         /* lsgd_dtype                                                                    */
   int32_t accumulate;

@@ -383,9 +383,9 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
     if (rows && !d->out.data) return LSGD_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(d->state) % ab) return LSGD_ERR_ALIGNMENT;
     LSGD_ROWS(d->out, T, D, ab, true, false);
-    const Extent ins[] = {extent(d->x, P, T, D, ab)};
+    const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->w, P, D, d->W, 4), extent(d->bias, P, 1, D, 4)};
     const Extent outs[] = {extent(d->out, P, T, D, ab), extent({d->state, D, (int64_t)d->seq.S * (d->W - 1) * D}, P, (int64_t)d->seq.S * (d->W - 1), D, ab)};
-    return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
+    return all_apart(outs, 2, ins, 3) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
   }
   if (d->state) return LSGD_ERR_INVALID_ARG;
   if (rows && (!d->d_out.data || !d->dx.data)) return LSGD_ERR_INVALID_ARG;

@@ -75,6 +75,7 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   const int64_t P = d->P, T = d->T, D = d->D, N = d->N;
   const int ab = elem_bytes(d->act_dtype);
   const bool rows = T > 0;
+  const int64_t states = D * N, groups = (T + kGroup - 1) / kGroup;
   if (!d->a_log.data || (rows && (!d->x.data || !d->dt.data || !d->b.data || !d->c.data))) return LSGD_ERR_INVALID_ARG;
 #define LSGD_ROWS(r, t, w, bytes, written, shared)                                                 \
   do {                                                                                            \
@@ -92,11 +93,12 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   if (!backward) {
     if (rows && !d->out.data) return LSGD_ERR_INVALID_ARG;
     LSGD_ROWS(d->out, T, D, ab, true, false);
-    const int64_t states = D * N, kept = (int64_t)d->seq.S, groups = (T + kGroup - 1) / kGroup;
-    const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->dt, P, T, D, ab), extent(d->z, P, T, D, ab), extent(d->b, P, T, N, ab), extent(d->c, P, T, N, ab)};
+    const int64_t kept = (int64_t)d->seq.S;
+    const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->dt, P, T, D, ab),  extent(d->z, P, T, D, ab),   extent(d->b, P, T, N, ab),
+                          extent(d->c, P, T, N, ab), extent(d->a_log, P, D, N, 4), extent(d->skip, P, 1, D, 4), extent(d->dt_bias, P, 1, D, 4)};
     const Extent outs[] = {extent(d->out, P, T, D, ab), extent({d->state, states, kept * states}, P, kept, states, 4),
                            extent({d->saved, states, groups * states}, P, groups, states, 4)};
-    return all_apart(outs, 3, ins, 5) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
+    return all_apart(outs, 3, ins, 8) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
   }
   if (d->state || (rows && (!d->saved || !d->d_out.data || !d->dx.data || !d->d_dt.data || !d->db.data || !d->dc.data))) return LSGD_ERR_INVALID_ARG;
   if (!d->d_a_log.data) return LSGD_ERR_INVALID_ARG;
@@ -115,10 +117,10 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
 #undef LSGD_ROWS
   const Extent ins[] = {extent(d->x, P, T, D, ab), extent(d->dt, P, T, D, ab),   extent(d->z, P, T, D, ab),     extent(d->b, P, T, N, ab),
                         extent(d->c, P, T, N, ab), extent(d->d_out, P, T, D, ab), extent(d->a_log, P, D, N, 4), extent(d->skip, P, 1, D, 4),
-                        extent(d->dt_bias, P, 1, D, 4)};
+                        extent(d->dt_bias, P, 1, D, 4), extent({d->saved, states, groups * states}, P, groups, states, 4)};
   const Extent outs[] = {extent(d->dx, P, T, D, ab),     extent(d->d_dt, P, T, D, ab),  extent(d->dz, P, T, D, ab),    extent(d->db, P, T, N, ab),
                          extent(d->dc, P, T, N, ab),     extent(d->d_a_log, P, D, N, 4), extent(d->d_skip, P, 1, D, 4), extent(d->d_dt_bias, P, 1, D, 4)};
-  return all_apart(outs, 8, ins, 9) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
+  return all_apart(outs, 8, ins, 10) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
 bool row_vec4(const lsgd_rows& r, int64_t P, int64_t T, int bytes) {

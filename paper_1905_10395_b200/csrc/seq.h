@@ -4,7 +4,8 @@
 
 namespace lsgd {
 
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;      // of all workers; a tile behind the last row still has a row number
+// Rows of all workers: a loop's next step behind the last row (65535 blocks of 4 sequences, a chain, a tile) is still a row number.
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 20);
 
 // Sequences given by their starts are looked up once: codes[p][t] is the sequence of row t, -1 in front of the first and behind
 // the last.  A row begins a sequence where its code differs from the row's before it (an empty sequence has no row).  Equal parts

@@ -131,6 +131,18 @@ def test_sequences_are_checked(api):
                 assert call(C.byref(make(api, seq=seq)), None) == status, (make, seq.starts, seq.stride, seq.S)
 
 
+def test_most_rows(api):
+    """2^31 - 2^20 rows are too many; one less passes, to the refusal of the scratch's alignment."""
+    L, T = api.lib(), (1 << 31) - (1 << 20)
+    rows = dict(P=1, seq=api.Sequences(1 << 50, 0, 5), scratch=8, scratch_bytes=1 << 60)
+    far = {k: api.Rows((1 + i) << 42, 16, 0) for i, k in enumerate(("x", "dt", "z", "out", "d_out", "dx", "d_dt", "dz", "b", "c", "db", "dc"))}
+    for make, calls in ((_conv, (L.lsgd_conv_forward, L.lsgd_conv_backward)), (_scan, (L.lsgd_scan_forward, L.lsgd_scan_backward))):
+        names = {f for f, _ in type(make(api))._fields_}
+        over = rows | {k: v for k, v in far.items() if k in names} | ({"saved": 1 << 52} if "saved" in names else {})
+        for call in calls:
+            assert call(C.byref(make(api, T=T, **over)), None) == 8 and call(C.byref(make(api, T=T - 1, **over)), None) == 3
+
+
 def test_conv_refuses_rows(api):
     fwd, bwd = api.lib().lsgd_conv_forward, api.lib().lsgd_conv_backward
     R = api.Rows
@@ -190,6 +202,12 @@ def test_outputs_overlap_no_input(api):
     ragged = dict(seq=api.Sequences(MB * 70, 0, 5))
     assert conv(C.byref(_conv(api, x=R(MB, 32, 3200), out=R(MB + 32, 32, 3200), scratch=MB * 30 + 8, scratch_bytes=1 << 30, **ragged)), None) == 3
     assert conv(C.byref(_conv(api, x=R(MB, 64, 32), out=R(MB + 32, 64, 32), scratch=MB * 30 + 8, scratch_bytes=1 << 30, **ragged)), None) == 3
+    # parameters, and the saved states that the backward pass reads, are inputs too
+    assert conv(C.byref(_conv(api, out=R(5 * MB, 16, 1600))), None) == 1 and conv(C.byref(_conv(api, out=R(7 * MB, 16, 1600))), None) == 1
+    d = _scan(api)
+    for at in (d.a_log.data, d.skip.data, d.dt_bias.data):
+        assert scan(C.byref(_scan(api, out=R(at, 16, 1600))), None) == 1
+    assert bwd(C.byref(_scan(api, d_dt=R(d.saved, 16, 1600))), None) == 1
     ortho = api.lib().lsgd_ortho
     for k, r in (("out", R(MB, 200, 6000)), ("momentum", R(MB, 200, 6000)), ("out", R(2 * MB + 4, 200, 6000))):
         assert ortho(C.byref(_ortho(api, **{k: r})), None) == 1
