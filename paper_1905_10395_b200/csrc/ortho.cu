@@ -14,14 +14,14 @@
 // whole chain is then off by at most 1.6e-3 of the result's norm instead of 2e-3 (300 x 300; 16 x 16: 1.4e-3 instead of 3.7e-3),
 // rounding to bf16 by 1.7e-3.  Larger matrices are off by less (1024 x 1024: 1.6e-3 to 1.8e-3), and would take 6 to 11 % longer.
 //
-// product_kernel is a persistent kernel of one CTA an SM on 128 x 128 tiles, or of pairs of CTAs on 256 x 256, with the roles of the
+// product_kernel is a persistent kernel of one CTA an SM on tiles of 128 x 128 or 128 x 64, or of pairs of CTAs on 256 x 256, with the roles of the
 // batched product of gemm_tc.cu: one thread fetches operands by tiled bulk copies into a ring, one issues tcgen05.mma into one of two
 // accumulators in tensor memory, one fetches the tiles that are added, eight warps run the epilogue.  Every wait is bounded by a clock
 // budget; on expiry the kernel raises a status bit, drains its copies, frees tensor memory and returns.
 //
 // What bounds it: large batches (2 x 4096 x 4096: 2.5 ms, 1090 TFLOP/s; 32 x 1024 x 1024: 895 us, 770) the operands' way from L2, at
-// 8 TB/s; a few small matrices (8 x 256 x 256: 113 us) the chain of 15 dependent products of 6 to 9 us, of which the contraction itself
-// takes 1.3, its first operands' latency 1.2, the epilogue with its store 1.5 and the change of kernels 1.6.
+// 8 TB/s; a few small matrices (8 x 256 x 256: 93 us) the chain of 15 dependent products of about 6 us each: its first operands'
+// latency 1.2, the contraction 1.3, the epilogue with its store 1, the change of kernels 1.6.
 #include <cuda_fp16.h>
 
 #include "seq.h"
@@ -35,9 +35,15 @@ namespace {
 __device__ uint32_t g_status;                    // of the device
 
 constexpr float kScale = 1024.f;                 // of X, G and Q as stored
-constexpr int BM = 128, BN = 128, BK = 64, kStages = 5;
-constexpr int kBoxBytes = 64 * 64 * 2, kStageBytes = (BM + BN) * BK * 2, kTileBytes = BM * BN * 2;
-constexpr int kSmemBytes = kStages * kStageBytes + 2 * kTileBytes + 1024;
+constexpr int BM = 128, BK = 64, kBoxBytes = 64 * 64 * 2, kTileBytes = BM * 128 * 2;
+// The products' forms: 128 columns a tile or 64, or pairs of CTAs of 128 rows and 256 columns each.
+template <bool PAIR, int BN>
+struct Form {
+  static constexpr int kM = PAIR ? 256 : 128, kN = PAIR ? 256 : BN;      // of a tile
+  static constexpr int kBoxesB = PAIR ? 2 : BN / 64;                     // of B, a CTA fetches 64 rows or columns at a time
+  static constexpr int kStageBytes = (2 + kBoxesB) * kBoxBytes, kStages = BN == 64 ? 6 : 5;
+  static constexpr int kSmemBytes = kStages * kStageBytes + 2 * kTileBytes + 1024;
+};
 constexpr int kTwofoldRows = 768;
 constexpr int kEpiWarps = 8, kThreads = 96 + 32 * kEpiWarps;    // operands, products, the added tile; the epilogue
 
@@ -199,7 +205,7 @@ struct Product {
   int b_mn;                  // B is stored [K][N] (else [N][K])
   int symmetric;             // square: tiles on and above the diagonal, stored twice
   int split;                 // blocks that share a tile's contraction (1: none do); the last of them to finish adds up
-  float* partial;            // split: [tiles][split][128 columns][128 rows]
+  float* partial;            // split: [tiles][split][columns of a tile][128 rows]
   uint32_t* done;            // split: blocks of a tile that have finished, 0 between products
   int add;                   // C = alpha acc + beta D + diag I
   int twofold;               // C = A B + A D, D of B's layout (instead of an added tile)
@@ -218,8 +224,8 @@ struct TileAt {
   int part, k0, k1;          // of the contraction's slices, [k0, k1)
   int number;                // of the tile, without its parts
 };
-// Tile number t: all of a row of tiles, or those from the diagonal on.
-template <int SIZE>
+// Tile number t: all of a row of tiles, or those from the diagonal on (of 64 columns: both halves of each square).
+template <typename F>
 __device__ __forceinline__ TileAt tile_of(const Product& p, int t, int nt, int per) {
   TileAt q;
   const int nk = p.nk();
@@ -236,12 +242,15 @@ __device__ __forceinline__ TileAt tile_of(const Product& p, int t, int nt, int p
   t -= q.z * per;
   int i = 0;
   if (p.symmetric) {
+    constexpr int kHalves = F::kM / F::kN;
+    const int half = t % kHalves;
+    t /= kHalves;
     while (t >= nt - i) t -= nt - i++;
-    q.m0 = i * SIZE;
-    q.n0 = (i + t) * SIZE;
+    q.m0 = i * F::kM;
+    q.n0 = (i + t) * F::kM + half * F::kN;
   } else {
-    q.m0 = t / nt * SIZE;
-    q.n0 = t % nt * SIZE;
+    q.m0 = t / nt * F::kM;
+    q.n0 = t % nt * F::kN;
   }
   return q;
 }
@@ -269,22 +278,24 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
 
 // PAIR: a cluster of two CTAs computes a 256 x 256 tile, each fetching its half of the rows of A and of B; the first one's issuer
 // drives both tensor cores (cta_group::2).  Its barriers count both CTAs' copies and epilogues.
-template <bool PAIR>
+template <bool PAIR, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ Product p) {
-  constexpr int kTile = PAIR ? 256 : 128, kHalves = PAIR ? 2 : 1;
-  constexpr uint32_t kTmemCols = 2 * kTile;      // two accumulators
+  using F = Form<PAIR, BN>;
+  constexpr int kStages = F::kStages, kStageBytes = F::kStageBytes, kHalves = PAIR ? 2 : 1;
+  constexpr uint32_t kTmemCols = 2 * F::kN;      // two accumulators
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* buf = smem + kStages * kStageBytes;   // 128 x 128: D in, C out; two boxes of [128][64]
+  uint8_t* buf = smem + kStages * kStageBytes;   // 128 x BN: D in, C out; boxes of [128][64]
   uint8_t* mirror = buf + kTileBytes;            // C transposed
   __shared__ uint64_t full_bar[kStages], empty_bar[kStages], acc_full[2], acc_empty[2], in_full, in_free;
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s, last_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)cluster_rank() : 0;
-  const int mt = (p.M + kTile - 1) / kTile, nt = (p.N + kTile - 1) / kTile, per = p.symmetric ? nt * (nt + 1) / 2 : mt * nt;
+  const int mt = (p.M + F::kM - 1) / F::kM, nt = p.symmetric ? mt : (p.N + F::kN - 1) / F::kN;
+  const int per = p.symmetric ? mt * (mt + 1) / 2 * (F::kM / F::kN) : mt * nt;
   const int n_tiles = per * p.batch * p.split, nk1 = p.nk1();
   const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, stride = PAIR ? gridDim.x >> 1 : gridDim.x;
   uint32_t* status = &g_status;
@@ -329,8 +340,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     uint32_t it = 0;
     bool ok = true;
     for (int t = first; t < n_tiles && ok; t += stride) {
-      const TileAt q = tile_of<kTile>(p, t, nt, per);
-      const int m0 = q.m0 + rank * 128, n0 = q.n0 + rank * 128;
+      const TileAt q = tile_of<F>(p, t, nt, per);
+      const int m0 = q.m0 + rank * 128, n0 = q.n0 + rank * 128;      // (of B a CTA of a pair fetches half)
       for (int kt = q.k0; kt < q.k1; ++kt, ++it) {
         const int s = it % kStages;
         ok = mbar_wait(&empty_bar[s], ((it / kStages) & 1) ^ 1, abort_flag, status);
@@ -344,13 +355,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int bx = p.b_mn ? n0 + 64 * j : k0, by = p.b_mn ? k0 : n0 + 64 * j;
-          if (PAIR) {
-            tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, k0, m0 + 64 * j, q.z);
-            tma_load_3d_pair(sb + j * kBoxBytes, from_b, bar, bx, by, q.z);
-          } else {
-            tma_load_3d(sa + j * kBoxBytes, &map_a, &full_bar[s], k0, m0 + 64 * j, q.z);
-            tma_load_3d(sb + j * kBoxBytes, from_b, &full_bar[s], bx, by, q.z);
-          }
+          if (PAIR) tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, k0, m0 + 64 * j, q.z);
+          else tma_load_3d(sa + j * kBoxBytes, &map_a, &full_bar[s], k0, m0 + 64 * j, q.z);
+          if (j >= F::kBoxesB) break;
+          if (PAIR) tma_load_3d_pair(sb + j * kBoxBytes, from_b, bar, bx, by, q.z);
+          else tma_load_3d(sb + j * kBoxBytes, from_b, &full_bar[s], bx, by, q.z);
         }
       }
     }
@@ -362,7 +371,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
   } else if (warp == 1 && lane == 0 && rank == 0) {
     // ---------------------------------------------------------------- products
-    const uint32_t idesc = (1u << 4) | ((uint32_t)(p.b_mn ? 1 : 0) << 16) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(p.b_mn ? 1 : 0) << 16) | ((uint32_t)(F::kN >> 3) << 17) | ((uint32_t)(F::kM >> 4) << 24);
     uint32_t it = 0;
     int local = 0;
     bool ok = true;
@@ -371,8 +380,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       ok = mbar_wait(&acc_empty[b], ((local >> 1) & 1) ^ 1, abort_flag, status);
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t tacc = tmem_base + (uint32_t)(b * kTile);
-      const TileAt q = tile_of<kTile>(p, t, nt, per);
+      const uint32_t tacc = tmem_base + (uint32_t)(b * F::kN);
+      const TileAt q = tile_of<F>(p, t, nt, per);
       for (int kt = q.k0; kt < q.k1; ++kt, ++it) {
         const int s = it % kStages;
         ok = mbar_wait(&full_bar[s], (it / kStages) & 1, abort_flag, status);
@@ -406,7 +415,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     uint32_t use = 0;
     bool ok = true;
     for (int t = first; t < n_tiles && ok; t += stride) {
-      const TileAt q = tile_of<kTile>(p, t, nt, per);
+      const TileAt q = tile_of<F>(p, t, nt, per);
       const int m0 = q.m0 + rank * 128;
       for (int half = 0; half < kHalves; ++half) {
         const int n0 = q.n0 + half * 128;
@@ -414,9 +423,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         ok = mbar_wait(&in_free, (use & 1) ^ 1, abort_flag, status);
         if (!ok) break;
         ++use;
-        mbar_expect_tx(&in_full, kTileBytes);
+        mbar_expect_tx(&in_full, BN / 64 * 2 * kBoxBytes);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) tma_load_3d(buf + j * 2 * kBoxBytes, &map_d, &in_full, n0 + 64 * j, m0, q.z);
+        for (int j = 0; j < BN / 64; ++j) tma_load_3d(buf + j * 2 * kBoxBytes, &map_d, &in_full, n0 + 64 * j, m0, q.z);
       }
     }
     if (!ok && use > 0) {
@@ -426,15 +435,16 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
   } else if (warp >= 2 && warp < 2 + kEpiWarps) {
     // ---------------------------------------------------------------- epilogue: this CTA's 128 rows, 128 columns at a time
+    constexpr int kEach = BN / 64;                 // pieces of 32 columns of a warp
     const int q4 = warp & 3, part = (warp - 2) >> 2, row = q4 * 32 + lane;
     const bool leader = threadIdx.x == 64;
     int local = 0;
     uint32_t use = 0;
     bool ok = true;
     for (int t = first; t < n_tiles && ok; t += stride, ++local) {
-      const TileAt q = tile_of<kTile>(p, t, nt, per);
+      const TileAt q = tile_of<F>(p, t, nt, per);
       const int b = local & 1, m0 = q.m0 + rank * 128;
-      const bool twice = p.symmetric && q.m0 != q.n0;
+      const bool twice = p.symmetric && q.n0 >= q.m0 + F::kM;
       ok = mbar_wait(&acc_full[b], (local >> 1) & 1, abort_flag, status);
 #pragma unroll 1
       for (int half = 0; half < kHalves; ++half) {
@@ -444,12 +454,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         ok = epi_all(ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t tacc = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * kTile + half * 128);
+        const uint32_t tacc = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * F::kN + half * 128);
         float* partial = nullptr;                                // of the tile, where its contraction is shared
         if (!PAIR && p.split > 1) {
           partial = p.partial + (int64_t)q.number * p.split * BM * BN + row;
 #pragma unroll 1
-          for (int c = 2 * part; c < 2 * part + 2; ++c) {
+          for (int c = kEach * part; c < kEach * part + kEach; ++c) {
             if (n0 + c * 32 >= p.N) break;
             uint32_t r[32];
             tmem_ld32(tacc + (uint32_t)(c * 32), r);
@@ -470,16 +480,21 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           if (leader) p.done[q.number] = 0;
         }
 #pragma unroll 1
-        for (int c = 2 * part; c < 2 * part + 2; ++c) {
+        for (int c = kEach * part; c < kEach * part + kEach; ++c) {
           if (!there || n0 + c * 32 >= p.N) break;
           uint32_t r[32];
           if (partial) {                                         // the parts in order
             float sum[32] = {};
 #pragma unroll 1
-            for (int k = 0; k < p.split; ++k) {
-              const float* from = partial + ((int64_t)k * BN + c * 32) * BM;
+            for (int k = 0; k < p.split; k += 2) {               // two of them fetched at a time
+              const float *from = partial + ((int64_t)k * BN + c * 32) * BM, *then = k + 1 < p.split ? from + (int64_t)BN * BM : nullptr;
+              float f[32], g[32];
 #pragma unroll
-              for (int j = 0; j < 32; ++j) sum[j] += __ldcg(from + j * BM);
+              for (int j = 0; j < 32; ++j) f[j] = __ldcg(from + j * BM);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) g[j] = then ? __ldcg(then + j * BM) : 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sum[j] = (sum[j] + f[j]) + g[j];
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(sum[j]);
@@ -505,7 +520,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               }
             }
             const int d = m0 + row - n0 - c * 32;                // the diagonal's column in this piece
-            // selects: every lane has its own j, and 32 branches in turn made this the slowest warp (8 x 256 x 256: 118 us for 113)
+            // selects: every lane has its own j, and 32 branches in turn made this the slowest warp (8 x 256 x 256: 118 us for 113, with
+            // squares)
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = fmaf(j == d ? 1.f : 0.f, p.diag, v[j]);
           }
@@ -545,7 +561,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 make_uint4(half_pair(v[8 * u], v[8 * u + 1]), half_pair(v[8 * u + 2], v[8 * u + 3]),
                            half_pair(v[8 * u + 4], v[8 * u + 5]), half_pair(v[8 * u + 6], v[8 * u + 7]));
           if (twice) {
-            uint8_t* mbox = mirror + (row >> 6) * 2 * kBoxBytes;
+            uint8_t* mbox = mirror + (row >> 6) * (BN * 128);
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               *reinterpret_cast<__half*>(mbox + swz(c * 32 + j, (row & 63) >> 3) + (row & 7) * 2) = __float2half_rn(v[j]);
@@ -574,13 +590,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         epi_barrier();
         if (leader) {
+          // boxes of BN rows: of C's 128 rows one or two
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (n0 + 64 * j < p.N) tma_store_3d(buf + j * 2 * kBoxBytes, &map_c, n0 + 64 * j, m0, q.z);
-          if (twice) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              if (m0 + 64 * j < p.M) tma_store_3d(mirror + j * 2 * kBoxBytes, &map_c, m0 + 64 * j, n0, q.z);
+          for (int j = 0; j < 2; ++j) {
+            if (BN == 64 && m0 + 64 * j < p.M) tma_store_3d(buf + j * kBoxBytes, &map_c, n0, m0 + 64 * j, q.z);
+            if (BN == 128 && n0 + 64 * j < p.N) tma_store_3d(buf + j * 2 * kBoxBytes, &map_c, n0 + 64 * j, m0, q.z);
+            if (twice && m0 + 64 * j < p.M) tma_store_3d(mirror + j * (BN * 128), &map_c, m0 + 64 * j, n0, q.z);
           }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -872,24 +887,25 @@ lsgd_status check_ortho(const lsgd_ortho_desc* d) {
   return all_apart(outs, 2, ins, 1) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
-// Blocks that share the contraction of G's tiles, where there are few of them and many columns.  In units of 10 ns a block takes 45
-// for a slice of 64 columns (35 to 45 measured), and the last one adds a part up in 60 (300 x 5000: 327 us unshared, 216 so; 1024 x
-// 4096: 288, 235).
+// Blocks that share the contraction of G's tiles, where there are few of them and many columns.  In units of 10 ns a block takes 33
+// for a slice of 64 columns (45 with tiles of 128), and where it is shared 100 and 60 for every part that the last one adds up (300 x
+// 5000: 233 us unshared, 143 so; 256 x 4096: 194, 128; 1024 x 4096: 274, 231).
 int split_of(int r, int n, int P) {
-  const int64_t nt = (r + BM - 1) / BM, tiles = nt * (nt + 1) / 2 * P, nk = (n + BK - 1) / BK;
-  if (nk < 24 || 2 * tiles > sm_count()) return 1;
-  int64_t best = 1, cost = 45 * nk;
-  for (int64_t s = 2; s <= 16 && s * tiles <= sm_count(); ++s) {
-    const int64_t c = 45 * ((nk + s - 1) / s) + 60 * s + 100;
-    // (every part has a slice)
-    if (c < cost && (nk + s - 1) / s * (s - 1) < nk) best = s, cost = c;
+  const int64_t mt = (r + BM - 1) / BM, tiles = mt * (mt + 1) / 2 * P, nk = (n + BK - 1) / BK;
+  int64_t best = 1, least = INT64_MAX;
+  for (int64_t s = 1; s <= 16 && s * tiles <= sm_count(); ++s) {
+    const int64_t share = (nk + s - 1) / s;
+    if (s > 1 && share * (s - 1) >= nk) continue;            // every part has a slice
+    const bool half = 2 * s * tiles <= sm_count();
+    const int64_t cost = (half ? 33 : 45) * share + (s > 1 ? 100 + 60 * s : 0);
+    if (cost < least) best = s, least = cost;
   }
   return (int)best;
 }
 struct Plan {
   int r, n;                  // rows and columns of X
   int64_t ldx, ldg;
-  uint32_t blocks, tiles;    // of the norm; of G
+  uint32_t blocks, tiles;    // of the norm; of G, of 64 columns
   bool small;                // one block a matrix
   bool twofold;              // the first X as two fp16 numbers
   int split;                 // of G's contraction
@@ -919,10 +935,10 @@ Plan plan_of(const lsgd_ortho_desc* d) {
     if (d->steps > 1) m.x1 = take(x);
     if (m.twofold) m.lo = take(x);
     m.split = split_of(m.r, m.n, d->P);
-    m.tiles = (uint32_t)(((m.r + BM - 1) / BM) * ((m.r + BM - 1) / BM + 1) / 2 * (int64_t)d->P);
+    m.tiles = (uint32_t)(((m.r + BM - 1) / BM) * ((m.r + BM - 1) / BM + 1) * (int64_t)d->P);
     if (m.split > 1) {
-      m.done = take(sizeof(uint32_t) * m.tiles);
-      m.partial = take(sizeof(float) * (uint64_t)BM * BN * m.tiles * m.split);
+      m.done = take(sizeof(uint32_t) * m.tiles);             // (of 64 columns)
+      m.partial = take(sizeof(float) * (uint64_t)BM * 64 * m.tiles * m.split);
     }
     m.g = take(g);
     m.q = take(g);
@@ -938,13 +954,12 @@ bool tile_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, 
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, 128);
 }
 
-// Pairs of CTAs where their larger tiles' rounds over the machine take less: such a tile is four of the others on two SMs, and
-// runs at about 1.4 times their rate.
-template <bool PAIR>
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, int64_t tiles, cudaStream_t s) {
+template <bool PAIR, int BN>
+cudaError_t launch_form(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, int64_t tiles, cudaStream_t s) {
   static OncePerDevice attr;
+  constexpr int kSmemBytes = Form<PAIR, BN>::kSmemBytes;
   if (!attr.here()) {
-    const cudaError_t e = cudaFuncSetAttribute(product_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    const cudaError_t e = cudaFuncSetAttribute(product_kernel<PAIR, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
     attr.here() = true;
   }
@@ -962,17 +977,24 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = PAIR ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, product_kernel<PAIR>, a, b, c, d, p);
+  return cudaLaunchKernelEx(&cfg, product_kernel<PAIR, BN>, a, b, c, d, p);
 }
-int64_t tiles_of(const Product& p, int size) {
-  const int64_t mt = (p.M + size - 1) / size, nt = (p.N + size - 1) / size;
-  return (p.symmetric ? nt * (nt + 1) / 2 : mt * nt) * p.batch;
+template <typename F>
+int64_t tiles_of(const Product& p) {
+  const int64_t mt = (p.M + F::kM - 1) / F::kM, nt = (p.N + F::kN - 1) / F::kN;
+  return (p.symmetric ? mt * (mt + 1) / 2 * (F::kM / F::kN) : mt * nt) * p.batch * p.split;
 }
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, cudaStream_t s) {
-  const int64_t one = tiles_of(p, 128) * p.split, two = tiles_of(p, 256), sms = sm_count();
-  if (one >= int64_t(1) << 31) return cudaErrorInvalidValue;
-  const int64_t t_one = (one + sms - 1) / sms * 14, t_two = (two + sms / 2 - 1) / (sms / 2) * 20;
-  return t_two <= t_one && p.split == 1 ? launch_product<true>(a, b, c, d, p, two, s) : launch_product<false>(a, b, c, d, p, one, s);
+// The form whose rounds over the machine take least.  A pair's tile is four of 128 x 128 on two SMs and runs at about 1.4 times their
+// rate (32 x 1024 x 1024: 1131 us instead of 1334).  One of 64 columns fetches three quarters of a square's operands and has half its
+// epilogue, so it takes about 11 of its 14: where there are few (3 x 1001 x 333: 131 us instead of 147; 768 x 768: 140 instead of 158; 8 x 256
+// x 256: 93 instead of 113).  c64: the stored tensor in boxes of 64 rows.
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& c64, const CUtensorMap& d, const Product& p,
+                           cudaStream_t s) {
+  const int64_t half = tiles_of<Form<false, 64>>(p), one = tiles_of<Form<false, 128>>(p), two = tiles_of<Form<true, 128>>(p), sms = sm_count();
+  if (half >= int64_t(1) << 31) return cudaErrorInvalidValue;
+  const int64_t t_half = (half + sms - 1) / sms * 11, t_one = (one + sms - 1) / sms * 14, t_two = (two + sms / 2 - 1) / (sms / 2) * 20;
+  if (t_half < t_one && t_half < t_two) return launch_form<false, 64>(a, b, c64, d, p, half, s);
+  return t_two <= t_one && p.split == 1 ? launch_form<true, 128>(a, b, c, d, p, two, s) : launch_form<false, 128>(a, b, c, d, p, one, s);
 }
 
 template <typename T>
@@ -1019,11 +1041,11 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     const void* from = x[step & 1];
     void* to = x[(step & 1) ^ 1];
     const bool last = step + 1 == d->steps;
-    CUtensorMap x_op, lo_op, g_op, q_op, g_tile, q_tile, to_tile;
+    CUtensorMap x_op, lo_op, to_op, g_op, q_op, g_tile, q_tile, to_tile;
     if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&lo_op, m.twofold ? scratch + m.lo : from, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
         !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) ||
         !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P) ||
-        !tile_map(&to_tile, last ? from : to, m.n, m.r, m.ldx, d->P))
+        !operand_map(&to_op, last ? from : to, m.n, m.r, m.ldx, d->P) || !tile_map(&to_tile, last ? from : to, m.n, m.r, m.ldx, d->P))
       return LSGD_ERR_CUDA;
     Product p{};
     p.batch = d->P;
@@ -1034,14 +1056,14 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.partial = reinterpret_cast<float*>(scratch + m.partial);
     p.done = a.done;
     p.alpha = down;
-    if (launch_product(x_op, x_op, g_tile, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(x_op, x_op, g_tile, g_op, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.K = m.r;
     p.split = 1;
     p.add = 1;
     p.alpha = d->c * down;
     p.beta = d->b;
     p.diag = d->a * kScale;
-    if (launch_product(g_op, g_op, q_tile, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(g_op, g_op, q_tile, q_op, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.N = m.n;
     p.symmetric = 0;
     p.b_mn = 1;
@@ -1056,7 +1078,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
       p.out_wide = a.out_wide;
       p.scale = d->scale * down;
     }
-    if (launch_product(q_op, x_op, to_tile, lo_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(q_op, x_op, to_tile, to_op, lo_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
   }
   return LSGD_OK;
 }
