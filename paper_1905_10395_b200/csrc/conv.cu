@@ -3,11 +3,13 @@
 // A thread owns `VEC` neighbouring channels of a run of rows and keeps the last W - 1 inputs in registers, so each input is read
 // once (and W - 1 rows again where a run begins) and each output written once: the operator is bound by memory.  The next rows are
 // fetched while the present ones are used (8 x 2048 x 2048 in bf16: 31 us forward, 38 with one set of rows in flight; 21 at the rate
-// of a copy), and a run's rows are found span by span of a sequence, not row by row.
+// of a copy; a ring of 16 rows in shared memory, copied asynchronously: 34 and 75 backward), and a run's rows are found span by span of a sequence, not row by row.
 //
 // The gradient walks W - 1 rows further than its run: row t's d = d_out act'(pre) is made from the window of inputs and added to
 // the W sums dx[t - k] that wait in registers; the sums of dw and d_bias stay in registers over the run, are added up by
-// the block and then by a second kernel in a fixed order (67 us for the above; 31 at the rate of a copy).
+// the block and then by a second kernel in a fixed order (56 us for the above; 31 at the rate of a copy).
+#include <type_traits>
+
 #include "activations.h"
 #include "seq.h"
 
@@ -16,7 +18,9 @@ namespace {
 
 constexpr int kMaxW = 4, kAhead = 8, kLanes = 32, kRuns = 4;       // a block: 32 channel pieces x 4 runs of rows
 constexpr int kMostRows = 64;                                      // of a run
-constexpr int kForwardBlocks = 5, kBackwardBlocks = 4;              // resident on an SM (registers: two sets of rows in flight)
+// Blocks of a kernel that are resident on an SM: as many as leave a thread the registers for two sets of rows in flight.
+constexpr int forward_blocks(int vec) { return vec == 4 ? 5 : 7; }
+constexpr int backward_blocks(int vec) { return vec == 2 ? 5 : 4; }
 
 __global__ void __launch_bounds__(256) codes_kernel(const SeqView q, int32_t* codes) {
   pdl_wait();
@@ -44,7 +48,7 @@ __device__ __forceinline__ Rows<T> view(const lsgd_rows& r) {
   return Rows<T>{static_cast<T*>(r.data), r.ld, r.stride};
 }
 
-// VEC (4 or 1) neighbouring values as pairs, two to an instruction (of a single value the second is idle).
+// VEC (4, 2 or 1) neighbouring values as pairs, two to an instruction (of a single value the second is idle).
 template <int VEC>
 struct Vals {
   static constexpr int kPairs = (VEC + 1) / 2;
@@ -125,7 +129,7 @@ __device__ __forceinline__ void window(const ConvArgs& a, int p, int t, int ch, 
 }
 
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(kLanes * kRuns, kForwardBlocks) conv_forward_kernel(const __grid_constant__ ConvArgs a) {
+__global__ void __launch_bounds__(kLanes * kRuns, forward_blocks(VEC)) conv_forward_kernel(const __grid_constant__ ConvArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   const int ch = (blockIdx.x * kLanes + threadIdx.x) * VEC, p = blockIdx.z;
@@ -158,14 +162,22 @@ __global__ void __launch_bounds__(kLanes * kRuns, kForwardBlocks) conv_forward_k
         in[i] = next[i];
         if (t + kAhead + i < end) next[i].load(px + (kAhead + i) * ldx);
       }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        if (t + i >= end) break;
+      auto row = [&](int i) {
         const Vals<VEC> last = values<T, VEC>(in[i]);
         put<T, VEC>(activate(taps.apply(win, last), silu), po + i * ldo);
 #pragma unroll
         for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
         if (W > 1) win[W > 1 ? W - 2 : 0] = last;
+      };
+      if (t + kAhead <= end) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) row(i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (t + i >= end) break;
+          row(i);
+        }
       }
       px += kAhead * ldx;
       po += kAhead * ldo;
@@ -214,10 +226,10 @@ __global__ void __launch_bounds__(kLanes * kRuns) conv_state_kernel(const __grid
 }
 
 template <typename T, int VEC, int W>
-__global__ void __launch_bounds__(kLanes * kRuns, kBackwardBlocks) conv_backward_kernel(const __grid_constant__ ConvArgs a) {
+__global__ void __launch_bounds__(kLanes * kRuns, backward_blocks(VEC)) conv_backward_kernel(const __grid_constant__ ConvArgs a) {
   pdl_wait();
   pdl_launch_dependents();
-  constexpr int kPairs = Vals<VEC>::kPairs, kTake = 4;
+  constexpr int kPairs = Vals<VEC>::kPairs, kTake = VEC * sizeof(T) <= 4 ? 8 : 4;      // rows a set
   const int ch = (blockIdx.x * kLanes + threadIdx.x) * VEC, p = blockIdx.z;
   int t = (blockIdx.y * kRuns + threadIdx.y) * a.run;
   const int t1 = min(a.q.T, t + a.run);
@@ -257,9 +269,8 @@ __global__ void __launch_bounds__(kLanes * kRuns, kBackwardBlocks) conv_backward
             next_up[i].load(pu + (kTake + i) * ldu);
           }
         }
-#pragma unroll
-        for (int i = 0; i < kTake; ++i) {
-          if (t + i >= end) break;
+        // row t + i; plain: it is this run's, as is the row W - 1 before it
+        auto row = [&](int i, auto plain) {
           const Vals<VEC> last = values<T, VEC>(in[i]);
           Vals<VEC> g = values<T, VEC>(up[i]);
           if (silu) {
@@ -267,28 +278,38 @@ __global__ void __launch_bounds__(kLanes * kRuns, kBackwardBlocks) conv_backward
 #pragma unroll
             for (int v = 0; v < kPairs; ++v) {
               const float2 sg = sigmoid(s.v[v]), sl = mul2(s.v[v], sg);
-              g.v[v] = mul2(g.v[v], fma2(sl, make_float2(1.f - sg.x, 1.f - sg.y), sg));
+              g.v[v] = mul2(g.v[v], fma2(sl, fma2(sg, both(-1.f), both(1.f)), sg));
             }
           }
-          const bool mine = t + i < own;
+          const bool mine = plain || t + i < own;
 #pragma unroll
           for (int v = 0; v < kPairs; ++v) {
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) wait[j].v[v] = fma2(taps.w[j].v[v], g.v[v], wait[j].v[v]);
             wait[W - 1].v[v] = mul2(taps.w[W - 1].v[v], g.v[v]);
             if (mine) {
-              db.v[v] = make_float2(db.v[v].x + g.v[v].x, db.v[v].y + g.v[v].y);
+              db.v[v] = add2(db.v[v], g.v[v]);
 #pragma unroll
               for (int j = 0; j < W - 1; ++j) dw[j].v[v] = fma2(win[j].v[v], g.v[v], dw[j].v[v]);
               dw[W - 1].v[v] = fma2(last.v[v], g.v[v], dw[W - 1].v[v]);
             }
           }
-          if (t + i - (W - 1) >= first) put<T, VEC>(wait[0], pd + (i - (W - 1)) * ldd);      // complete W - 1 rows on
+          if (plain || t + i - (W - 1) >= first) put<T, VEC>(wait[0], pd + (i - (W - 1)) * ldd);      // complete W - 1 rows on
 #pragma unroll
           for (int j = 0; j + 1 < W; ++j) wait[j] = wait[j + 1];
 #pragma unroll
           for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
           if (W > 1) win[W > 1 ? W - 2 : 0] = last;
+        };
+        if (t - (W - 1) >= first && t + kTake <= own) {
+#pragma unroll
+          for (int i = 0; i < kTake; ++i) row(i, std::true_type());
+        } else {
+#pragma unroll
+          for (int i = 0; i < kTake; ++i) {
+            if (t + i >= end) break;
+            row(i, std::false_type());
+          }
         }
         px += kTake * ldx;
         pu += kTake * ldu;
@@ -401,15 +422,20 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
   return all_apart(outs, 3, ins, 4) ? LSGD_OK : LSGD_ERR_INVALID_ARG;
 }
 
-// Four values a thread where every row allows it, else one.
+// Values a thread: 8 bytes of a row where every row allows it (of fp32, four would not fit the registers: 8 x 2048 x 2048 took 66 + 129
+// us instead of 46 + 77).  In bf16 two do where four leave SMs with few blocks (8 x 1024 x 512: 8.5 + 15 us instead of 6.1
+// + 13.5; 3 x 1000 x 256: 4.4 + 11 instead of 3.6 + 10).
 int conv_vec(const lsgd_conv_desc* d, bool backward) {
   const int ab = elem_bytes(d->act_dtype);
-  auto fits = [&](const lsgd_rows& r) {
-    return !r.data || (reinterpret_cast<uintptr_t>(r.data) % (4 * ab) == 0 && (d->T <= 1 || r.ld % 4 == 0) && (d->P <= 1 || r.stride % 4 == 0));
+  auto fits = [&](const lsgd_rows& r, int v) {
+    return !r.data || (reinterpret_cast<uintptr_t>(r.data) % (v * ab) == 0 && (d->T <= 1 || r.ld % v == 0) && (d->P <= 1 || r.stride % v == 0));
   };
-  const bool ok = d->D % 4 == 0 && fits(d->x) &&
-                  (backward ? fits(d->d_out) && fits(d->dx) : fits(d->out) && reinterpret_cast<uintptr_t>(d->state) % (4 * ab) == 0);
-  return ok ? 4 : 1;
+  auto all = [&](int v) {
+    return d->D % v == 0 && fits(d->x, v) &&
+           (backward ? fits(d->d_out, v) && fits(d->dx, v) : fits(d->out, v) && reinterpret_cast<uintptr_t>(d->state) % (v * ab) == 0);
+  };
+  const int64_t blocks = (d->D + kLanes * 4 - 1) / (kLanes * 4) * d->P * ((d->T + 8 * kRuns - 1) / (8 * kRuns));      // of 8 rows a thread
+  return ab == 2 && blocks >= 32 * sm_count() && all(4) ? 4 : all(2) ? 2 : 1;
 }
 
 struct ConvPlan {
@@ -420,13 +446,15 @@ ConvPlan conv_plan(const lsgd_conv_desc* d, bool backward) {
   ConvPlan c{};
   c.vec = conv_vec(d, backward);
   c.blocks_d = (uint32_t)((d->D + kLanes * c.vec - 1) / (kLanes * c.vec));
-  // rows of a thread: those that take the least time by the rounds of blocks over the machine (so many of them resident on an SM),
-  // each of as many rows and the W - 1 that are read again
-  const int64_t resident = (int64_t)sm_count() * (backward ? kBackwardBlocks : kForwardBlocks), columns = (int64_t)c.blocks_d * d->P;
+  // rows of a thread: those that take the least time by the rounds of blocks over the machine, each of as many rows and what a run
+  // begins with.  Forwards by whole rounds; backwards, where a run begins and ends with more, between whole rounds and their fraction, and
+  // powers of two, which seldom cross from one sequence to the next (8 x 2048 x 2048 in two sequences each: 56 us with runs of 64 rows, 64 with
+  // 40, 62 with 32)
+  const int64_t resident = (int64_t)sm_count() * (backward ? backward_blocks(c.vec) : forward_blocks(c.vec)), columns = (int64_t)c.blocks_d * d->P;
   int64_t least = INT64_MAX;
-  for (int run = 8; run <= kMostRows; run += 8) {
-    const int64_t blocks = columns * ((d->T + (int64_t)run * kRuns - 1) / ((int64_t)run * kRuns));
-    const int64_t cost = (blocks + resident - 1) / resident * (run + d->W + 2);
+  for (int run = 8; run <= kMostRows; run = backward ? 2 * run : run + 8) {
+    const int64_t blocks = columns * ((d->T + (int64_t)run * kRuns - 1) / ((int64_t)run * kRuns)), rounds = (blocks + resident - 1) / resident;
+    const int64_t cost = backward ? (rounds * resident + blocks) * (run + 16) : rounds * (run + d->W + 2);
     if (cost < least) {
       least = cost;
       c.run = run;
@@ -473,8 +501,10 @@ lsgd_status run_conv(const lsgd_conv_desc* d, bool backward, cudaStream_t s) {
   if (d->T > 0) {
     if (d->seq.starts) e = launch_codes(a.q, codes, d->P, s);
     if (e == cudaSuccess)
-      e = d->act_dtype == LSGD_BF16 ? (c.vec == 4 ? launch_conv<__nv_bfloat16, 4>(a, c, backward, s) : launch_conv<__nv_bfloat16, 1>(a, c, backward, s))
-                                    : (c.vec == 4 ? launch_conv<float, 4>(a, c, backward, s) : launch_conv<float, 1>(a, c, backward, s));
+      e = d->act_dtype == LSGD_F32 ? (c.vec == 2 ? launch_conv<float, 2>(a, c, backward, s) : launch_conv<float, 1>(a, c, backward, s))
+          : c.vec == 4             ? launch_conv<__nv_bfloat16, 4>(a, c, backward, s)
+          : c.vec == 2             ? launch_conv<__nv_bfloat16, 2>(a, c, backward, s)
+                                   : launch_conv<__nv_bfloat16, 1>(a, c, backward, s);
   }
   if (e == cudaSuccess && backward) {
     const unsigned n = (unsigned)d->D * (d->W + 1);
