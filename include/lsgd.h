@@ -408,7 +408,9 @@ LSGD_API lsgd_status lsgd_bgemm_check_device(uint32_t* flag_out /* HOST, may be 
 
 /* ------------------------------------------------------------------------------------------------------
  * Operators of a language model's training step, for populations whose workers are language models: the
- * embedding lookup and its gradient, the norms at a block boundary and their gradient, and the AdamW step.
+ * embedding lookup and its gradient, the norms at a block boundary and their gradient, a short causal convolution and a
+ * selective state space scan along sequences and their gradients (prompts and single tokens too), orthogonalised updates of
+ * matrices, and the AdamW step.
  * The matrix products between them are lsgd_bgemm_bf16's; the leaders' election and pulls are lsgd_elect's and
  * lsgd_step's (objective EXTERNAL).  Each operator works on all P workers in one call: worker p's token t is
  * row (p, t).  Conventions as above; the descriptors are HOST structs read during the call, all buffers in them
@@ -666,10 +668,11 @@ LSGD_API lsgd_status lsgd_scan_backward(const lsgd_scan_desc* desc, void* stream
  * (of X^T where m > n: the smaller side's products);   out = scale X.  Each step maps every singular value v to
  * a v + b v^3 + c v^5; with the usual (3.4445, -4.7750, 2.0315) five steps bring all that are not tiny to about one.
  * The products' operands are fp16 with a power-of-two scale (11 significant bits; X, G and the polynomial are bounded by about 4,
- * which bf16's wider range would only pay for with three bits less), sums are fp32.  grad: P x m rows of n values
- * of grad_dtype; momentum: the same in fp32, updated in place; out: P x m rows of n values, bf16.  A zero matrix gives zeros; one with a
- * value that is not finite gives NaN.  Coefficients that let singular values pass 16 are out of range: the result is then not
- * finite, or saturated.  Scratch: lsgd_ortho_scratch_bytes(d), 256-byte aligned; as for the convolution.         */
+ * which bf16's wider range would only pay for with three bits less), sums are fp32; the first X counts as two such numbers where
+ * the smaller side is 768 at most.  grad: P x m rows of n values of grad_dtype; momentum: the same in fp32, updated in place; out: P
+ * x m rows of n values, bf16.  A zero matrix gives zeros; one with a value that is not finite gives NaN.  Coefficients that let
+ * singular values pass 16 are out of range: the result is then not finite, or saturated.  Scratch: lsgd_ortho_scratch_bytes(d), which
+ * is 0 up to 128 x 256, 256-byte aligned; as for the convolution.                                                 */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(lsgd_ortho_desc)                                                      */
   int32_t P;                 /* [1, 65535]                                                                    */

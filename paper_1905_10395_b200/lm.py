@@ -6,7 +6,8 @@ outlive the object.  Work is enqueued on the stream given at construction (defau
 the one that is current at the call; a tensor last used on another stream has to be ordered with it by the caller.  An operator
 that is to be captured is given the capture's stream: under a capture that its stream is not part of, a call is refused
 (ERR_STATE).  The tensors' device has to be the current one at
-every call (ERR_STATE otherwise).  There is no CPU path.
+every call (ERR_STATE otherwise).  There is no CPU path.  An operator has one scratch buffer: its calls, the replays of graphs that
+captured it among them, run one after another (as they do on one stream); what is to run at once is given operators of its own.
 
 Rows are [P, T, D] (worker, token, channel) with a channel stride of 1 and any row and worker stride; one worker's may be
 given as [T, D].  Vectors are [P, D] or [D].  An input that is expanded over the workers (stride 0) is shared by them."""
@@ -385,8 +386,8 @@ class Orthogonalize:
     X = U / (|U| + eps), then `steps` times X <- a X + (b G + c G G) X with G = X X^T.
 
     grad [P, m, n] (or [m, n]) fp32 or bf16; out the same in bf16.  momentum, fp32: M <- mu M + grad, in place, and U = M, or
-    grad + mu M with nesterov; without it U = grad.  The products run on fp16 operands with a power-of-two scale: a result is within
-    about 2^-9 of its matrix's norm of the exact one, as its rounding to bf16 is."""
+    grad + mu M with nesterov; without it U = grad.  The products run on fp16 operands with a power-of-two scale: with these
+    coefficients and steps a result is within about 2^-9 of its matrix's norm of the exact one, as its rounding to bf16 is."""
 
     def __init__(self, grad: torch.Tensor, out: torch.Tensor, *, momentum: Optional[torch.Tensor] = None, mu: float = 0.95,
                  nesterov: bool = True, steps: int = 5, coefficients: Sequence[float] = (3.4445, -4.7750, 2.0315),
