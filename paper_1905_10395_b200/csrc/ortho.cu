@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
   pdl_wait();
   pdl_launch_dependents();
   const int p = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;       // of the matrix as given
-  const float inv = inverse_norm(a, p);
+  float inv = 0.f;
   __shared__ float tile[64][65];
   constexpr int kPieces = 64 * (64 / VEC) / 256, kTake = kPieces < 8 ? kPieces : 8;
 #pragma unroll 1
@@ -163,6 +163,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
       const int i = threadIdx.x + (k0 + k) * 256, row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
       if (r0 + row < a.d.m && c0 + col < a.d.n) piece[k].load(a, p, r0 + row, c0 + col);
     }
+    if (k0 == 0) inv = inverse_norm(a, p);         // behind the first pieces' loads
 #pragma unroll
     for (int k = 0; k < kTake; ++k) {
       const int i = threadIdx.x + (k0 + k) * 256, row = i / (64 / VEC), col = i % (64 / VEC) * VEC;
@@ -917,7 +918,8 @@ Plan plan_of(const lsgd_ortho_desc* d) {
   m.n = d->m < d->n ? d->n : d->m;
   m.ldx = (m.n + 7) / 8 * 8;
   m.ldg = (m.r + 7) / 8 * 8;
-  const int64_t want = ((int64_t)d->m * d->n + 4095) / 4096, cap = (4 * (int64_t)sm_count() + d->P - 1) / d->P;
+  const int64_t each = d->n % 4 == 0 ? 4096 : 1024;       // values of a block: 4 pieces a thread, all under way at once
+  const int64_t want = ((int64_t)d->m * d->n + each - 1) / each, cap = (4 * (int64_t)sm_count() + d->P - 1) / d->P;
   m.blocks = (uint32_t)(want < cap ? want : cap);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) {
