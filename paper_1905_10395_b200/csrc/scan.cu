@@ -38,30 +38,6 @@ __global__ void __launch_bounds__(256) chain_kernel(const __grid_constant__ Args
   }
 }
 
-// Gradients of a_log, skip and dt_bias: the chains' sums in order (of all workers where they share the vector).  Columns of a
-// worker: D x N of a_log, D of skip, D of dt_bias.
-__global__ void __launch_bounds__(256) join_params_kernel(const __grid_constant__ Args a) {
-  pdl_wait();
-  const int64_t n = (int64_t)a.d.D * a.d.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n + 2 * a.d.D) return;
-  const int which = i < n ? 0 : i < n + a.d.D ? 1 : 2;
-  const lsgd_rows& o = which == 0 ? a.d.d_a_log : which == 1 ? a.d.d_skip : a.d.d_dt_bias;
-  const bool shared = a.d.P > 1 && o.stride == 0;
-  if (!o.data || (shared && blockIdx.y > 0)) return;
-  const int64_t width = which == 0 ? n : 2 * a.d.D;
-  const float* src = (which == 0 ? a.part_a + i : a.part_v + (i - n));
-  float total = 0.f;
-  const int p0 = shared ? 0 : blockIdx.y, p1 = shared ? a.d.P : p0 + 1;
-  for (int p = p0; p < p1; ++p) {
-    const float* s = src + (int64_t)p * a.chains * width;
-#pragma unroll 8
-    for (int c = 0; c < a.chains; ++c) total += s[c * width];
-  }
-  const int64_t col = which == 0 ? i / a.d.N * o.ld + i % a.d.N : i - n - (which == 1 ? 0 : a.d.D);
-  float* dst = static_cast<float*>(o.data) + (shared ? 0 : blockIdx.y * o.stride) + col;
-  *dst = a.d.accumulate ? *dst + total : total;
-}
-
 // ------------------------------------------------------------------------------------------------ host
 lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   if (!d || d->struct_size != sizeof(lsgd_scan_desc)) return LSGD_ERR_INVALID_ARG;
@@ -234,10 +210,9 @@ lsgd_status run_scan(const lsgd_scan_desc* d, bool backward, cudaStream_t s) {
       e = backward ? (f32 ? launch_backward_f32(a, m.l, s) : launch_backward_bf16(a, m.l, s))
                    : (f32 ? launch_forward_f32(a, m.l, s) : launch_forward_bf16(a, m.l, s));
   }
-  if (e == cudaSuccess && backward) {
-    if (d->T == 0) a.chains = 0;
-    const int64_t cols = (int64_t)d->D * (d->N + 2);
-    e = launch_pdl(join_params_kernel, dim3((unsigned)((cols + 255) / 256), d->P), dim3(256), 0, s, a);
+  if (e == cudaSuccess && backward && d->T == 0) {
+    a.chains = 0;
+    e = launch_join_f32(a, s);                               // no rows, whatever their type
   }
   return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
 }

@@ -1059,23 +1059,51 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
   if (which < 2 && col < d.D) a.part_v[(((int64_t)p * a.chains + c) * 2 + which) * d.D + col] = column;
 }
 
-// db and dc: the channel blocks' sums in order.
+// The backward pass's last sums.  The first blocks, which take longest: gradients of a_log, skip and dt_bias, the chains' sums in order (of
+// all workers where they share the vector); columns of a worker: D x N of a_log, D of skip, D of dt_bias.  The others: db and dc,
+// the channel blocks' sums in order.
 template <typename T>
-__global__ void __launch_bounds__(256) join_bc_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Args a, const uint32_t blocks_params) {
   pdl_wait();
   pdl_launch_dependents();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n2 = 2 * a.d.N;
   const int p = blockIdx.y;
-  if (i >= (int64_t)a.q.T * n2) return;
-  const int t = (int)(i / n2), which = (int)(i % n2) / a.d.N, n = (int)(i % n2) % a.d.N;
-  if (a.q.starts && a.q.code(p, t) < 0) return;
-  const float* src = a.part_bc + (int64_t)p * a.tiles * a.q.T * n2 + i;
-  float s = 0.f;
+  if (blockIdx.x >= blocks_params) {
+    const int64_t i = (int64_t)(blockIdx.x - blocks_params) * 256 + threadIdx.x, n2 = 2 * a.d.N;
+    if (i >= (int64_t)a.q.T * n2) return;
+    const int t = (int)(i / n2), which = (int)(i % n2) / a.d.N, n = (int)(i % n2) % a.d.N;
+    if (a.q.starts && a.q.code(p, t) < 0) return;
+    const float* src = a.part_bc + (int64_t)p * a.tiles * a.q.T * n2 + i;
+    float s = 0.f;
 #pragma unroll 8
-  for (uint32_t k = 0; k < a.tiles; ++k) s += src[(int64_t)k * a.q.T * n2];
-  Pack<T, 1> one;
-  one.set(&s);
-  one.store(view<T>(which ? a.d.dc : a.d.db).row(p, t) + n);
+    for (uint32_t k = 0; k < a.tiles; ++k) s += src[(int64_t)k * a.q.T * n2];
+    Pack<T, 1> one;
+    one.set(&s);
+    one.store(view<T>(which ? a.d.dc : a.d.db).row(p, t) + n);
+    return;
+  }
+  const int64_t n = (int64_t)a.d.D * a.d.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n + 2 * a.d.D) return;
+  const int which = i < n ? 0 : i < n + a.d.D ? 1 : 2;
+  const lsgd_rows& o = which == 0 ? a.d.d_a_log : which == 1 ? a.d.d_skip : a.d.d_dt_bias;
+  const bool shared = a.d.P > 1 && o.stride == 0;
+  if (!o.data || (shared && p > 0)) return;
+  const int64_t width = which == 0 ? n : 2 * a.d.D;
+  const float* src = which == 0 ? a.part_a + i : a.part_v + (i - n);
+  float total = 0.f;
+  const int p0 = shared ? 0 : p, p1 = shared ? a.d.P : p + 1;
+  for (int w = p0; w < p1; ++w) {
+    const float* s = src + (int64_t)w * a.chains * width;
+#pragma unroll 8
+    for (int c = 0; c < a.chains; ++c) total += s[c * width];
+  }
+  const int64_t col = which == 0 ? i / a.d.N * o.ld + i % a.d.N : i - n - (which == 1 ? 0 : a.d.D);
+  float* dst = static_cast<float*>(o.data) + (shared ? 0 : p * o.stride) + col;
+  *dst = a.d.accumulate ? *dst + total : total;
+}
+template <typename T>
+cudaError_t launch_join(const Args& a, cudaStream_t s) {
+  const int64_t bc = ((int64_t)a.q.T * 2 * a.d.N + 255) / 256, params = ((int64_t)a.d.D * (a.d.N + 2) + 255) / 256;
+  return launch_pdl(join_kernel<T>, dim3((unsigned)(bc + params), a.d.P), dim3(256), 0, s, a, (uint32_t)params);
 }
 
 struct Launch {
@@ -1087,6 +1115,7 @@ cudaError_t launch_forward_f32(const Args& a, const Launch& l, cudaStream_t s);
 cudaError_t launch_forward_bf16(const Args& a, const Launch& l, cudaStream_t s);
 cudaError_t launch_backward_f32(const Args& a, const Launch& l, cudaStream_t s);
 cudaError_t launch_backward_bf16(const Args& a, const Launch& l, cudaStream_t s);
+cudaError_t launch_join_f32(const Args& a, cudaStream_t s);
 // split: from what every chain adds to what every chain starts from, forwards or backwards (scan.cu)
 cudaError_t launch_chain_join(const Args& a, bool reverse, cudaStream_t s);
 
@@ -1115,9 +1144,7 @@ cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
     if (e == cudaSuccess) e = launch_chain_join(a, true, s);
   }
   if (e == cudaSuccess) e = launch_pdl(backward_kernel<T, L>, l.grid, dim3(kThreads), smem, s, a);
-  if (e != cudaSuccess) return e;
-  const int64_t values = (int64_t)a.q.T * 2 * a.d.N;
-  return launch_pdl(join_bc_kernel<T>, dim3((unsigned)((values + 255) / 256), a.d.P), dim3(256), 0, s, a);
+  return e == cudaSuccess ? launch_join<T>(a, s) : e;
 }
 template <typename T>
 cudaError_t forward_any(const Args& a, const Launch& l, cudaStream_t s) {
