@@ -596,8 +596,9 @@ typedef struct {
  * with all arithmetic in fp32 and each output rounded once.  x, out, d_out, dx: P x T rows of D values of act_dtype; outputs
  * overlap no input.  w, dw: P x D rows of W values, fp32; bias, d_bias: P rows of D values, fp32.  dw and d_bias with a
  * worker stride of 0 are summed over the workers.  accumulate: they are added to what their buffers hold.
- * The backward pass, and both passes of sequences given by starts, need scratch (lsgd_conv_scratch_bytes(d, backward),
- * 256-byte aligned), whose contents are not kept between calls; so calls that share it are ordered by the caller.    */
+ * The backward pass, and both passes of sequences given by starts, need scratch (lsgd_conv_scratch_bytes(d, backward) of the
+ * descriptor with its addresses and strides, 256-byte aligned), whose contents are not kept between calls; so calls that share it
+ * are ordered by the caller.                                                                                     */
 typedef enum {
   LSGD_CONV_IDENTITY = 0,
   LSGD_CONV_SILU = 1

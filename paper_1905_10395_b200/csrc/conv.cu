@@ -3,7 +3,8 @@
 // A thread owns `VEC` neighbouring channels of a run of rows and keeps the last W - 1 inputs in registers, so each input is read
 // once (and W - 1 rows again where a run begins) and each output written once: the operator is bound by memory.  The next rows are
 // fetched while the present ones are used (8 x 2048 x 2048 in bf16: 31 us forward, 38 with one set of rows in flight; 21 at the rate
-// of a copy; a ring of 16 rows in shared memory, copied asynchronously: 34 and 75 backward), and a run's rows are found span by span of a sequence, not row by row.
+// of a copy; a ring of 16 rows in shared memory, copied asynchronously: 34 and 75 backward), and a run's rows are found span by
+// span of a sequence, not row by row.
 //
 // The gradient walks W - 1 rows further than its run: row t's d = d_out act'(pre) is made from the window of inputs and added to
 // the W sums dx[t - k] that wait in registers; the sums of dw and d_bias stay in registers over the run, are added up by
