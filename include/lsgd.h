@@ -584,7 +584,7 @@ LSGD_API lsgd_status lsgd_adamw_destroy(lsgd_adamw_handle h);   /* NULL is accep
 typedef struct {
   const int32_t* starts;
   int64_t stride;
-  int32_t S;                 /* >= 1                                                                         */
+  int32_t S;                 /* >= 1, P * S < 2^31 - 2^20                                                    */
 } lsgd_sequences;
 
 /* ---- Causal convolution -----------------------------------------------------------------------------------

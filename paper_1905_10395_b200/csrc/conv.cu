@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(256) codes_kernel(const SeqView q, int32_t* co
   if (t >= q.T) return;
   int lo = 0, hi = q.S + 1;                      // edges at or before t: [0, lo); behind t: [hi, S]
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + ((hi - lo) >> 1);       // (lo + hi may pass 2^31)
     if (q.edge(p, mid) <= t) lo = mid + 1; else hi = mid;
   }
   codes[(int64_t)p * q.T + t] = lo == 0 || lo > q.S ? -1 : lo - 1;
@@ -389,7 +389,6 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
   if (d->T >= kMaxRows / d->P) return LSGD_ERR_TOO_LARGE;
   lsgd_status st;
   if ((st = check_sequences(d->seq, d->P, d->T)) != LSGD_OK) return st;
-  if ((int64_t)d->seq.S * d->P >= int64_t(1) << 31) return LSGD_ERR_TOO_LARGE;
   const int64_t P = d->P, T = d->T, D = d->D;
   const int ab = elem_bytes(d->act_dtype);
   const bool rows = T > 0;

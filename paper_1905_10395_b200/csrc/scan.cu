@@ -47,7 +47,6 @@ lsgd_status check_scan(const lsgd_scan_desc* d, bool backward) {
   if (d->T >= kMaxRows / d->P) return LSGD_ERR_TOO_LARGE;
   lsgd_status st;
   if ((st = check_sequences(d->seq, d->P, d->T)) != LSGD_OK) return st;
-  if ((int64_t)d->seq.S * d->P >= int64_t(1) << 31) return LSGD_ERR_TOO_LARGE;
   const int64_t P = d->P, T = d->T, D = d->D, N = d->N;
   const int ab = elem_bytes(d->act_dtype);
   const bool rows = T > 0;

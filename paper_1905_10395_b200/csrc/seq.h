@@ -4,7 +4,8 @@
 
 namespace lsgd {
 
-// Rows of all workers: a loop's next step behind the last row (65535 blocks of 4 sequences, a chain, a tile) is still a row number.
+// Rows of all workers, and sequences of all: a loop's next step behind the last (65535 blocks of 4 sequences, a chain, a tile) is still
+// a number of 32 bits.
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 20);
 
 // Sequences given by their starts are looked up once: codes[p][t] is the sequence of row t, -1 in front of the first and behind
@@ -52,6 +53,7 @@ struct SeqView {
 
 inline lsgd_status check_sequences(const lsgd_sequences& q, int64_t P, int64_t T) {
   if (q.S < 1) return LSGD_ERR_INVALID_ARG;
+  if (q.S >= kMaxRows / P) return LSGD_ERR_TOO_LARGE;
   if (!q.starts) return T % q.S == 0 ? LSGD_OK : LSGD_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(q.starts) % 4) return LSGD_ERR_ALIGNMENT;
   if (q.stride < 0 || (q.stride > 0 && q.stride < q.S + 1 && P > 1)) return LSGD_ERR_INVALID_ARG;

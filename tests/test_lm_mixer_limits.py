@@ -1,0 +1,25 @@
+"""Host-only checks of what the convolution, the scan and the orthogonalisation refuse at the ends of their ranges.  No GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from tests.test_lm_binding import Devices
+from tests.test_lm_mixer_boundary import MB, _conv, _ortho, _refused, _scan, api, lm  # noqa: F401  (fixtures)
+
+
+@pytest.fixture
+def devices(monkeypatch, lm):  # noqa: F811
+    return Devices(monkeypatch, lm)
+
+
+def test_most_sequences(api):  # noqa: F811
+    """As many sequences as rows may be, of all workers together: kernels index both, and the step behind the last, in 32 bits.  One less passes,
+    to the refusal of the scratch's alignment."""
+    L, most = api.lib(), (1 << 31) - (1 << 20)
+    for make, calls in ((_conv, (L.lsgd_conv_forward, L.lsgd_conv_backward)), (_scan, (L.lsgd_scan_forward, L.lsgd_scan_backward))):
+        for P, S in ((2, most // 2), (1, most), (1, (1 << 31) - 1)):
+            for call in calls:
+                assert call(C.byref(make(api, P=P, T=5, seq=api.Sequences(MB * 70, 0, S), scratch=8, scratch_bytes=1 << 60)), None) == 8, (P, S)
+                assert call(C.byref(make(api, P=P, T=5, seq=api.Sequences(MB * 70, 0, most // P - 1), scratch=8, scratch_bytes=1 << 60)), None) == 3
+                assert call(C.byref(make(api, P=P, T=0, seq=api.Sequences(None, 0, S))), None) == 8
