@@ -330,7 +330,8 @@ class SelectiveScan(_Bound):
     dt_bias and theirs [P, D], fp32 (gradients expanded over the workers are summed over them).  z, skip and dt_bias may be
     absent.  sequences / starts as for CausalConv.  state [P, S, D, N] fp32: what every sequence starts from, replaced by what it
     ends with (forward only; zeros without it).  saved [P, ceil(T / 8), D, N] fp32, written by forward and read by backward
-    (allocated when not given).  accumulate: d_a_log, d_skip and d_dt_bias are added to."""
+    (allocated when not given; without `out`, which leaves the forward pass to another operator, that one's are given).  accumulate:
+    d_a_log, d_skip and d_dt_bias are added to."""
 
     def __init__(self, x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, b: torch.Tensor, c: torch.Tensor, *,
                  z: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
@@ -373,6 +374,8 @@ class SelectiveScan(_Bound):
         d.state = _state("state", state, (P, d.seq.S, D, N), torch.float32)
         shape = (P, (T + api.SAVED_EVERY - 1) // api.SAVED_EVERY, D, N)
         if saved is None and grads:
+            if out is None and T:
+                _fail("SelectiveScan: a backward pass without a forward one (out) needs the saved states of that pass")
             with torch.cuda.stream(stream):
                 saved = torch.empty(shape, dtype=torch.float32, device=device)
         d.saved = _state("saved", saved, shape, torch.float32)

@@ -23,3 +23,20 @@ def test_most_sequences(api):  # noqa: F811
                 assert call(C.byref(make(api, P=P, T=5, seq=api.Sequences(MB * 70, 0, S), scratch=8, scratch_bytes=1 << 60)), None) == 8, (P, S)
                 assert call(C.byref(make(api, P=P, T=5, seq=api.Sequences(MB * 70, 0, most // P - 1), scratch=8, scratch_bytes=1 << 60)), None) == 3
                 assert call(C.byref(make(api, P=P, T=0, seq=api.Sequences(None, 0, S))), None) == 8
+
+
+def test_a_backward_pass_needs_saved_states_that_something_has_written(lm, devices, monkeypatch):  # noqa: F811
+    """Without `out` the operator has no forward pass that would fill states of its own; with the caller's it has."""
+    real = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: real(*a, **k))
+    x, a, bc = torch.zeros(2, 12, 8), torch.zeros(2, 8, 4), torch.zeros(2, 12, 4)
+    new = lambda t: torch.zeros_like(t)  # noqa: E731
+    grads = dict(d_out=new(x), d_x=new(x), d_dt=new(x), d_a_log=new(a), d_b=new(bc), d_c=new(bc))
+    _refused(lm, lm.api.ERR_INVALID_ARG, lambda: lm.SelectiveScan(x, x, a, bc, bc, **grads))
+    saved = torch.zeros(2, 2, 8, 4)
+    assert lm.SelectiveScan(x, x, a, bc, bc, saved=saved, **grads).saved is saved
+    assert lm.SelectiveScan(x, x, a, bc, bc, out=new(x), **grads).saved.shape == saved.shape
+    # no rows: nothing is saved
+    none = lambda t: torch.zeros(2, 0, t.shape[2])  # noqa: E731
+    x, bc = none(x), none(bc)
+    lm.SelectiveScan(x, x, a, bc, bc, d_out=new(x), d_x=new(x), d_dt=new(x), d_a_log=new(a), d_b=new(bc), d_c=new(bc))
