@@ -31,6 +31,14 @@ def _fail(what: str) -> None:
     raise api.LsgdError(api.ERR_INVALID_ARG, what)
 
 
+def _int32(name: str, v) -> int:
+    """A size as a descriptor's 32-bit field holds it (ctypes would take a larger one modulo 2^32)."""
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise api.LsgdError(api.ERR_TOO_LARGE, f"{name}: {v}")
+    return v
+
+
 def _stream(stream, device: torch.device):
     """The stream that an operator keeps, for its calls and for the buffers that it allocates."""
     if stream is None:
@@ -248,7 +256,7 @@ def _given_rows(name: str, t: torch.Tensor):
 
 def _sequences(sequences: Optional[int], starts: Optional[torch.Tensor], P: int, T: int, device: torch.device) -> api.Sequences:
     if starts is None:
-        S = 1 if sequences is None else int(sequences)
+        S = 1 if sequences is None else _int32("sequences", sequences)
         if S < 1 or T % S:
             _fail(f"sequences: {S} equal parts of {T} rows")
         return api.Sequences(None, 0, S)
@@ -260,7 +268,8 @@ def _sequences(sequences: Optional[int], starts: Optional[torch.Tensor], P: int,
         _fail(f"starts: a tensor of {device}, got one of {starts.device}")
     if starts.dim() not in (1, 2) or starts.shape[-1] < 2 or (starts.dim() == 2 and starts.shape[0] != P) or starts.stride(-1) != 1:
         _fail("starts: [S + 1] or [P, S + 1], a worker's contiguous")
-    return api.Sequences(starts.data_ptr(), starts.stride(0) if starts.dim() == 2 and P > 1 else 0, starts.shape[-1] - 1)
+    S = _int32("starts", starts.shape[-1] - 1)
+    return api.Sequences(starts.data_ptr(), starts.stride(0) if starts.dim() == 2 and P > 1 else 0, S)
 
 
 def _table(name: str, t: Optional[torch.Tensor], P: int, rows: int, cols: int) -> api.Rows:
@@ -309,7 +318,7 @@ class CausalConv(_Bound):
             _fail("CausalConv: out, or the tensors of the backward pass, or both")
         d = api.ConvDesc()
         d.struct_size = C.sizeof(api.ConvDesc)
-        d.P, d.T, d.D, d.W = P, T, D, w.shape[-1]
+        d.P, d.T, d.D, d.W = _int32("x", P), T, _int32("x", D), _int32("w", w.shape[-1])
         d.act_dtype = _dtype("x", x, out, d_out, dx)
         d.act, d.accumulate = (api.CONV_SILU if act == "silu" else api.CONV_IDENTITY), int(accumulate)
         d.seq = _sequences(sequences, starts, P, T, device)
@@ -359,7 +368,7 @@ class SelectiveScan(_Bound):
             _fail("SelectiveScan: out, or the tensors of the backward pass, or both")
         d = api.ScanDesc()
         d.struct_size = C.sizeof(api.ScanDesc)
-        d.P, d.T, d.D, d.N = P, T, D, N
+        d.P, d.T, d.D, d.N = _int32("x", P), T, _int32("x", D), _int32("a_log", N)
         d.act_dtype = _dtype("x", x, dt, b, c, z, out, d_out, d_x, d_dt, d_b, d_c, d_z)
         d.accumulate = int(accumulate)
         d.seq = _sequences(sequences, starts, P, T, device)
@@ -405,7 +414,7 @@ class Orthogonalize:
             _fail("coefficients: a, b, c")
         d = api.OrthoDesc()
         d.struct_size = C.sizeof(api.OrthoDesc)
-        d.P, d.m, d.n, d.steps, d.nesterov = P, m, n, int(steps), int(nesterov)
+        d.P, d.m, d.n, d.steps, d.nesterov = _int32("grad", P), _int32("grad", m), _int32("grad", n), _int32("steps", steps), int(bool(nesterov))
         d.grad_dtype = _dtype("grad", grad)
         d.a, d.b, d.c = (float(v) for v in coefficients)
         d.mu, d.eps, d.scale = float(mu), float(eps), float(scale)

@@ -40,3 +40,35 @@ def test_a_backward_pass_needs_saved_states_that_something_has_written(lm, devic
     none = lambda t: torch.zeros(2, 0, t.shape[2])  # noqa: E731
     x, bc = none(x), none(bc)
     lm.SelectiveScan(x, x, a, bc, bc, d_out=new(x), d_x=new(x), d_dt=new(x), d_a_log=new(a), d_b=new(bc), d_c=new(bc))
+
+
+class Sized:
+    """A tensor's shape, type and strides, without its memory."""
+
+    def __init__(self, *shape, dtype=torch.float32):
+        self.t = torch.zeros(shape, dtype=dtype, device="meta")
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def data_ptr(self):
+        return MB
+
+
+@pytest.mark.parametrize("n", [(1 << 32) + 8, 1 << 31])
+def test_sizes_of_more_than_32_bits_are_refused(lm, devices, n):  # noqa: F811
+    """A size that the descriptor holds in 32 bits: not taken modulo 2^32, which would leave most of the output as it was."""
+    s, bf = Sized, torch.bfloat16
+    calls = [lambda: lm.CausalConv(s(1, 4, n), s(1, n, 2), out=s(1, 4, n)), lambda: lm.CausalConv(s(n, 4, 8), s(n, 8, 2), out=s(n, 4, 8)),
+             lambda: lm.CausalConv(s(1, 4, 8), s(1, 8, n), out=s(1, 4, 8)),
+             lambda: lm.CausalConv(s(1, 0, 8), s(1, 8, 2), out=s(1, 0, 8), sequences=n),
+             lambda: lm.SelectiveScan(s(1, 4, n), s(1, 4, n), s(1, n, 2), s(1, 4, 2), s(1, 4, 2), out=s(1, 4, n)),
+             lambda: lm.SelectiveScan(s(n, 4, 8), s(n, 4, 8), s(n, 8, 2), s(n, 4, 2), s(n, 4, 2), out=s(n, 4, 8)),
+             lambda: lm.SelectiveScan(s(1, 4, 8), s(1, 4, 8), s(1, 8, n), s(1, 4, n), s(1, 4, n), out=s(1, 4, 8)),
+             lambda: lm.Orthogonalize(s(1, n, 1), s(1, n, 1, dtype=bf)), lambda: lm.Orthogonalize(s(1, 1, n), s(1, 1, n, dtype=bf)),
+             lambda: lm.Orthogonalize(s(n, 1, 1), s(n, 1, 1, dtype=bf)), lambda: lm.Orthogonalize(s(1, 2, 2), s(1, 2, 2, dtype=bf), steps=n)]
+    for make in calls:
+        _refused(lm, lm.api.ERR_TOO_LARGE, make)
+    starts = torch.zeros(n + 1, dtype=torch.int32, device="meta")
+    for seq in (lambda: lm._sequences(None, starts, 1, 4, starts.device), lambda: lm._sequences(n, None, 1, 0, starts.device)):
+        _refused(lm, lm.api.ERR_TOO_LARGE, seq)
