@@ -13,18 +13,15 @@ __device__ __forceinline__ float ex2(float v) {
 }
 __device__ __forceinline__ float2 ex2(float2 v) { return make_float2(ex2(v.x), ex2(v.y)); }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
-// 1 / v of a v in [1, 2^126]
+// 1 / v of a v >= 1; zero beyond 2^126, where it would be subnormal
 __device__ __forceinline__ float rcp(float v) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 __device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
-// sigmoid(v); exp(-v) is held below 2^126, where the reciprocal ends
-__device__ __forceinline__ float2 sigmoid(float2 v) {
-  const float2 u = mul2(v, both(-kLog2e));
-  return rcp(add2(ex2(make_float2(fminf(u.x, 126.f), fminf(u.y, 126.f))), both(1.f)));
-}
+// sigmoid(v): zero where exp(-v) passes 2^126 (v below -87.3), infinities included.  (Held at 2^-126 there, v sigmoid(v) of -1e38 was -1.2.)
+__device__ __forceinline__ float2 sigmoid(float2 v) { return rcp(add2(ex2(mul2(v, both(-kLog2e))), both(1.f))); }
 __device__ __forceinline__ float sigmoid(float v) { return sigmoid(both(v)).x; }
 
 }  // namespace lsgd
