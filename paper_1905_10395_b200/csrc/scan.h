@@ -204,15 +204,17 @@ struct Range {
 __device__ __forceinline__ bool row_lives(const Args& a, int p, const Range& r, int t) {
   return t >= r.t0 && t < r.t1 && (!a.q.starts || a.q.code(p, t) >= 0);
 }
-// Which rows of a tile begin and end a sequence (its number, else -1).
+// Which rows of a tile begin and end a sequence (its number, else -1; of no sequence: kNoRow).
+constexpr int kNoRow = -2;
 template <int ROWS>
 __device__ __forceinline__ void mark_rows(const Args& a, int p, const Range& r, int base, int* begins, int* ends, int i) {
   if (i >= ROWS) return;
   const int t = base + i;
-  int b = -1, e = -1;
+  int b = kNoRow, e = kNoRow;
   if (t >= r.t0 && t < r.t1) {
     const int code = a.q.code(p, t);
     if (code >= 0) {
+      b = e = -1;
       if (a.q.code(p, t - 1) != code) b = code;
       if (a.q.code(p, t + 1) != code) e = code;
     }
@@ -312,11 +314,13 @@ __device__ __forceinline__ void barrier_wait(int id) { asm volatile("barrier.syn
 __device__ __forceinline__ void barrier_arrive(int id) { asm volatile("barrier.arrive %0, %1;" ::"r"(id), "n"(2 * kThreads) : "memory"); }
 
 // kEnds: only what the chain adds to the state behind it, and its summed time steps.
+// kSome: some of a channel's 4 L states do not exist.  They stay out of the sums: their h is zero, but infinite inputs make it NaN
+// (infinity times B's zero).
 // Half of the block's warps run the recurrence, the others stage the next tile and finish the last one meanwhile (two buffers; barriers
 // 1 + b: buffer b is staged, 3 + b: its tile is done), so that a block's staging, a chain of latencies, does not stop its recurrence:
 // ragged prompts of 8191 x 1500 take 203 us instead of 258.  (Two channels a thread would halve what is read of B and C, but leave
 // half the warps: 172 us instead of 197 for 32768 x 384 in fp32, 304 instead of 203 for the prompts.)
-template <typename T, int L, bool kEnds>
+template <typename T, int L, bool kEnds, bool kSome>
 __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
   pdl_wait();
@@ -443,6 +447,7 @@ __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __
   const int64_t saved_step = (int64_t)d.D * d.N;
   float* saved = !kEnds && d.saved && mine ? d.saved + ((int64_t)p * ((a.q.T + kGroup - 1) / kGroup) + r.base / kGroup) * saved_step + (int64_t)ch * d.N : nullptr;
   const int turn = 4 * (local >> 3);
+  auto only = [&](float2 v, int k) { return kSome ? make_float2(n0 + 2 * k < d.N ? v.x : 0.f, n0 + 2 * k + 1 < d.N ? v.y : 0.f) : v; };
   // four rows of the recurrence
   auto rows4 = [&](int base, int b, int t4, auto special) {
     if (!kEnds && saved && t4 % kGroup == 0) {
@@ -481,7 +486,7 @@ __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __
         sum += delta;
       } else {
         pairs(*reinterpret_cast<const float4*>(s_bc[b] + (Ti::kRows + t) * Ti::kN + n0), C);
-        const float2 s = fma2(C[0], h[0], mul2(C[1], h[1]));
+        const float2 s = fma2(C[0], only(h[0], 0), mul2(C[1], only(h[1], 1)));
         y[i] = s.x + s.y;
         if (special && with_state && mine && s_end[b][t] >= 0) {
           const float f[kQuad] = {h[0].x, h[0].y, h[1].x, h[1].y};
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __
 // Sequences of one row each: a thread takes 4 states of a channel of one sequence after another.  Everything that a row needs is under
 // way before the first of it, the decays' logarithms included, is used: what bounds a block is one latency of memory and its
 // own work, so many small blocks overlap (64 x 4096 x 16: 12 us; four rows a thread at a time, in half the warps, 16).
-template <typename T, int L>
+template <typename T, int L, bool kSome>
 __global__ void __launch_bounds__(kThreads, 10) single_kernel(const __grid_constant__ Args a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -575,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 10) single_kernel(const __grid_const
 #pragma unroll
     for (int k = 0; k < kQuad; ++k) {
       h[k] = fmaf(ex2(fmaf(delta, A2[k], kLift)), h[k], du * B[k]);
-      y = fmaf(C[k], h[k], y);
+      if (!kSome || n0 + k < d.N) y = fmaf(C[k], h[k], y);     // kSome: as for the forward kernel
     }
     if (d.state && mine) store_states(d.state, row, n0, d.N, h);
 #pragma unroll
@@ -745,7 +750,9 @@ struct BackSmem {
 };
 // Registers: the four rows in hand (states, decays, B, C and time steps, which both directions use), so that four blocks fit an SM;
 // what is fetched for the next tile therefore goes to shared memory.
-template <typename T, int L>
+// kSome: some of a channel's 4 L states do not exist, or some of the last block's channels.  They stay out of the sums: they are zero, but
+// infinite inputs make them NaN.
+template <typename T, int L, bool kSome>
 __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
   using Sm = BackSmem<T, L>;
@@ -845,6 +852,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
   float* part_bc = a.part_bc + ((int64_t)p * a.tiles + blockIdx.x) * a.q.T * 2 * d.N;
   float column = 0.f;                                              // of d skip or d dt_bias
   int buf = 0;
+  const int there = mine ? d.N - n0 : 0;
+  // (beside the recurrences, not in them)
+  auto only = [&](float2 v, int k) { return kSome ? make_float2(2 * k < there ? v.x : 0.f, 2 * k + 1 < there ? v.y : 0.f) : v; };
   // a group of 8 rows from row0 = base + g8: the later four first, whose states are found through the earlier ones'
   auto group = [&](int row0, int g8, auto special) {
     const float2 first[2] = {make_float2(next[0], next[1]), make_float2(next[2], next[3])};
@@ -856,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
       const float4 delta4 = *reinterpret_cast<const float4*>(s_delta + place), du4 = *reinterpret_cast<const float4*>(s_du + place);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (special && s_begin[g8 + i] >= 0) h[0] = h[1] = make_float2(0.f, 0.f);
+        if (special && s_begin[g8 + i] != -1) h[0] = h[1] = make_float2(0.f, 0.f);
         float2 B[2];
         pairs(*reinterpret_cast<const float4*>(s_bc + (g8 + i) * Ti::kN + n0), B);
         const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
@@ -876,7 +886,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
       const float *b_of = s_bc + (g8 + half) * Ti::kN + n0, *c_of = b_of + Ti::kRows * Ti::kN;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (special && s_begin[g8 + half + i] >= 0) h[0] = h[1] = make_float2(0.f, 0.f);
+        if (special && s_begin[g8 + half + i] != -1) h[0] = h[1] = make_float2(0.f, 0.f);
         pairs(*reinterpret_cast<const float4*>(b_of + i * Ti::kN), B[i]);
         pairs(*reinterpret_cast<const float4*>(c_of + i * Ti::kN), C[i]);
         const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i));
@@ -884,10 +894,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
         for (int k = 0; k < 2; ++k) {
           as[i][k] = decay(delta, A2[k]);
           h[k] = fma2(as[i][k], h[k], mul2(du, B[i][k]));
-          hs[i][k] = h[k];
+          hs[i][k] = only(h[k], k);
         }
         if (gated) {
-          const float2 s = fma2(C[i][0], h[0], mul2(C[i][1], h[1]));
+          const float2 s = fma2(C[i][0], hs[i][0], mul2(C[i][1], hs[i][1]));
           y[i] = s.x + s.y;
         }
       }
@@ -898,13 +908,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks) backward_kernel(const __gri
         const float2 delta = both(part_of(delta4, i)), du = both(part_of(du4, i)), dy = both(part_of(d4, i));
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float2 g = fma2(C[i][k], dy, carry[k]);
+          const float2 all = fma2(C[i][k], dy, carry[k]), g = only(all, k);
           db[k] = mul2(g, du);
           dc[k] = mul2(dy, hs[i][k]);
           sb = k == 0 ? mul2(g, B[i][k]) : fma2(g, B[i][k], sb);
-          carry[k] = mul2(as[i][k], g);
-          float2 q = mul2(carry[k], i > 0 ? hs[i > 0 ? i - 1 : 0][k] : prior[k]);
-          if (special && s_begin[g8 + half + i] >= 0) carry[k] = q = make_float2(0.f, 0.f);
+          carry[k] = mul2(as[i][k], all);
+          float2 q = only(mul2(carry[k], i > 0 ? hs[i > 0 ? i - 1 : 0][k] : prior[k]), k);
+          if (special && s_begin[g8 + half + i] != -1) carry[k] = q = make_float2(0.f, 0.f);
           sum_a[k] = fma2(q, delta, sum_a[k]);
           sq = k == 0 ? mul2(q, A2[k]) : fma2(q, A2[k], sq);
         }
@@ -1121,29 +1131,36 @@ cudaError_t launch_chain_join(const Args& a, bool reverse, cudaStream_t s);
 
 template <typename T, int L>
 cudaError_t forward_of(const Args& a, const Launch& l, cudaStream_t s) {
-  if (l.single) return launch_pdl(single_kernel<T, L>, l.grid, dim3(kThreads), 0, s, a);
+  const bool some = a.d.N % Tile<L>::kN;
+  if (l.single) return some ? launch_pdl(single_kernel<T, L, true>, l.grid, dim3(kThreads), 0, s, a) : launch_pdl(single_kernel<T, L, false>, l.grid, dim3(kThreads), 0, s, a);
   if (a.split) {
-    cudaError_t e = launch_pdl(forward_kernel<T, L, true>, l.grid, dim3(2 * kThreads), 0, s, a);
+    cudaError_t e = launch_pdl(forward_kernel<T, L, true, false>, l.grid, dim3(2 * kThreads), 0, s, a);
     if (e == cudaSuccess) e = launch_chain_join(a, false, s);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(forward_kernel<T, L, false>, l.grid, dim3(2 * kThreads), 0, s, a);
+  return some ? launch_pdl(forward_kernel<T, L, false, true>, l.grid, dim3(2 * kThreads), 0, s, a)
+              : launch_pdl(forward_kernel<T, L, false, false>, l.grid, dim3(2 * kThreads), 0, s, a);
 }
-template <typename T, int L>
-cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
+template <typename T, int L, bool kSome>
+cudaError_t launch_backward(const Args& a, const Launch& l, cudaStream_t s) {
   constexpr size_t smem = BackSmem<T, L>::bytes;
   static OncePerDevice attr;
   if (!attr.here()) {
-    const cudaError_t e = cudaFuncSetAttribute(backward_kernel<T, L>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(backward_kernel<T, L, kSome>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     attr.here() = true;
   }
+  return launch_pdl(backward_kernel<T, L, kSome>, l.grid, dim3(kThreads), smem, s, a);
+}
+template <typename T, int L>
+cudaError_t backward_of(const Args& a, const Launch& l, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (a.split) {
     e = launch_pdl(adjoint_kernel<T, L>, l.grid, dim3(kThreads), 0, s, a);
     if (e == cudaSuccess) e = launch_chain_join(a, true, s);
   }
-  if (e == cudaSuccess) e = launch_pdl(backward_kernel<T, L>, l.grid, dim3(kThreads), smem, s, a);
+  const bool some = a.d.N % Tile<L>::kN || a.d.D % Tile<L>::kCh;
+  if (e == cudaSuccess) e = some ? launch_backward<T, L, true>(a, l, s) : launch_backward<T, L, false>(a, l, s);
   return e == cudaSuccess ? launch_join<T>(a, s) : e;
 }
 template <typename T>
