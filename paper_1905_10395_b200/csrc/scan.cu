@@ -14,7 +14,7 @@ __global__ void __launch_bounds__(256) chain_kernel(const __grid_constant__ Args
   const int p = blockIdx.y;
   if (i >= n) return;
   const int ch = (int)(i / a.d.N), st = (int)(i % a.d.N);
-  const float A2 = -expf(static_cast<const float*>(a.d.a_log.data)[p * a.d.a_log.stride + ch * a.d.a_log.ld + st]) * kLog2e;
+  const float A2 = rate_of(static_cast<const float*>(a.d.a_log.data)[p * a.d.a_log.stride + ch * a.d.a_log.ld + st]);
   float* ends = a.ends + (int64_t)p * a.chains * n + i;
   const float* sums = a.sums + (int64_t)p * a.chains * a.d.D + ch;
   float carry = 0.f;

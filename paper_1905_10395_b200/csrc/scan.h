@@ -22,6 +22,7 @@
 // back through them.  dB and dC are sums over channels: over a warp's by exchanges that halve the number of values at
 // each step, over the warps in shared memory, over the blocks by a second kernel; all in a fixed order.
 #pragma once
+#include <cfloat>
 #include <type_traits>
 
 #include "activations.h"
@@ -134,13 +135,19 @@ __device__ __forceinline__ void pairs8(const float (&f)[8], float2 (&q)[4]) {
 #pragma unroll
   for (int v = 0; v < 4; ++v) q[v] = make_float2(f[2 * v], f[2 * v + 1]);
 }
-// A log2(e) of 4 states of a channel; 0 for those that do not exist (they stay zero, for B is zero there)
+// A log2(e); of a finite a_log whose exponential leaves fp32, the largest there is: times a time step of zero (of rows of no sequence,
+// or far below) it is no NaN.
+__device__ __forceinline__ float rate_of(float a_log) {
+  const float A2 = -expf(a_log) * kLog2e;
+  return a_log < __int_as_float(0x7F800000) && A2 < -FLT_MAX ? -FLT_MAX : A2;
+}
+// ... of 4 states of a channel; 0 for those that do not exist (they stay zero, for B is zero there)
 __device__ __forceinline__ void decay_rates(const Args& a, int p, int ch, int n0, float (&A2)[kQuad]) {
   const float* src = static_cast<const float*>(a.d.a_log.data) + p * a.d.a_log.stride + ch * a.d.a_log.ld + n0;
 #pragma unroll
   for (int k = 0; k < kQuad; ++k) A2[k] = ch < a.d.D && n0 + k < a.d.N ? src[k] : 0.f;
 #pragma unroll
-  for (int k = 0; k < kQuad; ++k) A2[k] = ch < a.d.D && n0 + k < a.d.N ? -expf(A2[k]) * kLog2e : 0.f;
+  for (int k = 0; k < kQuad; ++k) A2[k] = ch < a.d.D && n0 + k < a.d.N ? rate_of(A2[k]) : 0.f;
 }
 __device__ __forceinline__ void load_vector8(const lsgd_rows& v, int p, int ch, int D, float2 (&f)[4]) {
   const float* src = static_cast<const float*>(v.data) + p * v.stride + ch;
@@ -570,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 10) single_kernel(const __grid_const
     const Pack<T, 4> kb = four(d.b, t), kc = four(d.c, t);
     if (!rates) {
 #pragma unroll
-      for (int k = 0; k < kQuad; ++k) A2[k] = in && n0 + k < d.N ? -expf(A2[k]) * kLog2e : 0.f;
+      for (int k = 0; k < kQuad; ++k) A2[k] = in && n0 + k < d.N ? rate_of(A2[k]) : 0.f;
       rates = true;
     }
     float e, y = 0.f;

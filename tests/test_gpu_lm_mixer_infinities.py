@@ -82,3 +82,14 @@ def test_single_tokens_and_split_rows(N):
 def test_rows_behind_the_last_sequence(starts):
     """What a sequence ends with, infinite, does not meet the rows of no sequence that share its tile."""
     _run(40, 24, 16, {"x": (30, 3)}, S=2, starts=torch.tensor(starts, dtype=torch.int32), seed=5)
+
+
+@pytest.mark.parametrize("T,starts", [(20, None), (32, None), (40, [0, 20, 37]), (300, None), (300, [3, 100, 290])], ids=str)
+def test_states_that_forget_at_once(T, starts):
+    """exp(a_log) beyond fp32: a decay of zero; the definition's results are finite, whatever rows share a tile with the last one."""
+    S = 1 if starts is None else len(starts) - 1
+    _run(T, 24, 16, {}, S=S, starts=None if starts is None else torch.tensor(starts, dtype=torch.int32), rates=95.0, seed=T)
+
+
+def test_single_tokens_that_forget_at_once():
+    _run(30, 9, 3, {}, S=30, grads=False, rates=95.0)
