@@ -131,15 +131,23 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prep 
   }
 }
 
-// 1 / (|U| + eps) from the sum of squares; 0 for a zero matrix, NaN where a value is not finite.
-__device__ __forceinline__ float inverse_of(double sum, float eps) {
+// 1 / (|U| + eps) from the sum of squares, as a power of two and a factor of like size, which a value is multiplied by one after the
+// other: |U| may be that of the least subnormal or 2^31 times the largest value, whose inverse leaves fp32.  0 for a zero matrix, NaN
+// where a value is not finite.
+struct Inverse {
+  float power, factor;
+  __device__ __forceinline__ float times(float u) const { return u * power * factor; }
+};
+__device__ __forceinline__ Inverse inverse_of(double sum, float eps) {
   const double t = sqrt(sum) + (double)eps;
-  return t > 0.0 && t < 1e300 ? (float)fmin(1.0 / t, 1e35) : t == 0.0 ? 0.f : __int_as_float(0x7FC00000);
+  if (!(t > 0.0 && t < 1e300)) return {1.f, t == 0.0 ? 0.f : __int_as_float(0x7FC00000)};
+  const int half = -ilogb(t) / 2;
+  return {ldexpf(1.f, half), (float)(ldexp(1.0, -half) / t)};
 }
-__device__ __forceinline__ float inverse_norm(const Prep& a, int p) {
-  __shared__ float s;
+__device__ __forceinline__ Inverse inverse_norm(const Prep& a, int p) {
+  __shared__ Inverse s;
   if (threadIdx.x < 32) {
-    const float t = inverse_of(warp_sum_fixed(a.part + (int64_t)p * a.blocks, a.blocks), a.d.eps);
+    const Inverse t = inverse_of(warp_sum_fixed(a.part + (int64_t)p * a.blocks, a.blocks), a.d.eps);
     if (threadIdx.x == 0) s = t;
   }
   __syncthreads();
@@ -152,7 +160,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
   pdl_wait();
   pdl_launch_dependents();
   const int p = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;       // of the matrix as given
-  float inv = 0.f;
+  Inverse inv = {};
   __shared__ float tile[64][65];
   constexpr int kPieces = 64 * (64 / VEC) / 256, kTake = kPieces < 8 ? kPieces : 8;
 #pragma unroll 1
@@ -170,7 +178,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Prep
       float u[VEC] = {};
       if (r0 + row < a.d.m && c0 + col < a.d.n) piece[k].update(a, p, r0 + row, c0 + col, false, u);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) tile[row][col + v] = u[v] * inv;
+      for (int v = 0; v < VEC; ++v) tile[row][col + v] = inv.times(u[v]);
     }
   }
   __syncthreads();
@@ -687,7 +695,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   const uint32_t tmem = tmem_s;
   double total = 0.0;
   for (int w = 0; w < kSmallThreads / 32; ++w) total += warp_sums[w];
-  const float inv = inverse_of(total, a.d.eps) * kScale;
+  Inverse inv = inverse_of(total, a.d.eps);
+  inv.factor *= kScale;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     const int i = threadIdx.x + k * kSmallThreads;
@@ -696,7 +705,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
     __half hi[VEC], lo[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const float f = u[k][v] * inv;
+      const float f = inv.times(u[k][v]);
       hi[v] = __float2half_rn(f);
       lo[v] = __float2half_rn(f - __half2float(hi[v]));
     }

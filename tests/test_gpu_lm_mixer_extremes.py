@@ -65,3 +65,14 @@ def test_scan_gated_by_far_values(T, S):
     _near(out, got["out"], more * size["out"], 0.0)
     if grads:
         _near(d_z, got["d_z"], more * size["d_z"], 0.0)
+
+
+@pytest.mark.parametrize("m,n", [(60, 90), (90, 60), (200, 300)])
+@pytest.mark.parametrize("size", [1e-43, 1e-40, 1e-37, 1e-34, 1e36, 5e37])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_orthogonalisation_of_any_magnitude(m, n, size, dtype):
+    """X = U / |U| where 1 / |U| leaves fp32's range (|U| of 1e-40 or 1e40), without eps: bounds of test_gpu_lm_ortho.py."""
+    from tests.test_gpu_lm_ortho import run
+    if dtype == torch.bfloat16 and size < 2.0 ** -133:
+        pytest.skip("below the least bf16 value, 2^-133: zeros")
+    run(2, m, n, dtype, size=size, eps=0.0, seed=m)
