@@ -671,9 +671,10 @@ LSGD_API lsgd_status lsgd_scan_backward(const lsgd_scan_desc* desc, void* stream
  * The products' operands are fp16 with a power-of-two scale (11 significant bits; X, G and the polynomial are bounded by about 4,
  * which bf16's wider range would only pay for with three bits less), sums are fp32; the first X counts as two such numbers where
  * the smaller side is 768 at most.  grad: P x m rows of n values of grad_dtype; momentum: the same in fp32, updated in place; out: P
- * x m rows of n values, bf16.  A zero matrix gives zeros; one with a value that is not finite gives NaN.  Coefficients that let
- * singular values pass 16 are out of range: the result is then not finite, or saturated.  Scratch: lsgd_ortho_scratch_bytes(d), which
- * is 0 up to 128 x 256, 256-byte aligned; as for the convolution.                                                 */
+ * x m rows of n values, bf16.  A zero matrix gives zeros; one with a value that is not finite gives NaN.  Range: values of X, G and the
+ * polynomial's matrix are held below 2^6, so every step has to meet singular values v < 7.9 (they begin at 1 or less; the last step's
+ * results may be larger) with |a + b v^2 + c v^4| < 63; beyond, results are not finite.  Scratch: lsgd_ortho_scratch_bytes(d), which is
+ * 0 up to 128 x 256 with a step or more, 256-byte aligned; as for the convolution.                                */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(lsgd_ortho_desc)                                                      */
   int32_t P;                 /* [1, 65535]                                                                    */

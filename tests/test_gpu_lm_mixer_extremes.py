@@ -76,3 +76,22 @@ def test_orthogonalisation_of_any_magnitude(m, n, size, dtype):
     if dtype == torch.bfloat16 and size < 2.0 ** -133:
         pytest.skip("below the least bf16 value, 2^-133: zeros")
     run(2, m, n, dtype, size=size, eps=0.0, seed=m)
+
+
+@pytest.mark.parametrize("first", [7.9, 5.0])
+@pytest.mark.parametrize("m,n", [(1, 1), (2, 3), (130, 1), (1, 300)])
+def test_orthogonalisation_up_to_the_stated_range(first, m, n):
+    """The largest singular values in range, below 8, with a polynomial that brings them back.  A matrix of rank one, whose singular
+    value is 1 to begin with: 7.8, then 7.8 (7.9 - 0.1 61) = 14, which is the last."""
+    from paper_1905_10395_b200 import lm
+    gen = torch.Generator().manual_seed(m)
+    g = torch.randn((1, m, 1), generator=gen) * torch.randn((1, 1, n), generator=gen)
+    for steps, coefficients in ((1, (first, 0.0, 0.0)), (2, (first, -0.1, 0.0)), (3, (1.5, -0.5, 0.0)), (2, (first, 0.0, -0.01))):
+        out = torch.empty((1, m, n), dtype=torch.bfloat16, device="cuda")
+        lm.Orthogonalize(g.cuda(), out, coefficients=coefficients, steps=steps).forward()
+        torch.cuda.synchronize()
+        want, _ = ref.ortho(g.double(), coefficients=coefficients, steps=steps)
+        got = out.double().cpu()
+        # X and G are off by 2^-11 of them at most, so v^2 by 2^-9.4 and v^4 by 2^-8.4 of them: at v = 7.9 the step's factor by
+        # 0.1 62 2^-9.4 < 0.01 or 0.01 3900 2^-8.4 < 0.12, of a result whose factor is 1.7 or -31
+        assert (got - want).norm() <= 2.0 ** -5 * max(want.norm(), first), (steps, coefficients, got.norm(), want.norm())
