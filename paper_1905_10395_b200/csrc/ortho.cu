@@ -9,10 +9,17 @@
 //
 // Operands are fp16 times 2^10, sums fp32.  Entries of X and G are below 2 (singular values stay below 1.3 with the usual
 // coefficients) and those that matter are not below 2^-13 of their matrix's largest, so fp16's range holds them and its 11 bits
-// lose an eighth of what bf16's 8 would.  The first X's rounding is amplified by every later step where singular values are small:
-// for matrices of at most kTwofoldRows rows it is kept as two such numbers, of which the first step's last product takes both.  The
-// whole chain is then off by at most 1.6e-3 of the result's norm instead of 2e-3 (300 x 300; 16 x 16: 1.4e-3 instead of 3.7e-3),
-// rounding to bf16 by 1.7e-3.  Larger matrices are off by less (1024 x 1024: 1.6e-3 to 1.8e-3), and would take 6 to 11 % longer.
+// lose an eighth of what bf16's 8 would.
+//
+// A rounding of X also falls on directions whose singular values are small or zero, where every later step multiplies it by a = 3.4: by
+// 485 from the first X on, which a result of few large singular values (a gradient of few tokens) does not hide.  So what X is
+// rounded by, R, is kept too, in fp16, and X <- Q X + diag(Q) R: on directions that Q stretches by about a, so does its diagonal, and
+// elsewhere a rounding is not amplified.  That costs R's way from and to memory; the whole product Q R would take a third more time (2048 x
+// 8192: 958 us instead of 778, without R 720).  Up to kTwofoldRows rows the diagonal holds too much of the few large singular values (64 x
+// 64 of rank 1: off by 0.8 %, 16 x 16: 2.8), and the contraction is short: there it is the whole product.  The last step goes
+// without R: what X is rounded by in front of it is amplified once.
+// Off the exact result, relative to its norm (rounding to bf16 alone: 0.17 %), with and without R, by 1024 x 1024 matrices of rank 1:
+// 0.32 and 15 %; 4: 0.24, 7.4; 16: 0.24, 4.6; 64: 0.24, 2.4; 256: 0.23, 0.9; full: 0.195, 0.205.
 //
 // product_kernel is a persistent kernel of one CTA an SM on tiles of 128 x 128 or 128 x 64, or of pairs of CTAs on 256 x 256, with the roles of the
 // batched product of gemm_tc.cu: one thread fetches operands by tiled bulk copies into a ring, one issues tcgen05.mma into one of two
@@ -36,6 +43,7 @@ __device__ uint32_t g_status;                    // of the device
 
 constexpr float kScale = 1024.f;                 // of X, G and Q as stored
 constexpr int BM = 128, BK = 64, kBoxBytes = 64 * 64 * 2, kTileBytes = BM * 128 * 2;
+constexpr int kTwofoldRows = 128;
 // The products' forms: 128 columns a tile or 64, or pairs of CTAs of 128 rows and 256 columns each.
 template <bool PAIR, int BN>
 struct Form {
@@ -44,7 +52,6 @@ struct Form {
   static constexpr int kStageBytes = (2 + kBoxesB) * kBoxBytes, kStages = BN == 64 ? 6 : 5;
   static constexpr int kSmemBytes = kStages * kStageBytes + 2 * kTileBytes + 1024;
 };
-constexpr int kTwofoldRows = 768;
 constexpr int kEpiWarps = 8, kThreads = 96 + 32 * kEpiWarps;    // operands, products, the added tile; the epilogue
 
 // ------------------------------------------------------------------------------------------------ momentum and norm
@@ -217,15 +224,18 @@ struct Product {
   float* partial;            // split: [tiles][split][columns of a tile][128 rows]
   uint32_t* done;            // split: blocks of a tile that have finished, 0 between products
   int add;                   // C = alpha acc + beta D + diag I
+  const __half* rows;        // NULL, or beta counts times a value for every row: rows[batch][row (rows_ld)]
+  int64_t rows_ld, rows_stride;
   int twofold;               // C = A B + A D, D of B's layout (instead of an added tile)
+  int rest;                  // what C is rounded by is stored too
   float alpha, beta, diag;
   __nv_bfloat16* out;        // last product: bf16 rows instead of C, times scale
   int64_t out_ld, out_stride;
   int out_transposed, out_wide;
   float scale;
 
-  __host__ __device__ __forceinline__ int nk1() const { return (K + BK - 1) / BK; }
-  __host__ __device__ __forceinline__ int nk() const { return twofold ? 2 * nk1() : nk1(); }
+  __device__ __forceinline__ int nk1() const { return (K + BK - 1) / BK; }
+  __device__ __forceinline__ int nk() const { return twofold ? 2 * nk1() : nk1(); }
 };
 
 struct TileAt {
@@ -285,19 +295,26 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
+// What a pair is rounded by.
+__device__ __forceinline__ uint32_t rest_pair(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return half_pair(lo - __low2float(h), hi - __high2float(h));
+}
+
 // PAIR: a cluster of two CTAs computes a 256 x 256 tile, each fetching its half of the rows of A and of B; the first one's issuer
 // drives both tensor cores (cta_group::2).  Its barriers count both CTAs' copies and epilogues.
 template <bool PAIR, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ Product p) {
+               const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ CUtensorMap map_rest,
+               const __grid_constant__ Product p) {
   using F = Form<PAIR, BN>;
   constexpr int kStages = F::kStages, kStageBytes = F::kStageBytes, kHalves = PAIR ? 2 : 1;
   constexpr uint32_t kTmemCols = 2 * F::kN;      // two accumulators
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* buf = smem + kStages * kStageBytes;   // 128 x BN: D in, C out; boxes of [128][64]
-  uint8_t* mirror = buf + kTileBytes;            // C transposed
+  uint8_t* mirror = buf + kTileBytes;            // C transposed; or its rest, laid out as C
   __shared__ uint64_t full_bar[kStages], empty_bar[kStages], acc_full[2], acc_empty[2], in_full, in_free;
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s, last_s;
@@ -325,6 +342,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_c) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_d) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_rest) : "memory");
   }
   if (warp == 1) {
     if (PAIR) {
@@ -454,6 +472,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const TileAt q = tile_of<F>(p, t, nt, per);
       const int b = local & 1, m0 = q.m0 + rank * 128;
       const bool twice = p.symmetric && q.n0 >= q.m0 + F::kM;
+      float beta = p.beta;
+      if (p.rows) beta *= m0 + row < p.M ? __half2float(p.rows[q.z * p.rows_stride + (m0 + row) * p.rows_ld]) : 0.f;
       ok = mbar_wait(&acc_full[b], (local >> 1) & 1, abort_flag, status);
 #pragma unroll 1
       for (int half = 0; half < kHalves; ++half) {
@@ -524,10 +544,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const float2 f = __half22float2(h[j]);
-                v[8 * u + 2 * j] = fmaf(p.beta, f.x, v[8 * u + 2 * j]);
-                v[8 * u + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * u + 2 * j + 1]);
+                v[8 * u + 2 * j] = fmaf(beta, f.x, v[8 * u + 2 * j]);
+                v[8 * u + 2 * j + 1] = fmaf(beta, f.y, v[8 * u + 2 * j + 1]);
               }
             }
+          }
+          if (p.add && !p.rows) {
             const int d = m0 + row - n0 - c * 32;                // the diagonal's column in this piece
             // selects: every lane has its own j, and 32 branches in turn made this the slowest warp (8 x 256 x 256: 118 us for 113, with
             // squares)
@@ -569,6 +591,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             *reinterpret_cast<uint4*>(box + swz(row, u0 + u)) =
                 make_uint4(half_pair(v[8 * u], v[8 * u + 1]), half_pair(v[8 * u + 2], v[8 * u + 3]),
                            half_pair(v[8 * u + 4], v[8 * u + 5]), half_pair(v[8 * u + 6], v[8 * u + 7]));
+          if (p.rest) {
+            uint8_t* rbox = mirror + (c >> 1) * 2 * kBoxBytes;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              *reinterpret_cast<uint4*>(rbox + swz(row, u0 + u)) =
+                  make_uint4(rest_pair(v[8 * u], v[8 * u + 1]), rest_pair(v[8 * u + 2], v[8 * u + 3]),
+                             rest_pair(v[8 * u + 4], v[8 * u + 5]), rest_pair(v[8 * u + 6], v[8 * u + 7]));
+          }
           if (twice) {
             uint8_t* mbox = mirror + (row >> 6) * (BN * 128);
 #pragma unroll
@@ -604,6 +634,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           for (int j = 0; j < 2; ++j) {
             if (BN == 64 && m0 + 64 * j < p.M) tma_store_3d(buf + j * kBoxBytes, &map_c, n0, m0 + 64 * j, q.z);
             if (BN == 128 && n0 + 64 * j < p.N) tma_store_3d(buf + j * 2 * kBoxBytes, &map_c, n0 + 64 * j, m0, q.z);
+            if (BN == 64 && p.rest && m0 + 64 * j < p.M) tma_store_3d(mirror + j * kBoxBytes, &map_rest, n0, m0 + 64 * j, q.z);
+            if (BN == 128 && p.rest && n0 + 64 * j < p.N) tma_store_3d(mirror + j * 2 * kBoxBytes, &map_rest, n0 + 64 * j, m0, q.z);
             if (twice && m0 + 64 * j < p.M) tma_store_3d(mirror + j * (BN * 128), &map_c, m0 + 64 * j, n0, q.z);
           }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -797,7 +829,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       }
     }
     ok = product([&] {
-      for (int twice = 0; twice < (step == 0 ? 2 : 1); ++twice)
+      for (int twice = 0; twice < (step + 1 < a.d.steps ? 2 : 1); ++twice)
         for (int k = 0; k < rows16; ++k) {
           const uint64_t da = smem_desc(aq + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
           mma_bf16(tx, da, smem_desc((twice ? alo : ax) + k * 2048, kSmallBox, 1024), idesc_x, (k | twice) > 0);
@@ -844,12 +876,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        uint4 w;
-        w.x = half_pair(__uint_as_float(r[8 * u]) * down, __uint_as_float(r[8 * u + 1]) * down);
-        w.y = half_pair(__uint_as_float(r[8 * u + 2]) * down, __uint_as_float(r[8 * u + 3]) * down);
-        w.z = half_pair(__uint_as_float(r[8 * u + 4]) * down, __uint_as_float(r[8 * u + 5]) * down);
-        w.w = half_pair(__uint_as_float(r[8 * u + 6]) * down, __uint_as_float(r[8 * u + 7]) * down);
-        if (c + 8 * u < cols16 * 16) *reinterpret_cast<uint4*>(sx + small_at(row, c + 8 * u)) = w;
+        if (c + 8 * u >= cols16 * 16) continue;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(r[8 * u + j]) * down;
+        *reinterpret_cast<uint4*>(sx + small_at(row, c + 8 * u)) =
+            make_uint4(half_pair(f[0], f[1]), half_pair(f[2], f[3]), half_pair(f[4], f[5]), half_pair(f[6], f[7]));
+        if (step + 2 < a.d.steps)
+          *reinterpret_cast<uint4*>(slo + small_at(row, c + 8 * u)) =
+              make_uint4(rest_pair(f[0], f[1]), rest_pair(f[2], f[3]), rest_pair(f[4], f[5]), rest_pair(f[6], f[7]));
       }
     }
   }
@@ -917,9 +952,8 @@ struct Plan {
   int64_t ldx, ldg;
   uint32_t blocks, tiles;    // of the norm; of G, of 64 columns
   bool small;                // one block a matrix
-  bool twofold;              // the first X as two fp16 numbers
   int split;                 // of G's contraction
-  uint64_t part, done, partial, x0, x1, lo, g, q, total;
+  uint64_t part, done, partial, x[2], rest[2], g, q, total;      // X of even and odd steps, and what it was rounded by
 };
 Plan plan_of(const lsgd_ortho_desc* d) {
   Plan m{};
@@ -938,13 +972,11 @@ Plan plan_of(const lsgd_ortho_desc* d) {
   };
   m.small = m.r <= kSmallRows && m.n <= kSmallCols && d->steps > 0;
   if (m.small) return m;
-  m.twofold = m.r <= kTwofoldRows;
   m.part = take(sizeof(double) * (uint64_t)d->P * m.blocks);
   if (d->steps > 0) {
     const uint64_t x = 2 * (uint64_t)d->P * m.r * m.ldx, g = 2 * (uint64_t)d->P * m.r * m.ldg;
-    m.x0 = take(x);
-    if (d->steps > 1) m.x1 = take(x);
-    if (m.twofold) m.lo = take(x);
+    for (int i = 0; i < 2 && i < d->steps; ++i) m.x[i] = take(x);
+    for (int i = 0; i < 2 && i + 1 < d->steps; ++i) m.rest[i] = take(x);
     m.split = split_of(m.r, m.n, d->P);
     m.tiles = (uint32_t)(((m.r + BM - 1) / BM) * ((m.r + BM - 1) / BM + 1) * (int64_t)d->P);
     if (m.split > 1) {
@@ -966,7 +998,8 @@ bool tile_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, 
 }
 
 template <bool PAIR, int BN>
-cudaError_t launch_form(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const Product& p, int64_t tiles, cudaStream_t s) {
+cudaError_t launch_form(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d, const CUtensorMap& rest, const Product& p,
+                        int64_t tiles, cudaStream_t s) {
   static OncePerDevice attr;
   constexpr int kSmemBytes = Form<PAIR, BN>::kSmemBytes;
   if (!attr.here()) {
@@ -988,7 +1021,7 @@ cudaError_t launch_form(const CUtensorMap& a, const CUtensorMap& b, const CUtens
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = PAIR ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, product_kernel<PAIR, BN>, a, b, c, d, p);
+  return cudaLaunchKernelEx(&cfg, product_kernel<PAIR, BN>, a, b, c, d, rest, p);
 }
 template <typename F>
 int64_t tiles_of(const Product& p) {
@@ -998,14 +1031,14 @@ int64_t tiles_of(const Product& p) {
 // The form whose rounds over the machine take least.  A pair's tile is four of 128 x 128 on two SMs and runs at about 1.4 times their
 // rate (32 x 1024 x 1024: 1131 us instead of 1334).  One of 64 columns fetches three quarters of a square's operands and has half its
 // epilogue, so it takes about 11 of its 14: where there are few (3 x 1001 x 333: 131 us instead of 147; 768 x 768: 140 instead of 158; 8 x 256
-// x 256: 93 instead of 113).  c64: the stored tensor in boxes of 64 rows.
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& c64, const CUtensorMap& d, const Product& p,
-                           cudaStream_t s) {
+// x 256: 93 instead of 113).  c64, rest64: the stored tensors in boxes of 64 rows.
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& c64, const CUtensorMap& d,
+                           const CUtensorMap& rest, const CUtensorMap& rest64, const Product& p, cudaStream_t s) {
   const int64_t half = tiles_of<Form<false, 64>>(p), one = tiles_of<Form<false, 128>>(p), two = tiles_of<Form<true, 128>>(p), sms = sm_count();
   if (half >= int64_t(1) << 31) return cudaErrorInvalidValue;
   const int64_t t_half = (half + sms - 1) / sms * 11, t_one = (one + sms - 1) / sms * 14, t_two = (two + sms / 2 - 1) / (sms / 2) * 20;
-  if (t_half < t_one && t_half < t_two) return launch_form<false, 64>(a, b, c64, d, p, half, s);
-  return t_two <= t_one && p.split == 1 ? launch_form<true, 128>(a, b, c, d, p, two, s) : launch_form<false, 128>(a, b, c, d, p, one, s);
+  if (t_half < t_one && t_half < t_two) return launch_form<false, 64>(a, b, c64, d, rest64, p, half, s);
+  return t_two <= t_one && p.split == 1 ? launch_form<true, 128>(a, b, c, d, rest, p, two, s) : launch_form<false, 128>(a, b, c, d, rest, p, one, s);
 }
 
 template <typename T>
@@ -1025,8 +1058,8 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   a.blocks = m.blocks;
   a.done = reinterpret_cast<uint32_t*>(scratch + m.done);
   a.n_done = m.split > 1 ? m.tiles : 0;
-  a.x = reinterpret_cast<__half*>(scratch + m.x0);
-  a.lo = m.twofold ? reinterpret_cast<__half*>(scratch + m.lo) : nullptr;
+  a.x = reinterpret_cast<__half*>(scratch + m.x[0]);
+  a.lo = d->steps > 1 ? reinterpret_cast<__half*>(scratch + m.rest[0]) : nullptr;
   a.r = m.r;
   a.n = m.n;
   a.tall = d->m > d->n;
@@ -1045,18 +1078,18 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   if (m.small) return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
   e = d->grad_dtype == LSGD_BF16 ? launch_prep<__nv_bfloat16>(a, vec, s) : launch_prep<float>(a, vec, s);
   if (e != cudaSuccess) return LSGD_ERR_CUDA;
-  void* x[2] = {scratch + m.x0, scratch + m.x1};
   void *g = scratch + m.g, *q = scratch + m.q;
   const float down = 1.f / kScale;
   for (int step = 0; step < d->steps; ++step) {
-    const void* from = x[step & 1];
-    void* to = x[(step & 1) ^ 1];
+    // the last step takes no rest of X, and stores neither X nor a rest: the maps that it does not use are X's
     const bool last = step + 1 == d->steps;
-    CUtensorMap x_op, lo_op, to_op, g_op, q_op, g_tile, q_tile, to_tile;
-    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&lo_op, m.twofold ? scratch + m.lo : from, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
-        !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) ||
-        !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P) ||
-        !operand_map(&to_op, last ? from : to, m.n, m.r, m.ldx, d->P) || !tile_map(&to_tile, last ? from : to, m.n, m.r, m.ldx, d->P))
+    char *from = scratch + m.x[step & 1], *to = last ? from : scratch + m.x[(step & 1) ^ 1];
+    char *rest = last ? from : scratch + m.rest[step & 1], *to_rest = last ? from : scratch + m.rest[(step & 1) ^ 1];
+    CUtensorMap x_op, to_op, g_op, q_op, rest_op, to_rest_op, to_tile, g_tile, q_tile, rest_tile, to_rest_tile;
+    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&to_op, to, m.n, m.r, m.ldx, d->P) || !tile_map(&to_tile, to, m.n, m.r, m.ldx, d->P) ||
+        !operand_map(&rest_op, rest, m.n, m.r, m.ldx, d->P) || !tile_map(&rest_tile, rest, m.n, m.r, m.ldx, d->P) || !operand_map(&to_rest_op, to_rest, m.n, m.r, m.ldx, d->P) ||
+        !tile_map(&to_rest_tile, to_rest, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
+        !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) || !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P))
       return LSGD_ERR_CUDA;
     Product p{};
     p.batch = d->P;
@@ -1067,20 +1100,25 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.partial = reinterpret_cast<float*>(scratch + m.partial);
     p.done = a.done;
     p.alpha = down;
-    if (launch_product(x_op, x_op, g_tile, g_op, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(x_op, x_op, g_tile, g_op, g_tile, g_tile, g_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.K = m.r;
     p.split = 1;
     p.add = 1;
     p.alpha = d->c * down;
     p.beta = d->b;
     p.diag = d->a * kScale;
-    if (launch_product(g_op, g_op, q_tile, q_op, g_tile, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(g_op, g_op, q_tile, q_op, g_tile, q_tile, q_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.N = m.n;
     p.symmetric = 0;
     p.b_mn = 1;
-    p.add = 0;
-    p.twofold = step == 0 && m.twofold;
-    p.alpha = down;
+    p.twofold = !last && m.r <= kTwofoldRows;
+    p.add = !last && !p.twofold;
+    p.alpha = p.beta = down;
+    p.diag = 0.f;
+    p.rows = p.add ? static_cast<const __half*>(q) : nullptr;    // Q's diagonal
+    p.rows_ld = m.ldg + 1;
+    p.rows_stride = m.ldg * m.r;
+    p.rest = step + 2 < d->steps;
     if (last) {
       p.out = static_cast<__nv_bfloat16*>(d->out.data);
       p.out_ld = d->out.ld;
@@ -1089,7 +1127,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
       p.out_wide = a.out_wide;
       p.scale = d->scale * down;
     }
-    if (launch_product(q_op, x_op, to_tile, to_op, lo_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(q_op, x_op, to_tile, to_op, p.twofold ? rest_op : rest_tile, to_rest_tile, to_rest_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
   }
   return LSGD_OK;
 }
