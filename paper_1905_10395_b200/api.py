@@ -297,6 +297,15 @@ def lsgd_embed_check_device() -> int:
     return f.value
 
 
+def lsgd_ortho_check_device() -> int:
+    """Status word of lsgd_ortho on the current device (read and cleared); 0 = no kernel reported anything."""
+    f = C.c_uint32()
+    s = lib().lsgd_ortho_check_device(C.byref(f))
+    if s not in (OK, ERR_DEVICE_FLAG):
+        raise LsgdError(s, "lsgd_ortho_check_device")
+    return f.value
+
+
 def adamw_state_values(sizes: Sequence[int]) -> int:
     """Values of the moment buffers of lsgd_adamw: every tensor begins at a multiple of 256."""
     a = np.ascontiguousarray(sizes, dtype=np.int64)

@@ -443,6 +443,14 @@ class Orthogonalize:
         if s:
             raise api.LsgdError(s, "lsgd_ortho")
 
+    def check(self) -> None:
+        """Waits for the device and raises (ERR_DEVICE_FLAG) if a wait of the products' kernels ran out since it was last asked, of any
+        operator on this device: what such a call left in `out` is not its result."""
+        with torch.cuda.device(self.device):
+            flag = api.lsgd_ortho_check_device()
+        if flag:
+            raise api.LsgdError(api.ERR_DEVICE_FLAG, f"lsgd_ortho: status {flag:#x}")
+
 
 class AdamW:
     """One AdamW step over many tensors, in one launch.  params fp32, grads fp32 or bf16 (all of one type), each of them

@@ -118,7 +118,7 @@ class LmPopulation:
             self.momentum = torch.zeros_like(self.x)
             for name, shape, _, decayed in self.segs:
                 if decayed and name != "table":
-                    out = torch.empty((P, *shape), **bf)
+                    out = torch.zeros((P, *shape), **bf)
                     op = lm.Orthogonalize(view(self.g, name), out, momentum=view(self.momentum, name), scale=0.2 * max(shape) ** 0.5)
                     self.ortho.append((op, out, view(self.x, name), view(self.copy, name)))
         adamw = [s for s in self.segs if not (self.ortho and s[3] and s[0] != "table")]
@@ -271,6 +271,8 @@ class LmPopulation:
                 copy.copy_(x)
             self.t += 1
             if self.t % self.tau == 0:
+                if self.ortho:
+                    self.ortho[0][0].check()     # one status word of them all: no leader is followed from a failed update
                 self.lsgd.elect(loss)
                 self.lsgd.step()
                 self.copy.copy_(self.x)          # the pulls moved the parameters: the products' copies follow

@@ -72,3 +72,60 @@ def test_sizes_of_more_than_32_bits_are_refused(lm, devices, n):  # noqa: F811
     starts = torch.zeros(n + 1, dtype=torch.int32, device="meta")
     for seq in (lambda: lm._sequences(None, starts, 1, 4, starts.device), lambda: lm._sequences(n, None, 1, 0, starts.device)):
         _refused(lm, lm.api.ERR_TOO_LARGE, seq)
+
+
+def test_a_wait_that_ran_out_is_reported(lm, devices, monkeypatch):  # noqa: F811
+    """The status word reaches the caller: of an operator that is asked, and of a population at its next pull, before any leader is
+    followed."""
+    from contextlib import nullcontext
+
+    from paper_1905_10395_b200 import lm_population
+    real, word = torch.empty, [0]
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: real(*a, **k))
+    op = lm.Orthogonalize(torch.zeros(1, 16, 8), torch.zeros(1, 16, 8, dtype=torch.bfloat16))
+    op._call = lambda *a: 0
+
+    library = lm.api.lib()
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(library, name)
+
+        def lsgd_ortho_check_device(self, f):
+            assert devices.current == 1                  # the operator's device, whichever is current
+            f._obj.value, was = word[0], word[0]
+            word[0] = 0
+            return lm.api.ERR_DEVICE_FLAG if was else 0
+
+    monkeypatch.setattr(lm.api, "lib", lambda: Library())
+    op.check()
+    word[0] = 4
+    devices.current = 0
+    _refused(lm, lm.api.ERR_DEVICE_FLAG, op.check)
+    devices.current = 1
+    op.check()                                           # read and cleared
+
+    pop, log = lm_population.LmPopulation.__new__(lm_population.LmPopulation), []
+
+    class Leaders:
+        def elect(self, loss):
+            log.append("elect")
+
+        def step(self):
+            log.append("pull")
+
+    class Step:
+        def step(self, lr):
+            log.append("adamw")
+
+    x = torch.zeros(1, 16, 8)
+    pop.forward, pop._backward, pop._in_order = (lambda a, b: None), (lambda: None), nullcontext
+    pop.opt, pop.lsgd, pop.lr, pop.lr_ortho, pop.tau, pop.t = Step(), Leaders(), 0.1, 0.1, 2, 0
+    pop.ortho, pop.x, pop.copy = [(op, torch.zeros(1, 16, 8), x, x.clone())], x, x.clone()
+    pop.step(None, None)
+    word[0] = 4
+    _refused(lm, lm.api.ERR_DEVICE_FLAG, lambda: pop.step(None, None))
+    assert log == ["adamw", "adamw"]
+    pop.step(None, None)
+    pop.step(None, None)
+    assert log[2:] == ["adamw", "adamw", "elect", "pull"]
