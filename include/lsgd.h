@@ -622,6 +622,9 @@ typedef struct {
 LSGD_API uint64_t lsgd_conv_scratch_bytes(const lsgd_conv_desc* desc, int32_t backward);
 LSGD_API lsgd_status lsgd_conv_forward(const lsgd_conv_desc* desc, void* stream);
 LSGD_API lsgd_status lsgd_conv_backward(const lsgd_conv_desc* desc, void* stream);
+/* Which form a call takes on the current device (for tests that are to reach all of them): values a thread, rows a thread, and warps that
+ * share a last sum (0 forwards).                                                                                  */
+LSGD_API lsgd_status lsgd_conv_plan(const lsgd_conv_desc* desc, int32_t backward, int32_t plan[3]);
 
 /* ---- Selective state space scan -----------------------------------------------------------------------------
  * Every channel d has N states, which its time step delta moves:
@@ -662,6 +665,8 @@ typedef struct {
 LSGD_API uint64_t lsgd_scan_scratch_bytes(const lsgd_scan_desc* desc, int32_t backward);
 LSGD_API lsgd_status lsgd_scan_forward(const lsgd_scan_desc* desc, void* stream);
 LSGD_API lsgd_status lsgd_scan_backward(const lsgd_scan_desc* desc, void* stream);
+/* As lsgd_conv_plan: lanes a channel, chains of a worker, rows of a chain where the rows are split (else 0), and 1 for single tokens.     */
+LSGD_API lsgd_status lsgd_scan_plan(const lsgd_scan_desc* desc, int32_t backward, int32_t plan[4]);
 
 /* ---- Orthogonalised updates -------------------------------------------------------------------------------
  * For every worker's m x n matrix: U = grad, or with a momentum  M <- mu M + grad,  U = M (nesterov: grad + mu M);
@@ -692,6 +697,9 @@ typedef struct {
 } lsgd_ortho_desc;
 LSGD_API uint64_t lsgd_ortho_scratch_bytes(const lsgd_ortho_desc* desc);
 LSGD_API lsgd_status lsgd_ortho(const lsgd_ortho_desc* desc, void* stream);
+/* As lsgd_conv_plan: columns of the tiles of X X^T, of the polynomial and of the product with X (64, 128; 256: by pairs of blocks; 0: one block
+ * a matrix), most tiles that one block (pair) takes of each, and blocks that share a tile of X X^T.                  */
+LSGD_API lsgd_status lsgd_ortho_plan(const lsgd_ortho_desc* desc, int32_t plan[7]);
 /* Synchronises the current device, then reads and clears the status word of lsgd_ortho on it (its products' bounded waits record
  * LSGD_DEVFLAG_WAIT_TIMEOUT there): LSGD_ERR_DEVICE_FLAG if it was set.                                         */
 LSGD_API lsgd_status lsgd_ortho_check_device(uint32_t* flag_out /* HOST, may be NULL */);

@@ -198,7 +198,10 @@ def lib() -> C.CDLL:
             for direction in ("forward", "backward"):
                 f = getattr(L, f"lsgd_{name}_{direction}")
                 f.argtypes, f.restype = [C.POINTER(desc), C.c_void_p], C.c_int
+        L.lsgd_ortho_plan.argtypes, L.lsgd_ortho_plan.restype = [C.POINTER(OrthoDesc), C.POINTER(C.c_int32)], C.c_int
         for name, desc in (("conv", ConvDesc), ("scan", ScanDesc)):
+            f = getattr(L, f"lsgd_{name}_plan")
+            f.argtypes, f.restype = [C.POINTER(desc), C.c_int32, C.POINTER(C.c_int32)], C.c_int
             f = getattr(L, f"lsgd_{name}_scratch_bytes")
             f.argtypes, f.restype = [C.POINTER(desc), C.c_int32], C.c_uint64
             for direction in ("forward", "backward"):

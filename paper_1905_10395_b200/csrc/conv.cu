@@ -439,7 +439,7 @@ int conv_vec(const lsgd_conv_desc* d, bool backward) {
 }
 
 struct ConvPlan {
-  int vec, run;
+  int vec, run, join;        // values and rows of a thread; warps of a last sum
   uint32_t blocks_d, blocks_t;
 };
 ConvPlan conv_plan(const lsgd_conv_desc* d, bool backward) {
@@ -463,6 +463,7 @@ ConvPlan conv_plan(const lsgd_conv_desc* d, bool backward) {
   // no more than 65535 blocks of rows (gridDim.y)
   while ((d->T + (int64_t)c.run * kRuns - 1) / ((int64_t)c.run * kRuns) > 65535) c.run *= 2;
   c.blocks_t = (uint32_t)((d->T + (int64_t)c.run * kRuns - 1) / ((int64_t)c.run * kRuns));
+  c.join = !backward ? 0 : c.blocks_t <= 32 ? 1 : 8;
   return c;
 }
 
@@ -508,7 +509,7 @@ lsgd_status run_conv(const lsgd_conv_desc* d, bool backward, cudaStream_t s) {
   }
   if (e == cudaSuccess && backward) {
     const unsigned n = (unsigned)d->D * (d->W + 1);
-    e = c.blocks_t <= 32 ? launch_pdl(conv_join_kernel<1>, dim3((n + 255) / 256, d->P), dim3(256), 0, s, a)
+    e = c.join == 1      ? launch_pdl(conv_join_kernel<1>, dim3((n + 255) / 256, d->P), dim3(256), 0, s, a)
                          : launch_pdl(conv_join_kernel<8>, dim3((n + 31) / 32, d->P), dim3(256), 0, s, a);
   }
   return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
@@ -532,6 +533,15 @@ uint64_t lsgd_conv_scratch_bytes(const lsgd_conv_desc* d, int32_t backward) {
   uint64_t n = codes_bytes(d->seq, d->P, d->T);
   if (backward) n += sizeof(float) * (uint64_t)d->P * conv_plan(d, true).blocks_t * d->D * (d->W + 1);
   return align256(n);
+}
+
+lsgd_status lsgd_conv_plan(const lsgd_conv_desc* d, int32_t backward, int32_t plan[3]) {
+  using namespace lsgd;
+  const lsgd_status st = check_conv(d, backward);
+  if (st != LSGD_OK || !plan) return st != LSGD_OK ? st : LSGD_ERR_INVALID_ARG;
+  const ConvPlan c = conv_plan(d, backward);
+  plan[0] = c.vec, plan[1] = c.run, plan[2] = c.join;
+  return LSGD_OK;
 }
 
 #define LSGD_CONV_CALL(name, backward)                                                            \

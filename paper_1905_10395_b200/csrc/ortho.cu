@@ -1032,13 +1032,23 @@ int64_t tiles_of(const Product& p) {
 // rate (32 x 1024 x 1024: 1131 us instead of 1334).  One of 64 columns fetches three quarters of a square's operands and has half its
 // epilogue, so it takes about 11 of its 14: where there are few (3 x 1001 x 333: 131 us instead of 147; 768 x 768: 140 instead of 158; 8 x 256
 // x 256: 93 instead of 113).  c64, rest64: the stored tensors in boxes of 64 rows.
+struct Chosen {
+  int columns;               // 64, 128, or 256: pairs
+  int64_t tiles, each;       // in all; most that a block (a pair) takes
+};
+Chosen form_of(const Product& p) {
+  const int64_t half = tiles_of<Form<false, 64>>(p), one = tiles_of<Form<false, 128>>(p), two = tiles_of<Form<true, 128>>(p), sms = sm_count();
+  const int64_t n_half = (half + sms - 1) / sms, n_one = (one + sms - 1) / sms, n_two = (two + sms / 2 - 1) / (sms / 2);
+  if (11 * n_half < 14 * n_one && 11 * n_half < 20 * n_two) return {64, half, n_half};
+  return 20 * n_two <= 14 * n_one && p.split == 1 ? Chosen{256, two, n_two} : Chosen{128, one, n_one};
+}
 cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& c64, const CUtensorMap& d,
                            const CUtensorMap& rest, const CUtensorMap& rest64, const Product& p, cudaStream_t s) {
-  const int64_t half = tiles_of<Form<false, 64>>(p), one = tiles_of<Form<false, 128>>(p), two = tiles_of<Form<true, 128>>(p), sms = sm_count();
-  if (half >= int64_t(1) << 31) return cudaErrorInvalidValue;
-  const int64_t t_half = (half + sms - 1) / sms * 11, t_one = (one + sms - 1) / sms * 14, t_two = (two + sms / 2 - 1) / (sms / 2) * 20;
-  if (t_half < t_one && t_half < t_two) return launch_form<false, 64>(a, b, c64, d, rest64, p, half, s);
-  return t_two <= t_one && p.split == 1 ? launch_form<true, 128>(a, b, c, d, rest, p, two, s) : launch_form<false, 128>(a, b, c, d, rest, p, one, s);
+  if (tiles_of<Form<false, 64>>(p) >= int64_t(1) << 31) return cudaErrorInvalidValue;
+  const Chosen f = form_of(p);
+  return f.columns == 64    ? launch_form<false, 64>(a, b, c64, d, rest64, p, f.tiles, s)
+         : f.columns == 256 ? launch_form<true, 128>(a, b, c, d, rest, p, f.tiles, s)
+                            : launch_form<false, 128>(a, b, c, d, rest, p, f.tiles, s);
 }
 
 template <typename T>
@@ -1152,6 +1162,28 @@ lsgd_status lsgd_ortho(const lsgd_ortho_desc* d, void* stream) {
   if (need && (!d->scratch || d->scratch_bytes < need)) return LSGD_ERR_INVALID_ARG;
   if (need && reinterpret_cast<uintptr_t>(d->scratch) % 256) return LSGD_ERR_ALIGNMENT;
   return run_ortho(d, static_cast<cudaStream_t>(stream));
+}
+
+lsgd_status lsgd_ortho_plan(const lsgd_ortho_desc* d, int32_t plan[7]) {
+  using namespace lsgd::ortho;
+  const lsgd_status st = check_ortho(d);
+  if (st != LSGD_OK || !plan) return st != LSGD_OK ? st : LSGD_ERR_INVALID_ARG;
+  const Plan m = plan_of(d);
+  for (int i = 0; i < 7; ++i) plan[i] = 0;
+  if (m.small || d->steps == 0) return LSGD_OK;
+  for (int i = 0; i < 3; ++i) {
+    Product p{};
+    p.batch = d->P;
+    p.M = m.r;
+    p.N = i < 2 ? m.r : m.n;
+    p.symmetric = i < 2;
+    p.split = i == 0 ? m.split : 1;
+    const Chosen f = form_of(p);
+    plan[i] = f.columns;
+    plan[3 + i] = (int32_t)f.each;
+  }
+  plan[6] = m.split;
+  return LSGD_OK;
 }
 
 lsgd_status lsgd_ortho_check_device(uint32_t* flag_out) {

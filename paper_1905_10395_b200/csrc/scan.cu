@@ -237,6 +237,15 @@ uint64_t lsgd_scan_scratch_bytes(const lsgd_scan_desc* d, int32_t backward) {
   return plan_of(d, backward).total;
 }
 
+lsgd_status lsgd_scan_plan(const lsgd_scan_desc* d, int32_t backward, int32_t plan[4]) {
+  using namespace lsgd;
+  const lsgd_status st = scan::check_scan(d, backward);
+  if (st != LSGD_OK || !plan) return st != LSGD_OK ? st : LSGD_ERR_INVALID_ARG;
+  const scan::Plan m = scan::plan_of(d, backward);
+  plan[0] = m.l.L, plan[1] = m.chains, plan[2] = m.split ? m.per : 0, plan[3] = m.l.single;
+  return LSGD_OK;
+}
+
 #define LSGD_SCAN_CALL(name, backward)                                                            \
   lsgd_status name(const lsgd_scan_desc* d, void* stream) {                                       \
     using namespace lsgd;                                                                         \

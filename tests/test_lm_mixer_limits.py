@@ -129,3 +129,14 @@ def test_a_wait_that_ran_out_is_reported(lm, devices, monkeypatch):  # noqa: F81
     pop.step(None, None)
     pop.step(None, None)
     assert log[2:] == ["adamw", "adamw", "elect", "pull"]
+
+
+def test_plans_are_refused_as_the_calls_are(api):  # noqa: F811
+    L, out = api.lib(), (C.c_int32 * 7)()
+    for back in (0, 1):
+        assert L.lsgd_conv_plan(C.byref(_conv(api)), back, out) == 0 and L.lsgd_scan_plan(C.byref(_scan(api)), back, out) == 0
+        assert L.lsgd_conv_plan(C.byref(_conv(api)), back, None) == 1 and L.lsgd_scan_plan(C.byref(_scan(api)), back, None) == 1
+        assert L.lsgd_conv_plan(C.byref(_conv(api, W=5)), back, out) == 6 and L.lsgd_scan_plan(C.byref(_scan(api, N=65)), back, out) == 6
+        assert L.lsgd_conv_plan(None, back, out) == 1 and L.lsgd_scan_plan(None, back, out) == 1
+    assert L.lsgd_ortho_plan(C.byref(_ortho(api)), out) == 0 and L.lsgd_ortho_plan(C.byref(_ortho(api)), None) == 1
+    assert L.lsgd_ortho_plan(C.byref(_ortho(api, steps=33)), out) == 6 and L.lsgd_ortho_plan(None, out) == 1
