@@ -990,11 +990,8 @@ Plan plan_of(const lsgd_ortho_desc* d) {
   return m;
 }
 
-bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int64_t P) {
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, 64);
-}
-bool tile_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int64_t P) {
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, 128);
+bool encode_boxes(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int64_t P, int rows) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, inner, outer, ld, P, ld * outer, 64, rows);
 }
 
 template <bool PAIR, int BN>
@@ -1088,19 +1085,21 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
   if (m.small) return e == cudaSuccess ? LSGD_OK : LSGD_ERR_CUDA;
   e = d->grad_dtype == LSGD_BF16 ? launch_prep<__nv_bfloat16>(a, vec, s) : launch_prep<float>(a, vec, s);
   if (e != cudaSuccess) return LSGD_ERR_CUDA;
-  void *g = scratch + m.g, *q = scratch + m.q;
+  if (d->steps == 0) return LSGD_OK;
+  // a matrix in boxes of 64 and of 128 rows; those without a place (few steps) are not reached
+  struct Maps {
+    CUtensorMap op, tile;
+  } x[2], rest[2], g, q;
+  auto map = [&](Maps& t, uint64_t at, int64_t inner, int64_t ld) {
+    return encode_boxes(&t.op, scratch + at, inner, m.r, ld, d->P, 64) && encode_boxes(&t.tile, scratch + at, inner, m.r, ld, d->P, 128);
+  };
+  if (!map(g, m.g, m.r, m.ldg) || !map(q, m.q, m.r, m.ldg)) return LSGD_ERR_CUDA;
+  for (int i = 0; i < 2; ++i)
+    if (!map(x[i], m.x[i], m.n, m.ldx) || !map(rest[i], m.rest[i], m.n, m.ldx)) return LSGD_ERR_CUDA;
   const float down = 1.f / kScale;
   for (int step = 0; step < d->steps; ++step) {
-    // the last step takes no rest of X, and stores neither X nor a rest: the maps that it does not use are X's
-    const bool last = step + 1 == d->steps;
-    char *from = scratch + m.x[step & 1], *to = last ? from : scratch + m.x[(step & 1) ^ 1];
-    char *rest = last ? from : scratch + m.rest[step & 1], *to_rest = last ? from : scratch + m.rest[(step & 1) ^ 1];
-    CUtensorMap x_op, to_op, g_op, q_op, rest_op, to_rest_op, to_tile, g_tile, q_tile, rest_tile, to_rest_tile;
-    if (!operand_map(&x_op, from, m.n, m.r, m.ldx, d->P) || !operand_map(&to_op, to, m.n, m.r, m.ldx, d->P) || !tile_map(&to_tile, to, m.n, m.r, m.ldx, d->P) ||
-        !operand_map(&rest_op, rest, m.n, m.r, m.ldx, d->P) || !tile_map(&rest_tile, rest, m.n, m.r, m.ldx, d->P) || !operand_map(&to_rest_op, to_rest, m.n, m.r, m.ldx, d->P) ||
-        !tile_map(&to_rest_tile, to_rest, m.n, m.r, m.ldx, d->P) || !operand_map(&g_op, g, m.r, m.r, m.ldg, d->P) ||
-        !operand_map(&q_op, q, m.r, m.r, m.ldg, d->P) || !tile_map(&g_tile, g, m.r, m.r, m.ldg, d->P) || !tile_map(&q_tile, q, m.r, m.r, m.ldg, d->P))
-      return LSGD_ERR_CUDA;
+    const bool last = step + 1 == d->steps;          // takes no rest of X, and stores neither X nor a rest
+    const Maps &from = x[step & 1], &to = x[(step & 1) ^ 1], &from_rest = rest[step & 1], &to_rest = rest[(step & 1) ^ 1];
     Product p{};
     p.batch = d->P;
     p.M = p.N = m.r;
@@ -1110,14 +1109,14 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.partial = reinterpret_cast<float*>(scratch + m.partial);
     p.done = a.done;
     p.alpha = down;
-    if (launch_product(x_op, x_op, g_tile, g_op, g_tile, g_tile, g_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(from.op, from.op, g.tile, g.op, g.tile, g.tile, g.op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.K = m.r;
     p.split = 1;
     p.add = 1;
     p.alpha = d->c * down;
     p.beta = d->b;
     p.diag = d->a * kScale;
-    if (launch_product(g_op, g_op, q_tile, q_op, g_tile, q_tile, q_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(g.op, g.op, q.tile, q.op, g.tile, q.tile, q.op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
     p.N = m.n;
     p.symmetric = 0;
     p.b_mn = 1;
@@ -1125,7 +1124,7 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
     p.add = !last && !p.twofold;
     p.alpha = p.beta = down;
     p.diag = 0.f;
-    p.rows = p.add ? static_cast<const __half*>(q) : nullptr;    // Q's diagonal
+    p.rows = p.add ? reinterpret_cast<const __half*>(scratch + m.q) : nullptr;    // Q's diagonal
     p.rows_ld = m.ldg + 1;
     p.rows_stride = m.ldg * m.r;
     p.rest = step + 2 < d->steps;
@@ -1137,7 +1136,8 @@ lsgd_status run_ortho(const lsgd_ortho_desc* d, cudaStream_t s) {
       p.out_wide = a.out_wide;
       p.scale = d->scale * down;
     }
-    if (launch_product(q_op, x_op, to_tile, to_op, p.twofold ? rest_op : rest_tile, to_rest_tile, to_rest_op, p, s) != cudaSuccess) return LSGD_ERR_CUDA;
+    if (launch_product(q.op, from.op, to.tile, to.op, p.twofold ? from_rest.op : from_rest.tile, to_rest.tile, to_rest.op, p, s) != cudaSuccess)
+      return LSGD_ERR_CUDA;
   }
   return LSGD_OK;
 }
