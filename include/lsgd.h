@@ -675,8 +675,8 @@ LSGD_API lsgd_status lsgd_scan_plan(const lsgd_scan_desc* desc, int32_t backward
  * a v + b v^3 + c v^5; with the usual (3.4445, -4.7750, 2.0315) five steps bring all that are not tiny to about one.
  * The products' operands are fp16 with a power-of-two scale (11 significant bits; X, G and the polynomial are bounded by about 4,
  * which bf16's wider range would only pay for with three bits less), sums are fp32; what X is rounded by is carried to the next step, so
- * that results are off by 0.4 % of their norm at most, whatever the rank.  grad: P x m rows of n values of grad_dtype; momentum: the same in fp32, updated in place; out: P
- * x m rows of n values, bf16.  A zero matrix gives zeros; one with a value that is not finite gives NaN.  Range: values of X, G and the
+ * that five usual steps are off by 0.4 % of the result's norm at most, whatever the rank.  grad: P x m rows of n values of grad_dtype;
+ * momentum: the same in fp32, updated in place; out: P x m rows of n values, bf16.  A zero matrix gives zeros; one with a value that is not finite gives NaN.  Range: values of X, G and the
  * polynomial's matrix are held below 2^6, so every step has to meet singular values v < 7.9 (they begin at 1 or less; the last step's
  * results may be larger) with |a + b v^2 + c v^4| < 63; beyond, results are not finite.  Scratch: lsgd_ortho_scratch_bytes(d), which is
  * 0 up to 128 x 256 with a step or more, 256-byte aligned; as for the convolution.                                */

@@ -413,7 +413,6 @@ lsgd_status check_conv(const lsgd_conv_desc* d, bool backward) {
   if (!d->dw.data || (d->bias.data != nullptr) != (d->d_bias.data != nullptr)) return LSGD_ERR_INVALID_ARG;
   LSGD_ROWS(d->d_out, T, D, ab, false, false);
   LSGD_ROWS(d->dx, T, D, ab, true, false);
-  if (D > 1 && d->dw.ld < d->W) return LSGD_ERR_INVALID_ARG;
   LSGD_ROWS(d->dw, D, d->W, 4, true, true);
   LSGD_ROWS(d->d_bias, 1, D, 4, true, true);
 #undef LSGD_ROWS

@@ -197,7 +197,7 @@ bgemm_bf16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int k = 0; k < BK / 16; ++k) {
           const uint64_t da = p.a_mn ? smem_desc(sa + k * 2048, 8192, 1024) : smem_desc(sa + k * 32, 16, 1024);
           const uint64_t db = p.b_mn ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024);
-          mma_bf16(tacc, da, db, idesc, (kt | k) != 0 ? 1u : 0u);
+          mma_f16(tacc, da, db, idesc, (kt | k) != 0 ? 1u : 0u);
         }
         mma_commit(&empty_bar[s]);   // the stage is free once these MMAs have read it
       }
@@ -461,7 +461,7 @@ bgemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const uint32_t sa = smem_u32(smem + s * kPairStageBytes), sb = sa + kABytes;
 #pragma unroll
         for (int k = 0; k < BK / 16; ++k)
-          mma_bf16_pair(tacc, smem_desc(sa + k * 32, 16, 1024), smem_desc(sb + k * 32, 16, 1024), idesc, (kt | k) != 0 ? 1u : 0u);
+          mma_f16_pair(tacc, smem_desc(sa + k * 32, 16, 1024), smem_desc(sb + k * 32, 16, 1024), idesc, (kt | k) != 0 ? 1u : 0u);
         // the stage is free in both CTAs once these products have read it
         mma_commit_pair(map_to_rank(smem_u32(&empty_bar[s]), 0));
         mma_commit_pair(map_to_rank(smem_u32(&empty_bar[s]), 1));

@@ -26,8 +26,8 @@
 // accumulators in tensor memory, one fetches the tiles that are added, eight warps run the epilogue.  Every wait is bounded by a clock
 // budget; on expiry the kernel raises a status bit, drains its copies, frees tensor memory and returns.
 //
-// What bounds it: large batches (2 x 4096 x 4096: 2.5 ms, 1090 TFLOP/s; 32 x 1024 x 1024: 895 us, 770) the operands' way from L2, at
-// 8 TB/s; a few small matrices (8 x 256 x 256: 93 us) the chain of 15 dependent products of about 6 us each: its first operands'
+// What bounds it: large batches (2 x 4096 x 4096: 2.6 ms, 1070 TFLOP/s; 32 x 1024 x 1024 with momentum: 1.2 ms, 570) the operands' way from L2, at
+// 8 TB/s; a few small matrices (8 x 256 x 256: 88 us) the chain of 15 dependent products of about 6 us each: its first operands'
 // latency 1.2, the contraction 1.3, the epilogue with its store 1, the change of kernels 1.6.
 #include <cuda_fp16.h>
 
@@ -419,8 +419,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int k = 0; k < BK / 16; ++k) {
           const uint64_t da = smem_desc(sa + k * 32, 16, 1024);
           const uint64_t db = p.b_mn ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024);
-          if (PAIR) mma_bf16_pair(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
-          else mma_bf16(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
+          if (PAIR) mma_f16_pair(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
+          else mma_f16(tacc, da, db, idesc, kt > q.k0 || k > 0 ? 1u : 0u);
         }
         if (PAIR) {
           mma_commit_pair(map_to_rank(smem_u32(&empty_bar[s]), 0));
@@ -781,7 +781,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
     ok = product([&] {
       for (int k = 0; k < cols16; ++k) {
         const uint64_t d = smem_desc(ax + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
-        mma_bf16(tg, d, d, idesc, k > 0);
+        mma_f16(tg, d, d, idesc, k > 0);
       }
     });
     if (__syncthreads_or(!ok)) break;
@@ -802,7 +802,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
     ok = product([&] {
       for (int k = 0; k < rows16; ++k) {
         const uint64_t d = smem_desc(ag + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
-        mma_bf16(tg, d, d, idesc, k > 0);
+        mma_f16(tg, d, d, idesc, k > 0);
       }
     });
     if (__syncthreads_or(!ok)) break;
@@ -832,7 +832,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       for (int twice = 0; twice < (step + 1 < a.d.steps ? 2 : 1); ++twice)
         for (int k = 0; k < rows16; ++k) {
           const uint64_t da = smem_desc(aq + (k >> 2) * kSmallBox + (k & 3) * 32, 16, 1024);
-          mma_bf16(tx, da, smem_desc((twice ? alo : ax) + k * 2048, kSmallBox, 1024), idesc_x, (k | twice) > 0);
+          mma_f16(tx, da, smem_desc((twice ? alo : ax) + k * 2048, kSmallBox, 1024), idesc_x, (k | twice) > 0);
         }
     });
     if (__syncthreads_or(!ok)) break;
@@ -1026,7 +1026,7 @@ int64_t tiles_of(const Product& p) {
   return (p.symmetric ? mt * (mt + 1) / 2 * (F::kM / F::kN) : mt * nt) * p.batch * p.split;
 }
 // The form whose rounds over the machine take least.  A pair's tile is four of 128 x 128 on two SMs and runs at about 1.4 times their
-// rate (32 x 1024 x 1024: 1131 us instead of 1334).  One of 64 columns fetches three quarters of a square's operands and has half its
+// rate (32 x 1024 x 1024: 1131 us instead of 1334 when it was chosen).  One of 64 columns fetches three quarters of a square's operands and has half its
 // epilogue, so it takes about 11 of its 14: where there are few (3 x 1001 x 333: 131 us instead of 147; 768 x 768: 140 instead of 158; 8 x 256
 // x 256: 93 instead of 113).  c64, rest64: the stored tensors in boxes of 64 rows.
 struct Chosen {

@@ -2,8 +2,8 @@
 //
 //   h_t = exp(delta_t A) h_(t-1) + delta_t x_t B_t,   y_t = C_t . h_t
 //
-// for N states of every channel.  L lanes share a channel and hold 4 of its states each in registers (N <= 4 L), two to an
-// instruction.  A block takes some channels of a run of rows (a chain), a tile of rows at a time: the tile's next rows are fetched into
+// for N states of every channel.  L lanes (2, 4, 8 or 16) share a channel and hold 4 of its states each in registers (N <= 4 L; states up to
+// the next of 8, 16, 32 and 64 are computed and left out of the sums), two to an instruction.  A block takes some channels of a run of rows (a chain), a tile of rows at a time: the tile's next rows are fetched into
 // registers while the present ones run, and are staged in shared memory as what the recurrence reads: delta and delta x (one
 // softplus a row and channel), B and C as fp32.  delta and delta x lie [channel][row], so that a lane reads four rows at once.  The
 // sums over a channel's states go through its L lanes, four rows at a time (each lane ends up with one row's sum), and are finished
@@ -326,7 +326,7 @@ __device__ __forceinline__ void barrier_arrive(int id) { asm volatile("barrier.a
 // Half of the block's warps run the recurrence, the others stage the next tile and finish the last one meanwhile (two buffers; barriers
 // 1 + b: buffer b is staged, 3 + b: its tile is done), so that a block's staging, a chain of latencies, does not stop its recurrence:
 // ragged prompts of 8191 x 1500 take 203 us instead of 258.  (Two channels a thread would halve what is read of B and C, but leave
-// half the warps: 172 us instead of 197 for 32768 x 384 in fp32, 304 instead of 203 for the prompts.)
+// half the warps: the prompts took 304 us instead of 203, though 32768 x 384 in fp32, which lacks no warps, 172 instead of 197.)
 template <typename T, int L, bool kEnds, bool kSome>
 __global__ void __launch_bounds__(2 * kThreads, kBlocks) forward_kernel(const __grid_constant__ Args a) {
   using Ti = Tile<L>;
