@@ -4,8 +4,8 @@
 //
 // for N states of every channel.  L lanes (2, 4, 8 or 16) share a channel and hold 4 of its states each in registers (N <= 4 L; states up
 // to the next of 8, 16, 32 and 64 are computed and left out of the sums), two to an instruction.  A block takes some channels of a run of
-// rows (a chain), a tile of rows at a time: the tile's next rows are fetched into registers while the present ones run, and are staged in shared memory as what the recurrence reads: delta and delta x (one
-// softplus a row and channel), B and C as fp32.  delta and delta x lie [channel][row], so that a lane reads four rows at once.  The
+// rows (a chain), a tile of rows at a time: the tile's next rows are fetched into registers while the present ones run, and are staged in
+// shared memory as what the recurrence reads: delta and delta x (one softplus a row and channel), B and C as fp32.  delta and delta x lie [channel][row], so that a lane reads four rows at once.  The
 // sums over a channel's states go through its L lanes, four rows at a time (each lane ends up with one row's sum), and are finished
 // (skip, gate) by the thread that staged the row's piece of 8 channels.
 //
